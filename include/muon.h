@@ -522,6 +522,140 @@ int muon_momentum_norm_static(const void* g, float* m, int rows, int cols, int64
                               int g_dtype, float mu, int nesterov, float* norm_out, int device,
                               void* stream);
 
+/*
+ * Losses at the LM head, with their gradients.  The head is the largest matrix
+ * of a model and its logits [tokens, vocab] the largest activation; these calls
+ * compute a loss over the whole vocabulary, and the gradients of the hidden
+ * states and of the head, without ever holding the logits: they stay in tensor
+ * memory, only a bf16 gradient of one piece of the vocabulary at a time is kept
+ * in the workspace.  dX goes on into the layers whose matrices muon_step
+ * updates, dW to muon_adamw_step (Sec. 2.2: the LM head stays with AdamW).
+ *
+ *   l   = logit_scale * x w^T            (distillation: / temperature as well)
+ *   lse = log sum_j exp(l_j),  q = exp(l - lse)
+ *
+ * Every token has a sparse target distribution p over a few vocabulary entries,
+ * c = sum p.  A token that has none is masked: its loss and lse are 0, its row
+ * of dX is 0, and nothing of it - not even an infinity or a NaN in its row of x -
+ * reaches any other output.  Only the other tokens are computed.
+ *
+ *   coefficient of a token  g = scale * weight, with `mean` divided by the sum of
+ *                           the weights of the tokens that are not masked
+ *                           (weight 1 each without a weight array; 0 if the sum is 0)
+ *   *total   = sum_t g_t loss_t     and dx, dw are the gradients of *total
+ *
+ * Arithmetic: products of bf16 operands with fp32 sums; softmax statistics, losses
+ * and sums in fp32; the gradient of the logits is rounded to bf16 once, as an
+ * operand of the products that form dX and dW, those are summed in fp32 and
+ * rounded once where the output is bf16.  Results are the same bits from call to
+ * call.
+ *
+ *   tokens  : rows of x; 0 is allowed.  dim: columns of x and w.  vocab: rows of w.
+ *   x, w    : DEVICE, bf16, row strides ld_x, ld_w elements (any stride >= dim; a
+ *             head whose rows are not 16-byte aligned costs a copy of it).
+ *   weight  : DEVICE, one float per token, or NULL.
+ *   loss    : DEVICE, one float per token: the token's own loss, without g.
+ *   lse     : DEVICE, one float per token, or NULL.
+ *   total   : DEVICE, one float, or NULL.
+ *   dx, dw  : DEVICE, bf16 or fp32, [tokens, dim] and [vocab, dim], each NULL if not
+ *             wanted.  dw_accumulate: dw is added to instead of written (several
+ *             micro-batches into one fp32 gradient).
+ *   Every pointer aligned to its element size.  Outputs must not overlap inputs or
+ *   one another.
+ */
+typedef struct muon_head_args {
+  int32_t tokens;
+  int32_t dim;
+  int32_t vocab;
+  int32_t mean;
+  const void* x;
+  const void* w;
+  int64_t ld_x;
+  int64_t ld_w;
+  int32_t x_dtype; /* MUON_DTYPE_BF16 */
+  int32_t w_dtype; /* MUON_DTYPE_BF16 */
+  const float* weight;
+  float scale;
+  float logit_scale;
+  float* loss;
+  float* lse;
+  float* total;
+  void* dx;
+  void* dw;
+  int64_t ld_dx;
+  int64_t ld_dw;
+  int32_t dx_dtype;
+  int32_t dw_dtype;
+  int32_t dw_accumulate;
+  int32_t reserved;
+} muon_head_args;
+
+/*
+ * Bytes of DEVICE workspace (1024-byte aligned) one call needs: pure host
+ * computation on the sizes, the types, the alignment and stride of w, and which of
+ * dx and dw are wanted.  top: teacher entries per token, 0 for cross entropy.
+ * It stays bounded as tokens x vocab grows: the gradient of the logits takes at
+ * most 1 GiB (or 256 vocabulary entries, if that is more).
+ */
+int muon_head_workspace_bytes(const muon_head_args* args, int top, size_t* out_bytes);
+
+/*
+ * Softmax cross entropy.  targets: DEVICE, one int64 per token; a token whose target
+ * lies outside [0, vocab) (-100, say) is masked.
+ *
+ *   loss = lse - l_target + z_loss * lse^2
+ *
+ * z_loss (0: none) keeps the softmax normaliser near 1.  Asynchronous on `stream`;
+ * allocates nothing, does not synchronise; may be captured into a CUDA graph.
+ * The workspace must not be shared by calls that can overlap on the GPU.
+ */
+int muon_head_xent(const muon_head_args* args, const int64_t* targets, float z_loss, void* workspace,
+                   size_t workspace_bytes, int device, void* stream);
+
+/*
+ * Distillation from the `top` (1 to 128) most likely entries of a teacher:
+ * forward Kullback-Leibler divergence from the teacher's distribution over the
+ * entries it kept to the student's over the whole vocabulary.
+ *
+ *   without teacher_lse: p = softmax(top_logits / temperature) over the entries
+ *   with teacher_lse:    p = exp(top_logits / temperature - teacher_lse), where
+ *                        teacher_lse is the log-sum-exp of ALL of the teacher's
+ *                        logits / temperature; the mass it did not keep adds nothing
+ *   loss = sum_k p_k (log p_k - (l_k - lse)),  gradient of l: c q - p
+ *
+ * The usual factor temperature^2 is the caller's (`scale`).
+ *
+ *   top_ids    : DEVICE, int64 [tokens, top], row stride ld_ids.  In any order; an
+ *                index outside [0, vocab) is an entry that is not there; an index
+ *                listed twice counts with both its probabilities.
+ *   top_logits : DEVICE, bf16 or fp32 [tokens, top], row stride ld_logits; minus
+ *                infinity is probability 0.
+ *   teacher_lse: DEVICE, one float per token, or NULL.
+ * A token with no entry in the vocabulary, or only entries of minus infinity, is
+ * masked.  Streams, workspace and errors as muon_head_xent.
+ */
+typedef struct muon_head_teacher {
+  const int64_t* top_ids;
+  const void* top_logits;
+  int64_t ld_ids;
+  int64_t ld_logits;
+  const float* teacher_lse;
+  int32_t top;
+  int32_t logits_dtype;
+  float temperature;
+  int32_t reserved;
+} muon_head_teacher;
+
+int muon_head_distill(const muon_head_args* args, const muon_head_teacher* teacher, void* workspace,
+                      size_t workspace_bytes, int device, void* stream);
+
+/*
+ * Synchronise `stream` and read the status of the last call that used this
+ * workspace: 0, or MUON_ERR_TIMEOUT if a bounded device-side wait expired (its
+ * outputs are then not valid).
+ */
+int muon_head_status(const void* workspace, int device, void* stream, int* device_status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmuon_b200.so")
@@ -37,6 +37,7 @@ EXPORTED = [
     "muon_debug_wait_expiry",
     "muon_profile_enable", "muon_profile_read", "muon_debug_tmem_bases",
     "muon_momentum_norm_static", "muon_adamw_step",
+    "muon_head_workspace_bytes", "muon_head_xent", "muon_head_distill", "muon_head_status",
 ]
 MUON_STATIC_MAX_TILES = 65536
 KERNEL_KINDS = ["momentum", "norm", "gram", "poly", "comb", "update"]
@@ -71,6 +72,23 @@ class muon_adamw_tensor(C.Structure):
 class muon_adamw_hparams(C.Structure):
     _fields_ = [("lr", C.c_float), ("wd", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
                 ("eps", C.c_float), ("step", C.c_int32)]
+
+
+class muon_head_args(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("dim", C.c_int32), ("vocab", C.c_int32), ("mean", C.c_int32),
+                ("x", C.c_void_p), ("w", C.c_void_p), ("ld_x", C.c_int64), ("ld_w", C.c_int64),
+                ("x_dtype", C.c_int32), ("w_dtype", C.c_int32), ("weight", C.c_void_p),
+                ("scale", C.c_float), ("logit_scale", C.c_float),
+                ("loss", C.c_void_p), ("lse", C.c_void_p), ("total", C.c_void_p),
+                ("dx", C.c_void_p), ("dw", C.c_void_p), ("ld_dx", C.c_int64), ("ld_dw", C.c_int64),
+                ("dx_dtype", C.c_int32), ("dw_dtype", C.c_int32), ("dw_accumulate", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class muon_head_teacher(C.Structure):
+    _fields_ = [("top_ids", C.c_void_p), ("top_logits", C.c_void_p), ("ld_ids", C.c_int64),
+                ("ld_logits", C.c_int64), ("teacher_lse", C.c_void_p), ("top", C.c_int32),
+                ("logits_dtype", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32)]
 
 
 class MuonError(RuntimeError):
@@ -127,6 +145,12 @@ def lib():
     L.muon_debug_wait_expiry.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_uint]
     L.muon_adamw_step.argtypes = [C.POINTER(muon_adamw_tensor), C.c_int, C.POINTER(muon_adamw_hparams), C.c_int,
                                   C.c_void_p]
+    L.muon_head_workspace_bytes.argtypes = [C.POINTER(muon_head_args), C.c_int, C.POINTER(C.c_size_t)]
+    L.muon_head_xent.argtypes = [C.POINTER(muon_head_args), C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_int,
+                                 C.c_void_p]
+    L.muon_head_distill.argtypes = [C.POINTER(muon_head_args), C.POINTER(muon_head_teacher), C.c_void_p, C.c_size_t,
+                                    C.c_int, C.c_void_p]
+    L.muon_head_status.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)]
     for name in EXPORTED:
         if name == "muon_debug_set_chunk_bytes":
             getattr(L, name).restype = C.c_size_t
@@ -278,6 +302,160 @@ def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, 
     s = torch.cuda.current_stream(dev) if stream is None else stream
     hp = muon_adamw_hparams(lr, wd, beta1, beta2, eps, int(step))
     _check(lib().muon_adamw_step(arr, n, C.byref(hp), dev, C.c_void_p(s.cuda_stream)))
+
+
+class HeadLoss(NamedTuple):
+    """What a head loss gives: per-token ``loss`` and ``lse`` (fp32), ``total`` (one
+    fp32 element), the gradients of ``total`` (None where not asked for) and the
+    workspace that held the call's intermediates."""
+    loss: "torch.Tensor"
+    lse: "torch.Tensor"
+    total: "torch.Tensor"
+    dx: Optional["torch.Tensor"]
+    dw: Optional["torch.Tensor"]
+    workspace: "torch.Tensor"
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace, stream,
+               call):
+    """Checks, outputs and workspace shared by the head losses; ``call(args,
+    workspace pointer, bytes, device, stream)`` makes the C call."""
+    import torch
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.shape[1] < 1 or w.shape[0] < 1:
+        raise MuonError(MUON_ERR_INVALID_ARG, "x must be [tokens, dim] and w [vocab, dim]")
+    if not x.is_cuda or x.device != w.device:
+        raise MuonError(MUON_ERR_INVALID_ARG, "x and w must be on one CUDA device")
+    tokens, dim = x.shape
+    dev = x.device
+
+    def rows_contiguous(t):
+        return t.shape[1] == 1 or t.stride(1) == 1
+
+    def vector(t, what, n=tokens, new=False):
+        if t is None:
+            return torch.empty(n, dtype=torch.float32, device=dev) if new else None
+        if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.device != dev:
+            raise MuonError(MUON_ERR_INVALID_ARG, "%s must be %d contiguous fp32 values on x's device" % (what, n))
+        return t
+
+    def grad(t, like, what):
+        if t is None or t is False:
+            return None
+        if t is True:
+            return torch.empty(like.shape, dtype=like.dtype, device=dev)
+        if t.shape != like.shape or not rows_contiguous(t) or t.device != dev:
+            raise MuonError(MUON_ERR_INVALID_ARG, "%s must be shaped like its tensor, rows contiguous" % what)
+        return t
+
+    for t, what in ((x, "x"), (w, "w")):
+        if not rows_contiguous(t):
+            raise MuonError(MUON_ERR_INVALID_ARG, "%s must have contiguous rows" % what)
+    if accumulate_dw and not isinstance(dw, torch.Tensor):
+        raise MuonError(MUON_ERR_INVALID_ARG, "accumulate_dw needs the dw to add to")
+    loss, lse = vector(loss, "loss", new=True), vector(lse, "lse", new=True)
+    total = vector(total, "total", 1, new=True)
+    weight = vector(weight, "weight")
+    dx, dw = grad(dx, x, "dx"), grad(dw, w, "dw")
+    a = muon_head_args(tokens, dim, w.shape[0], int(bool(mean)), x.data_ptr(), w.data_ptr(), _row_stride(x) if tokens else dim,
+                       _row_stride(w), _dtype_code(x), _dtype_code(w), None if weight is None else weight.data_ptr(),
+                       float(scale), float(logit_scale), loss.data_ptr(), lse.data_ptr(), total.data_ptr())
+    if dx is not None:
+        a.dx, a.ld_dx, a.dx_dtype = dx.data_ptr(), _row_stride(dx) if tokens else dim, _dtype_code(dx)
+    if dw is not None:
+        a.dw, a.ld_dw, a.dw_dtype, a.dw_accumulate = dw.data_ptr(), _row_stride(dw), _dtype_code(dw), int(bool(accumulate_dw))
+    need = C.c_size_t(0)
+    _check(lib().muon_head_workspace_bytes(C.byref(a), top, C.byref(need)))
+    s = torch.cuda.current_stream(dev) if stream is None else stream
+    if workspace is None:
+        # from the caching allocator, for the stream the kernels run on
+        with torch.cuda.stream(s):
+            workspace = torch.empty(need.value + 1024, dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+        raise MuonError(MUON_ERR_WORKSPACE, "workspace must be a contiguous uint8 tensor on x's device")
+    base = (workspace.data_ptr() + 1023) // 1024 * 1024
+    room = workspace.data_ptr() + workspace.numel() - base
+    _check(call(C.byref(a), C.c_void_p(base), max(room, 0), dev.index, C.c_void_p(s.cuda_stream)))
+    return HeadLoss(loss, lse, total, dx, dw, workspace)
+
+
+def muon_head_workspace_bytes(tokens: int, dim: int, vocab: int, top: int = 0, dx: bool = True, dw: bool = True,
+                              packed_head: bool = True) -> int:
+    """Workspace bytes of one head-loss call (``top``: teacher entries per token, 0
+    for cross entropy), 1024 for aligning a tensor's start included.
+    ``packed_head``: the head's rows are 16-byte aligned."""
+    ld = (dim + 7) // 8 * 8 if packed_head else dim | 1
+    a = muon_head_args(tokens, dim, vocab, 1, None, None, dim, ld, MUON_DTYPE_BF16, MUON_DTYPE_BF16)
+    a.dx, a.dw = (1024 if dx else None), (1024 if dw else None)  # only whether they are there counts
+    out = C.c_size_t(0)
+    _check(lib().muon_head_workspace_bytes(C.byref(a), int(top), C.byref(out)))
+    return out.value + 1024
+
+
+def muon_head_xent(x, w, targets, loss=None, lse=None, total=None, dx=None, dw=None, weight=None, mean=True,
+                   scale=1.0, logit_scale=1.0, z_loss=0.0, accumulate_dw=False, workspace=None, stream=None) -> HeadLoss:
+    """Softmax cross entropy of ``x w^T`` over the vocabulary, with its gradients and
+    without the logits.  ``x`` [tokens, dim] and ``w`` [vocab, dim] are bf16,
+    ``targets`` int64 [tokens] (outside [0, vocab): the token is masked).
+    ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True to allocate one like x / w,
+    None to leave the gradient out.  Other outputs and the workspace are allocated
+    unless given.  Argument marshalling only; the formulas are in include/muon.h.
+    Tensors used on another stream than the one they were allocated on are the
+    caller's to keep alive (``record_stream``)."""
+    import torch
+    if targets.dtype != torch.int64 or targets.dim() != 1 or targets.numel() != x.shape[0] or not targets.is_contiguous() or targets.device != x.device:
+        raise MuonError(MUON_ERR_INVALID_ARG, "targets must be contiguous int64 [tokens] on x's device")
+
+    def call(a, ws, nbytes, dev, s):
+        return lib().muon_head_xent(a, C.c_void_p(targets.data_ptr()), float(z_loss), ws, nbytes, dev, s)
+
+    return _head_call(x, w, 0, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace,
+                      stream, call)
+
+
+def muon_head_distill(x, w, top_ids, top_logits, temperature=1.0, teacher_lse=None, loss=None, lse=None, total=None,
+                      dx=None, dw=None, weight=None, mean=True, scale=1.0, logit_scale=1.0, accumulate_dw=False,
+                      workspace=None, stream=None) -> HeadLoss:
+    """Distillation from a teacher's top logits: ``top_ids`` int64 and ``top_logits``
+    bf16 or fp32, both [tokens, top], ``teacher_lse`` fp32 [tokens] or None.
+    Everything else as :func:`muon_head_xent`."""
+    import torch
+    for t, what in ((top_ids, "top_ids"), (top_logits, "top_logits")):
+        if t.dim() != 2 or t.shape != top_ids.shape or t.shape[0] != x.shape[0] or t.device != x.device or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise MuonError(MUON_ERR_INVALID_ARG, "%s must be [tokens, top] on x's device, rows contiguous" % what)
+    if top_ids.dtype != torch.int64:
+        raise MuonError(MUON_ERR_INVALID_ARG, "top_ids must be int64")
+    if teacher_lse is not None and (teacher_lse.dtype != torch.float32 or teacher_lse.dim() != 1 or teacher_lse.numel() != x.shape[0]
+                                    or not teacher_lse.is_contiguous() or teacher_lse.device != x.device):
+        raise MuonError(MUON_ERR_INVALID_ARG, "teacher_lse must be contiguous fp32 [tokens] on x's device")
+    top = top_ids.shape[1]
+    if top < 1:
+        raise MuonError(MUON_ERR_INVALID_ARG, "at least one teacher entry per token")
+    t = muon_head_teacher(top_ids.data_ptr(), top_logits.data_ptr(), _row_stride(top_ids) if x.shape[0] else top,
+                          _row_stride(top_logits) if x.shape[0] else top,
+                          None if teacher_lse is None else teacher_lse.data_ptr(), top, _dtype_code(top_logits),
+                          float(temperature), 0)
+
+    def call(a, ws, nbytes, dev, s):
+        return lib().muon_head_distill(a, C.byref(t), ws, nbytes, dev, s)
+
+    return _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace,
+                      stream, call)
+
+
+def muon_head_status(result: HeadLoss, stream=None) -> int:
+    """Synchronises the stream; 0, or MUON_ERR_TIMEOUT if a device-side wait of the
+    last call on the result's workspace expired."""
+    import torch
+    ws = result.workspace
+    s = torch.cuda.current_stream(ws.device) if stream is None else stream
+    st = C.c_int(0)
+    _check(lib().muon_head_status(C.c_void_p((ws.data_ptr() + 1023) // 1024 * 1024), ws.device.index,
+                                  C.c_void_p(s.cuda_stream), C.byref(st)))
+    return st.value
 
 
 def muon_partition(shapes, world: int):

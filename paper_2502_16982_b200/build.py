@@ -13,8 +13,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuon_b200.so")
-SOURCES = ["muon_api.cu", "stream_kernels.cu", "stream_tma.cu", "ns_gemm.cu", "no_alloc.cu", "adamw.cu"]
-HEADERS = ["internal.h", "ptx.cuh", os.path.join("..", "..", "include", "muon.h")]
+SOURCES = ["muon_api.cu", "stream_kernels.cu", "stream_tma.cu", "ns_gemm.cu", "no_alloc.cu", "adamw.cu",
+           "head_api.cu", "head_gemm.cu", "head_rows.cu"]
+HEADERS = ["internal.h", "ptx.cuh", "head.h", os.path.join("..", "..", "include", "muon.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-lineinfo", "-O3", "-std=c++17",

@@ -1,0 +1,138 @@
+// Structures shared by the host side and the kernels of the losses at the LM
+// head (softmax cross entropy, distillation from a teacher's top logits).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace muon {
+namespace head {
+
+constexpr int kTileM = 256;   // output rows of a CTA pair's tile (128 per CTA)
+constexpr int kTileN = 256;   // widest output tile, and the vocabulary columns of one statistics entry
+constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
+constexpr int kMaxTop = 128;  // sparse target entries of one token
+constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
+
+// Control block at the start of the workspace.
+struct Ctrl {
+  int status;      // 0 or MUON_ERR_TIMEOUT
+  int n_valid;     // tokens that count
+  unsigned ticket; // blocks of the finalisation that are done
+  float coef;      // scale, divided by the sum of the weights where a mean is asked for
+};
+
+// One product of a launch: D[m][n] = sum_k A[m][k] B[n][k].
+struct Product {
+  CUtensorMap map_a, map_b;
+  int a_mn, b_mn;    // operand stored with M (N) contiguous instead of K
+  int n_tile;        // 128 or 256
+  int m_tiles;       // row tiles of 256; -1: from the number of tokens that count
+  int n_tiles;
+  int k_blocks;      // K blocks of 64 in all; -1: from the number of tokens that count
+  int splits;        // the K blocks are cut into this many runs, each its own tile
+  int b_k0;          // first K coordinate of operand B (vocabulary piece in W)
+  int b_n0;          // first row of operand B
+  int group;         // row tiles that are walked together for each column tile
+  int swap_order;    // walk the column tiles innermost
+};
+
+enum { kModeStats = 0, kModeGrad = 1, kModeOut = 2 };
+
+struct GemmParams {
+  Product prod[2];
+  int n_prod;
+  Ctrl* ctrl;
+
+  // statistics and gradient of the logits
+  int vocab;          // columns of the whole problem
+  int v0;             // first vocabulary column of this launch
+  float scale2;       // logit scale * log2(e)
+  int top;            // sparse entries per token; 1: one target
+  const int* ids;     // [rows][top], ascending within a row
+  const unsigned char* starts;  // [rows][n_starts]: entries below each 256-column tile (top > 1)
+  int n_starts;
+  float* entry_logit; // [rows][top] raw logit of each entry
+  float2* stats;      // [rows][stats_ld]: maximum and sum of exponentials per 256-column tile
+  int stats_ld;
+  const float2* row_q;   // [rows]: coefficient of q, log2 of the softmax denominator
+  const float* entry_g;  // [rows][top]: gradient of the logit at the entry
+  __nv_bfloat16* g;      // [padded rows][g_ld]: gradient of the logits of one vocabulary piece
+  long long g_ld;
+
+  // product 0 of kModeOut: partial dX
+  float* part;        // [splits][padded rows][part_ld]
+  long long part_ld, part_stride;
+  int part_cols;
+  int part_add;       // add to what an earlier piece left
+  // product 1 of kModeOut: dW
+  void* dw;
+  long long ld_dw;
+  int dw_fp32, dw_add, dw_vec;  // dw_vec: widest aligned store in bytes (32, 16) or 0
+  int dw_row0, dw_rows, dw_cols;
+};
+
+struct RowParams {
+  Ctrl* ctrl;
+  int tokens, padded, dim, vocab;
+  const __nv_bfloat16* x;
+  long long ld_x;
+  __nv_bfloat16* xc;     // [padded][ld_xc] rows of the tokens that count, then zeros
+  long long ld_xc;
+  int x_vec;             // rows can be copied in 16-byte pieces
+  const int64_t* ids_in; // [tokens][top]
+  long long ld_ids;
+  const void* z;         // teacher logits [tokens][top], NULL: one target per token
+  long long ld_z;
+  int z_fp32;
+  const float* teacher_lse;
+  float inv_t;           // 1 / temperature
+  int top;
+  const float* weight;
+  float scale;
+  int mean;
+  unsigned char* flags;  // [tokens] token counts (distillation)
+  int* pos_of;           // [tokens]: row of the token, -1 if it does not count
+  int* row_of;           // [padded]
+  int* ids;              // [padded][top]
+  float* p;              // [padded][top]
+  float* row_h;          // [padded]: sum p log p
+  float* row_c;          // [padded]: sum p
+  unsigned char* starts;
+  int n_starts;
+  float* entry_logit;
+  float2* stats;
+  int stats_ld, stats_n;
+  float scale2;          // logit scale * log2(e)
+  float logit_scale;
+  float z_loss;
+  float2* row_q;
+  float* entry_g;
+  float* row_l;          // [padded]: coefficient * loss
+  float* loss;           // [tokens]
+  float* lse;            // [tokens] or NULL
+  float* total;          // [1] or NULL
+  // dX
+  const float* part;
+  long long part_ld, part_stride;
+  int splits;
+  void* dx;
+  long long ld_dx;
+  int dx_fp32, dx_vec;
+};
+
+cudaError_t gemm_configure();
+cudaError_t gemm_max_clusters(int* out);
+cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, cudaStream_t stream);
+
+cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
+cudaError_t launch_finalise(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
+                        int cols, cudaStream_t stream);
+
+}  // namespace head
+}  // namespace muon

@@ -1,0 +1,463 @@
+// Host side of the LM-head losses: argument checks, the plan (vocabulary pieces,
+// splits, workspace layout) and the launch sequence.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "../../include/muon.h"
+#include "head.h"
+
+namespace muon {
+void set_last_error(const char* msg);
+}
+
+namespace {
+
+using namespace muon::head;
+
+int fail(int code, const char* fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  muon::set_last_error(buf);
+  return code;
+}
+
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+// Bytes of logit gradients (bf16) that one vocabulary piece may take.
+constexpr long long kPieceBytes = 1ll << 30;
+// Bytes of partial dX that splitting its long axis may take.
+constexpr long long kPartBytes = 1ll << 28;
+
+struct Plan {
+  int tokens, padded, dim, vocab, top;
+  bool want_dx, want_dw, grads, distill, pack;
+  int v_tiles;               // 256-column tiles of the vocabulary
+  int piece_tiles, n_pieces;
+  int splits, dx_n_tile, dx_n_tiles;
+  long long ld_xc, ld_wc, part_ld, part_stride;
+  size_t ctrl, xc, wc, flags, pos_of, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
+      part, bytes;
+};
+
+// How many runs the K blocks of dX's tiles are cut into.  dX has few tiles with
+// a long axis (the vocabulary piece), dW many with a short one; both are dealt
+// out to the CTA pairs in turn, dX first.  The split with the smallest load of
+// the fullest pair is taken, a tile counted as its K blocks plus kTileCost for
+// its epilogue and the traffic of a partial sum.
+constexpr int kTileCost = 6;
+int choose_splits(int dx_tiles, int dx_kb, int dw_tiles, int dw_kb, int pairs, int most) {
+  int best = 1;
+  long long best_load = -1;
+  for (int s = 1; s <= most; ++s) {
+    if (s > 1 && dx_kb / s < 4) break;
+    const long long nx = static_cast<long long>(dx_tiles) * s;
+    long long load = 0;
+    for (int w = 0; w < pairs; ++w) {
+      const long long x = nx / pairs + (w < nx % pairs);
+      const long long all = (nx + dw_tiles) / pairs + (w < (nx + dw_tiles) % pairs);
+      const long long l = x * ((dx_kb + s - 1) / s + kTileCost) + (all - x) * (dw_kb + kTileCost);
+      if (l > load) load = l;
+    }
+    if (best_load < 0 || load < best_load) {
+      best_load = load;
+      best = s;
+    }
+  }
+  return best;
+}
+
+int make_plan(const muon_head_args* a, int top, bool distill, int pairs, Plan* P) {
+  P->tokens = a->tokens;
+  P->dim = a->dim;
+  P->vocab = a->vocab;
+  P->top = top;
+  P->distill = distill;
+  P->padded = static_cast<int>(round_up(a->tokens > 0 ? a->tokens : 1, kTileM));
+  P->want_dx = a->dx != nullptr && a->tokens > 0;
+  P->want_dw = a->dw != nullptr;
+  P->grads = P->want_dx || P->want_dw;
+  P->pack = (reinterpret_cast<uintptr_t>(a->w) & 15) != 0 || (a->ld_w & 7) != 0;
+  P->v_tiles = static_cast<int>((static_cast<long long>(a->vocab) + kTileN - 1) / kTileN);
+  P->ld_xc = round_up(a->dim, 8);
+  P->ld_wc = round_up(a->dim, 8);
+  P->part_ld = round_up(a->dim, 8);
+  P->part_stride = P->padded * P->part_ld;
+
+  long long tiles = kPieceBytes / (2ll * P->padded * kTileN);
+  if (tiles < 1) tiles = 1;
+  if (tiles > P->v_tiles) tiles = P->v_tiles;
+  P->n_pieces = static_cast<int>((P->v_tiles + tiles - 1) / tiles);
+  P->piece_tiles = (P->v_tiles + P->n_pieces - 1) / P->n_pieces;
+  P->n_pieces = (P->v_tiles + P->piece_tiles - 1) / P->piece_tiles;
+
+  P->dx_n_tile = a->dim <= 128 ? 128 : 256;
+  P->dx_n_tiles = (a->dim + P->dx_n_tile - 1) / P->dx_n_tile;
+  P->splits = 1;
+  if (P->want_dx) {
+    long long most = kPartBytes / (P->part_stride * 4);
+    most = most < 1 ? 1 : (most > 64 ? 64 : most);
+    P->splits = choose_splits(P->padded / kTileM * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
+                              P->want_dw ? P->piece_tiles * P->dx_n_tiles : 0, P->padded / kBK, pairs,
+                              static_cast<int>(most));
+  }
+
+  const size_t rows = static_cast<size_t>(P->padded), entries = rows * top;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = static_cast<size_t>(round_up(static_cast<long long>(off + bytes), 1024));
+    return at;
+  };
+  P->ctrl = take(sizeof(Ctrl));
+  P->xc = take(rows * P->ld_xc * 2);
+  P->pos_of = take(rows * 4);
+  P->row_of = take(rows * 4);
+  P->ids = take(entries * 4);
+  P->entry_logit = take(entries * 4);
+  P->entry_g = take(entries * 4);
+  P->stats = take(rows * P->v_tiles * sizeof(float2));
+  P->row_q = take(rows * sizeof(float2));
+  P->row_l = take(rows * 4);
+  P->flags = P->p = P->row_h = P->row_c = P->starts = P->wc = P->g = P->part = 0;
+  if (distill) {
+    P->flags = take(rows);
+    P->p = take(entries * 4);
+    P->row_h = take(rows * 4);
+    P->row_c = take(rows * 4);
+    P->starts = take(rows * (P->v_tiles + 1));
+  }
+  if (P->pack) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
+  if (P->grads) P->g = take(rows * P->piece_tiles * kTileN * 2);
+  if (P->want_dx) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
+  P->bytes = off;
+  return MUON_OK;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+
+// bf16 matrix [rows][cols] with row pitch ld, 128-byte swizzled boxes of 64 x box_rows.
+int encode(CUtensorMap* out, const void* base, long long rows, long long cols, long long ld, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return fail(MUON_ERR_CUDA, "cuTensorMapEncodeTiled entry point not available");
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), 1};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * 2 * static_cast<cuuint64_t>(rows)};
+  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(MUON_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
+  return MUON_OK;
+}
+
+// CTA pairs that fit the device, looked up once per device.
+int device_pairs(int device, int* out) {
+  constexpr int kMaxDevices = 64;
+  static int cached[kMaxDevices] = {};
+  if (device < 0 || device >= kMaxDevices) return fail(MUON_ERR_INVALID_ARG, "device ordinal %d", device);
+  if (cached[device] == 0) {
+    cudaError_t e = gemm_configure();
+    int n = 0;
+    if (e == cudaSuccess) e = gemm_max_clusters(&n);
+    if (e != cudaSuccess) return fail(MUON_ERR_CUDA, "%s", cudaGetErrorString(e));
+    if (n < 1) return fail(MUON_ERR_CUDA, "no CTA pair fits the device");
+    cached[device] = n;
+  }
+  *out = cached[device];
+  return MUON_OK;
+}
+
+// Pairs assumed where the workspace is sized: the plan must not depend on the device.
+constexpr int kPlanPairs = 74;
+
+bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+int check(const muon_head_args* a, int top, bool need_ptrs) {
+  if (!a) return fail(MUON_ERR_INVALID_ARG, "args is null");
+  if (a->tokens < 0 || a->dim <= 0 || a->vocab <= 0)
+    return fail(MUON_ERR_INVALID_ARG, "tokens must not be negative, dim and vocab must be positive");
+  if (a->tokens > (1 << 24) || a->dim > (1 << 20) || a->vocab > (1 << 24))
+    return fail(MUON_ERR_UNSUPPORTED, "more than 2^24 tokens, 2^24 vocabulary entries or 2^20 dimensions");
+  if (top < 1 || top > kMaxTop) return fail(MUON_ERR_UNSUPPORTED, "1 to %d teacher entries per token", kMaxTop);
+  if (a->x_dtype != MUON_DTYPE_BF16 || a->w_dtype != MUON_DTYPE_BF16)
+    return fail(MUON_ERR_UNSUPPORTED, "x and w must be bf16 (fp32 weights: pass their bf16 copy)");
+  if ((a->dx_dtype != MUON_DTYPE_BF16 && a->dx_dtype != MUON_DTYPE_FP32) ||
+      (a->dw_dtype != MUON_DTYPE_BF16 && a->dw_dtype != MUON_DTYPE_FP32))
+    return fail(MUON_ERR_UNSUPPORTED, "gradients must be bf16 or fp32");
+  if (!need_ptrs) return MUON_OK;
+  if (!a->w || (a->tokens > 0 && (!a->x || !a->loss))) return fail(MUON_ERR_INVALID_ARG, "x, w or loss is null");
+  if (a->ld_w < a->dim || (a->tokens > 0 && a->ld_x < a->dim) || (a->dx && a->tokens > 0 && a->ld_dx < a->dim) ||
+      (a->dw && a->ld_dw < a->dim))
+    return fail(MUON_ERR_INVALID_ARG, "a row stride is smaller than dim");
+  if (!std::isfinite(a->scale) || !std::isfinite(a->logit_scale) || !(a->logit_scale > 0.f))
+    return fail(MUON_ERR_INVALID_ARG, "scale must be finite, logit_scale finite and positive");
+  if (misaligned(a->x, 2) || misaligned(a->w, 2) || misaligned(a->weight, 4) || misaligned(a->loss, 4) ||
+      misaligned(a->lse, 4) || misaligned(a->total, 4) || misaligned(a->dx, a->dx_dtype == MUON_DTYPE_FP32 ? 4 : 2) ||
+      misaligned(a->dw, a->dw_dtype == MUON_DTYPE_FP32 ? 4 : 2))
+    return fail(MUON_ERR_ALIGNMENT, "pointer not aligned to its element size");
+  return MUON_OK;
+}
+
+struct DeviceGuard {
+  int before = -1;
+  cudaError_t set(int device) {
+    cudaError_t e = cudaGetDevice(&before);
+    return e == cudaSuccess && before != device ? cudaSetDevice(device) : e;
+  }
+  ~DeviceGuard() {
+    int now = -1;
+    if (before >= 0 && cudaGetDevice(&now) == cudaSuccess && now != before) cudaSetDevice(before);
+  }
+};
+
+#define HEAD_CUDA(call)                                                              \
+  do {                                                                               \
+    cudaError_t e_ = (call);                                                         \
+    if (e_ != cudaSuccess) return fail(MUON_ERR_CUDA, "%s", cudaGetErrorString(e_)); \
+  } while (0)
+#define HEAD_TRY(call)             \
+  do {                             \
+    int rc_ = (call);              \
+    if (rc_ != MUON_OK) return rc_; \
+  } while (0)
+
+int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targets, float z_loss, void* workspace,
+        size_t workspace_bytes, int device, cudaStream_t stream) {
+  const bool distill = t != nullptr;
+  const int top = distill ? t->top : 1;
+  Plan P;
+  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, &P));
+  if (!workspace || workspace_bytes < P.bytes || misaligned(workspace, 1024))
+    return fail(MUON_ERR_WORKSPACE, "workspace: need %zu bytes, 1024-byte aligned", P.bytes);
+  DeviceGuard guard;
+  HEAD_CUDA(guard.set(device));
+  int pairs = 0;
+  HEAD_TRY(device_pairs(device, &pairs));
+
+  char* ws = static_cast<char*>(workspace);
+  const float logit_scale = distill ? a->logit_scale / t->temperature : a->logit_scale;
+
+  RowParams R = {};
+  R.ctrl = reinterpret_cast<Ctrl*>(ws + P.ctrl);
+  R.tokens = P.tokens;
+  R.padded = P.padded;
+  R.dim = P.dim;
+  R.vocab = P.vocab;
+  R.x = static_cast<const __nv_bfloat16*>(a->x);
+  R.ld_x = a->ld_x;
+  R.xc = reinterpret_cast<__nv_bfloat16*>(ws + P.xc);
+  R.ld_xc = P.ld_xc;
+  R.x_vec = !misaligned(a->x, 16) && (a->ld_x & 7) == 0;
+  R.ids_in = distill ? t->top_ids : targets;
+  R.ld_ids = distill ? t->ld_ids : 1;
+  R.z = distill ? t->top_logits : nullptr;
+  R.ld_z = distill ? t->ld_logits : 0;
+  R.z_fp32 = distill && t->logits_dtype == MUON_DTYPE_FP32;
+  R.teacher_lse = distill ? t->teacher_lse : nullptr;
+  R.inv_t = distill ? 1.0f / t->temperature : 1.0f;
+  R.top = top;
+  R.weight = a->weight;
+  R.scale = a->scale;
+  R.mean = a->mean;
+  R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
+  R.pos_of = reinterpret_cast<int*>(ws + P.pos_of);
+  R.row_of = reinterpret_cast<int*>(ws + P.row_of);
+  R.ids = reinterpret_cast<int*>(ws + P.ids);
+  R.p = reinterpret_cast<float*>(ws + P.p);
+  R.row_h = reinterpret_cast<float*>(ws + P.row_h);
+  R.row_c = reinterpret_cast<float*>(ws + P.row_c);
+  R.starts = reinterpret_cast<unsigned char*>(ws + P.starts);
+  R.n_starts = P.v_tiles + 1;
+  R.entry_logit = reinterpret_cast<float*>(ws + P.entry_logit);
+  R.stats = reinterpret_cast<float2*>(ws + P.stats);
+  R.stats_ld = R.stats_n = P.v_tiles;
+  R.scale2 = static_cast<float>(logit_scale * 1.4426950408889634);
+  R.logit_scale = logit_scale;
+  R.z_loss = z_loss;
+  R.row_q = reinterpret_cast<float2*>(ws + P.row_q);
+  R.entry_g = reinterpret_cast<float*>(ws + P.entry_g);
+  R.row_l = reinterpret_cast<float*>(ws + P.row_l);
+  R.loss = a->loss;
+  R.lse = a->lse;
+  R.total = a->total;
+  R.part = reinterpret_cast<const float*>(ws + P.part);
+  R.part_ld = P.part_ld;
+  R.part_stride = P.part_stride;
+  R.splits = P.splits;
+  R.dx = a->dx;
+  R.ld_dx = a->ld_dx;
+  R.dx_fp32 = a->dx_dtype == MUON_DTYPE_FP32;
+  R.dx_vec = !misaligned(a->dx, 16) && (a->ld_dx & (R.dx_fp32 ? 3 : 7)) == 0;
+
+  const void* w = a->w;
+  long long ld_w = a->ld_w;
+  if (P.pack) {
+    w = ws + P.wc;
+    ld_w = P.ld_wc;
+  }
+
+  GemmParams S = {};
+  S.n_prod = 1;
+  S.ctrl = R.ctrl;
+  S.vocab = P.vocab;
+  S.scale2 = R.scale2;
+  S.top = top;
+  S.ids = R.ids;
+  S.starts = R.starts;
+  S.n_starts = R.n_starts;
+  S.entry_logit = R.entry_logit;
+  S.stats = R.stats;
+  S.stats_ld = R.stats_ld;
+  S.row_q = R.row_q;
+  S.entry_g = R.entry_g;
+  S.g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
+  S.g_ld = static_cast<long long>(P.piece_tiles) * kTileN;
+  Product& L = S.prod[0];  // logits: tokens x vocabulary
+  HEAD_TRY(encode(&L.map_a, R.xc, P.padded, P.dim, P.ld_xc, 128));
+  HEAD_TRY(encode(&L.map_b, w, P.vocab, P.dim, ld_w, 128));
+  L.n_tile = kTileN;
+  L.m_tiles = -1;
+  L.n_tiles = P.v_tiles;
+  L.k_blocks = (P.dim + kBK - 1) / kBK;
+  L.splits = 1;
+  L.group = 16;  // 16 row tiles of x (16 MB at 2048 columns) stay in L2 while w streams past
+
+  GemmParams O = S;
+  if (P.grads) {
+    O.n_prod = 0;
+    Product& X = O.prod[0];  // dX: tokens x dim, over the vocabulary piece
+    X = Product{};
+    HEAD_TRY(encode(&X.map_a, S.g, P.padded, S.g_ld, S.g_ld, 128));
+    HEAD_TRY(encode(&X.map_b, w, P.vocab, P.dim, ld_w, 64));
+    X.b_mn = 1;
+    X.n_tile = P.dx_n_tile;
+    X.m_tiles = P.want_dx ? -1 : 0;
+    X.n_tiles = P.dx_n_tiles;
+    X.splits = P.splits;
+    X.swap_order = 1;
+    Product& W = O.prod[1];  // dW: vocabulary piece x dim, over the tokens
+    W = Product{};
+    HEAD_TRY(encode(&W.map_a, S.g, P.padded, S.g_ld, S.g_ld, 64));
+    HEAD_TRY(encode(&W.map_b, R.xc, P.padded, P.dim, P.ld_xc, 64));
+    W.a_mn = W.b_mn = 1;
+    W.n_tile = P.dx_n_tile;
+    W.n_tiles = P.dx_n_tiles;
+    W.k_blocks = -1;
+    W.splits = 1;
+    W.swap_order = 1;
+    O.n_prod = P.want_dw ? 2 : 1;
+    O.part = reinterpret_cast<float*>(ws + P.part);
+    O.part_ld = P.part_ld;
+    O.part_stride = P.part_stride;
+    O.part_cols = static_cast<int>(P.part_ld);
+    O.dw = a->dw;
+    O.ld_dw = a->ld_dw;
+    O.dw_fp32 = a->dw_dtype == MUON_DTYPE_FP32;
+    O.dw_add = a->dw_accumulate != 0;
+    O.dw_cols = P.dim;
+    const long long pitch = a->ld_dw * (O.dw_fp32 ? 4 : 2);
+    O.dw_vec = !misaligned(a->dw, 32) && (pitch & 31) == 0 ? 32 : (!misaligned(a->dw, 16) && (pitch & 15) == 0 ? 16 : 0);
+  }
+
+  if (P.pack)
+    HEAD_CUDA(launch_pack(static_cast<const __nv_bfloat16*>(a->w), a->ld_w, reinterpret_cast<__nv_bfloat16*>(ws + P.wc),
+                          P.ld_wc, P.vocab, P.dim, stream));
+  if (distill && P.tokens > 0) HEAD_CUDA(launch_flags(R, stream));
+  HEAD_CUDA(launch_prepare(R, distill && P.tokens > 0, stream));
+  const long long m_tiles = P.tokens > 0 ? P.padded / kTileM : 0;
+  HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, stream));
+  HEAD_CUDA(launch_finalise(R, stream));
+  if (P.grads) {
+    for (int i = 0; i < P.n_pieces; ++i) {
+      const int tile0 = i * P.piece_tiles;
+      const int tiles = P.v_tiles - tile0 < P.piece_tiles ? P.v_tiles - tile0 : P.piece_tiles;
+      const int v0 = tile0 * kTileN;
+      const int cols = P.vocab - v0 < tiles * kTileN ? P.vocab - v0 : tiles * kTileN;
+      S.v0 = v0;
+      L.b_n0 = v0;
+      L.n_tiles = tiles;
+      HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
+      O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
+      O.prod[0].b_k0 = v0;
+      O.part_add = i > 0;
+      O.prod[1].m_tiles = tiles;
+      O.dw_row0 = v0;
+      O.dw_rows = cols;
+      const long long out_tiles = (P.want_dx ? m_tiles * P.dx_n_tiles * P.splits : 0) +
+                                  (P.want_dw ? static_cast<long long>(tiles) * P.dx_n_tiles : 0);
+      HEAD_CUDA(launch_gemm(kModeOut, O, out_tiles, pairs, stream));
+    }
+    if (P.want_dx) HEAD_CUDA(launch_dx(R, stream));
+  }
+  return MUON_OK;
+}
+
+}  // namespace
+
+extern "C" int muon_head_workspace_bytes(const muon_head_args* a, int top, size_t* out_bytes) {
+  if (!out_bytes) return fail(MUON_ERR_INVALID_ARG, "out_bytes is null");
+  // top = 0: cross entropy
+  HEAD_TRY(check(a, top > 0 ? top : (top == 0 ? 1 : top), false));
+  Plan P;
+  HEAD_TRY(make_plan(a, top > 0 ? top : 1, top > 0, kPlanPairs, &P));
+  *out_bytes = P.bytes;
+  return MUON_OK;
+}
+
+extern "C" int muon_head_xent(const muon_head_args* a, const int64_t* targets, float z_loss, void* workspace,
+                              size_t workspace_bytes, int device, void* stream) {
+  HEAD_TRY(check(a, 1, true));
+  if (a->tokens > 0 && !targets) return fail(MUON_ERR_INVALID_ARG, "targets is null");
+  if (misaligned(targets, 8)) return fail(MUON_ERR_ALIGNMENT, "targets not aligned to 8 bytes");
+  if (!std::isfinite(z_loss)) return fail(MUON_ERR_INVALID_ARG, "z_loss must be finite");
+  return run(a, nullptr, targets, z_loss, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int muon_head_distill(const muon_head_args* a, const muon_head_teacher* t, void* workspace,
+                                 size_t workspace_bytes, int device, void* stream) {
+  if (!t) return fail(MUON_ERR_INVALID_ARG, "teacher is null");
+  HEAD_TRY(check(a, t->top, true));
+  if (a->tokens > 0 && (!t->top_ids || !t->top_logits)) return fail(MUON_ERR_INVALID_ARG, "top_ids or top_logits is null");
+  if (a->tokens > 0 && (t->ld_ids < t->top || t->ld_logits < t->top))
+    return fail(MUON_ERR_INVALID_ARG, "a row stride of the teacher's entries is smaller than top");
+  if (t->logits_dtype != MUON_DTYPE_BF16 && t->logits_dtype != MUON_DTYPE_FP32)
+    return fail(MUON_ERR_UNSUPPORTED, "top_logits must be bf16 or fp32");
+  if (!std::isfinite(t->temperature) || !(t->temperature > 0.f))
+    return fail(MUON_ERR_INVALID_ARG, "temperature must be finite and positive");
+  if (misaligned(t->top_ids, 8) || misaligned(t->top_logits, t->logits_dtype == MUON_DTYPE_FP32 ? 4 : 2) ||
+      misaligned(t->teacher_lse, 4))
+    return fail(MUON_ERR_ALIGNMENT, "pointer not aligned to its element size");
+  return run(a, t, nullptr, 0.f, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int muon_head_status(const void* workspace, int device, void* stream, int* device_status) {
+  if (!workspace || !device_status) return fail(MUON_ERR_INVALID_ARG, "workspace or device_status is null");
+  DeviceGuard guard;
+  HEAD_CUDA(guard.set(device));
+  Ctrl c;
+  HEAD_CUDA(cudaMemcpyAsync(&c, workspace, sizeof(c), cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream)));
+  HEAD_CUDA(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
+  *device_status = c.status;
+  return MUON_OK;
+}

@@ -1,0 +1,412 @@
+// Row kernels around the products of the LM-head losses: which tokens count and
+// their rows gathered (prepare), the softmax statistics joined into losses and
+// gradient coefficients (finalise), partial dX joined and put back in token
+// order (dx).  All of them are short streaming kernels, one warp per token.
+#include <cuda_bf16.h>
+
+#include "head.h"
+#include "ptx.cuh"
+
+namespace muon {
+namespace head {
+
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int kRowWarps = kRowThreads / 32;
+constexpr float kLn2 = 0.693147180559945309f;
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+  return v;
+}
+
+// Sum over the block in a fixed order; every thread gets it.
+template <typename T>
+__device__ __forceinline__ T block_sum(T v, T* scratch) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  __syncthreads();
+  T s = scratch[0];
+  for (int i = 1; i < kRowWarps; ++i) s += scratch[i];
+  return s;
+}
+
+__device__ __forceinline__ float teacher_logit(const RowParams& R, int t, int k) {
+  const long long at = static_cast<long long>(t) * R.ld_z + k;
+  return R.z_fp32 ? static_cast<const float*>(R.z)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(R.z)[at]);
+}
+
+__device__ __forceinline__ bool in_vocab(const RowParams& R, int64_t id) { return id >= 0 && id < R.vocab; }
+
+// Distillation: a token counts if one of its entries has an index in the
+// vocabulary and a logit above minus infinity (a NaN counts, and shows).
+__global__ void __launch_bounds__(kRowThreads) flags_kernel(const RowParams R) {
+  const int t = blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (t < R.tokens) {
+    bool any = false;
+    for (int k = lane; k < R.top; k += 32)
+      any |= in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids + k]) && !(teacher_logit(R, t, k) == -INFINITY);
+    any = __any_sync(0xFFFFFFFFu, any);
+    if (lane == 0) R.flags[t] = any;
+  }
+}
+
+// Token t counts?
+template <bool kDistill>
+__device__ __forceinline__ bool counts(const RowParams& R, int t) {
+  return kDistill ? R.flags[t] != 0 : in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids]);
+}
+
+// Gathers the rows of the tokens that count, in token order, so that masked
+// tokens cost nothing in the products and whatever they hold reaches no sum.
+// Every block counts the tokens before its own by itself (8 bytes a token out of
+// L2) instead of waiting for a scan.  Distillation: the teacher's entries become
+// probabilities, sorted by index, with the number of entries below every
+// 256-column tile, so that an epilogue finds its entries without a search.
+template <bool kDistill>
+__global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R) {
+  __shared__ int s_int[kRowWarps];
+  __shared__ float s_f[kRowWarps];
+  __shared__ int s_id[kDistill ? kRowWarps : 1][kMaxTop];
+  __shared__ int s_sorted[kDistill ? kRowWarps : 1][kMaxTop];
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int first = blockIdx.x * kRowWarps;
+
+  int before = 0, total = 0;
+  float wsum = 0.f;
+  const bool sum_weights = blockIdx.x == 0 && R.weight != nullptr;
+  for (int t = tid; t < R.tokens; t += kRowThreads) {
+    const bool c = counts<kDistill>(R, t);
+    total += c;
+    before += c && t < first;
+    if (sum_weights && c) wsum += R.weight[t];
+  }
+  total = block_sum(total, s_int);
+  before = block_sum(before, s_int);
+  if (sum_weights) wsum = block_sum(wsum, s_f);
+  if (blockIdx.x == 0 && tid == 0) {
+    const float norm = R.weight != nullptr ? wsum : static_cast<float>(total);
+    R.ctrl->status = 0;
+    R.ctrl->n_valid = total;
+    R.ctrl->ticket = 0;
+    R.ctrl->coef = !R.mean ? R.scale : (norm == 0.f ? 0.f : R.scale / norm);
+  }
+
+  const int t = first + warp;
+  const bool mine = t < R.tokens && counts<kDistill>(R, t);
+  const int peer = first + lane;
+  const unsigned ahead = __ballot_sync(0xFFFFFFFFu, lane < warp && peer < R.tokens && counts<kDistill>(R, peer));
+  const int pos = before + __popc(ahead);
+  if (t < R.tokens && lane == 0) {
+    R.pos_of[t] = mine ? pos : -1;
+    if (mine) {
+      R.row_of[pos] = t;
+    } else {
+      R.loss[t] = 0.f;
+      if (R.lse != nullptr) R.lse[t] = 0.f;
+    }
+  }
+  if (mine) {
+    const __nv_bfloat16* src = R.x + static_cast<long long>(t) * R.ld_x;
+    __nv_bfloat16* dst = R.xc + static_cast<long long>(pos) * R.ld_xc;
+    int done = 0;
+    if (R.x_vec) {
+      done = R.dim & ~7;
+      for (int c = lane * 8; c < done; c += 256)
+        *reinterpret_cast<uint4*>(dst + c) = __ldg(reinterpret_cast<const uint4*>(src + c));
+    }
+    for (int c = done + lane; c < R.dim; c += 32) dst[c] = src[c];
+
+    if (!kDistill) {
+      if (lane == 0) R.ids[pos] = static_cast<int>(R.ids_in[static_cast<long long>(t) * R.ld_ids]);
+    } else {
+      constexpr int kPer = kMaxTop / 32;
+      const int K = R.top;
+      int id[kPer];
+      float z[kPer], p[kPer];
+      float zmax = -INFINITY;
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int k = lane + 32 * i;
+        id[i] = kNoId;
+        z[i] = -INFINITY;
+        if (k < K) {
+          const int64_t raw = R.ids_in[static_cast<long long>(t) * R.ld_ids + k];
+          if (in_vocab(R, raw)) {
+            id[i] = static_cast<int>(raw);
+            z[i] = teacher_logit(R, t, k) * R.inv_t;
+            bad |= z[i] != z[i];
+          }
+          s_id[warp][k] = id[i];
+        }
+        zmax = fmaxf(zmax, z[i]);
+      }
+      zmax = warp_max(zmax);
+      bad = __any_sync(0xFFFFFFFFu, bad);
+      const float ref = R.teacher_lse != nullptr ? R.teacher_lse[t] : zmax;
+      float psum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        p[i] = id[i] == kNoId ? 0.f : expf(z[i] - ref);
+        psum += p[i];
+      }
+      psum = warp_sum(psum);
+      float log_norm = ref;  // log p = z - log_norm
+      if (R.teacher_lse == nullptr) {
+        log_norm = ref + logf(psum);
+        const float inv = 1.0f / psum;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) p[i] *= inv;
+        psum = bad ? NAN : 1.0f;
+      }
+      float h = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) h += p[i] > 0.f ? p[i] * (z[i] - log_norm) : (p[i] == 0.f ? 0.f : p[i]);
+      h = warp_sum(h);
+      __syncwarp();
+      // place of an entry = how many come before it by (index, position)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int k = lane + 32 * i;
+        if (k < K) {
+          int place = 0;
+          for (int j = 0; j < K; ++j) {
+            const int other = s_id[warp][j];
+            place += other < id[i] || (other == id[i] && j < k);
+          }
+          s_sorted[warp][place] = id[i];
+          R.ids[static_cast<long long>(pos) * K + place] = id[i];
+          R.p[static_cast<long long>(pos) * K + place] = p[i];
+        }
+      }
+      __syncwarp();
+      if (lane == 0) {
+        R.row_h[pos] = h;
+        R.row_c[pos] = psum;
+      }
+      for (int tile = lane; tile < R.n_starts; tile += 32) {
+        const long long bound = static_cast<long long>(tile) * kTileN;
+        int lo = 0, hi = K;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (s_sorted[warp][mid] < bound) lo = mid + 1;
+          else hi = mid;
+        }
+        // the last boundary lies past the vocabulary: entries that do not count stay above it
+        R.starts[static_cast<long long>(pos) * R.n_starts + tile] = static_cast<unsigned char>(lo);
+      }
+    }
+  }
+  // zero rows up to the next K block of dW's product
+  const int rows = (total + kBK - 1) / kBK * kBK;
+  for (int r = total + blockIdx.x * kRowWarps + warp; r < rows; r += gridDim.x * kRowWarps)
+    for (int c = lane; c < R.dim; c += 32) R.xc[static_cast<long long>(r) * R.ld_xc + c] = __float2bfloat16_rn(0.f);
+}
+
+// Joins a token's statistics over the vocabulary and forms, with l the scaled
+// logits, lse their log-sum-exp, p the sparse target distribution, c = sum p:
+//   loss = sum p log p - sum p (l - lse) + z_loss lse^2
+//   gradient of the raw logit: g a (c' q - p),  c' = c + 2 z_loss lse
+// row_q holds (g a c', log2-domain lse), entry_g the gradient at the entries.
+// Exponents are taken from one fused multiply-add on the raw logit, so that a
+// large logit costs a single rounding.
+template <bool kDistill>
+__global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R) {
+  __shared__ float s_f[kRowWarps];
+  __shared__ bool s_last;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_valid = R.ctrl->n_valid;
+  const float coef = R.ctrl->coef;
+  const int row = blockIdx.x * kRowWarps + warp;
+  if (row < n_valid) {
+    const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
+    float m = -INFINITY, s = 0.f;
+    for (int i = lane; i < R.stats_n; i += 32) {
+      const float2 v = st[i];
+      const float mx = fmaxf(m, v.x);
+      const float base = mx == -INFINITY ? 0.f : mx;
+      s = s * exp2f(m - base) + v.y * exp2f(v.x - base);
+      m = mx;
+    }
+    const float mx = warp_max(m);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    s = warp_sum(s * exp2f(m - base));
+    const float lse2 = base + log2f(s);
+    const float lse = lse2 * kLn2;
+    const int t = R.row_of[row];
+    const float g = coef * (R.weight != nullptr ? R.weight[t] : 1.0f);
+    const float ga = g * R.logit_scale;
+    const float c = kDistill ? R.row_c[row] : 1.0f;
+    const float cq = c + 2.0f * R.z_loss * lse;
+    float ce = 0.f;
+    if (!kDistill) {
+      const float lq2 = fmaf(R.entry_logit[row], R.scale2, -lse2);
+      ce = -lq2 * kLn2;
+      if (lane == 0) R.entry_g[row] = ga * (cq * exp2f(lq2) - 1.0f);
+    } else {
+      const int K = R.top;
+      const long long at = static_cast<long long>(row) * K;
+      for (int k = lane; k < K; k += 32) {
+        const int id = R.ids[at + k];
+        if (id != kNoId) {
+          const float lq2 = fmaf(R.entry_logit[at + k], R.scale2, -lse2);
+          const float pk = R.p[at + k];
+          ce -= pk == 0.f ? 0.f : pk * lq2 * kLn2;
+          // an index listed more than once: its entries share the gradient of the one logit
+          float pj = pk;
+          for (int j = k - 1; j >= 0 && R.ids[at + j] == id; --j) pj += R.p[at + j];
+          for (int j = k + 1; j < K && R.ids[at + j] == id; ++j) pj += R.p[at + j];
+          R.entry_g[at + k] = ga * (cq * exp2f(lq2) - pj);
+        }
+      }
+      ce = warp_sum(ce) + R.row_h[row];
+    }
+    if (lane == 0) {
+      const float loss = ce + R.z_loss * lse * lse;
+      R.loss[t] = loss;
+      if (R.lse != nullptr) R.lse[t] = lse;
+      R.row_q[row] = make_float2(ga * cq, lse2);
+      R.row_l[row] = g * loss;
+    }
+  }
+  if (R.total == nullptr) return;
+  // the last block to finish adds the tokens up, always in the same order
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) s_last = atomicAdd(&R.ctrl->ticket, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (s_last) {
+    __threadfence();
+    float sum = 0.f;
+    for (int i = threadIdx.x; i < n_valid; i += kRowThreads) sum += __ldcg(R.row_l + i);
+    sum = block_sum(sum, s_f);
+    if (threadIdx.x == 0) *R.total = sum;
+  }
+}
+
+// dX in token order: the partial sums of the token's row joined, zeros for a
+// token that does not count.  Eight columns a thread.
+__global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int per_row = (R.dim + 7) >> 3;
+  const long long n = static_cast<long long>(R.tokens) * per_row;
+  const long long i = static_cast<long long>(blockIdx.x) * kRowThreads + threadIdx.x;
+  if (i >= n) return;
+  const int t = static_cast<int>(i / per_row);
+  const int c = static_cast<int>(i - static_cast<long long>(t) * per_row) * 8;
+  const int pos = R.pos_of[t];
+  float v[8] = {};
+  if (pos >= 0) {
+    const float* src = R.part + static_cast<long long>(pos) * R.part_ld + c;
+    for (int s = 0; s < R.splits; ++s, src += R.part_stride) {
+      const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+      v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    }
+  }
+  const long long off = static_cast<long long>(t) * R.ld_dx + c;
+  if (R.dx_fp32) {
+    float* d = static_cast<float*>(R.dx) + off;
+    if (R.dx_vec && c + 8 <= R.dim) {
+      *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(d + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < R.dim) d[e] = v[e];
+    }
+  } else {
+    __nv_bfloat16* d = static_cast<__nv_bfloat16*>(R.dx) + off;
+    if (R.dx_vec && c + 8 <= R.dim) {
+      __nv_bfloat162 h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+      *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(h);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < R.dim) d[e] = __float2bfloat16_rn(v[e]);
+    }
+  }
+}
+
+// Copy of a head whose rows TMA cannot address (16-byte aligned rows) into rows
+// that it can; one warp per row.
+__global__ void __launch_bounds__(kRowThreads) pack_kernel(const __nv_bfloat16* src, long long ld_src,
+                                                           __nv_bfloat16* dst, long long ld_dst, int rows, int cols) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const long long step = static_cast<long long>(gridDim.x) * kRowWarps;
+  for (long long r = static_cast<long long>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5); r < rows; r += step) {
+    const unsigned short* s = reinterpret_cast<const unsigned short*>(src + r * ld_src);
+    uint32_t* d = reinterpret_cast<uint32_t*>(dst + r * ld_dst);
+    for (int c = lane * 2; c < cols; c += 64) {
+      const uint32_t lo = s[c], hi = c + 1 < cols ? s[c + 1] : 0u;
+      d[c >> 1] = lo | (hi << 16);
+    }
+  }
+}
+
+template <typename... Args>
+cudaError_t launch(void (*kernel)(Args...), unsigned blocks, bool overlap, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks, 1, 1);
+  cfg.blockDim = dim3(kRowThreads, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = overlap ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+unsigned row_blocks(int tokens) { return tokens > 0 ? static_cast<unsigned>((tokens + kRowWarps - 1) / kRowWarps) : 1u; }
+
+}  // namespace
+
+cudaError_t launch_flags(const RowParams& R, cudaStream_t stream) {
+  return launch(flags_kernel, row_blocks(R.tokens), false, stream, R);
+}
+
+cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream) {
+  return launch(R.z != nullptr ? prepare_kernel<true> : prepare_kernel<false>, row_blocks(R.tokens), overlap, stream, R);
+}
+
+cudaError_t launch_finalise(const RowParams& R, cudaStream_t stream) {
+  return launch(R.z != nullptr ? finalise_kernel<true> : finalise_kernel<false>, row_blocks(R.tokens), true, stream, R);
+}
+
+cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
+  const long long n = static_cast<long long>(R.tokens) * ((R.dim + 7) >> 3);
+  if (n == 0) return cudaSuccess;
+  return launch(dx_kernel, static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads), true, stream, R);
+}
+
+cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
+                        int cols, cudaStream_t stream) {
+  const long long blocks = (rows + kRowWarps - 1) / kRowWarps;
+  return launch(pack_kernel, static_cast<unsigned>(blocks < 4096 ? blocks : 4096), false, stream, src, ld_src, dst,
+                ld_dst, rows, cols);
+}
+
+}  // namespace head
+}  // namespace muon
