@@ -526,9 +526,10 @@ int muon_momentum_norm_static(const void* g, float* m, int rows, int cols, int64
  * Losses at the LM head, with their gradients.  The head is the largest matrix
  * of a model and its logits [tokens, vocab] the largest activation; these calls
  * compute a loss over the whole vocabulary, and the gradients of the hidden
- * states and of the head, without ever holding the logits: they stay in tensor
- * memory, only a bf16 gradient of one piece of the vocabulary at a time is kept
- * in the workspace.  dX goes on into the layers whose matrices muon_step
+ * states and of the head, in pieces of the vocabulary and without an array of
+ * logits: they stay in tensor memory, the workspace holds the bf16 gradient of one
+ * piece at a time (and, where it has room, pieces of logits as 16-bit codes, see
+ * muon_head_workspace_bytes).  dX goes on into the layers whose matrices muon_step
  * updates, dW to muon_adamw_step (Sec. 2.2: the LM head stays with AdamW).
  *
  *   l   = logit_scale * x w^T            (distillation: / temperature as well)
@@ -548,7 +549,7 @@ int muon_momentum_norm_static(const void* g, float* m, int rows, int cols, int64
  * and sums in fp32; the gradient of the logits is rounded to bf16 once, as an
  * operand of the products that form dX and dW, those are summed in fp32 and
  * rounded once where the output is bf16.  Results are the same bits from call to
- * call.
+ * call with the same workspace size.
  *
  *   tokens  : rows of x; 0 is allowed.  dim: columns of x and w.  vocab: rows of w.
  *   x, w    : DEVICE, bf16, row strides ld_x, ld_w elements (any stride >= dim; a
@@ -591,13 +592,18 @@ typedef struct muon_head_args {
 } muon_head_args;
 
 /*
- * Bytes of DEVICE workspace (1024-byte aligned) one call needs: pure host
- * computation on the sizes, the types, the alignment and stride of w, and which of
- * dx and dw are wanted.  top: teacher entries per token, 0 for cross entropy.
- * It stays bounded as tokens x vocab grows: the gradient of the logits takes at
- * most 1 GiB (or 256 vocabulary entries, if that is more).
+ * Bytes of DEVICE workspace (1024-byte aligned) of one call: pure host computation
+ * on the sizes, the types, the alignment and stride of w, and which of dx and dw
+ * are wanted.  top: teacher entries per token, 0 for cross entropy.
+ *   *least_bytes: what the call cannot do without (either pointer may be NULL).  It
+ *       holds the gradient of the logits of one piece of the vocabulary: at most
+ *       256 MiB, or 256 vocabulary entries if that is more.
+ *   *out_bytes: with up to 3 GiB more the call keeps the logits of as many pieces
+ *       as 16-bit codes between the pass that forms the softmax sums and the one
+ *       that forms the gradients, instead of computing them twice (a quarter of
+ *       all FLOPs).  A call uses what it is given between the two.
  */
-int muon_head_workspace_bytes(const muon_head_args* args, int top, size_t* out_bytes);
+int muon_head_workspace_bytes(const muon_head_args* args, int top, size_t* out_bytes, size_t* least_bytes);
 
 /*
  * Softmax cross entropy.  targets: DEVICE, one int64 per token; a token whose target
@@ -655,6 +661,17 @@ int muon_head_distill(const muon_head_args* args, const muon_head_teacher* teach
  * outputs are then not valid).
  */
 int muon_head_status(const void* workspace, int device, void* stream, int* device_status);
+
+/*
+ * Knobs, process-wide, read by muon_head_workspace_bytes and by every call.
+ * muon_debug_set_head_piece_bytes: bytes of logit gradients of one vocabulary
+ * piece (0 restores the default of 256 MiB); tests lower it to run several pieces
+ * on small sizes.  muon_debug_set_head_codes: 0 (default) keeps codes of logits
+ * where that is faster, 1 never, 2 always; the ways agree to rounding, not bit
+ * for bit.  Both return the previous value; a mode outside 0..2 only queries.
+ */
+size_t muon_debug_set_head_piece_bytes(size_t bytes);
+int muon_debug_set_head_codes(int mode);
 
 #ifdef __cplusplus
 }

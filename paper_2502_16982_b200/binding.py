@@ -38,6 +38,7 @@ EXPORTED = [
     "muon_profile_enable", "muon_profile_read", "muon_debug_tmem_bases",
     "muon_momentum_norm_static", "muon_adamw_step",
     "muon_head_workspace_bytes", "muon_head_xent", "muon_head_distill", "muon_head_status",
+    "muon_debug_set_head_piece_bytes", "muon_debug_set_head_codes",
 ]
 MUON_STATIC_MAX_TILES = 65536
 KERNEL_KINDS = ["momentum", "norm", "gram", "poly", "comb", "update"]
@@ -145,14 +146,17 @@ def lib():
     L.muon_debug_wait_expiry.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_uint]
     L.muon_adamw_step.argtypes = [C.POINTER(muon_adamw_tensor), C.c_int, C.POINTER(muon_adamw_hparams), C.c_int,
                                   C.c_void_p]
-    L.muon_head_workspace_bytes.argtypes = [C.POINTER(muon_head_args), C.c_int, C.POINTER(C.c_size_t)]
+    L.muon_head_workspace_bytes.argtypes = [C.POINTER(muon_head_args), C.c_int, C.POINTER(C.c_size_t),
+                                            C.POINTER(C.c_size_t)]
+    L.muon_debug_set_head_piece_bytes.argtypes = [C.c_size_t]
+    L.muon_debug_set_head_codes.argtypes = [C.c_int]
     L.muon_head_xent.argtypes = [C.POINTER(muon_head_args), C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_int,
                                  C.c_void_p]
     L.muon_head_distill.argtypes = [C.POINTER(muon_head_args), C.POINTER(muon_head_teacher), C.c_void_p, C.c_size_t,
                                     C.c_int, C.c_void_p]
     L.muon_head_status.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)]
     for name in EXPORTED:
-        if name == "muon_debug_set_chunk_bytes":
+        if name in ("muon_debug_set_chunk_bytes", "muon_debug_set_head_piece_bytes"):
             getattr(L, name).restype = C.c_size_t
         elif name != "muon_last_error":
             getattr(L, name).restype = C.c_int
@@ -368,7 +372,7 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
     if dw is not None:
         a.dw, a.ld_dw, a.dw_dtype, a.dw_accumulate = dw.data_ptr(), _row_stride(dw), _dtype_code(dw), int(bool(accumulate_dw))
     need = C.c_size_t(0)
-    _check(lib().muon_head_workspace_bytes(C.byref(a), top, C.byref(need)))
+    _check(lib().muon_head_workspace_bytes(C.byref(a), top, C.byref(need), None))
     s = torch.cuda.current_stream(dev) if stream is None else stream
     if workspace is None:
         # from the caching allocator, for the stream the kernels run on
@@ -383,16 +387,25 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
 
 
 def muon_head_workspace_bytes(tokens: int, dim: int, vocab: int, top: int = 0, dx: bool = True, dw: bool = True,
-                              packed_head: bool = True) -> int:
+                              packed_head: bool = True, least: bool = False) -> int:
     """Workspace bytes of one head-loss call (``top``: teacher entries per token, 0
-    for cross entropy), 1024 for aligning a tensor's start included.
+    for cross entropy), 1024 for aligning a tensor's start included.  ``least``: the
+    smallest workspace a call accepts instead of the one it makes full use of.
     ``packed_head``: the head's rows are 16-byte aligned."""
     ld = (dim + 7) // 8 * 8 if packed_head else dim | 1
     a = muon_head_args(tokens, dim, vocab, 1, None, None, dim, ld, MUON_DTYPE_BF16, MUON_DTYPE_BF16)
     a.dx, a.dw = (1024 if dx else None), (1024 if dw else None)  # only whether they are there counts
-    out = C.c_size_t(0)
-    _check(lib().muon_head_workspace_bytes(C.byref(a), int(top), C.byref(out)))
-    return out.value + 1024
+    out, low = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().muon_head_workspace_bytes(C.byref(a), int(top), C.byref(out), C.byref(low)))
+    return (low if least else out).value + 1024
+
+
+def muon_debug_set_head_piece_bytes(nbytes: int) -> int:
+    return lib().muon_debug_set_head_piece_bytes(int(nbytes))
+
+
+def muon_debug_set_head_codes(mode: int) -> int:
+    return lib().muon_debug_set_head_codes(int(mode))
 
 
 def muon_head_xent(x, w, targets, loss=None, lse=None, total=None, dx=None, dw=None, weight=None, mean=True,

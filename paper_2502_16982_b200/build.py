@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuon_b200.so")
 SOURCES = ["muon_api.cu", "stream_kernels.cu", "stream_tma.cu", "ns_gemm.cu", "no_alloc.cu", "adamw.cu",
            "head_api.cu", "head_gemm.cu", "head_rows.cu"]
-HEADERS = ["internal.h", "ptx.cuh", "head.h", os.path.join("..", "..", "include", "muon.h")]
+HEADERS = ["internal.h", "ptx.cuh", "head.h", "head_codes.cuh", os.path.join("..", "..", "include", "muon.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-lineinfo", "-O3", "-std=c++17",

@@ -33,10 +33,28 @@ struct Product {
   int n_tiles;
   int k_blocks;      // K blocks of 64 in all; -1: from the number of tokens that count
   int splits;        // the K blocks are cut into this many runs, each its own tile
+  int a_m0, a_k0;    // first row and K coordinate of operand A (buffer of the vocabulary piece)
   int b_k0;          // first K coordinate of operand B (vocabulary piece in W)
   int b_n0;          // first row of operand B
   int group;         // row tiles that are walked together for each column tile
   int swap_order;    // walk the column tiles innermost
+};
+
+// A piece of the vocabulary whose logits are kept as codes (head_codes.cuh), to be
+// turned into the bf16 gradient of the logits in place.
+struct ConvertParams {
+  __nv_bfloat16* g;  // [padded][ld]; NULL: nothing to convert
+  long long ld;
+  int tiles;         // 256-column tiles of the piece
+  int v_tile0;       // its first tile in the vocabulary
+  const float2* row_q;
+  const float2* stats;
+  int stats_ld;
+  int top;
+  const int* ids;
+  const float* entry_g;
+  const unsigned char* starts;
+  int n_starts;
 };
 
 enum { kModeStats = 0, kModeGrad = 1, kModeOut = 2 };
@@ -61,6 +79,13 @@ struct GemmParams {
   const float* entry_g;  // [rows][top]: gradient of the logit at the entry
   __nv_bfloat16* g;      // [padded rows][g_ld]: gradient of the logits of one vocabulary piece
   long long g_ld;
+  // statistics: codes of the logits of the first `code_tiles` tiles, in pieces of
+  // piece_tiles tiles, piece_stride elements apart, rows g_ld apart
+  unsigned short* codes;
+  int code_tiles, piece_tiles;
+  long long piece_stride;
+  // outputs: the next piece's codes are converted while the products run
+  ConvertParams convert;
 
   // product 0 of kModeOut: partial dX
   float* part;        // [splits][padded rows][part_ld]
@@ -79,6 +104,8 @@ struct RowParams {
   int tokens, padded, dim, vocab;
   const __nv_bfloat16* x;
   long long ld_x;
+  const __nv_bfloat16* w;  // head with 16-byte aligned rows
+  long long ld_w;
   __nv_bfloat16* xc;     // [padded][ld_xc] rows of the tokens that count, then zeros
   long long ld_xc;
   int x_vec;             // rows can be copied in 16-byte pieces
@@ -130,6 +157,7 @@ cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
 cudaError_t launch_finalise(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_convert(const ConvertParams& C, const Ctrl* ctrl, int max_rows, int sms, cudaStream_t stream);
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
                         int cols, cudaStream_t stream);

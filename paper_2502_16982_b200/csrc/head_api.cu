@@ -30,8 +30,13 @@ int fail(int code, const char* fmt, ...) {
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
 
-// Bytes of logit gradients (bf16) that one vocabulary piece may take.
-constexpr long long kPieceBytes = 1ll << 30;
+// Bytes of logit gradients (bf16) that one vocabulary piece takes, at most, and of
+// the pieces together whose logits are kept as codes in the workspace that
+// muon_head_workspace_bytes asks for.
+constexpr long long kPieceBytes = 1ll << 28;
+constexpr long long kCodeBytes = 3ll << 30;
+long long g_piece_bytes = kPieceBytes;
+int g_codes = 0;
 // Bytes of partial dX that splitting its long axis may take.
 constexpr long long kPartBytes = 1ll << 28;
 
@@ -40,10 +45,11 @@ struct Plan {
   bool want_dx, want_dw, grads, distill, pack;
   int v_tiles;               // 256-column tiles of the vocabulary
   int piece_tiles, n_pieces;
+  int n_stored, n_buffers;   // pieces kept as codes; piece buffers in the workspace
   int splits, dx_n_tile, dx_n_tiles;
   long long ld_xc, ld_wc, part_ld, part_stride;
   size_t ctrl, xc, wc, flags, pos_of, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
-      part, bytes;
+      part, bytes, least;
 };
 
 // How many runs the K blocks of dX's tiles are cut into.  dX has few tiles with
@@ -73,7 +79,15 @@ int choose_splits(int dx_tiles, int dx_kb, int dw_tiles, int dw_kb, int pairs, i
   return best;
 }
 
-int make_plan(const muon_head_args* a, int top, bool distill, int pairs, Plan* P) {
+// Codes or a second product x w^T?  The second product costs 2 dim FLOPs for every
+// logit, the codes 2 bytes written and 4 bytes of conversion.
+bool want_codes(int tokens, int dim) {
+  if (g_codes != 0) return g_codes == 2;
+  return dim >= 768 || dim >= 2 * tokens;
+}
+
+// `room`: bytes of workspace to plan for; 0 plans for as many as are useful.
+int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t room, Plan* P) {
   P->tokens = a->tokens;
   P->dim = a->dim;
   P->vocab = a->vocab;
@@ -90,7 +104,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, Plan* P
   P->part_ld = round_up(a->dim, 8);
   P->part_stride = P->padded * P->part_ld;
 
-  long long tiles = kPieceBytes / (2ll * P->padded * kTileN);
+  long long tiles = g_piece_bytes / (2ll * P->padded * kTileN);
   if (tiles < 1) tiles = 1;
   if (tiles > P->v_tiles) tiles = P->v_tiles;
   P->n_pieces = static_cast<int>((P->v_tiles + tiles - 1) / tiles);
@@ -134,8 +148,20 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, Plan* P
     P->starts = take(rows * (P->v_tiles + 1));
   }
   if (P->pack) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
-  if (P->grads) P->g = take(rows * P->piece_tiles * kTileN * 2);
   if (P->want_dx) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
+  P->n_stored = P->n_buffers = 0;
+  P->least = off;
+  if (P->grads) {
+    const long long one = static_cast<long long>(rows) * P->piece_tiles * kTileN * 2;
+    P->n_buffers = 1;
+    if (want_codes(P->tokens, P->dim)) {
+      long long fit = (room ? static_cast<long long>(room) - static_cast<long long>(off) : kCodeBytes) / one;
+      P->n_buffers = static_cast<int>(fit < 1 ? 1 : (fit > P->n_pieces ? P->n_pieces : fit));
+      P->n_stored = P->n_buffers;
+    }
+    P->least = off + static_cast<size_t>(round_up(one, 1024));
+    P->g = take(static_cast<size_t>(one) * P->n_buffers);
+  }
   P->bytes = off;
   return MUON_OK;
 }
@@ -247,15 +273,21 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   const bool distill = t != nullptr;
   const int top = distill ? t->top : 1;
   Plan P;
-  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, &P));
-  if (!workspace || workspace_bytes < P.bytes || misaligned(workspace, 1024))
-    return fail(MUON_ERR_WORKSPACE, "workspace: need %zu bytes, 1024-byte aligned", P.bytes);
+  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, workspace_bytes ? workspace_bytes : 1, &P));
+  if (!workspace || workspace_bytes < P.least || misaligned(workspace, 1024))
+    return fail(MUON_ERR_WORKSPACE, "workspace: need at least %zu bytes, 1024-byte aligned", P.least);
   DeviceGuard guard;
   HEAD_CUDA(guard.set(device));
   int pairs = 0;
   HEAD_TRY(device_pairs(device, &pairs));
 
   char* ws = static_cast<char*>(workspace);
+  const void* w = a->w;
+  long long ld_w = a->ld_w;
+  if (P.pack) {
+    w = ws + P.wc;
+    ld_w = P.ld_wc;
+  }
   const float logit_scale = distill ? a->logit_scale / t->temperature : a->logit_scale;
 
   RowParams R = {};
@@ -266,6 +298,8 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.vocab = P.vocab;
   R.x = static_cast<const __nv_bfloat16*>(a->x);
   R.ld_x = a->ld_x;
+  R.w = static_cast<const __nv_bfloat16*>(w);
+  R.ld_w = ld_w;
   R.xc = reinterpret_cast<__nv_bfloat16*>(ws + P.xc);
   R.ld_xc = P.ld_xc;
   R.x_vec = !misaligned(a->x, 16) && (a->ld_x & 7) == 0;
@@ -310,13 +344,6 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.dx_fp32 = a->dx_dtype == MUON_DTYPE_FP32;
   R.dx_vec = !misaligned(a->dx, 16) && (a->ld_dx & (R.dx_fp32 ? 3 : 7)) == 0;
 
-  const void* w = a->w;
-  long long ld_w = a->ld_w;
-  if (P.pack) {
-    w = ws + P.wc;
-    ld_w = P.ld_wc;
-  }
-
   GemmParams S = {};
   S.n_prod = 1;
   S.ctrl = R.ctrl;
@@ -333,6 +360,10 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   S.entry_g = R.entry_g;
   S.g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
   S.g_ld = static_cast<long long>(P.piece_tiles) * kTileN;
+  S.codes = reinterpret_cast<unsigned short*>(S.g);
+  S.piece_tiles = P.piece_tiles;
+  S.piece_stride = P.padded * S.g_ld;
+  S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
   Product& L = S.prod[0];  // logits: tokens x vocabulary
   HEAD_TRY(encode(&L.map_a, R.xc, P.padded, P.dim, P.ld_xc, 128));
   HEAD_TRY(encode(&L.map_b, w, P.vocab, P.dim, ld_w, 128));
@@ -348,7 +379,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     O.n_prod = 0;
     Product& X = O.prod[0];  // dX: tokens x dim, over the vocabulary piece
     X = Product{};
-    HEAD_TRY(encode(&X.map_a, S.g, P.padded, S.g_ld, S.g_ld, 128));
+    HEAD_TRY(encode(&X.map_a, S.g, static_cast<long long>(P.padded) * P.n_buffers, S.g_ld, S.g_ld, 128));
     HEAD_TRY(encode(&X.map_b, w, P.vocab, P.dim, ld_w, 64));
     X.b_mn = 1;
     X.n_tile = P.dx_n_tile;
@@ -358,7 +389,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     X.swap_order = 1;
     Product& W = O.prod[1];  // dW: vocabulary piece x dim, over the tokens
     W = Product{};
-    HEAD_TRY(encode(&W.map_a, S.g, P.padded, S.g_ld, S.g_ld, 64));
+    HEAD_TRY(encode(&W.map_a, S.g, static_cast<long long>(P.padded) * P.n_buffers, S.g_ld, S.g_ld, 64));
     HEAD_TRY(encode(&W.map_b, R.xc, P.padded, P.dim, P.ld_xc, 64));
     W.a_mn = W.b_mn = 1;
     W.n_tile = P.dx_n_tile;
@@ -389,18 +420,48 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, stream));
   HEAD_CUDA(launch_finalise(R, stream));
   if (P.grads) {
+    ConvertParams C = {};
+    C.ld = S.g_ld;
+    C.row_q = R.row_q;
+    C.stats = R.stats;
+    C.stats_ld = R.stats_ld;
+    C.top = top;
+    C.ids = R.ids;
+    C.entry_g = R.entry_g;
+    C.starts = R.starts;
+    C.n_starts = R.n_starts;
+    auto tiles_of = [&](int piece) {
+      const int left = P.v_tiles - piece * P.piece_tiles;
+      return left < P.piece_tiles ? left : P.piece_tiles;
+    };
+    auto codes_of = [&](int piece) {
+      C.g = S.g + piece * S.piece_stride;
+      C.tiles = tiles_of(piece);
+      C.v_tile0 = piece * P.piece_tiles;
+      return C;
+    };
     for (int i = 0; i < P.n_pieces; ++i) {
-      const int tile0 = i * P.piece_tiles;
-      const int tiles = P.v_tiles - tile0 < P.piece_tiles ? P.v_tiles - tile0 : P.piece_tiles;
-      const int v0 = tile0 * kTileN;
+      // stored pieces lie in a buffer each, the others use the first one after them
+      const bool stored = i < P.n_stored;
+      const int buffer = stored ? i : 0;
+      const int tiles = tiles_of(i);
+      const int v0 = i * P.piece_tiles * kTileN;
       const int cols = P.vocab - v0 < tiles * kTileN ? P.vocab - v0 : tiles * kTileN;
-      S.v0 = v0;
-      L.b_n0 = v0;
-      L.n_tiles = tiles;
-      HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
+      if (stored) {
+        if (i == 0) HEAD_CUDA(launch_convert(codes_of(0), R.ctrl, P.padded, 2 * pairs, stream));
+      } else {
+        S.v0 = v0;
+        L.b_n0 = v0;
+        L.n_tiles = tiles;
+        HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
+      }
+      O.convert = ConvertParams{};
+      if (i + 1 < P.n_stored) O.convert = codes_of(i + 1);
+      O.prod[0].a_m0 = buffer * P.padded;
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;
       O.part_add = i > 0;
+      O.prod[1].a_k0 = buffer * P.padded;
       O.prod[1].m_tiles = tiles;
       O.dw_row0 = v0;
       O.dw_rows = cols;
@@ -415,14 +476,27 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
 
 }  // namespace
 
-extern "C" int muon_head_workspace_bytes(const muon_head_args* a, int top, size_t* out_bytes) {
-  if (!out_bytes) return fail(MUON_ERR_INVALID_ARG, "out_bytes is null");
+extern "C" int muon_head_workspace_bytes(const muon_head_args* a, int top, size_t* out_bytes, size_t* least_bytes) {
+  if (!out_bytes && !least_bytes) return fail(MUON_ERR_INVALID_ARG, "out_bytes and least_bytes are null");
   // top = 0: cross entropy
   HEAD_TRY(check(a, top > 0 ? top : (top == 0 ? 1 : top), false));
   Plan P;
-  HEAD_TRY(make_plan(a, top > 0 ? top : 1, top > 0, kPlanPairs, &P));
-  *out_bytes = P.bytes;
+  HEAD_TRY(make_plan(a, top > 0 ? top : 1, top > 0, kPlanPairs, 0, &P));
+  if (out_bytes) *out_bytes = P.bytes;
+  if (least_bytes) *least_bytes = P.least;
   return MUON_OK;
+}
+
+extern "C" size_t muon_debug_set_head_piece_bytes(size_t bytes) {
+  const size_t before = static_cast<size_t>(g_piece_bytes);
+  g_piece_bytes = bytes ? static_cast<long long>(bytes) : kPieceBytes;
+  return before;
+}
+
+extern "C" int muon_debug_set_head_codes(int mode) {
+  const int before = g_codes;
+  if (mode >= 0 && mode <= 2) g_codes = mode;
+  return before;
 }
 
 extern "C" int muon_head_xent(const muon_head_args* a, const int64_t* targets, float z_loss, void* workspace,

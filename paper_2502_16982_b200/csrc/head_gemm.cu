@@ -11,14 +11,16 @@
 //   warp 0     TMA producer: this CTA's 128 rows of A and its half of B per K
 //              block, into a ring of kStages; no multicast
 //   warp 1     leader CTA only: UMMA issuer, two TMEM accumulator stages
-//   warps 2-5  epilogue: lane = row of the tile, so that a row's running maximum
-//              and sum stay in one thread's registers
+//   warps 2-5  epilogue: lane = row of the tile, so that a row's maximum and sum
+//              stay in one thread's registers
+//   warps 6-9  outputs only: turn the next piece's codes (head_codes.cuh) into the
+//              gradient of its logits while the tensor cores work on this piece
 //
 // Every wait is bounded (ptx::mbar_wait); on expiry the CTA records
 // MUON_ERR_TIMEOUT, all roles drain and the kernel returns.
 #include <cuda_bf16.h>
 
-#include "head.h"
+#include "head_codes.cuh"
 #include "ptx.cuh"
 
 namespace muon {
@@ -26,7 +28,8 @@ namespace head {
 
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kConvertWarps = 4;
+constexpr int threads_of(int mode) { return mode == kModeOut ? 192 + 32 * kConvertWarps : 192; }
 constexpr int kStages = 6;
 constexpr int kTileABytes = 128 * kBK * 2;
 constexpr int kTileBBytes = 128 * kBK * 2;
@@ -53,12 +56,6 @@ __device__ __forceinline__ void report_timeout(const GemmParams& P) { atomicExch
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&h);
-}
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 
 __device__ __forceinline__ void st_global_32(void* dst, const uint32_t (&v)[8]) {
@@ -157,7 +154,7 @@ struct Entries {
 };
 
 template <int kMode>
-__global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_constant__ GemmParams P) {
+__global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const __grid_constant__ GemmParams P) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -218,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
       const Tile tl = locate(P, s0, s1, t);
       const Product& pr = P.prod[tl.prod];
       const int half_n = pr.n_tile >> 1;
-      const int a_row = tl.mi * kTileM + static_cast<int>(rank) * 128;
+      const int a_row = pr.a_m0 + tl.mi * kTileM + static_cast<int>(rank) * 128;
       const int b_row = pr.b_n0 + tl.ni * pr.n_tile + static_cast<int>(rank) * half_n;
       const uint32_t stage_tx = 2u * static_cast<uint32_t>(kTileABytes + half_n * 128);
       const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
@@ -233,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
           const uint32_t leader_full = leader_full0 + stage * 8;
           const uint32_t sa = ring_u32 + stage * kStageBytes;
           const uint32_t sb = sa + kTileABytes;
-          const int ka = kb * kBK, kbb = pr.b_k0 + kb * kBK;
+          const int ka = pr.a_k0 + kb * kBK, kbb = pr.b_k0 + kb * kBK;
           if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + stage * 8, stage_tx);
           if (!a_mn) {
             ptx::tma_load_3d_pair(sa, &pr.map_a, ka, a_row, 0, leader_full);
@@ -323,6 +320,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         }
       }
     }
+  } else if (kMode == kModeOut && warp >= 6) {
+    // ---------------------------------- codes of the next piece, meanwhile ----
+    if (P.convert.g != nullptr)
+      convert_piece(P.convert, n_valid, static_cast<int>(blockIdx.x) * kConvertWarps + warp - 6,
+                    static_cast<int>(gridDim.x) * kConvertWarps, lane);
   } else {
     // ----------------------------------------------------------- epilogue ----
     const int q = warp & 3;  // TMEM lane quarter this warp may read
@@ -351,7 +353,46 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         if (__any_sync(0xFFFFFFFFu, row_ok)) {
           Entries en;
           en.open(P, row, c0, row_ok);
-          float m = -INFINITY, s = 0.f;
+          // the row's maximum over the tile first, then exponentials and codes against it
+          float m = -INFINITY;
+          {
+            uint32_t va[32], vb[32];
+            auto top_of = [&](const uint32_t (&v)[32], int c) {
+              if (limit < c + 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (c + i < limit) m = fmaxf(m, __uint_as_float(v[i]));
+              } else {
+                float a = __uint_as_float(v[0]), b = __uint_as_float(v[1]);
+#pragma unroll
+                for (int i = 2; i < 32; i += 2) {
+                  a = fmaxf(a, __uint_as_float(v[i]));
+                  b = fmaxf(b, __uint_as_float(v[i + 1]));
+                }
+                m = fmaxf(m, fmaxf(a, b));
+              }
+            };
+            ptx::tmem_ld_32x32(taddr, va);
+            ptx::tmem_ld_wait();
+#pragma unroll 1
+            for (int c = 0; c < kTileN; c += 64) {
+              ptx::tmem_ld_32x32(taddr + c + 32, vb);
+              top_of(va, c);
+              ptx::tmem_ld_wait();
+              if (c + 64 < kTileN) ptx::tmem_ld_32x32(taddr + c + 64, va);
+              top_of(vb, c + 32);
+              ptx::tmem_ld_wait();
+            }
+          }
+          m *= P.scale2;
+          const float base = m == -INFINITY ? 0.f : m;  // nothing but -inf
+          unsigned short* crow = nullptr;
+          if (tl.ni < P.code_tiles && row_ok) {
+            const int piece = tl.ni / P.piece_tiles;
+            crow = P.codes + piece * P.piece_stride + static_cast<long long>(row) * P.g_ld +
+                   (tl.ni - piece * P.piece_tiles) * kTileN;
+          }
+          float s = 0.f;
           auto chunk = [&](uint32_t (&v)[32], int c) {
             // logits of entries that lie in these 32 columns
             while (__any_sync(0xFFFFFFFFu, en.col - c < 32)) {
@@ -366,22 +407,28 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
               for (int i = 0; i < 32; ++i)
                 if (c + i >= limit) v[i] = 0xFF800000u;  // -inf
             }
-            float mx = __uint_as_float(v[0]);
-#pragma unroll
-            for (int i = 1; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(v[i]));
-            mx = fmaxf(m, mx * P.scale2);
-            const float base = mx == -INFINITY ? 0.f : mx;  // nothing but -inf so far
-            s *= ex2(m - base);
-            m = mx;
             float s0_ = 0.f, s1_ = 0.f, s2_ = 0.f, s3_ = 0.f;
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
-              s0_ += ex2(fmaf(__uint_as_float(v[i]), P.scale2, -base));
-              s1_ += ex2(fmaf(__uint_as_float(v[i + 1]), P.scale2, -base));
-              s2_ += ex2(fmaf(__uint_as_float(v[i + 2]), P.scale2, -base));
-              s3_ += ex2(fmaf(__uint_as_float(v[i + 3]), P.scale2, -base));
+              const float y0 = fmaf(__uint_as_float(v[i]), P.scale2, -base);
+              const float y1 = fmaf(__uint_as_float(v[i + 1]), P.scale2, -base);
+              const float y2 = fmaf(__uint_as_float(v[i + 2]), P.scale2, -base);
+              const float y3 = fmaf(__uint_as_float(v[i + 3]), P.scale2, -base);
+              s0_ += ex2_fast(y0);
+              s1_ += ex2_fast(y1);
+              s2_ += ex2_fast(y2);
+              s3_ += ex2_fast(y3);
+              v[i >> 1] = __byte_perm(encode_logit(y0), encode_logit(y1), 0x5410);
+              v[(i >> 1) + 1] = __byte_perm(encode_logit(y2), encode_logit(y3), 0x5410);
             }
             s += (s0_ + s1_) + (s2_ + s3_);
+            if (crow != nullptr) {
+              const uint32_t lo[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+              const uint32_t hi[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
+              st_global_32(crow + c, lo);
+              st_global_32(crow + c + 16, hi);
+            }
+            __syncwarp();
           };
           uint32_t va[32], vb[32];
           ptx::tmem_ld_32x32(taddr, va);
@@ -410,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_gemm_kernel(const __grid_con
         auto chunk = [&](uint32_t (&v)[32], int c) {
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            float y = rq.x * ex2(fmaf(__uint_as_float(v[i]), P.scale2, -rq.y));
+            float y = rq.x * ex2_fast(fmaf(__uint_as_float(v[i]), P.scale2, -rq.y));
             v[i] = __float_as_uint(y);
           }
           if (!row_ok) {
@@ -586,7 +633,7 @@ template <int kMode>
 cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * clusters, 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(threads_of(kMode), 1, 1);
   cfg.dynamicSmemBytes = kSmemBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -614,7 +661,7 @@ cudaError_t gemm_configure() {
 cudaError_t gemm_max_clusters(int* out) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2, 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(threads_of(kModeOut), 1, 1);
   cfg.dynamicSmemBytes = kSmemBytes;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;

@@ -4,7 +4,7 @@
 // order (dx).  All of them are short streaming kernels, one warp per token.
 #include <cuda_bf16.h>
 
-#include "head.h"
+#include "head_codes.cuh"
 #include "ptx.cuh"
 
 namespace muon {
@@ -217,6 +217,30 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
     for (int c = lane; c < R.dim; c += 32) R.xc[static_cast<long long>(r) * R.ld_xc + c] = __float2bfloat16_rn(0.f);
 }
 
+// Entries with at least this share of the distribution get their logits again in
+// plain fp32: at most 16 a token, two or three in practice.  The rounding of the
+// others' logits reaches the loss through a sixteenth or less of the mass, about
+// what fp32 sums leave anyway; recomputing every entry would read top rows of w a
+// token (1 GB for 4096 tokens, 64 entries and 2048 columns).
+constexpr float kExactMass = 1.0f / 16.0f;
+
+// x . w in fp32 by one warp; both rows 16-byte aligned.  Every lane gets the sum.
+__device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfloat16* w, int dim, int lane) {
+  float a = 0.f, b = 0.f;
+  const int whole = dim & ~7;
+  for (int c = lane * 8; c < whole; c += 256) {
+    const uint4 u = *reinterpret_cast<const uint4*>(x + c), v = __ldg(reinterpret_cast<const uint4*>(w + c));
+    const uint32_t uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a = fmaf(__uint_as_float(uu[e] << 16), __uint_as_float(vv[e] << 16), a);
+      b = fmaf(__uint_as_float(uu[e] & 0xFFFF0000u), __uint_as_float(vv[e] & 0xFFFF0000u), b);
+    }
+  }
+  if (whole + lane < dim) a = fmaf(__bfloat162float(x[whole + lane]), __bfloat162float(w[whole + lane]), a);
+  return warp_sum(a + b);
+}
+
 // Joins a token's statistics over the vocabulary and forms, with l the scaled
 // logits, lse their log-sum-exp, p the sparse target distribution, c = sum p:
 //   loss = sum p log p - sum p (l - lse) + z_loss lse^2
@@ -247,36 +271,66 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     const float mx = warp_max(m);
     const float base = mx == -INFINITY ? 0.f : mx;
     s = warp_sum(s * exp2f(m - base));
-    const float lse2 = base + log2f(s);
-    const float lse = lse2 * kLn2;
     const int t = R.row_of[row];
     const float g = coef * (R.weight != nullptr ? R.weight[t] : 1.0f);
     const float ga = g * R.logit_scale;
     const float c = kDistill ? R.row_c[row] : 1.0f;
+    constexpr int kPer = kDistill ? kMaxTop / 32 : 1;
+    const int K = kDistill ? R.top : 1;
+    const long long at = static_cast<long long>(row) * K;
+    int id[kPer];
+    float raw[kPer], p[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int k = lane + 32 * i;
+      id[i] = k < K ? R.ids[at + k] : kNoId;
+      raw[i] = id[i] != kNoId ? R.entry_logit[at + k] : 0.f;
+      p[i] = id[i] != kNoId ? (kDistill ? R.p[at + k] : 1.0f) : 0.f;
+    }
+    // The logits that carry the loss, again as plain fp32 dot products, and the
+    // softmax sum with them in place of the tensor cores' values: the tensor cores
+    // truncate at every step of 16 products, which shifts a logit of 15 over 2048
+    // columns by about 1e-5.
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      unsigned todo = __ballot_sync(0xFFFFFFFFu, p[i] >= kExactMass);
+      while (todo) {
+        const int src = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const int which = __shfl_sync(0xFFFFFFFFu, id[i], src);
+        const float exact = warp_dot(R.xc + static_cast<long long>(row) * R.ld_xc,
+                                     R.w + static_cast<long long>(which) * R.ld_w, R.dim, lane);
+        const float was = __shfl_sync(0xFFFFFFFFu, raw[i], src);
+        bool again = false;  // an index listed more than once is one logit
+        if (kDistill) {
+          const int k = src + 32 * i;
+          for (int j = k - 1; j >= 0 && R.ids[at + j] == which; --j) again |= R.p[at + j] >= kExactMass;
+        }
+        if (!again) s += exp2f(fmaf(exact, R.scale2, -base)) - exp2f(fmaf(was, R.scale2, -base));
+        if (lane == src) raw[i] = exact;
+      }
+    }
+    const float lse2 = base + log2f(s);
+    const float lse = lse2 * kLn2;
     const float cq = c + 2.0f * R.z_loss * lse;
     float ce = 0.f;
-    if (!kDistill) {
-      const float lq2 = fmaf(R.entry_logit[row], R.scale2, -lse2);
-      ce = -lq2 * kLn2;
-      if (lane == 0) R.entry_g[row] = ga * (cq * exp2f(lq2) - 1.0f);
-    } else {
-      const int K = R.top;
-      const long long at = static_cast<long long>(row) * K;
-      for (int k = lane; k < K; k += 32) {
-        const int id = R.ids[at + k];
-        if (id != kNoId) {
-          const float lq2 = fmaf(R.entry_logit[at + k], R.scale2, -lse2);
-          const float pk = R.p[at + k];
-          ce -= pk == 0.f ? 0.f : pk * lq2 * kLn2;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int k = lane + 32 * i;
+      if (id[i] != kNoId) {
+        const float lq2 = fmaf(raw[i], R.scale2, -lse2);
+        ce -= p[i] == 0.f ? 0.f : p[i] * lq2 * kLn2;
+        float pj = p[i];
+        if (kDistill) {
           // an index listed more than once: its entries share the gradient of the one logit
-          float pj = pk;
-          for (int j = k - 1; j >= 0 && R.ids[at + j] == id; --j) pj += R.p[at + j];
-          for (int j = k + 1; j < K && R.ids[at + j] == id; ++j) pj += R.p[at + j];
-          R.entry_g[at + k] = ga * (cq * exp2f(lq2) - pj);
+          for (int j = k - 1; j >= 0 && R.ids[at + j] == id[i]; --j) pj += R.p[at + j];
+          for (int j = k + 1; j < K && R.ids[at + j] == id[i]; ++j) pj += R.p[at + j];
         }
+        R.entry_g[at + k] = ga * (cq * exp2f(lq2) - pj);
       }
-      ce = warp_sum(ce) + R.row_h[row];
     }
+    ce = warp_sum(ce);
+    if (kDistill) ce += R.row_h[row];
     if (lane == 0) {
       const float loss = ce + R.z_loss * lse * lse;
       R.loss[t] = loss;
@@ -298,6 +352,15 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     sum = block_sum(sum, s_f);
     if (threadIdx.x == 0) *R.total = sum;
   }
+}
+
+// The first stored piece's codes; those of the later ones are converted beside the
+// products (head_gemm.cu).
+__global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParams C, const Ctrl* ctrl) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  convert_piece(C, ctrl->n_valid, static_cast<int>(blockIdx.x) * kRowWarps + static_cast<int>(threadIdx.x >> 5),
+                static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
 }
 
 // dX in token order: the partial sums of the token's row joined, zeros for a
@@ -393,6 +456,12 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
 
 cudaError_t launch_finalise(const RowParams& R, cudaStream_t stream) {
   return launch(R.z != nullptr ? finalise_kernel<true> : finalise_kernel<false>, row_blocks(R.tokens), true, stream, R);
+}
+
+cudaError_t launch_convert(const ConvertParams& C, const Ctrl* ctrl, int max_rows, int sms, cudaStream_t stream) {
+  const long long tasks = static_cast<long long>(max_rows) * ((C.tiles + kConvertTiles - 1) / kConvertTiles);
+  const long long blocks = (tasks + kRowWarps - 1) / kRowWarps, most = 8ll * sms;
+  return launch(convert_kernel, static_cast<unsigned>(blocks < most ? blocks : most), true, stream, C, ctrl);
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
