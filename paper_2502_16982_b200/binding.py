@@ -8,6 +8,7 @@ usual init / step / status / destroy life cycle.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -308,6 +309,9 @@ def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, 
     _check(lib().muon_adamw_step(arr, n, C.byref(hp), dev, C.c_void_p(s.cuda_stream)))
 
 
+_no_context = contextlib.nullcontext()
+
+
 class HeadLoss(NamedTuple):
     """What a head loss gives: per-token ``loss`` and ``lse`` (fp32), ``total`` (one
     fp32 element), the gradients of ``total`` (None where not asked for) and the
@@ -324,65 +328,83 @@ def _row_stride(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
+_head_bytes = {}  # workspace bytes of a plan, by everything the plan depends on
+
+
+def _raw_stream(stream, dev):
+    import torch
+    if stream is not None:
+        return stream.cuda_stream
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # a tenth of the cost of building a Stream object
+    return get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _head_vector(t, what, n, dev):
+    import torch
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != dev:
+        raise MuonError(MUON_ERR_INVALID_ARG, "%s must be %d contiguous fp32 values on x's device" % (what, n))
+    return t
+
+
+def _head_matrix(t, what, shape, dev):
+    if t.shape != shape or (shape[1] > 1 and t.stride(1) != 1) or t.device != dev:
+        raise MuonError(MUON_ERR_INVALID_ARG, "%s must be shaped like its tensor, with contiguous rows, on x's device" % what)
+    return t
+
+
 def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace, stream,
                call):
     """Checks, outputs and workspace shared by the head losses; ``call(args,
-    workspace pointer, bytes, device, stream)`` makes the C call."""
+    workspace address, bytes, device, stream)`` makes the C call."""
     import torch
     if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.shape[1] < 1 or w.shape[0] < 1:
         raise MuonError(MUON_ERR_INVALID_ARG, "x must be [tokens, dim] and w [vocab, dim]")
-    if not x.is_cuda or x.device != w.device:
-        raise MuonError(MUON_ERR_INVALID_ARG, "x and w must be on one CUDA device")
-    tokens, dim = x.shape
     dev = x.device
-
-    def rows_contiguous(t):
-        return t.shape[1] == 1 or t.stride(1) == 1
-
-    def vector(t, what, n=tokens, new=False):
-        if t is None:
-            return torch.empty(n, dtype=torch.float32, device=dev) if new else None
-        if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.device != dev:
-            raise MuonError(MUON_ERR_INVALID_ARG, "%s must be %d contiguous fp32 values on x's device" % (what, n))
-        return t
-
-    def grad(t, like, what):
-        if t is None or t is False:
-            return None
-        if t is True:
-            return torch.empty(like.shape, dtype=like.dtype, device=dev)
-        if t.shape != like.shape or not rows_contiguous(t) or t.device != dev:
-            raise MuonError(MUON_ERR_INVALID_ARG, "%s must be shaped like its tensor, rows contiguous" % what)
-        return t
-
-    for t, what in ((x, "x"), (w, "w")):
-        if not rows_contiguous(t):
-            raise MuonError(MUON_ERR_INVALID_ARG, "%s must have contiguous rows" % what)
+    if dev.type != "cuda" or w.device != dev:
+        raise MuonError(MUON_ERR_INVALID_ARG, "x and w must be on one CUDA device")
+    (tokens, dim), vocab = x.shape, w.shape[0]
+    if dim > 1 and (x.stride(1) != 1 or w.stride(1) != 1):
+        raise MuonError(MUON_ERR_INVALID_ARG, "x and w must have contiguous rows")
     if accumulate_dw and not isinstance(dw, torch.Tensor):
         raise MuonError(MUON_ERR_INVALID_ARG, "accumulate_dw needs the dw to add to")
-    loss, lse = vector(loss, "loss", new=True), vector(lse, "lse", new=True)
-    total = vector(total, "total", 1, new=True)
-    weight = vector(weight, "weight")
-    dx, dw = grad(dx, x, "dx"), grad(dw, w, "dw")
-    a = muon_head_args(tokens, dim, w.shape[0], int(bool(mean)), x.data_ptr(), w.data_ptr(), _row_stride(x) if tokens else dim,
-                       _row_stride(w), _dtype_code(x), _dtype_code(w), None if weight is None else weight.data_ptr(),
-                       float(scale), float(logit_scale), loss.data_ptr(), lse.data_ptr(), total.data_ptr())
-    if dx is not None:
-        a.dx, a.ld_dx, a.dx_dtype = dx.data_ptr(), _row_stride(dx) if tokens else dim, _dtype_code(dx)
-    if dw is not None:
-        a.dw, a.ld_dw, a.dw_dtype, a.dw_accumulate = dw.data_ptr(), _row_stride(dw), _dtype_code(dw), int(bool(accumulate_dw))
-    need = C.c_size_t(0)
-    _check(lib().muon_head_workspace_bytes(C.byref(a), top, C.byref(need), None))
-    s = torch.cuda.current_stream(dev) if stream is None else stream
-    if workspace is None:
-        # from the caching allocator, for the stream the kernels run on
-        with torch.cuda.stream(s):
-            workspace = torch.empty(need.value + 1024, dtype=torch.uint8, device=dev)
-    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
-        raise MuonError(MUON_ERR_WORKSPACE, "workspace must be a contiguous uint8 tensor on x's device")
-    base = (workspace.data_ptr() + 1023) // 1024 * 1024
-    room = workspace.data_ptr() + workspace.numel() - base
-    _check(call(C.byref(a), C.c_void_p(base), max(room, 0), dev.index, C.c_void_p(s.cuda_stream)))
+    empty, f32 = torch.empty, torch.float32
+    # allocated for the stream the kernels run on
+    with torch.cuda.stream(stream) if stream is not None else _no_context:
+        loss = empty(tokens, dtype=f32, device=dev) if loss is None else _head_vector(loss, "loss", tokens, dev)
+        lse = empty(tokens, dtype=f32, device=dev) if lse is None else _head_vector(lse, "lse", tokens, dev)
+        total = empty(1, dtype=f32, device=dev) if total is None else _head_vector(total, "total", 1, dev)
+        if dx is False:
+            dx = None
+        elif dx is not None:
+            dx = empty(x.shape, dtype=x.dtype, device=dev) if dx is True else _head_matrix(dx, "dx", x.shape, dev)
+        if dw is False:
+            dw = None
+        elif dw is not None:
+            dw = empty(w.shape, dtype=w.dtype, device=dev) if dw is True else _head_matrix(dw, "dw", w.shape, dev)
+        ld_w, w_ptr = _row_stride(w), w.data_ptr()
+        a = muon_head_args(tokens, dim, vocab, 1 if mean else 0, x.data_ptr(), w_ptr, _row_stride(x) if tokens else dim, ld_w,
+                           _dtype_code(x), _dtype_code(w),
+                           None if weight is None else _head_vector(weight, "weight", tokens, dev).data_ptr(), scale,
+                           logit_scale, loss.data_ptr(), lse.data_ptr(), total.data_ptr())
+        if dx is not None:
+            a.dx, a.ld_dx, a.dx_dtype = dx.data_ptr(), _row_stride(dx) if tokens else dim, _dtype_code(dx)
+        if dw is not None:
+            a.dw, a.ld_dw, a.dw_dtype, a.dw_accumulate = dw.data_ptr(), _row_stride(dw), _dtype_code(dw), 1 if accumulate_dw else 0
+        if workspace is None:
+            key = (tokens, dim, vocab, top, dx is None, dw is None, ld_w & 7, w_ptr & 15)
+            need = _head_bytes.get(key)
+            if need is None:
+                out = C.c_size_t(0)
+                _check(lib().muon_head_workspace_bytes(C.byref(a), top, C.byref(out), None))
+                if len(_head_bytes) >= 1024:
+                    _head_bytes.clear()
+                need = _head_bytes[key] = out.value + 1024
+            workspace = empty(need, dtype=torch.uint8, device=dev)
+        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise MuonError(MUON_ERR_WORKSPACE, "workspace must be a contiguous uint8 tensor on x's device")
+    first = workspace.data_ptr()
+    base = (first + 1023) // 1024 * 1024
+    _check(call(C.byref(a), base, max(first + workspace.numel() - base, 0), dev.index, _raw_stream(stream, dev.index)))
     return HeadLoss(loss, lse, total, dx, dw, workspace)
 
 
@@ -401,10 +423,12 @@ def muon_head_workspace_bytes(tokens: int, dim: int, vocab: int, top: int = 0, d
 
 
 def muon_debug_set_head_piece_bytes(nbytes: int) -> int:
+    _head_bytes.clear()
     return lib().muon_debug_set_head_piece_bytes(int(nbytes))
 
 
 def muon_debug_set_head_codes(mode: int) -> int:
+    _head_bytes.clear()
     return lib().muon_debug_set_head_codes(int(mode))
 
 
@@ -419,11 +443,11 @@ def muon_head_xent(x, w, targets, loss=None, lse=None, total=None, dx=None, dw=N
     Tensors used on another stream than the one they were allocated on are the
     caller's to keep alive (``record_stream``)."""
     import torch
-    if targets.dtype != torch.int64 or targets.dim() != 1 or targets.numel() != x.shape[0] or not targets.is_contiguous() or targets.device != x.device:
+    if targets.dtype != torch.int64 or targets.dim() != 1 or targets.shape[0] != x.shape[0] or not targets.is_contiguous() or targets.device != x.device:
         raise MuonError(MUON_ERR_INVALID_ARG, "targets must be contiguous int64 [tokens] on x's device")
 
     def call(a, ws, nbytes, dev, s):
-        return lib().muon_head_xent(a, C.c_void_p(targets.data_ptr()), float(z_loss), ws, nbytes, dev, s)
+        return lib().muon_head_xent(a, targets.data_ptr(), z_loss, ws, nbytes, dev, s)
 
     return _head_call(x, w, 0, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace,
                       stream, call)

@@ -11,7 +11,8 @@ namespace muon {
 namespace head {
 
 constexpr int kTileM = 256;   // output rows of a CTA pair's tile (128 per CTA)
-constexpr int kTileN = 256;   // widest output tile, and the vocabulary columns of one statistics entry
+constexpr int kTileN = 256;   // widest output tile
+constexpr int kStatN = 128;   // vocabulary columns of one statistics entry: what one epilogue warp sees of a row
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
@@ -73,29 +74,27 @@ struct GemmParams {
   const unsigned char* starts;  // [rows][n_starts]: entries below each 256-column tile (top > 1)
   int n_starts;
   float* entry_logit; // [rows][top] raw logit of each entry
-  float2* stats;      // [rows][stats_ld]: maximum and sum of exponentials per 256-column tile
+  float2* stats;      // [rows][stats_ld]: maximum and sum of exponentials per 128 columns
   int stats_ld;
   const float2* row_q;   // [rows]: coefficient of q, log2 of the softmax denominator
   const float* entry_g;  // [rows][top]: gradient of the logit at the entry
-  __nv_bfloat16* g;      // [padded rows][g_ld]: gradient of the logits of one vocabulary piece
-  long long g_ld;
-  // statistics: codes of the logits of the first `code_tiles` tiles, in pieces of
-  // piece_tiles tiles, piece_stride elements apart, rows g_ld apart
-  unsigned short* codes;
-  int code_tiles, piece_tiles;
-  long long piece_stride;
+  // Piece buffers [buffers * padded][piece columns], box {64, 32}: where the
+  // gradient of one piece's logits is stored, or the codes of the logits of the
+  // first `code_tiles` tiles, in pieces of piece_tiles tiles.
+  CUtensorMap map_g;
+  int code_tiles, piece_tiles, padded;
   // outputs: the next piece's codes are converted while the products run
   ConvertParams convert;
 
-  // product 0 of kModeOut: partial dX
-  float* part;        // [splits][padded rows][part_ld]
-  long long part_ld, part_stride;
+  // product 0 of kModeOut: partial dX, fp32 [splits * padded][cols], box {32, 32}
+  CUtensorMap map_part;
   int part_cols;
   int part_add;       // add to what an earlier piece left
-  // product 1 of kModeOut: dW
+  // product 1 of kModeOut: dW, box {64, 32} bf16 or {32, 32} fp32
+  CUtensorMap map_dw;
   void* dw;
   long long ld_dw;
-  int dw_fp32, dw_add, dw_vec;  // dw_vec: widest aligned store in bytes (32, 16) or 0
+  int dw_fp32, dw_add, dw_tma;  // dw_tma: tiles leave through map_dw, else element by element
   int dw_row0, dw_rows, dw_cols;
 };
 
@@ -156,8 +155,7 @@ cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_
 
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
-cudaError_t launch_finalise(const RowParams& R, cudaStream_t stream);
-cudaError_t launch_convert(const ConvertParams& C, const Ctrl* ctrl, int max_rows, int sms, cudaStream_t stream);
+cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
                         int cols, cudaStream_t stream);

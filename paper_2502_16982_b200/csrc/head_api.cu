@@ -56,21 +56,24 @@ struct Plan {
 // a long axis (the vocabulary piece), dW many with a short one; both are dealt
 // out to the CTA pairs in turn, dX first.  The split with the smallest load of
 // the fullest pair is taken, a tile counted as its K blocks plus kTileCost for
-// its epilogue and the traffic of a partial sum.
+// its epilogue, and `split_cost` K blocks for joining one more partial sum.
 constexpr int kTileCost = 6;
-int choose_splits(int dx_tiles, int dx_kb, int dw_tiles, int dw_kb, int pairs, int most) {
+int choose_splits(long long dx_tiles, int dx_kb, long long dw_tiles, int dw_kb, int pairs, int most, double split_cost) {
   int best = 1;
-  long long best_load = -1;
+  double best_load = -1;
   for (int s = 1; s <= most; ++s) {
     if (s > 1 && dx_kb / s < 4) break;
-    const long long nx = static_cast<long long>(dx_tiles) * s;
-    long long load = 0;
-    for (int w = 0; w < pairs; ++w) {
-      const long long x = nx / pairs + (w < nx % pairs);
-      const long long all = (nx + dw_tiles) / pairs + (w < (nx + dw_tiles) % pairs);
-      const long long l = x * ((dx_kb + s - 1) / s + kTileCost) + (all - x) * (dw_kb + kTileCost);
+    const long long nx = dx_tiles * s, n = nx + dw_tiles;
+    const int rx = static_cast<int>(nx % pairs), rn = static_cast<int>(n % pairs);
+    double load = 0;
+    // the load is one of these pairs' at its largest: it changes after pair rx - 1 and rn - 1
+    for (int w : {0, rx % pairs, rn % pairs, pairs - 1}) {
+      const long long x = nx / pairs + (w < rx), all = n / pairs + (w < rn);
+      const double l = static_cast<double>(x) * ((dx_kb + s - 1) / s + kTileCost) +
+                       static_cast<double>(all - x) * (dw_kb + kTileCost);
       if (l > load) load = l;
     }
+    load += s * split_cost;
     if (best_load < 0 || load < best_load) {
       best_load = load;
       best = s;
@@ -117,9 +120,12 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   if (P->want_dx) {
     long long most = kPartBytes / (P->part_stride * 4);
     most = most < 1 ? 1 : (most > 64 ? 64 : most);
-    P->splits = choose_splits(P->padded / kTileM * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
-                              P->want_dw ? P->piece_tiles * P->dx_n_tiles : 0, P->padded / kBK, pairs,
-                              static_cast<int>(most));
+    // a partial sum costs its bytes (1.7 MB in the time of a K block, 0.27 us) once a call
+    // and its place in the loop of dx_kernel
+    const double split_cost = 1.0 + static_cast<double>(P->part_stride) * 4 / 1.7e6 / P->n_pieces;
+    P->splits = choose_splits(static_cast<long long>(P->padded) / kTileM * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
+                              P->want_dw ? static_cast<long long>(P->piece_tiles) * P->dx_n_tiles : 0,
+                              (P->tokens + kBK - 1) / kBK, pairs, static_cast<int>(most), split_cost);
   }
 
   const size_t rows = static_cast<size_t>(P->padded), entries = rows * top;
@@ -136,7 +142,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   P->ids = take(entries * 4);
   P->entry_logit = take(entries * 4);
   P->entry_g = take(entries * 4);
-  P->stats = take(rows * P->v_tiles * sizeof(float2));
+  P->stats = take(rows * P->v_tiles * 2 * sizeof(float2));
   P->row_q = take(rows * sizeof(float2));
   P->row_l = take(rows * 4);
   P->flags = P->p = P->row_h = P->row_c = P->starts = P->wc = P->g = P->part = 0;
@@ -182,17 +188,20 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// bf16 matrix [rows][cols] with row pitch ld, 128-byte swizzled boxes of 64 x box_rows.
-int encode(CUtensorMap* out, const void* base, long long rows, long long cols, long long ld, int box_rows) {
+// bf16 or fp32 matrix [rows][cols] with row pitch ld, 128-byte swizzled boxes of
+// 128 bytes x box_rows.
+int encode(CUtensorMap* out, const void* base, long long rows, long long cols, long long ld, int box_rows,
+           bool fp32 = false) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return fail(MUON_ERR_CUDA, "cuTensorMapEncodeTiled entry point not available");
+  const cuuint64_t pitch = static_cast<cuuint64_t>(ld) * (fp32 ? 4 : 2);
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), 1};
-  cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * 2 * static_cast<cuuint64_t>(rows)};
-  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1};
+  cuuint64_t strides[2] = {pitch, pitch * static_cast<cuuint64_t>(rows)};
+  cuuint32_t box[3] = {fp32 ? 32u : 64u, static_cast<cuuint32_t>(box_rows), 1};
   cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  CUresult r = fn(out, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                  const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(MUON_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
   return MUON_OK;
 }
@@ -325,7 +334,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.n_starts = P.v_tiles + 1;
   R.entry_logit = reinterpret_cast<float*>(ws + P.entry_logit);
   R.stats = reinterpret_cast<float2*>(ws + P.stats);
-  R.stats_ld = R.stats_n = P.v_tiles;
+  R.stats_ld = R.stats_n = 2 * P.v_tiles;
   R.scale2 = static_cast<float>(logit_scale * 1.4426950408889634);
   R.logit_scale = logit_scale;
   R.z_loss = z_loss;
@@ -358,12 +367,12 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   S.stats_ld = R.stats_ld;
   S.row_q = R.row_q;
   S.entry_g = R.entry_g;
-  S.g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
-  S.g_ld = static_cast<long long>(P.piece_tiles) * kTileN;
-  S.codes = reinterpret_cast<unsigned short*>(S.g);
+  __nv_bfloat16* const g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
+  const long long g_ld = static_cast<long long>(P.piece_tiles) * kTileN, g_rows = static_cast<long long>(P.padded) * P.n_buffers;
   S.piece_tiles = P.piece_tiles;
-  S.piece_stride = P.padded * S.g_ld;
+  S.padded = P.padded;
   S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
+  if (P.grads) HEAD_TRY(encode(&S.map_g, g, g_rows, g_ld, g_ld, 32));
   Product& L = S.prod[0];  // logits: tokens x vocabulary
   HEAD_TRY(encode(&L.map_a, R.xc, P.padded, P.dim, P.ld_xc, 128));
   HEAD_TRY(encode(&L.map_b, w, P.vocab, P.dim, ld_w, 128));
@@ -379,7 +388,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     O.n_prod = 0;
     Product& X = O.prod[0];  // dX: tokens x dim, over the vocabulary piece
     X = Product{};
-    HEAD_TRY(encode(&X.map_a, S.g, static_cast<long long>(P.padded) * P.n_buffers, S.g_ld, S.g_ld, 128));
+    HEAD_TRY(encode(&X.map_a, g, g_rows, g_ld, g_ld, 128));
     HEAD_TRY(encode(&X.map_b, w, P.vocab, P.dim, ld_w, 64));
     X.b_mn = 1;
     X.n_tile = P.dx_n_tile;
@@ -389,7 +398,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     X.swap_order = 1;
     Product& W = O.prod[1];  // dW: vocabulary piece x dim, over the tokens
     W = Product{};
-    HEAD_TRY(encode(&W.map_a, S.g, static_cast<long long>(P.padded) * P.n_buffers, S.g_ld, S.g_ld, 64));
+    HEAD_TRY(encode(&W.map_a, g, g_rows, g_ld, g_ld, 64));
     HEAD_TRY(encode(&W.map_b, R.xc, P.padded, P.dim, P.ld_xc, 64));
     W.a_mn = W.b_mn = 1;
     W.n_tile = P.dx_n_tile;
@@ -398,17 +407,17 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     W.splits = 1;
     W.swap_order = 1;
     O.n_prod = P.want_dw ? 2 : 1;
-    O.part = reinterpret_cast<float*>(ws + P.part);
-    O.part_ld = P.part_ld;
-    O.part_stride = P.part_stride;
     O.part_cols = static_cast<int>(P.part_ld);
+    if (P.want_dx)
+      HEAD_TRY(encode(&O.map_part, ws + P.part, static_cast<long long>(P.splits) * P.padded, P.part_ld, P.part_ld, 32, true));
     O.dw = a->dw;
     O.ld_dw = a->ld_dw;
     O.dw_fp32 = a->dw_dtype == MUON_DTYPE_FP32;
     O.dw_add = a->dw_accumulate != 0;
     O.dw_cols = P.dim;
     const long long pitch = a->ld_dw * (O.dw_fp32 ? 4 : 2);
-    O.dw_vec = !misaligned(a->dw, 32) && (pitch & 31) == 0 ? 32 : (!misaligned(a->dw, 16) && (pitch & 15) == 0 ? 16 : 0);
+    O.dw_tma = P.want_dw && !misaligned(a->dw, 16) && (pitch & 15) == 0 && (O.dw_fp32 || !O.dw_add);
+    if (O.dw_tma) HEAD_TRY(encode(&O.map_dw, a->dw, P.vocab, P.dim, a->ld_dw, 32, O.dw_fp32 != 0));
   }
 
   if (P.pack)
@@ -418,28 +427,29 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   HEAD_CUDA(launch_prepare(R, distill && P.tokens > 0, stream));
   const long long m_tiles = P.tokens > 0 ? P.padded / kTileM : 0;
   HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, stream));
-  HEAD_CUDA(launch_finalise(R, stream));
+  ConvertParams C = {};
+  C.ld = g_ld;
+  C.row_q = R.row_q;
+  C.stats = R.stats;
+  C.stats_ld = R.stats_ld;
+  C.top = top;
+  C.ids = R.ids;
+  C.entry_g = R.entry_g;
+  C.starts = R.starts;
+  C.n_starts = R.n_starts;
+  auto tiles_of = [&](int piece) {
+    const int left = P.v_tiles - piece * P.piece_tiles;
+    return left < P.piece_tiles ? left : P.piece_tiles;
+  };
+  auto codes_of = [&](int piece) {
+    ConvertParams D = C;
+    if (piece < P.n_stored) D.g = g + piece * P.padded * g_ld;
+    D.tiles = tiles_of(piece);
+    D.v_tile0 = piece * P.piece_tiles;
+    return D;
+  };
+  HEAD_CUDA(launch_finalise(R, codes_of(0), 2 * pairs, stream));
   if (P.grads) {
-    ConvertParams C = {};
-    C.ld = S.g_ld;
-    C.row_q = R.row_q;
-    C.stats = R.stats;
-    C.stats_ld = R.stats_ld;
-    C.top = top;
-    C.ids = R.ids;
-    C.entry_g = R.entry_g;
-    C.starts = R.starts;
-    C.n_starts = R.n_starts;
-    auto tiles_of = [&](int piece) {
-      const int left = P.v_tiles - piece * P.piece_tiles;
-      return left < P.piece_tiles ? left : P.piece_tiles;
-    };
-    auto codes_of = [&](int piece) {
-      C.g = S.g + piece * S.piece_stride;
-      C.tiles = tiles_of(piece);
-      C.v_tile0 = piece * P.piece_tiles;
-      return C;
-    };
     for (int i = 0; i < P.n_pieces; ++i) {
       // stored pieces lie in a buffer each, the others use the first one after them
       const bool stored = i < P.n_stored;
@@ -447,16 +457,13 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       const int tiles = tiles_of(i);
       const int v0 = i * P.piece_tiles * kTileN;
       const int cols = P.vocab - v0 < tiles * kTileN ? P.vocab - v0 : tiles * kTileN;
-      if (stored) {
-        if (i == 0) HEAD_CUDA(launch_convert(codes_of(0), R.ctrl, P.padded, 2 * pairs, stream));
-      } else {
+      if (!stored) {
         S.v0 = v0;
         L.b_n0 = v0;
         L.n_tiles = tiles;
         HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
       }
-      O.convert = ConvertParams{};
-      if (i + 1 < P.n_stored) O.convert = codes_of(i + 1);
+      O.convert = i + 1 < P.n_stored ? codes_of(i + 1) : ConvertParams{};
       O.prod[0].a_m0 = buffer * P.padded;
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;

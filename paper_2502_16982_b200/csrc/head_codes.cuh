@@ -1,6 +1,6 @@
 // 16-bit codes of logits.  Where the workspace has room, the statistics pass keeps
-// every logit as its distance below the largest one of its row and 256-column
-// tile, in steps of 2^-11 on the log2 scale: code = round((max - y) 2^11), capped at
+// every logit as its distance below the largest one of its row in the same 128
+// columns, in steps of 2^-11 on the log2 scale: code = round((max - y) 2^11), capped at
 // 65535, y = scale2 * logit.  Decoding gives q within 2^-12 ln 2 = 1.7e-4, a
 // twentieth of the bf16 rounding of the gradient that follows; what lies 2^-32
 // or more below its tile's largest becomes 0.  The gradient of the logits is then
@@ -30,39 +30,35 @@ __device__ __forceinline__ uint32_t encode_logit(float below) {
   return __float_as_uint(fminf(fmaf(below, -kCodeSteps, kCodeMagic), kCodeMagic + 65535.0f));
 }
 
-// Codes of `tiles` 256-column tiles of one row -> bf16 gradient of the logits, in
-// place, by one warp (8 columns a lane and tile, so that a tile is one coalesced
-// 512-byte access).  A row past the tokens that count becomes zeros.
+// Codes of up to kConvertTiles 256-column tiles of one row -> bf16 gradient of the
+// logits, in place, by one warp (8 columns a lane and tile, so that a tile is one
+// coalesced 512-byte access).  rq: the row's coefficient of q and log2 softmax
+// denominator; ids, entry_g: its sparse entries, ascending.
 constexpr int kConvertTiles = 8;  // independent loads in flight
 
-__device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int tile0, int n_valid, int lane) {
+__device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int tile0, float2 rq, const int* ids,
+                                            const float* entry_g, int lane) {
   const int tiles = min(kConvertTiles, C.tiles - tile0);
   uint4* cell = reinterpret_cast<uint4*>(C.g + static_cast<long long>(row) * C.ld + tile0 * kTileN) + lane;
-  if (row >= n_valid) {
-    for (int i = 0; i < tiles; ++i) cell[i * 32] = make_uint4(0u, 0u, 0u, 0u);
-    return;
-  }
-  const float2 rq = C.row_q[row];
-  // lane i: what tile i of the run adds to the exponent
+  uint4 v[kConvertTiles];
+#pragma unroll
+  for (int i = 0; i < kConvertTiles; ++i)
+    if (i < tiles) v[i] = __ldcs(cell + i * 32);
+  // lane i: what the i-th 128 columns of the run add to the exponent
   float shift = 0.f;
-  if (lane < tiles) shift = C.stats[static_cast<long long>(row) * C.stats_ld + C.v_tile0 + tile0 + lane].x - rq.y;
-  const int* ids = C.ids + static_cast<long long>(row) * C.top;
+  if (lane < 2 * tiles) shift = C.stats[static_cast<long long>(row) * C.stats_ld + 2 * (C.v_tile0 + tile0) + lane].x - rq.y;
   int next = 0, end = 1;
   if (C.top > 1) {
     const unsigned char* s = C.starts + static_cast<long long>(row) * C.n_starts + C.v_tile0 + tile0;
     next = s[0];
     end = s[tiles];
   }
-  uint4 v[kConvertTiles];
-#pragma unroll
-  for (int i = 0; i < kConvertTiles; ++i)
-    if (i < tiles) v[i] = __ldcs(cell + i * 32);
   int id = next < end ? ids[next] - (C.v_tile0 + tile0) * kTileN : kNoId;
   if (id < 0) id = kNoId;
 #pragma unroll
   for (int i = 0; i < kConvertTiles; ++i) {
     if (i < tiles) {
-      const float a = __shfl_sync(0xFFFFFFFFu, shift, i);
+      const float a = __shfl_sync(0xFFFFFFFFu, shift, 2 * i + (lane >> 4));
       uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
       float g[8];
 #pragma unroll
@@ -74,7 +70,7 @@ __device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int
       }
       // sparse entries of this tile (all lanes see the same list)
       while (id < (i + 1) * kTileN) {
-        const float eg = C.entry_g[static_cast<long long>(row) * C.top + next];
+        const float eg = entry_g[next];
         const int at = id - i * kTileN;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -92,6 +88,13 @@ __device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int
   }
 }
 
+// A row past the tokens that count becomes zeros.
+__device__ __forceinline__ void clear_row(const ConvertParams& C, int row, int tile0, int lane) {
+  const int tiles = min(kConvertTiles, C.tiles - tile0);
+  uint4* cell = reinterpret_cast<uint4*>(C.g + static_cast<long long>(row) * C.ld + tile0 * kTileN) + lane;
+  for (int i = 0; i < tiles; ++i) cell[i * 32] = make_uint4(0u, 0u, 0u, 0u);
+}
+
 // All rows of a piece, dealt out to `warps` warps.
 __device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_valid, int warp, int warps, int lane) {
   const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
@@ -99,7 +102,10 @@ __device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_vali
   const long long tasks = static_cast<long long>(rows) * runs;
   for (long long t = warp; t < tasks; t += warps) {
     const int row = static_cast<int>(t / runs);
-    convert_row(C, row, static_cast<int>(t - static_cast<long long>(row) * runs) * kConvertTiles, n_valid, lane);
+    const int tile0 = static_cast<int>(t - static_cast<long long>(row) * runs) * kConvertTiles;
+    const long long at = static_cast<long long>(row) * C.top;
+    if (row < n_valid) convert_row(C, row, tile0, C.row_q[row], C.ids + at, C.entry_g + at, lane);
+    else clear_row(C, row, tile0, lane);
   }
 }
 

@@ -11,10 +11,15 @@
 //   warp 0     TMA producer: this CTA's 128 rows of A and its half of B per K
 //              block, into a ring of kStages; no multicast
 //   warp 1     leader CTA only: UMMA issuer, two TMEM accumulator stages
-//   warps 2-5  epilogue: lane = row of the tile, so that a row's maximum and sum
-//              stay in one thread's registers
+//   epilogue   statistics and gradient: warps 2-9, a lane per row and half of the
+//              tile's columns per warp, so that a row's maximum and sum over 128
+//              columns stay in one thread's registers; outputs: warps 2-5
 //   warps 6-9  outputs only: turn the next piece's codes (head_codes.cuh) into the
 //              gradient of its logits while the tensor cores work on this piece
+//
+// Everything a tile stores goes through 4 KiB of shared memory per warp and leaves
+// as a TMA store (or a TMA reduction, where dX or dW is added to): 32 rows by 128
+// bytes at a time.
 //
 // Every wait is bounded (ptx::mbar_wait); on expiry the CTA records
 // MUON_ERR_TIMEOUT, all roles drain and the kernel returns.
@@ -28,16 +33,20 @@ namespace head {
 
 namespace {
 
-constexpr int kConvertWarps = 4;
-constexpr int threads_of(int mode) { return mode == kModeOut ? 192 + 32 * kConvertWarps : 192; }
 constexpr int kStages = 6;
 constexpr int kTileABytes = 128 * kBK * 2;
 constexpr int kTileBBytes = 128 * kBK * 2;
 constexpr int kStageBytes = kTileABytes + kTileBBytes;
-constexpr int kEpiWarps = 4;
 constexpr int kNumAcc = 2;
 constexpr int kAccCols = 256;
 constexpr int kTmemCols = kNumAcc * kAccCols;
+constexpr int kStageOut = 32 * 128;  // one warp's 32 rows x 128 bytes
+constexpr int kStaging = 8 * kStageOut;  // eight warps with one buffer each, or four with two
+__host__ __device__ constexpr int epi_warps(int mode) { return mode == kModeOut ? 4 : 8; }
+constexpr int kConvertWarps = 4;
+__host__ __device__ constexpr int threads_of(int mode) { return 64 + 32 * (epi_warps(mode) + (mode == kModeOut ? kConvertWarps : 0)); }
+
+constexpr int kOutside = 1 << 30;  // a row coordinate past every tensor
 
 struct Barriers {
   unsigned long long full[kStages];    // leader's copy is the live one
@@ -48,7 +57,7 @@ struct Barriers {
   int abort_flag;
 };
 
-constexpr int kSmemBytes = 1024 + kStages * kStageBytes + 512;
+constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
 static_assert(sizeof(Barriers) <= 512 && kSmemBytes <= 232448, "exceeds the 227 KiB shared-memory limit");
 
 __device__ __forceinline__ void report_timeout(const GemmParams& P) { atomicExch(&P.ctrl->status, -6); }
@@ -58,21 +67,29 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
-__device__ __forceinline__ void st_global_32(void* dst, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]),
-               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w0), "r"(w1), "r"(w2), "r"(w3) : "memory");
 }
 
-__device__ __forceinline__ void ld_global_32(const void* src, uint32_t (&v)[8]) {
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-               : "l"(src));
+// Address of 16-byte chunk `c` of row `lane` in a 32-row staging buffer, 128-byte swizzle.
+__device__ __forceinline__ uint32_t staged(uint32_t buf, int lane, int c) {
+  return buf + static_cast<uint32_t>(lane * 128 + ((c ^ (lane & 7)) << 4));
+}
+
+// t / d for a tile number: a multiplication by the reciprocal, off by at most one
+// below 2^24, put right by the remainder.
+__device__ __forceinline__ int quotient(int t, int d, float reciprocal) {
+  if (t >= (1 << 24)) return t / d;
+  int q = static_cast<int>(static_cast<float>(t) * reciprocal);
+  const int r = t - q * d;
+  q += (r >= d) - (r < 0);
+  return q;
 }
 
 // Sizes of product `i` that depend on how many tokens count.
 struct Shape {
   int m_tiles, n_tiles, k_blocks, splits, tiles;
+  float per_split, per_column;  // reciprocals of the tiles of a split and of a row (or group) of tiles
 };
 
 __device__ __forceinline__ Shape shape_of(const GemmParams& P, int i, int n_valid) {
@@ -83,6 +100,8 @@ __device__ __forceinline__ Shape shape_of(const GemmParams& P, int i, int n_vali
   s.n_tiles = p.n_tiles;
   s.splits = p.splits;
   s.tiles = s.m_tiles * s.n_tiles * s.splits;
+  s.per_split = __frcp_rn(static_cast<float>(max(1, s.m_tiles * s.n_tiles)));
+  s.per_column = __frcp_rn(static_cast<float>(p.swap_order ? s.n_tiles : p.group * s.n_tiles));
   return s;
 }
 
@@ -100,22 +119,27 @@ __device__ __forceinline__ Tile locate(const GemmParams& P, const Shape& s0, con
   if (r.prod) t -= s0.tiles;
   const Shape& s = r.prod ? s1 : s0;
   const Product& p = P.prod[r.prod];
-  const int per_split = s.m_tiles * s.n_tiles;
-  r.split = t / per_split;
-  t -= r.split * per_split;
+  r.split = 0;
+  r.kb0 = 0;
+  r.kb1 = s.k_blocks;
+  if (s.splits > 1) {  // at most 2^18 K blocks and 64 splits
+    const int per_split = s.m_tiles * s.n_tiles;
+    r.split = quotient(t, per_split, s.per_split);
+    t -= r.split * per_split;
+    r.kb0 = static_cast<int>(static_cast<unsigned>(s.k_blocks) * r.split / s.splits);
+    r.kb1 = static_cast<int>(static_cast<unsigned>(s.k_blocks) * (r.split + 1) / s.splits);
+  }
   if (p.swap_order) {
-    r.mi = t / s.n_tiles;
+    r.mi = quotient(t, s.n_tiles, s.per_column);
     r.ni = t - r.mi * s.n_tiles;
   } else {
     const int per_group = p.group * s.n_tiles;
-    const int grp = t / per_group;
+    const int grp = quotient(t, per_group, s.per_column);
     t -= grp * per_group;
     const int rows = min(p.group, s.m_tiles - grp * p.group);
-    r.ni = t / rows;
+    r.ni = quotient(t, rows, __frcp_rn(static_cast<float>(rows)));
     r.mi = grp * p.group + (t - r.ni * rows);
   }
-  r.kb0 = static_cast<int>(static_cast<long long>(s.k_blocks) * r.split / s.splits);
-  r.kb1 = static_cast<int>(static_cast<long long>(s.k_blocks) * (r.split + 1) / s.splits);
   return r;
 }
 
@@ -127,29 +151,30 @@ __device__ __forceinline__ float pick(const uint32_t (&v)[32], int i) {
   return __uint_as_float(r);
 }
 
-// The sparse entries of one row that fall into one 256-column tile.
+// The sparse entries of one row that fall into 128 columns from `col0` on.
 struct Entries {
   int next, end;  // positions in the row's list
-  int col;        // column of entry `next` within the tile, or past every column
+  int col;        // column of entry `next` from col0, or past every column
   const int* ids;
 
-  __device__ __forceinline__ void open(const GemmParams& P, int row, int tile_col0, bool row_ok) {
+  __device__ __forceinline__ void open(const GemmParams& P, int row, int col0, bool row_ok) {
     next = end = 0;
     ids = P.ids + static_cast<long long>(row) * P.top;
     if (row_ok) {
       if (P.top == 1) {
         end = 1;
       } else {
-        const unsigned char* s = P.starts + static_cast<long long>(row) * P.n_starts + tile_col0 / kTileN;
+        const unsigned char* s = P.starts + static_cast<long long>(row) * P.n_starts + col0 / kTileN;
         next = s[0];
         end = s[1];
+        while (next < end && ids[next] < col0) ++next;
       }
     }
-    fetch(tile_col0);
+    fetch(col0);
   }
-  __device__ __forceinline__ void fetch(int tile_col0) {
-    col = next < end ? ids[next] - tile_col0 : kNoId;
-    if (col < 0 || col >= kTileN) col = kNoId;
+  __device__ __forceinline__ void fetch(int col0) {
+    col = next < end ? ids[next] - col0 : kNoId;
+    if (col < 0 || col >= kStatN) col = kNoId;
   }
 };
 
@@ -158,7 +183,9 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  Barriers* bars = reinterpret_cast<Barriers*>(ring + kStages * kStageBytes);
+  uint8_t* staging = ring + kStages * kStageBytes;
+  Barriers* bars = reinterpret_cast<Barriers*>(staging + kStaging);
+  constexpr int kEpiWarps = epi_warps(kMode);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -215,7 +242,9 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       const Tile tl = locate(P, s0, s1, t);
       const Product& pr = P.prod[tl.prod];
       const int half_n = pr.n_tile >> 1;
-      const int a_row = pr.a_m0 + tl.mi * kTileM + static_cast<int>(rank) * 128;
+      // rows past the tokens that count are asked for outside the tensor: zeros, without traffic
+      const int m_row = tl.mi * kTileM + static_cast<int>(rank) * 128;
+      const int a_row = pr.m_tiles < 0 && m_row >= n_valid ? kOutside : pr.a_m0 + m_row;
       const int b_row = pr.b_n0 + tl.ni * pr.n_tile + static_cast<int>(rank) * half_n;
       const uint32_t stage_tx = 2u * static_cast<uint32_t>(kTileABytes + half_n * 128);
       const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
@@ -330,10 +359,23 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
     const int q = warp & 3;  // TMEM lane quarter this warp may read
     int acc = 0;
     uint32_t acc_phase = 0;
+    int turn = 0;  // staging buffer last used (outputs)
     bool ok = true;
+    // accumulator fully read: hand the TMEM stage back to the leader's issuer
+    auto release = [&]() {
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0)
+        ptx::mbar_arrive_cluster_no_release(ptx::map_to_cta(ptx::smem_u32(&bars->acc_empty[acc]), 0));
+      if (++acc == kNumAcc) {
+        acc = 0;
+        acc_phase ^= 1u;
+      }
+    };
     for (int t = cluster; t < total_tiles && ok; t += num_clusters) {
       const Tile tl = locate(P, s0, s1, t);
-      const int row = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32 + lane;
+      const int row0 = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32;
+      const int row = row0 + lane;
       const bool have_acc = tl.kb0 != tl.kb1;
       if (have_acc) {
         ok = ptx::mbar_wait_relaxed(ptx::smem_u32(&bars->acc_full[acc]), acc_phase, abort_flag);
@@ -344,274 +386,228 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         }
         ptx::tc_fence_after();
       }
-      const uint32_t taddr = tmem_base + static_cast<uint32_t>(acc * kAccCols) + (static_cast<uint32_t>(q * 32) << 16);
+      uint32_t taddr = tmem_base + static_cast<uint32_t>(acc * kAccCols) + (static_cast<uint32_t>(q * 32) << 16);
 
-      if (kMode == kModeStats) {
-        const int c0 = tl.ni * kTileN;  // first vocabulary column of the tile
+      if (kMode != kModeOut) {
+        const int half = (warp - 2) >> 2;  // columns [128 half, 128 half + 128) of the tile
+        const uint32_t buf = ptx::smem_u32(staging + (warp - 2) * kStageOut);
+        const int g0 = tl.ni * kTileN + half * kStatN;       // column within the launch
+        const int c0 = (kMode == kModeGrad ? P.v0 : 0) + g0;  // and in the vocabulary
         const int limit = P.vocab - c0;
         const bool row_ok = row < n_valid;
-        if (__any_sync(0xFFFFFFFFu, row_ok)) {
-          Entries en;
-          en.open(P, row, c0, row_ok);
-          // the row's maximum over the tile first, then exponentials and codes against it
-          float m = -INFINITY;
-          {
-            uint32_t va[32], vb[32];
-            auto top_of = [&](const uint32_t (&v)[32], int c) {
-              if (limit < c + 32) {
+        // statistics: nothing is asked of rows past the tokens that count, or of columns
+        // past the vocabulary that no piece buffer holds
+        const bool codes = kMode == kModeStats && tl.ni < P.code_tiles;
+        const bool idle = kMode == kModeStats && (row0 >= n_valid || (limit <= 0 && !codes));
+        uint32_t v[4][32];
+        if (!idle) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (c + i < limit) m = fmaxf(m, __uint_as_float(v[i]));
-              } else {
-                float a = __uint_as_float(v[0]), b = __uint_as_float(v[1]);
+          for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(taddr + half * kStatN + 32 * i, v[i]);
+          ptx::tmem_ld_wait();
+        }
+        release();
+        if (idle) {
+          if (row_ok) P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * 2 + half] = make_float2(-INFINITY, 0.f);
+          continue;
+        }
+        Entries en;
+        en.open(P, row, c0, row_ok);
+        float2 rq = make_float2(0.f, 0.f);
+        if (kMode == kModeGrad && row_ok) rq = P.row_q[row];
+        float m = -INFINITY, base = 0.f, sum = 0.f;
+        if (kMode == kModeStats) {
+          // logits of the sparse entries
 #pragma unroll
-                for (int i = 2; i < 32; i += 2) {
-                  a = fmaxf(a, __uint_as_float(v[i]));
-                  b = fmaxf(b, __uint_as_float(v[i + 1]));
-                }
-                m = fmaxf(m, fmaxf(a, b));
-              }
-            };
-            ptx::tmem_ld_32x32(taddr, va);
-            ptx::tmem_ld_wait();
-#pragma unroll 1
-            for (int c = 0; c < kTileN; c += 64) {
-              ptx::tmem_ld_32x32(taddr + c + 32, vb);
-              top_of(va, c);
-              ptx::tmem_ld_wait();
-              if (c + 64 < kTileN) ptx::tmem_ld_32x32(taddr + c + 64, va);
-              top_of(vb, c + 32);
-              ptx::tmem_ld_wait();
-            }
-          }
-          m *= P.scale2;
-          const float base = m == -INFINITY ? 0.f : m;  // nothing but -inf
-          unsigned short* crow = nullptr;
-          if (tl.ni < P.code_tiles && row_ok) {
-            const int piece = tl.ni / P.piece_tiles;
-            crow = P.codes + piece * P.piece_stride + static_cast<long long>(row) * P.g_ld +
-                   (tl.ni - piece * P.piece_tiles) * kTileN;
-          }
-          float s = 0.f;
-          auto chunk = [&](uint32_t (&v)[32], int c) {
-            // logits of entries that lie in these 32 columns
-            while (__any_sync(0xFFFFFFFFu, en.col - c < 32)) {
-              if (en.col - c < 32) {
-                P.entry_logit[static_cast<long long>(row) * P.top + en.next] = pick(v, en.col - c);
+          for (int i = 0; i < 4; ++i) {
+            while (__any_sync(0xFFFFFFFFu, en.col - 32 * i < 32)) {
+              if (en.col - 32 * i < 32) {
+                P.entry_logit[static_cast<long long>(row) * P.top + en.next] = pick(v[i], en.col - 32 * i);
                 ++en.next;
                 en.fetch(c0);
               }
             }
-            if (limit < c + 32) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c + i >= limit) v[i] = 0xFF800000u;  // -inf
-            }
-            float s0_ = 0.f, s1_ = 0.f, s2_ = 0.f, s3_ = 0.f;
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              const float y0 = fmaf(__uint_as_float(v[i]), P.scale2, -base);
-              const float y1 = fmaf(__uint_as_float(v[i + 1]), P.scale2, -base);
-              const float y2 = fmaf(__uint_as_float(v[i + 2]), P.scale2, -base);
-              const float y3 = fmaf(__uint_as_float(v[i + 3]), P.scale2, -base);
-              s0_ += ex2_fast(y0);
-              s1_ += ex2_fast(y1);
-              s2_ += ex2_fast(y2);
-              s3_ += ex2_fast(y3);
-              v[i >> 1] = __byte_perm(encode_logit(y0), encode_logit(y1), 0x5410);
-              v[(i >> 1) + 1] = __byte_perm(encode_logit(y2), encode_logit(y3), 0x5410);
-            }
-            s += (s0_ + s1_) + (s2_ + s3_);
-            if (crow != nullptr) {
-              const uint32_t lo[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-              const uint32_t hi[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
-              st_global_32(crow + c, lo);
-              st_global_32(crow + c + 16, hi);
-            }
-            __syncwarp();
-          };
-          uint32_t va[32], vb[32];
-          ptx::tmem_ld_32x32(taddr, va);
-          ptx::tmem_ld_wait();
-#pragma unroll 1
-          for (int c = 0; c < kTileN; c += 64) {
-            ptx::tmem_ld_32x32(taddr + c + 32, vb);
-            chunk(va, c);
-            ptx::tmem_ld_wait();
-            if (c + 64 < kTileN) ptx::tmem_ld_32x32(taddr + c + 64, va);
-            chunk(vb, c + 32);
-            ptx::tmem_ld_wait();
           }
-          if (row_ok) P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni] = make_float2(m, s);
+          if (limit < kStatN) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (32 * i + j >= limit) v[i][j] = 0xFF800000u;  // -inf
+          }
+          // the row's maximum first, then exponentials and codes against it
+          float mm[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            mm[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+            for (int j = 1; j < 32; ++j) mm[i] = fmaxf(mm[i], __uint_as_float(v[i][j]));
+          }
+          m = fmaxf(fmaxf(mm[0], mm[1]), fmaxf(mm[2], mm[3])) * P.scale2;
+          base = m == -INFINITY ? 0.f : m;  // nothing but -inf
         }
-      } else if (kMode == kModeGrad) {
-        const int g0 = tl.ni * kTileN;    // first column within the piece
-        const int c0 = P.v0 + g0;         // and in the vocabulary
-        const int limit = P.vocab - c0;
-        const bool row_ok = row < n_valid;
-        float2 rq = make_float2(0.f, 0.f);
-        if (row_ok) rq = P.row_q[row];
-        Entries en;
-        en.open(P, row, c0, row_ok);
-        __nv_bfloat16* grow = P.g + static_cast<long long>(row) * P.g_ld + g0;
-        auto chunk = [&](uint32_t (&v)[32], int c) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float y = rq.x * ex2_fast(fmaf(__uint_as_float(v[i]), P.scale2, -rq.y));
-            v[i] = __float_as_uint(y);
+        for (int h = 0; h < 2; ++h) {  // 64 columns: one staged row of 128 bytes
+          uint32_t w[32];
+          if (kMode == kModeStats) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 64; j += 2) {
+              const float y0 = fmaf(__uint_as_float(v[2 * h + (j >> 5)][j & 31]), P.scale2, -base);
+              const float y1 = fmaf(__uint_as_float(v[2 * h + (j >> 5)][(j & 31) + 1]), P.scale2, -base);
+              s[j & 2] += ex2_fast(y0);
+              s[(j & 2) + 1] += ex2_fast(y1);
+              w[j >> 1] = __byte_perm(encode_logit(y0), encode_logit(y1), 0x5410);
+            }
+            sum += (s[0] + s[1]) + (s[2] + s[3]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 64; j += 2) {
+              float y0 = rq.x * ex2_fast(fmaf(__uint_as_float(v[2 * h + (j >> 5)][j & 31]), P.scale2, -rq.y));
+              float y1 = rq.x * ex2_fast(fmaf(__uint_as_float(v[2 * h + (j >> 5)][(j & 31) + 1]), P.scale2, -rq.y));
+              w[j >> 1] = row_ok ? pack2(y0, y1) : 0u;
+            }
+            if (limit < 64 * h + 64) {  // columns past the vocabulary
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                w[j] &= (64 * h + 2 * j < limit ? 0x0000FFFFu : 0u) | (64 * h + 2 * j + 1 < limit ? 0xFFFF0000u : 0u);
+            }
           }
-          if (!row_ok) {
+          if (kMode == kModeGrad || codes) {
+            if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sts128(staged(buf, lane, c), w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+            if (kMode == kModeGrad) {
+              // the entries' gradients replace what the same thread just wrote
+              while (en.col < 64 * h + 64) {
+                const int c = en.col - 64 * h;
+                const __nv_bfloat16 e = __float2bfloat16_rn(P.entry_g[static_cast<long long>(row) * P.top + en.next]);
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane, c >> 3) + 2u * (c & 7)),
+                             "h"(*reinterpret_cast<const unsigned short*>(&e))
+                             : "memory");
+                ++en.next;
+                en.fetch(c0);
+              }
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              int y = row0, x = g0 + 64 * h;
+              if (kMode == kModeStats) {
+                const int piece = tl.ni / P.piece_tiles;
+                y += piece * P.padded;
+                x -= piece * P.piece_tiles * kTileN;
+              }
+              ptx::tma_store_3d(&P.map_g, x, y, 0, buf);
+              ptx::tma_store_commit();
+            }
+          }
+        }
+        if (kMode == kModeStats && row_ok)
+          P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * 2 + half] = make_float2(m, sum);
+      } else {
+        const uint32_t buf0 = ptx::smem_u32(staging + (warp - 2) * 2 * kStageOut);
+        const bool is_dx = tl.prod == 0;
+        const int n_tile = P.prod[tl.prod].n_tile;
+        const int c0 = tl.ni * n_tile;
+        const int limit = min(n_tile, (is_dx ? P.part_cols : P.dw_cols) - c0);
+        const bool rows_ok = is_dx ? row0 < n_valid : row0 < P.dw_rows;
+        // two buffers in turn: the store before last has been read
+        auto next_buffer = [&]() {
+          if (lane == 0) ptx::tma_store_wait_read_all_but_one();
+          __syncwarp();
+          turn ^= 1;
+          return buf0 + static_cast<uint32_t>(turn * kStageOut);
+        };
+        auto send = [&](uint32_t buf, const CUtensorMap* map, int x, int y, bool add) {
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (add) ptx::tma_reduce_add_3d(map, x, y, 0, buf);
+            else ptx::tma_store_3d(map, x, y, 0, buf);
+            ptx::tma_store_commit();
+          }
+        };
+        auto load = [&](uint32_t (&v)[32], int c) {
+          if (have_acc) {
+            ptx::tmem_ld_32x32(taddr + c, v);
+          } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0u;
           }
-          if (limit < c + 32) {
+        };
+        if (rows_ok && (is_dx || (P.dw_fp32 && P.dw_tma))) {
+          const CUtensorMap* map = is_dx ? &P.map_part : &P.map_dw;
+          const int y = is_dx ? tl.split * P.padded + row0 : P.dw_row0 + row0;
+          const bool add = is_dx ? P.part_add != 0 : P.dw_add != 0;
+#pragma unroll 1
+          for (int c = 0; c < limit; c += 32) {
+            uint32_t v[32];
+            load(v, c);
+            ptx::tmem_ld_wait();
+            const uint32_t buf = next_buffer();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sts128(staged(buf, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            send(buf, map, c0 + c, y, add);
+          }
+        } else if (rows_ok && P.dw_tma) {
+#pragma unroll 1
+          for (int c = 0; c < limit; c += 64) {
+            uint32_t v[32], u[32];
+            load(v, c);
+            load(u, c + 32);
+            ptx::tmem_ld_wait();
+            const uint32_t buf = next_buffer();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t w[4], z[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                w[e] = pack2(__uint_as_float(v[8 * i + 2 * e]), __uint_as_float(v[8 * i + 2 * e + 1]));
+                z[e] = pack2(__uint_as_float(u[8 * i + 2 * e]), __uint_as_float(u[8 * i + 2 * e + 1]));
+              }
+              sts128(staged(buf, lane, i), w[0], w[1], w[2], w[3]);
+              sts128(staged(buf, lane, i + 4), z[0], z[1], z[2], z[3]);
+            }
+            send(buf, &P.map_dw, c0 + c, P.dw_row0 + row0, false);
+          }
+        } else if (rows_ok) {
+          // rows TMA cannot address, or sums into bf16: through shared memory, so that
+          // a warp's accesses run along a row
+#pragma unroll 1
+          for (int c = 0; c < limit; c += 32) {
+            uint32_t v[32];
+            load(v, c);
+            ptx::tmem_ld_wait();
+            if (lane == 0) ptx::tma_store_wait_read();
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (c + i >= limit) v[i] = 0u;
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              w[i] = pack2(__uint_as_float(v[16 * h + 2 * i]), __uint_as_float(v[16 * h + 2 * i + 1]));
-            st_global_32(grow + c + 16 * h, w);
-          }
-          // the entries' gradients replace what was just written, by the same thread
-          while (en.col - c < 32) {
-            grow[en.col] = __float2bfloat16_rn(P.entry_g[static_cast<long long>(row) * P.top + en.next]);
-            ++en.next;
-            en.fetch(c0);
-          }
-          __syncwarp();
-        };
-        uint32_t va[32], vb[32];
-        ptx::tmem_ld_32x32(taddr, va);
-        ptx::tmem_ld_wait();
-#pragma unroll 1
-        for (int c = 0; c < kTileN; c += 64) {
-          ptx::tmem_ld_32x32(taddr + c + 32, vb);
-          chunk(va, c);
-          ptx::tmem_ld_wait();
-          if (c + 64 < kTileN) ptx::tmem_ld_32x32(taddr + c + 64, va);
-          chunk(vb, c + 32);
-          ptx::tmem_ld_wait();
-        }
-      } else {
-        const int n_tile = P.prod[tl.prod].n_tile;
-        const int c0 = tl.ni * n_tile;
-        if (tl.prod == 0) {
-          // partial dX, fp32
-          float* prow = P.part + tl.split * P.part_stride + static_cast<long long>(row) * P.part_ld + c0;
-          const bool row_ok = row < n_valid;
-          const int limit = P.part_cols - c0;
-#pragma unroll 1
-          for (int c = 0; c < n_tile && c < limit; c += 32) {
-            uint32_t v[32];
-            ptx::tmem_ld_32x32(taddr + c, v);
-            ptx::tmem_ld_wait();
-            if (row_ok) {
-#pragma unroll
-              for (int h = 0; h < 4; ++h) {
-                if (c + 8 * h < limit) {  // part_cols is a multiple of 8
-                  uint32_t w[8];
-                  if (P.part_add) {
-                    ld_global_32(prow + c + 8 * h, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                      w[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(v[8 * h + i]));
-                  } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = v[8 * h + i];
-                  }
-                  st_global_32(prow + c + 8 * h, w);
-                }
-              }
-            }
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(buf0 + 4u * (lane * 32 + (i ^ lane))), "r"(v[i]) : "memory");
             __syncwarp();
-          }
-        } else {
-          // dW rows of this vocabulary piece
-          const bool row_ok = row < P.dw_rows;
-          const int limit = P.dw_cols - c0;
-          const long long off = static_cast<long long>(P.dw_row0 + row) * P.ld_dw + c0;
-#pragma unroll 1
-          for (int c = 0; c < n_tile && c < limit; c += 32) {
-            uint32_t v[32];
-            if (have_acc) {
-              ptx::tmem_ld_32x32(taddr + c, v);
-              ptx::tmem_ld_wait();
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = 0u;
-            }
-            if (row_ok) {
-              if (P.dw_fp32) {
-                float* d = static_cast<float*>(P.dw) + off + c;
-                if (P.dw_vec == 32 && c + 32 <= limit) {
-#pragma unroll
-                  for (int h = 0; h < 4; ++h) {
-                    uint32_t w[8];
-                    if (P.dw_add) {
-                      ld_global_32(d + 8 * h, w);
-#pragma unroll
-                      for (int i = 0; i < 8; ++i)
-                        w[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(v[8 * h + i]));
-                    } else {
-#pragma unroll
-                      for (int i = 0; i < 8; ++i) w[i] = v[8 * h + i];
-                    }
-                    st_global_32(d + 8 * h, w);
-                  }
+            const int rows = min(32, P.dw_rows - row0);
+            if (c + lane < limit) {
+              long long off = static_cast<long long>(P.dw_row0 + row0) * P.ld_dw + c0 + c + lane;
+#pragma unroll 4
+              for (int r = 0; r < rows; ++r, off += P.ld_dw) {
+                float y;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=f"(y) : "r"(buf0 + 4u * (r * 32 + (lane ^ r))));
+                if (P.dw_fp32) {
+                  float* d = static_cast<float*>(P.dw) + off;
+                  *d = P.dw_add ? *d + y : y;
                 } else {
-#pragma unroll
-                  for (int i = 0; i < 32; ++i)
-                    if (c + i < limit) d[i] = __uint_as_float(v[i]) + (P.dw_add ? d[i] : 0.f);
-                }
-              } else {
-                __nv_bfloat16* d = static_cast<__nv_bfloat16*>(P.dw) + off + c;
-                if (P.dw_add) {
-#pragma unroll
-                  for (int i = 0; i < 32; ++i)
-                    if (c + i < limit) v[i] = __float_as_uint(__uint_as_float(v[i]) + __bfloat162float(d[i]));
-                }
-                if (P.dw_vec >= 16 && c + 32 <= limit) {
-#pragma unroll
-                  for (int h = 0; h < 2; ++h) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                      w[i] = pack2(__uint_as_float(v[16 * h + 2 * i]), __uint_as_float(v[16 * h + 2 * i + 1]));
-                    if (P.dw_vec == 32) {
-                      st_global_32(d + 16 * h, w);
-                    } else {
-                      *reinterpret_cast<uint4*>(d + 16 * h) = make_uint4(w[0], w[1], w[2], w[3]);
-                      *reinterpret_cast<uint4*>(d + 16 * h + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
-                  }
-                } else {
-#pragma unroll
-                  for (int i = 0; i < 32; ++i)
-                    if (c + i < limit) d[i] = __float2bfloat16_rn(__uint_as_float(v[i]));
+                  __nv_bfloat16* d = static_cast<__nv_bfloat16*>(P.dw) + off;
+                  *d = __float2bfloat16_rn(P.dw_add ? __bfloat162float(*d) + y : y);
                 }
               }
             }
             __syncwarp();
           }
         }
-      }
-
-      if (have_acc) {
-        // accumulator fully read: hand the TMEM stage back to the leader's issuer
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_u32(&bars->acc_empty[acc]), 0));
-        if (++acc == kNumAcc) {
-          acc = 0;
-          acc_phase ^= 1u;
-        }
+        if (have_acc) release();
       }
     }
+    if (lane == 0) ptx::tma_store_wait_all();
   }
 
   // ---------------------------------------------------------------- teardown --

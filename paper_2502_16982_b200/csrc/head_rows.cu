@@ -248,114 +248,119 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 // row_q holds (g a c', log2-domain lse), entry_g the gradient at the entries.
 // Exponents are taken from one fused multiply-add on the raw logit, so that a
 // large logit costs a single rounding.
-template <bool kDistill>
-__global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R) {
+//
+// One block per row.  kConvert: for few rows, where a launch counts, gridDim.y blocks
+// per row, each joining the statistics by itself in the same order, and each then
+// turning its share of the first stored piece's codes into gradients.
+template <bool kDistill, bool kConvert>
+__global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R, const ConvertParams C) {
   __shared__ float s_f[kRowWarps];
+  __shared__ float s_max[kRowWarps];
+  __shared__ int s_id[kMaxTop];
+  __shared__ float s_p[kMaxTop], s_raw[kMaxTop], s_exact[kMaxTop], s_g[kMaxTop];
   __shared__ bool s_last;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_valid = R.ctrl->n_valid;
-  const float coef = R.ctrl->coef;
-  const int row = blockIdx.x * kRowWarps + warp;
+  const int row = blockIdx.x;
+  const bool writes = blockIdx.y == 0;
+  const int runs = kConvert ? (C.tiles + kConvertTiles - 1) / kConvertTiles : 0;
+  const int run0 = static_cast<int>(blockIdx.y) * kRowWarps + warp, run_step = static_cast<int>(gridDim.y) * kRowWarps;
   if (row < n_valid) {
+    const int K = kDistill ? R.top : 1;
+    const long long at = static_cast<long long>(row) * K;
+    if (tid < K) {
+      const int id = R.ids[at + tid];
+      s_id[tid] = id;
+      s_p[tid] = id == kNoId ? 0.f : (kDistill ? R.p[at + tid] : 1.0f);
+      s_raw[tid] = id == kNoId ? 0.f : R.entry_logit[at + tid];
+    }
+    const float coef = R.ctrl->coef;
+    const int t = R.row_of[row];
     const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
     float m = -INFINITY, s = 0.f;
-    for (int i = lane; i < R.stats_n; i += 32) {
+#pragma unroll 4
+    for (int i = tid; i < R.stats_n; i += kRowThreads) {
       const float2 v = st[i];
       const float mx = fmaxf(m, v.x);
       const float base = mx == -INFINITY ? 0.f : mx;
       s = s * exp2f(m - base) + v.y * exp2f(v.x - base);
       m = mx;
     }
-    const float mx = warp_max(m);
-    const float base = mx == -INFINITY ? 0.f : mx;
-    s = warp_sum(s * exp2f(m - base));
-    const int t = R.row_of[row];
-    const float g = coef * (R.weight != nullptr ? R.weight[t] : 1.0f);
-    const float ga = g * R.logit_scale;
-    const float c = kDistill ? R.row_c[row] : 1.0f;
-    constexpr int kPer = kDistill ? kMaxTop / 32 : 1;
-    const int K = kDistill ? R.top : 1;
-    const long long at = static_cast<long long>(row) * K;
-    int id[kPer];
-    float raw[kPer], p[kPer];
+    const float wm = warp_max(m);
+    if (lane == 0) s_max[warp] = wm;
+    __syncthreads();
+    float mx = s_max[0];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int k = lane + 32 * i;
-      id[i] = k < K ? R.ids[at + k] : kNoId;
-      raw[i] = id[i] != kNoId ? R.entry_logit[at + k] : 0.f;
-      p[i] = id[i] != kNoId ? (kDistill ? R.p[at + k] : 1.0f) : 0.f;
-    }
+    for (int i = 1; i < kRowWarps; ++i) mx = fmaxf(mx, s_max[i]);
+    const float base = mx == -INFINITY ? 0.f : mx;
     // The logits that carry the loss, again as plain fp32 dot products, and the
     // softmax sum with them in place of the tensor cores' values: the tensor cores
     // truncate at every step of 16 products, which shifts a logit of 15 over 2048
     // columns by about 1e-5.
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      unsigned todo = __ballot_sync(0xFFFFFFFFu, p[i] >= kExactMass);
-      while (todo) {
-        const int src = __ffs(todo) - 1;
-        todo &= todo - 1;
-        const int which = __shfl_sync(0xFFFFFFFFu, id[i], src);
+    for (int e = warp; e < K; e += kRowWarps)
+      if (s_p[e] >= kExactMass) {
         const float exact = warp_dot(R.xc + static_cast<long long>(row) * R.ld_xc,
-                                     R.w + static_cast<long long>(which) * R.ld_w, R.dim, lane);
-        const float was = __shfl_sync(0xFFFFFFFFu, raw[i], src);
-        bool again = false;  // an index listed more than once is one logit
-        if (kDistill) {
-          const int k = src + 32 * i;
-          for (int j = k - 1; j >= 0 && R.ids[at + j] == which; --j) again |= R.p[at + j] >= kExactMass;
-        }
-        if (!again) s += exp2f(fmaf(exact, R.scale2, -base)) - exp2f(fmaf(was, R.scale2, -base));
-        if (lane == src) raw[i] = exact;
+                                     R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
+        if (lane == 0) s_exact[e] = exact;
       }
-    }
+    s = block_sum(s * exp2f(m - base), s_f);
+    for (int e = 0; e < K; ++e)
+      if (s_p[e] >= kExactMass) {
+        bool again = false;  // an index listed more than once is one logit
+        for (int j = e - 1; j >= 0 && s_id[j] == s_id[e]; --j) again |= s_p[j] >= kExactMass;
+        if (!again) s += exp2f(fmaf(s_exact[e], R.scale2, -base)) - exp2f(fmaf(s_raw[e], R.scale2, -base));
+      }
     const float lse2 = base + log2f(s);
     const float lse = lse2 * kLn2;
-    const float cq = c + 2.0f * R.z_loss * lse;
+    const float g = coef * (R.weight != nullptr ? R.weight[t] : 1.0f);
+    const float ga = g * R.logit_scale;
+    const float cq = (kDistill ? R.row_c[row] : 1.0f) + 2.0f * R.z_loss * lse;
     float ce = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int k = lane + 32 * i;
-      if (id[i] != kNoId) {
-        const float lq2 = fmaf(raw[i], R.scale2, -lse2);
-        ce -= p[i] == 0.f ? 0.f : p[i] * lq2 * kLn2;
-        float pj = p[i];
-        if (kDistill) {
-          // an index listed more than once: its entries share the gradient of the one logit
-          for (int j = k - 1; j >= 0 && R.ids[at + j] == id[i]; --j) pj += R.p[at + j];
-          for (int j = k + 1; j < K && R.ids[at + j] == id[i]; ++j) pj += R.p[at + j];
-        }
-        R.entry_g[at + k] = ga * (cq * exp2f(lq2) - pj);
-      }
+    if (tid < K && s_id[tid] != kNoId) {
+      const float p = s_p[tid];
+      const float lq2 = fmaf(p >= kExactMass ? s_exact[tid] : s_raw[tid], R.scale2, -lse2);
+      ce = p == 0.f ? 0.f : -p * lq2 * kLn2;
+      // an index listed more than once: its entries share the gradient of the one logit
+      float pj = p;
+      for (int j = tid - 1; j >= 0 && s_id[j] == s_id[tid]; --j) pj += s_p[j];
+      for (int j = tid + 1; j < K && s_id[j] == s_id[tid]; ++j) pj += s_p[j];
+      s_g[tid] = ga * (cq * exp2f(lq2) - pj);
+      if (writes) R.entry_g[at + tid] = s_g[tid];
     }
-    ce = warp_sum(ce);
-    if (kDistill) ce += R.row_h[row];
-    if (lane == 0) {
-      const float loss = ce + R.z_loss * lse * lse;
+    ce = block_sum(ce, s_f);  // a barrier, too: s_g is complete
+    const float2 rq = make_float2(ga * cq, lse2);
+    if (writes && tid == 0) {
+      const float loss = ce + (kDistill ? R.row_h[row] : 0.f) + R.z_loss * lse * lse;
       R.loss[t] = loss;
       if (R.lse != nullptr) R.lse[t] = lse;
-      R.row_q[row] = make_float2(ga * cq, lse2);
+      R.row_q[row] = rq;
       R.row_l[row] = g * loss;
     }
+    if (kConvert)
+      for (int r = run0; r < runs; r += run_step) convert_row(C, row, r * kConvertTiles, rq, s_id, s_g, lane);
+  } else if (kConvert && row < (n_valid + kBK - 1) / kBK * kBK) {
+    for (int r = run0; r < runs; r += run_step) clear_row(C, row, r * kConvertTiles, lane);
   }
-  if (R.total == nullptr) return;
-  // the last block to finish adds the tokens up, always in the same order
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) s_last = atomicAdd(&R.ctrl->ticket, 1u) == gridDim.x - 1;
+  if (R.total == nullptr || !writes) return;
+  // the last row's block adds the tokens up, always in the same order
+  if (tid == 0) {
+    __threadfence();
+    s_last = atomicAdd(&R.ctrl->ticket, 1u) == gridDim.x - 1;
+  }
   __syncthreads();
   if (s_last) {
     __threadfence();
     float sum = 0.f;
-    for (int i = threadIdx.x; i < n_valid; i += kRowThreads) sum += __ldcg(R.row_l + i);
+    for (int i = tid; i < n_valid; i += kRowThreads) sum += __ldcg(R.row_l + i);
     sum = block_sum(sum, s_f);
-    if (threadIdx.x == 0) *R.total = sum;
+    if (tid == 0) *R.total = sum;
   }
 }
 
-// The first stored piece's codes; those of the later ones are converted beside the
-// products (head_gemm.cu).
+// The first stored piece's codes where there are many rows; those of the later
+// pieces are converted beside the products (head_gemm.cu).
 __global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParams C, const Ctrl* ctrl) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
@@ -378,6 +383,7 @@ __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   float v[8] = {};
   if (pos >= 0) {
     const float* src = R.part + static_cast<long long>(pos) * R.part_ld + c;
+#pragma unroll 8
     for (int s = 0; s < R.splits; ++s, src += R.part_stride) {
       const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
       v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
@@ -429,9 +435,9 @@ __global__ void __launch_bounds__(kRowThreads) pack_kernel(const __nv_bfloat16* 
 }
 
 template <typename... Args>
-cudaError_t launch(void (*kernel)(Args...), unsigned blocks, bool overlap, cudaStream_t stream, Args... args) {
+cudaError_t launch(void (*kernel)(Args...), dim3 blocks, bool overlap, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(blocks, 1, 1);
+  cfg.gridDim = blocks;
   cfg.blockDim = dim3(kRowThreads, 1, 1);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
@@ -447,33 +453,42 @@ unsigned row_blocks(int tokens) { return tokens > 0 ? static_cast<unsigned>((tok
 }  // namespace
 
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream) {
-  return launch(flags_kernel, row_blocks(R.tokens), false, stream, R);
+  return launch(flags_kernel, dim3(row_blocks(R.tokens)), false, stream, R);
 }
 
 cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream) {
-  return launch(R.z != nullptr ? prepare_kernel<true> : prepare_kernel<false>, row_blocks(R.tokens), overlap, stream, R);
+  return launch(R.z != nullptr ? prepare_kernel<true> : prepare_kernel<false>, dim3(row_blocks(R.tokens)), overlap, stream, R);
 }
 
-cudaError_t launch_finalise(const RowParams& R, cudaStream_t stream) {
-  return launch(R.z != nullptr ? finalise_kernel<true> : finalise_kernel<false>, row_blocks(R.tokens), true, stream, R);
-}
-
-cudaError_t launch_convert(const ConvertParams& C, const Ctrl* ctrl, int max_rows, int sms, cudaStream_t stream) {
-  const long long tasks = static_cast<long long>(max_rows) * ((C.tiles + kConvertTiles - 1) / kConvertTiles);
-  const long long blocks = (tasks + kRowWarps - 1) / kRowWarps, most = 8ll * sms;
-  return launch(convert_kernel, static_cast<unsigned>(blocks < most ? blocks : most), true, stream, C, ctrl);
+cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
+  const int runs = C.g != nullptr ? (C.tiles + kConvertTiles - 1) / kConvertTiles : 0;
+  if (C.g != nullptr && R.tokens < 2 * sms) {
+    // rows up to the next K block are cleared; enough blocks to spread the conversion over the device
+    const int rows = R.tokens > 0 ? (R.tokens + kBK - 1) / kBK * kBK : 1;
+    const int most = (runs + kRowWarps - 1) / kRowWarps, want = (2 * sms + R.tokens) / (R.tokens + 1);
+    const unsigned parts = static_cast<unsigned>(want < most ? want : most);
+    return launch(R.z != nullptr ? finalise_kernel<true, true> : finalise_kernel<false, true>,
+                  dim3(static_cast<unsigned>(rows), parts), true, stream, R, C);
+  }
+  cudaError_t e = launch(R.z != nullptr ? finalise_kernel<true, false> : finalise_kernel<false, false>,
+                         dim3(static_cast<unsigned>(R.tokens > 0 ? R.tokens : 1)), true, stream, R, C);
+  if (e != cudaSuccess || C.g == nullptr) return e;
+  const long long tasks = static_cast<long long>(R.padded) * runs;
+  const long long blocks = (tasks + kRowWarps - 1) / kRowWarps, many = 8ll * sms;
+  return launch(convert_kernel, dim3(static_cast<unsigned>(blocks < many ? blocks : many)), true, stream, C,
+                static_cast<const Ctrl*>(R.ctrl));
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
   const long long n = static_cast<long long>(R.tokens) * ((R.dim + 7) >> 3);
   if (n == 0) return cudaSuccess;
-  return launch(dx_kernel, static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads), true, stream, R);
+  return launch(dx_kernel, dim3(static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads)), true, stream, R);
 }
 
 cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
                         int cols, cudaStream_t stream) {
   const long long blocks = (rows + kRowWarps - 1) / kRowWarps;
-  return launch(pack_kernel, static_cast<unsigned>(blocks < 4096 ? blocks : 4096), false, stream, src, ld_src, dst,
+  return launch(pack_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), false, stream, src, ld_src, dst,
                 ld_dst, rows, cols);
 }
 

@@ -159,6 +159,18 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int 
       : "memory");
 }
 
+// Tiled 3-D reduction shared -> global: adds the tile's elements (of the map's type)
+// to what is there (clipped at the tensor's bounds).  Never issued with a negative
+// coordinate.
+__device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap* map, int x, int y, int z,
+                                                  uint32_t src_smem) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+      :
+      : "l"(reinterpret_cast<uint64_t>(map)), "r"(src_smem), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
 __device__ __forceinline__ void tma_store_commit() {
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
@@ -306,6 +318,14 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr)
                : "memory");
+}
+
+// The same without a cluster-wide release: for a signal that no memory write has to
+// be ordered before (a TMEM accumulator whose loads tcgen05.wait::ld has seen
+// complete).  The release form also waits for this thread's TMA stores: 2400 cycles
+// a tile in an epilogue that stores 64 KiB.
+__device__ __forceinline__ void mbar_arrive_cluster_no_release(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // Tiled 3-D load into this CTA's shared memory whose byte count is reported to
