@@ -34,7 +34,7 @@ struct Product {
   int n_tiles;
   int k_blocks;      // K blocks of 64 in all; -1: from the number of tokens that count
   int splits;        // the K blocks are cut into this many runs, each its own tile
-  int a_m0, a_k0;    // first row and K coordinate of operand A (buffer of the vocabulary piece)
+  int a_z;           // third coordinate of operand A (buffer of the vocabulary piece)
   int b_k0;          // first K coordinate of operand B (vocabulary piece in W)
   int b_n0;          // first row of operand B
   int group;         // row tiles that are walked together for each column tile
@@ -44,7 +44,7 @@ struct Product {
 // A piece of the vocabulary whose logits are kept as codes (head_codes.cuh), to be
 // turned into the bf16 gradient of the logits in place.
 struct ConvertParams {
-  __nv_bfloat16* g;  // [padded][ld]; NULL: nothing to convert
+  __nv_bfloat16* g;  // [token][ld]; NULL: nothing to convert
   long long ld;
   int tiles;         // 256-column tiles of the piece
   int v_tile0;       // its first tile in the vocabulary
@@ -65,28 +65,33 @@ struct GemmParams {
   int n_prod;
   Ctrl* ctrl;
 
+  int tokens;
+
   // statistics and gradient of the logits
   int vocab;          // columns of the whole problem
   int v0;             // first vocabulary column of this launch
   float scale2;       // logit scale * log2(e)
   int top;            // sparse entries per token; 1: one target
-  const int* ids;     // [rows][top], ascending within a row
-  const unsigned char* starts;  // [rows][n_starts]: entries below each 256-column tile (top > 1)
+  const int* ids;     // [token][top], ascending within a row
+  const unsigned char* starts;  // [token][n_starts]: entries below each 256-column tile (top > 1)
   int n_starts;
-  float* entry_logit; // [rows][top] raw logit of each entry
-  float2* stats;      // [rows][stats_ld]: maximum and sum of exponentials per 128 columns
+  float* entry_logit; // [token][top] raw logit of each entry
+  float2* stats;      // [token][stats_ld]: maximum and sum of exponentials per 128 columns
   int stats_ld;
-  const float2* row_q;   // [rows]: coefficient of q, log2 of the softmax denominator
-  const float* entry_g;  // [rows][top]: gradient of the logit at the entry
-  // Piece buffers [buffers * padded][piece columns], box {64, 32}: where the
+  const float2* row_q;   // [token]: coefficient of q, log2 of the softmax denominator
+  const float* entry_g;  // [token][top]: gradient of the logit at the entry
+  // Piece buffers [buffer][token][piece columns], box {64, 32}: where the
   // gradient of one piece's logits is stored, or the codes of the logits of the
   // first `code_tiles` tiles, in pieces of piece_tiles tiles.
   CUtensorMap map_g;
-  int code_tiles, piece_tiles, padded;
-  // outputs: the next piece's codes are converted while the products run
+  int code_tiles, piece_tiles;
+  // outputs: the next piece's codes are converted while the products run, and the
+  // tokens' weighted losses added up
   ConvertParams convert;
+  const float* row_l;
+  float* total;       // NULL: not here
 
-  // product 0 of kModeOut: partial dX, fp32 [splits * padded][cols], box {32, 32}
+  // product 0 of kModeOut: partial dX, fp32 [split][token][cols], box {32, 32}
   CUtensorMap map_part;
   int part_cols;
   int part_add;       // add to what an earlier piece left
@@ -100,12 +105,12 @@ struct GemmParams {
 
 struct RowParams {
   Ctrl* ctrl;
-  int tokens, padded, dim, vocab;
+  int tokens, dim, vocab;
   const __nv_bfloat16* x;
   long long ld_x;
   const __nv_bfloat16* w;  // head with 16-byte aligned rows
   long long ld_w;
-  __nv_bfloat16* xc;     // [padded][ld_xc] rows of the tokens that count, then zeros
+  __nv_bfloat16* xc;     // [token][ld_xc] rows of the tokens that count, then zeros to the next K block
   long long ld_xc;
   int x_vec;             // rows can be copied in 16-byte pieces
   const int64_t* ids_in; // [tokens][top]
@@ -121,11 +126,11 @@ struct RowParams {
   int mean;
   unsigned char* flags;  // [tokens] token counts (distillation)
   int* pos_of;           // [tokens]: row of the token, -1 if it does not count
-  int* row_of;           // [padded]
-  int* ids;              // [padded][top]
-  float* p;              // [padded][top]
-  float* row_h;          // [padded]: sum p log p
-  float* row_c;          // [padded]: sum p
+  int* row_of;           // [token]
+  int* ids;              // [token][top]
+  float* p;              // [token][top]
+  float* row_h;          // [token]: sum p log p
+  float* row_c;          // [token]: sum p
   unsigned char* starts;
   int n_starts;
   float* entry_logit;
@@ -136,7 +141,7 @@ struct RowParams {
   float z_loss;
   float2* row_q;
   float* entry_g;
-  float* row_l;          // [padded]: coefficient * loss
+  float* row_l;          // [token]: coefficient * loss
   float* loss;           // [tokens]
   float* lse;            // [tokens] or NULL
   float* total;          // [1] or NULL
@@ -153,6 +158,7 @@ cudaError_t gemm_configure();
 cudaError_t gemm_max_clusters(int* out);
 cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, cudaStream_t stream);
 
+bool flags_needed(const RowParams& R);
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);

@@ -41,7 +41,7 @@ int g_codes = 0;
 constexpr long long kPartBytes = 1ll << 28;
 
 struct Plan {
-  int tokens, padded, dim, vocab, top;
+  int tokens, rows, m_tiles, dim, vocab, top;  // rows: tokens, at least 1
   bool want_dx, want_dw, grads, distill, pack;
   int v_tiles;               // 256-column tiles of the vocabulary
   int piece_tiles, n_pieces;
@@ -96,7 +96,8 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   P->vocab = a->vocab;
   P->top = top;
   P->distill = distill;
-  P->padded = static_cast<int>(round_up(a->tokens > 0 ? a->tokens : 1, kTileM));
+  P->rows = a->tokens > 0 ? a->tokens : 1;
+  P->m_tiles = (a->tokens + kTileM - 1) / kTileM;
   P->want_dx = a->dx != nullptr && a->tokens > 0;
   P->want_dw = a->dw != nullptr;
   P->grads = P->want_dx || P->want_dw;
@@ -105,9 +106,9 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   P->ld_xc = round_up(a->dim, 8);
   P->ld_wc = round_up(a->dim, 8);
   P->part_ld = round_up(a->dim, 8);
-  P->part_stride = P->padded * P->part_ld;
+  P->part_stride = P->rows * P->part_ld;
 
-  long long tiles = g_piece_bytes / (2ll * P->padded * kTileN);
+  long long tiles = g_piece_bytes / (2ll * P->rows * kTileN);
   if (tiles < 1) tiles = 1;
   if (tiles > P->v_tiles) tiles = P->v_tiles;
   P->n_pieces = static_cast<int>((P->v_tiles + tiles - 1) / tiles);
@@ -123,12 +124,12 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     // a partial sum costs its bytes (1.7 MB in the time of a K block, 0.27 us) once a call
     // and its place in the loop of dx_kernel
     const double split_cost = 1.0 + static_cast<double>(P->part_stride) * 4 / 1.7e6 / P->n_pieces;
-    P->splits = choose_splits(static_cast<long long>(P->padded) / kTileM * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
+    P->splits = choose_splits(static_cast<long long>(P->m_tiles) * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
                               P->want_dw ? static_cast<long long>(P->piece_tiles) * P->dx_n_tiles : 0,
                               (P->tokens + kBK - 1) / kBK, pairs, static_cast<int>(most), split_cost);
   }
 
-  const size_t rows = static_cast<size_t>(P->padded), entries = rows * top;
+  const size_t rows = static_cast<size_t>(P->rows), entries = rows * top;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -188,14 +189,14 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// bf16 or fp32 matrix [rows][cols] with row pitch ld, 128-byte swizzled boxes of
-// 128 bytes x box_rows.
-int encode(CUtensorMap* out, const void* base, long long rows, long long cols, long long ld, int box_rows,
-           bool fp32 = false) {
+// bf16 or fp32 matrices [count][rows][cols] with row pitch ld, one behind the
+// other, 128-byte swizzled boxes of 128 bytes x box_rows.
+int encode(CUtensorMap* out, const void* base, long long count, long long rows, long long cols, long long ld,
+           int box_rows, bool fp32 = false) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return fail(MUON_ERR_CUDA, "cuTensorMapEncodeTiled entry point not available");
   const cuuint64_t pitch = static_cast<cuuint64_t>(ld) * (fp32 ? 4 : 2);
-  cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), 1};
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(count)};
   cuuint64_t strides[2] = {pitch, pitch * static_cast<cuuint64_t>(rows)};
   cuuint32_t box[3] = {fp32 ? 32u : 64u, static_cast<cuuint32_t>(box_rows), 1};
   cuuint32_t estr[3] = {1, 1, 1};
@@ -302,7 +303,6 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   RowParams R = {};
   R.ctrl = reinterpret_cast<Ctrl*>(ws + P.ctrl);
   R.tokens = P.tokens;
-  R.padded = P.padded;
   R.dim = P.dim;
   R.vocab = P.vocab;
   R.x = static_cast<const __nv_bfloat16*>(a->x);
@@ -323,7 +323,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.weight = a->weight;
   R.scale = a->scale;
   R.mean = a->mean;
-  R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
+  R.flags = nullptr;
   R.pos_of = reinterpret_cast<int*>(ws + P.pos_of);
   R.row_of = reinterpret_cast<int*>(ws + P.row_of);
   R.ids = reinterpret_cast<int*>(ws + P.ids);
@@ -356,6 +356,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   GemmParams S = {};
   S.n_prod = 1;
   S.ctrl = R.ctrl;
+  S.tokens = P.tokens;
   S.vocab = P.vocab;
   S.scale2 = R.scale2;
   S.top = top;
@@ -368,14 +369,13 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   S.row_q = R.row_q;
   S.entry_g = R.entry_g;
   __nv_bfloat16* const g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
-  const long long g_ld = static_cast<long long>(P.piece_tiles) * kTileN, g_rows = static_cast<long long>(P.padded) * P.n_buffers;
+  const long long g_ld = static_cast<long long>(P.piece_tiles) * kTileN;
   S.piece_tiles = P.piece_tiles;
-  S.padded = P.padded;
   S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
-  if (P.grads) HEAD_TRY(encode(&S.map_g, g, g_rows, g_ld, g_ld, 32));
+  if (P.grads) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, 32));
   Product& L = S.prod[0];  // logits: tokens x vocabulary
-  HEAD_TRY(encode(&L.map_a, R.xc, P.padded, P.dim, P.ld_xc, 128));
-  HEAD_TRY(encode(&L.map_b, w, P.vocab, P.dim, ld_w, 128));
+  HEAD_TRY(encode(&L.map_a, R.xc, 1, P.rows, P.dim, P.ld_xc, 128));
+  HEAD_TRY(encode(&L.map_b, w, 1, P.vocab, P.dim, ld_w, 128));
   L.n_tile = kTileN;
   L.m_tiles = -1;
   L.n_tiles = P.v_tiles;
@@ -388,8 +388,8 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     O.n_prod = 0;
     Product& X = O.prod[0];  // dX: tokens x dim, over the vocabulary piece
     X = Product{};
-    HEAD_TRY(encode(&X.map_a, g, g_rows, g_ld, g_ld, 128));
-    HEAD_TRY(encode(&X.map_b, w, P.vocab, P.dim, ld_w, 64));
+    HEAD_TRY(encode(&X.map_a, g, P.n_buffers, P.rows, g_ld, g_ld, 128));
+    HEAD_TRY(encode(&X.map_b, w, 1, P.vocab, P.dim, ld_w, 64));
     X.b_mn = 1;
     X.n_tile = P.dx_n_tile;
     X.m_tiles = P.want_dx ? -1 : 0;
@@ -398,8 +398,8 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     X.swap_order = 1;
     Product& W = O.prod[1];  // dW: vocabulary piece x dim, over the tokens
     W = Product{};
-    HEAD_TRY(encode(&W.map_a, g, g_rows, g_ld, g_ld, 64));
-    HEAD_TRY(encode(&W.map_b, R.xc, P.padded, P.dim, P.ld_xc, 64));
+    HEAD_TRY(encode(&W.map_a, g, P.n_buffers, P.rows, g_ld, g_ld, 64));
+    HEAD_TRY(encode(&W.map_b, R.xc, 1, P.rows, P.dim, P.ld_xc, 64));
     W.a_mn = W.b_mn = 1;
     W.n_tile = P.dx_n_tile;
     W.n_tiles = P.dx_n_tiles;
@@ -409,7 +409,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     O.n_prod = P.want_dw ? 2 : 1;
     O.part_cols = static_cast<int>(P.part_ld);
     if (P.want_dx)
-      HEAD_TRY(encode(&O.map_part, ws + P.part, static_cast<long long>(P.splits) * P.padded, P.part_ld, P.part_ld, 32, true));
+      HEAD_TRY(encode(&O.map_part, ws + P.part, P.splits, P.rows, P.part_ld, P.part_ld, 32, true));
     O.dw = a->dw;
     O.ld_dw = a->ld_dw;
     O.dw_fp32 = a->dw_dtype == MUON_DTYPE_FP32;
@@ -417,15 +417,19 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     O.dw_cols = P.dim;
     const long long pitch = a->ld_dw * (O.dw_fp32 ? 4 : 2);
     O.dw_tma = P.want_dw && !misaligned(a->dw, 16) && (pitch & 15) == 0 && (O.dw_fp32 || !O.dw_add);
-    if (O.dw_tma) HEAD_TRY(encode(&O.map_dw, a->dw, P.vocab, P.dim, a->ld_dw, 32, O.dw_fp32 != 0));
+    if (O.dw_tma) HEAD_TRY(encode(&O.map_dw, a->dw, 1, P.vocab, P.dim, a->ld_dw, 32, O.dw_fp32 != 0));
   }
 
   if (P.pack)
     HEAD_CUDA(launch_pack(static_cast<const __nv_bfloat16*>(a->w), a->ld_w, reinterpret_cast<__nv_bfloat16*>(ws + P.wc),
                           P.ld_wc, P.vocab, P.dim, stream));
-  if (distill && P.tokens > 0) HEAD_CUDA(launch_flags(R, stream));
-  HEAD_CUDA(launch_prepare(R, distill && P.tokens > 0, stream));
-  const long long m_tiles = P.tokens > 0 ? P.padded / kTileM : 0;
+  const bool flags = flags_needed(R);
+  if (flags) {
+    R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
+    HEAD_CUDA(launch_flags(R, stream));
+  }
+  HEAD_CUDA(launch_prepare(R, flags, stream));
+  const long long m_tiles = P.m_tiles;
   HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, stream));
   ConvertParams C = {};
   C.ld = g_ld;
@@ -443,11 +447,12 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   };
   auto codes_of = [&](int piece) {
     ConvertParams D = C;
-    if (piece < P.n_stored) D.g = g + piece * P.padded * g_ld;
+    if (piece < P.n_stored) D.g = g + piece * P.rows * g_ld;
     D.tiles = tiles_of(piece);
     D.v_tile0 = piece * P.piece_tiles;
     return D;
   };
+  if (P.grads) R.total = nullptr;  // the products' launch adds the losses up beside its work
   HEAD_CUDA(launch_finalise(R, codes_of(0), 2 * pairs, stream));
   if (P.grads) {
     for (int i = 0; i < P.n_pieces; ++i) {
@@ -464,11 +469,12 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
         HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
       }
       O.convert = i + 1 < P.n_stored ? codes_of(i + 1) : ConvertParams{};
-      O.prod[0].a_m0 = buffer * P.padded;
+      O.prod[0].a_z = O.prod[1].a_z = buffer;
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;
       O.part_add = i > 0;
-      O.prod[1].a_k0 = buffer * P.padded;
+      O.row_l = R.row_l;
+      O.total = i == 0 ? a->total : nullptr;
       O.prod[1].m_tiles = tiles;
       O.dw_row0 = v0;
       O.dw_rows = cols;

@@ -36,14 +36,26 @@ __device__ __forceinline__ uint32_t encode_logit(float below) {
 // denominator; ids, entry_g: its sparse entries, ascending.
 constexpr int kConvertTiles = 8;  // independent loads in flight
 
-__device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int tile0, float2 rq, const int* ids,
-                                            const float* entry_g, int lane) {
-  const int tiles = min(kConvertTiles, C.tiles - tile0);
-  uint4* cell = reinterpret_cast<uint4*>(C.g + static_cast<long long>(row) * C.ld + tile0 * kTileN) + lane;
+struct Codes {
   uint4 v[kConvertTiles];
+};
+
+__device__ __forceinline__ uint4* code_cell(const ConvertParams& C, int row, int tile0, int lane) {
+  return reinterpret_cast<uint4*>(C.g + static_cast<long long>(row) * C.ld + tile0 * kTileN) + lane;
+}
+
+__device__ __forceinline__ void load_codes(const ConvertParams& C, int row, int tile0, int lane, Codes& c) {
+  const int tiles = min(kConvertTiles, C.tiles - tile0);
+  const uint4* cell = code_cell(C, row, tile0, lane);
 #pragma unroll
   for (int i = 0; i < kConvertTiles; ++i)
-    if (i < tiles) v[i] = __ldcs(cell + i * 32);
+    if (i < tiles) c.v[i] = __ldcs(cell + i * 32);
+}
+
+__device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, int tile0, float2 rq, const int* ids,
+                                              const float* entry_g, int lane, const Codes& c) {
+  const int tiles = min(kConvertTiles, C.tiles - tile0);
+  uint4* cell = code_cell(C, row, tile0, lane);
   // lane i: what the i-th 128 columns of the run add to the exponent
   float shift = 0.f;
   if (lane < 2 * tiles) shift = C.stats[static_cast<long long>(row) * C.stats_ld + 2 * (C.v_tile0 + tile0) + lane].x - rq.y;
@@ -59,7 +71,7 @@ __device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int
   for (int i = 0; i < kConvertTiles; ++i) {
     if (i < tiles) {
       const float a = __shfl_sync(0xFFFFFFFFu, shift, 2 * i + (lane >> 4));
-      uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+      uint32_t w[4] = {c.v[i].x, c.v[i].y, c.v[i].z, c.v[i].w};
       float g[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -91,21 +103,26 @@ __device__ __forceinline__ void convert_row(const ConvertParams& C, int row, int
 // A row past the tokens that count becomes zeros.
 __device__ __forceinline__ void clear_row(const ConvertParams& C, int row, int tile0, int lane) {
   const int tiles = min(kConvertTiles, C.tiles - tile0);
-  uint4* cell = reinterpret_cast<uint4*>(C.g + static_cast<long long>(row) * C.ld + tile0 * kTileN) + lane;
+  uint4* cell = code_cell(C, row, tile0, lane);
   for (int i = 0; i < tiles; ++i) cell[i * 32] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // All rows of a piece, dealt out to `warps` warps.
-__device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_valid, int warp, int warps, int lane) {
+__device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_valid, int tokens, int warp, int warps, int lane) {
   const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
-  const int rows = (n_valid + kBK - 1) / kBK * kBK;  // dW's product reads whole K blocks of rows
+  const int rows = min(tokens, (n_valid + kBK - 1) / kBK * kBK);  // dW's product reads whole K blocks of rows
   const long long tasks = static_cast<long long>(rows) * runs;
   for (long long t = warp; t < tasks; t += warps) {
     const int row = static_cast<int>(t / runs);
     const int tile0 = static_cast<int>(t - static_cast<long long>(row) * runs) * kConvertTiles;
     const long long at = static_cast<long long>(row) * C.top;
-    if (row < n_valid) convert_row(C, row, tile0, C.row_q[row], C.ids + at, C.entry_g + at, lane);
-    else clear_row(C, row, tile0, lane);
+    if (row < n_valid) {
+      Codes c;
+      load_codes(C, row, tile0, lane, c);
+      convert_codes(C, row, tile0, C.row_q[row], C.ids + at, C.entry_g + at, lane, c);
+    } else {
+      clear_row(C, row, tile0, lane);
+    }
   }
 }
 

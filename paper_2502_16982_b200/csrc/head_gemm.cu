@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       const int half_n = pr.n_tile >> 1;
       // rows past the tokens that count are asked for outside the tensor: zeros, without traffic
       const int m_row = tl.mi * kTileM + static_cast<int>(rank) * 128;
-      const int a_row = pr.m_tiles < 0 && m_row >= n_valid ? kOutside : pr.a_m0 + m_row;
+      const int a_row = pr.m_tiles < 0 && m_row >= n_valid ? kOutside : m_row;
       const int b_row = pr.b_n0 + tl.ni * pr.n_tile + static_cast<int>(rank) * half_n;
       const uint32_t stage_tx = 2u * static_cast<uint32_t>(kTileABytes + half_n * 128);
       const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
@@ -259,13 +259,13 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           const uint32_t leader_full = leader_full0 + stage * 8;
           const uint32_t sa = ring_u32 + stage * kStageBytes;
           const uint32_t sb = sa + kTileABytes;
-          const int ka = pr.a_k0 + kb * kBK, kbb = pr.b_k0 + kb * kBK;
+          const int ka = kb * kBK, kbb = pr.b_k0 + kb * kBK;
           if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + stage * 8, stage_tx);
           if (!a_mn) {
-            ptx::tma_load_3d_pair(sa, &pr.map_a, ka, a_row, 0, leader_full);
+            ptx::tma_load_3d_pair(sa, &pr.map_a, ka, a_row, pr.a_z, leader_full);
           } else {
-            ptx::tma_load_3d_pair(sa, &pr.map_a, a_row, ka, 0, leader_full);
-            ptx::tma_load_3d_pair(sa + 8192, &pr.map_a, a_row + 64, ka, 0, leader_full);
+            ptx::tma_load_3d_pair(sa, &pr.map_a, a_row, ka, pr.a_z, leader_full);
+            ptx::tma_load_3d_pair(sa + 8192, &pr.map_a, a_row + 64, ka, pr.a_z, leader_full);
           }
           if (!b_mn) {
             ptx::tma_load_3d_pair(sb, &pr.map_b, kbb, b_row, 0, leader_full);
@@ -352,8 +352,19 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   } else if (kMode == kModeOut && warp >= 6) {
     // ---------------------------------- codes of the next piece, meanwhile ----
     if (P.convert.g != nullptr)
-      convert_piece(P.convert, n_valid, static_cast<int>(blockIdx.x) * kConvertWarps + warp - 6,
+      convert_piece(P.convert, n_valid, P.tokens, static_cast<int>(blockIdx.x) * kConvertWarps + warp - 6,
                     static_cast<int>(gridDim.x) * kConvertWarps, lane);
+    if (P.total != nullptr && blockIdx.x == gridDim.x - 1) {
+      // the tokens' weighted losses, always in the same order; one warp, so that no barrier is needed
+      if (warp == 6) {
+        float sum = 0.f;
+#pragma unroll 4
+        for (int i = lane; i < n_valid; i += 32) sum += P.row_l[i];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (lane == 0) *P.total = sum;
+      }
+    }
   } else {
     // ----------------------------------------------------------- epilogue ----
     const int q = warp & 3;  // TMEM lane quarter this warp may read
@@ -377,6 +388,15 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       const int row0 = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32;
       const int row = row0 + lane;
       const bool have_acc = tl.kb0 != tl.kb1;
+      const int half = (warp - 2) >> 2;  // logits: columns [128 half, 128 half + 128) of the tile
+      const int g0 = tl.ni * kTileN + half * kStatN;        // column within the launch
+      const int c0v = (kMode == kModeGrad ? P.v0 : 0) + g0;  // and in the vocabulary
+      Entries en;
+      float2 rq = make_float2(0.f, 0.f);
+      if (kMode != kModeOut) {  // these loads wait beside the accumulator
+        en.open(P, row, c0v, row < n_valid);
+        if (kMode == kModeGrad && row < n_valid) rq = P.row_q[row];
+      }
       if (have_acc) {
         ok = ptx::mbar_wait_relaxed(ptx::smem_u32(&bars->acc_full[acc]), acc_phase, abort_flag);
         ok = __all_sync(0xFFFFFFFFu, ok);
@@ -389,10 +409,8 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       uint32_t taddr = tmem_base + static_cast<uint32_t>(acc * kAccCols) + (static_cast<uint32_t>(q * 32) << 16);
 
       if (kMode != kModeOut) {
-        const int half = (warp - 2) >> 2;  // columns [128 half, 128 half + 128) of the tile
         const uint32_t buf = ptx::smem_u32(staging + (warp - 2) * kStageOut);
-        const int g0 = tl.ni * kTileN + half * kStatN;       // column within the launch
-        const int c0 = (kMode == kModeGrad ? P.v0 : 0) + g0;  // and in the vocabulary
+        const int c0 = c0v;
         const int limit = P.vocab - c0;
         const bool row_ok = row < n_valid;
         // statistics: nothing is asked of rows past the tokens that count, or of columns
@@ -410,10 +428,6 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           if (row_ok) P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * 2 + half] = make_float2(-INFINITY, 0.f);
           continue;
         }
-        Entries en;
-        en.open(P, row, c0, row_ok);
-        float2 rq = make_float2(0.f, 0.f);
-        if (kMode == kModeGrad && row_ok) rq = P.row_q[row];
         float m = -INFINITY, base = 0.f, sum = 0.f;
         if (kMode == kModeStats) {
           // logits of the sparse entries
@@ -492,13 +506,8 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             ptx::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-              int y = row0, x = g0 + 64 * h;
-              if (kMode == kModeStats) {
-                const int piece = tl.ni / P.piece_tiles;
-                y += piece * P.padded;
-                x -= piece * P.piece_tiles * kTileN;
-              }
-              ptx::tma_store_3d(&P.map_g, x, y, 0, buf);
+              const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
+              ptx::tma_store_3d(&P.map_g, g0 + 64 * h - piece * P.piece_tiles * kTileN, row0, piece, buf);
               ptx::tma_store_commit();
             }
           }
@@ -519,12 +528,12 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           turn ^= 1;
           return buf0 + static_cast<uint32_t>(turn * kStageOut);
         };
-        auto send = [&](uint32_t buf, const CUtensorMap* map, int x, int y, bool add) {
+        auto send = [&](uint32_t buf, const CUtensorMap* map, int x, int y, int z, bool add) {
           ptx::fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (add) ptx::tma_reduce_add_3d(map, x, y, 0, buf);
-            else ptx::tma_store_3d(map, x, y, 0, buf);
+            if (add) ptx::tma_reduce_add_3d(map, x, y, z, buf);
+            else ptx::tma_store_3d(map, x, y, z, buf);
             ptx::tma_store_commit();
           }
         };
@@ -538,7 +547,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         };
         if (rows_ok && (is_dx || (P.dw_fp32 && P.dw_tma))) {
           const CUtensorMap* map = is_dx ? &P.map_part : &P.map_dw;
-          const int y = is_dx ? tl.split * P.padded + row0 : P.dw_row0 + row0;
+          const int y = is_dx ? row0 : P.dw_row0 + row0, z = is_dx ? tl.split : 0;
           const bool add = is_dx ? P.part_add != 0 : P.dw_add != 0;
 #pragma unroll 1
           for (int c = 0; c < limit; c += 32) {
@@ -548,7 +557,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             const uint32_t buf = next_buffer();
 #pragma unroll
             for (int i = 0; i < 8; ++i) sts128(staged(buf, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            send(buf, map, c0 + c, y, add);
+            send(buf, map, c0 + c, y, z, add);
           }
         } else if (rows_ok && P.dw_tma) {
 #pragma unroll 1
@@ -569,7 +578,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
               sts128(staged(buf, lane, i), w[0], w[1], w[2], w[3]);
               sts128(staged(buf, lane, i + 4), z[0], z[1], z[2], z[3]);
             }
-            send(buf, &P.map_dw, c0 + c, P.dw_row0 + row0, false);
+            send(buf, &P.map_dw, c0 + c, P.dw_row0 + row0, 0, false);
           }
         } else if (rows_ok) {
           // rows TMA cannot address, or sums into bf16: through shared memory, so that

@@ -62,11 +62,16 @@ __global__ void __launch_bounds__(kRowThreads) flags_kernel(const RowParams R) {
   }
 }
 
-// Token t counts?
+// Token t counts?  flags: where distillation finds its answer.
 template <bool kDistill>
-__device__ __forceinline__ bool counts(const RowParams& R, int t) {
-  return kDistill ? R.flags[t] != 0 : in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids]);
+__device__ __forceinline__ bool counts(const RowParams& R, const unsigned char* flags, int t) {
+  return kDistill ? flags[t] != 0 : in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids]);
 }
+
+// Up to this many entries in all, every block looks at them by itself (4 KB out of
+// L2, about 1 us) instead of a launch before it (3 us).
+constexpr int kFewEntries = 2048;
+constexpr int kFewTokens = 128;
 
 // Gathers the rows of the tokens that count, in token order, so that masked
 // tokens cost nothing in the products and whatever they hold reaches no sum.
@@ -84,12 +89,25 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   ptx::grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int first = blockIdx.x * kRowWarps;
+  const unsigned char* flags = R.flags;
+  if (kDistill && flags == nullptr) {
+    __shared__ unsigned char s_flags[kFewTokens];
+    if (tid < kFewTokens) s_flags[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < R.tokens * R.top; i += kRowThreads) {
+      const int t = i / R.top, k = i - t * R.top;
+      if (in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids + k]) && !(teacher_logit(R, t, k) == -INFINITY))
+        s_flags[t] = 1;
+    }
+    __syncthreads();
+    flags = s_flags;
+  }
 
   int before = 0, total = 0;
   float wsum = 0.f;
   const bool sum_weights = blockIdx.x == 0 && R.weight != nullptr;
   for (int t = tid; t < R.tokens; t += kRowThreads) {
-    const bool c = counts<kDistill>(R, t);
+    const bool c = counts<kDistill>(R, flags, t);
     total += c;
     before += c && t < first;
     if (sum_weights && c) wsum += R.weight[t];
@@ -106,9 +124,9 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   }
 
   const int t = first + warp;
-  const bool mine = t < R.tokens && counts<kDistill>(R, t);
+  const bool mine = t < R.tokens && counts<kDistill>(R, flags, t);
   const int peer = first + lane;
-  const unsigned ahead = __ballot_sync(0xFFFFFFFFu, lane < warp && peer < R.tokens && counts<kDistill>(R, peer));
+  const unsigned ahead = __ballot_sync(0xFFFFFFFFu, lane < warp && peer < R.tokens && counts<kDistill>(R, flags, peer));
   const int pos = before + __popc(ahead);
   if (t < R.tokens && lane == 0) {
     R.pos_of[t] = mine ? pos : -1;
@@ -212,9 +230,10 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
     }
   }
   // zero rows up to the next K block of dW's product
-  const int rows = (total + kBK - 1) / kBK * kBK;
+  const int rows = min(R.tokens, (total + kBK - 1) / kBK * kBK);
   for (int r = total + blockIdx.x * kRowWarps + warp; r < rows; r += gridDim.x * kRowWarps)
-    for (int c = lane; c < R.dim; c += 32) R.xc[static_cast<long long>(r) * R.ld_xc + c] = __float2bfloat16_rn(0.f);
+    for (int c = lane * 8; c < R.dim; c += 256)  // ld_xc is a multiple of 8
+      *reinterpret_cast<uint4*>(R.xc + static_cast<long long>(r) * R.ld_xc + c) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Entries with at least this share of the distribution get their logits again in
@@ -262,39 +281,57 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int n_valid = R.ctrl->n_valid;
   const int row = blockIdx.x;
   const bool writes = blockIdx.y == 0;
   const int runs = kConvert ? (C.tiles + kConvertTiles - 1) / kConvertTiles : 0;
   const int run0 = static_cast<int>(blockIdx.y) * kRowWarps + warp, run_step = static_cast<int>(gridDim.y) * kRowWarps;
-  if (row < n_valid) {
-    const int K = kDistill ? R.top : 1;
-    const long long at = static_cast<long long>(row) * K;
+  // Everything whose address is known is asked for at once (rows past the tokens that
+  // count hold no news, but they are there), so that one memory latency covers it.
+  const int K = kDistill ? R.top : 1;
+  const long long at = static_cast<long long>(row) * K;
+  constexpr int kAhead = 5;  // statistics of 163840 columns
+  const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
+  float2 ahead[kAhead];
+  int my_id = kNoId, t = 0;
+  float my_p = 1.0f, my_raw = 0.f, row_c = 1.0f, row_h = 0.f;
+  Codes codes;
+  if (row < R.tokens) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      ahead[i] = tid + i * kRowThreads < R.stats_n ? st[tid + i * kRowThreads] : make_float2(-INFINITY, 0.f);
     if (tid < K) {
-      const int id = R.ids[at + tid];
-      s_id[tid] = id;
-      s_p[tid] = id == kNoId ? 0.f : (kDistill ? R.p[at + tid] : 1.0f);
-      s_raw[tid] = id == kNoId ? 0.f : R.entry_logit[at + tid];
+      my_id = R.ids[at + tid];
+      my_raw = R.entry_logit[at + tid];
+      if (kDistill) my_p = R.p[at + tid];
     }
-    const float coef = R.ctrl->coef;
-    const int t = R.row_of[row];
-    const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
+    t = R.row_of[row];
+    if (kDistill) {
+      row_c = R.row_c[row];
+      row_h = R.row_h[row];
+    }
+    if (kConvert && run0 < runs) load_codes(C, row, run0 * kConvertTiles, lane, codes);
+  }
+  const int n_valid = R.ctrl->n_valid;
+  const float coef = R.ctrl->coef;
+  if (row < n_valid) {
+    if (tid < K) {
+      s_id[tid] = my_id;
+      s_p[tid] = my_id == kNoId ? 0.f : my_p;
+      s_raw[tid] = my_id == kNoId ? 0.f : my_raw;
+    }
     float m = -INFINITY, s = 0.f;
-#pragma unroll 4
-    for (int i = tid; i < R.stats_n; i += kRowThreads) {
-      const float2 v = st[i];
+    auto join = [&](float2 v) {
       const float mx = fmaxf(m, v.x);
       const float base = mx == -INFINITY ? 0.f : mx;
       s = s * exp2f(m - base) + v.y * exp2f(v.x - base);
       m = mx;
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) join(ahead[i]);
+    for (int i = tid + kAhead * kRowThreads; i < R.stats_n; i += kRowThreads) join(st[i]);
     const float wm = warp_max(m);
     if (lane == 0) s_max[warp] = wm;
     __syncthreads();
-    float mx = s_max[0];
-#pragma unroll
-    for (int i = 1; i < kRowWarps; ++i) mx = fmaxf(mx, s_max[i]);
-    const float base = mx == -INFINITY ? 0.f : mx;
     // The logits that carry the loss, again as plain fp32 dot products, and the
     // softmax sum with them in place of the tensor cores' values: the tensor cores
     // truncate at every step of 16 products, which shifts a logit of 15 over 2048
@@ -305,6 +342,10 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
                                      R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
         if (lane == 0) s_exact[e] = exact;
       }
+    float mx = s_max[0];
+#pragma unroll
+    for (int i = 1; i < kRowWarps; ++i) mx = fmaxf(mx, s_max[i]);
+    const float base = mx == -INFINITY ? 0.f : mx;
     s = block_sum(s * exp2f(m - base), s_f);
     for (int e = 0; e < K; ++e)
       if (s_p[e] >= kExactMass) {
@@ -316,7 +357,7 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     const float lse = lse2 * kLn2;
     const float g = coef * (R.weight != nullptr ? R.weight[t] : 1.0f);
     const float ga = g * R.logit_scale;
-    const float cq = (kDistill ? R.row_c[row] : 1.0f) + 2.0f * R.z_loss * lse;
+    const float cq = row_c + 2.0f * R.z_loss * lse;
     float ce = 0.f;
     if (tid < K && s_id[tid] != kNoId) {
       const float p = s_p[tid];
@@ -332,19 +373,22 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     ce = block_sum(ce, s_f);  // a barrier, too: s_g is complete
     const float2 rq = make_float2(ga * cq, lse2);
     if (writes && tid == 0) {
-      const float loss = ce + (kDistill ? R.row_h[row] : 0.f) + R.z_loss * lse * lse;
+      const float loss = ce + row_h + R.z_loss * lse * lse;
       R.loss[t] = loss;
       if (R.lse != nullptr) R.lse[t] = lse;
       R.row_q[row] = rq;
       R.row_l[row] = g * loss;
     }
     if (kConvert)
-      for (int r = run0; r < runs; r += run_step) convert_row(C, row, r * kConvertTiles, rq, s_id, s_g, lane);
-  } else if (kConvert && row < (n_valid + kBK - 1) / kBK * kBK) {
+      for (int r = run0; r < runs; r += run_step) {
+        if (r != run0) load_codes(C, row, r * kConvertTiles, lane, codes);
+        convert_codes(C, row, r * kConvertTiles, rq, s_id, s_g, lane, codes);
+      }
+  } else if (kConvert && row < min(R.tokens, (n_valid + kBK - 1) / kBK * kBK)) {
     for (int r = run0; r < runs; r += run_step) clear_row(C, row, r * kConvertTiles, lane);
   }
   if (R.total == nullptr || !writes) return;
-  // the last row's block adds the tokens up, always in the same order
+  // no gradients: the last row's block adds the tokens up, always in the same order
   if (tid == 0) {
     __threadfence();
     s_last = atomicAdd(&R.ctrl->ticket, 1u) == gridDim.x - 1;
@@ -361,10 +405,10 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
 
 // The first stored piece's codes where there are many rows; those of the later
 // pieces are converted beside the products (head_gemm.cu).
-__global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParams C, const Ctrl* ctrl) {
+__global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParams C, const Ctrl* ctrl, int tokens) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  convert_piece(C, ctrl->n_valid, static_cast<int>(blockIdx.x) * kRowWarps + static_cast<int>(threadIdx.x >> 5),
+  convert_piece(C, ctrl->n_valid, tokens, static_cast<int>(blockIdx.x) * kRowWarps + static_cast<int>(threadIdx.x >> 5),
                 static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
 }
 
@@ -452,6 +496,10 @@ unsigned row_blocks(int tokens) { return tokens > 0 ? static_cast<unsigned>((tok
 
 }  // namespace
 
+bool flags_needed(const RowParams& R) {
+  return R.z != nullptr && (R.tokens > kFewTokens || static_cast<long long>(R.tokens) * R.top > kFewEntries);
+}
+
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream) {
   return launch(flags_kernel, dim3(row_blocks(R.tokens)), false, stream, R);
 }
@@ -463,8 +511,8 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
   const int runs = C.g != nullptr ? (C.tiles + kConvertTiles - 1) / kConvertTiles : 0;
   if (C.g != nullptr && R.tokens < 2 * sms) {
-    // rows up to the next K block are cleared; enough blocks to spread the conversion over the device
-    const int rows = R.tokens > 0 ? (R.tokens + kBK - 1) / kBK * kBK : 1;
+    // enough blocks to spread the conversion over the device
+    const int rows = R.tokens > 0 ? R.tokens : 1;
     const int most = (runs + kRowWarps - 1) / kRowWarps, want = (2 * sms + R.tokens) / (R.tokens + 1);
     const unsigned parts = static_cast<unsigned>(want < most ? want : most);
     return launch(R.z != nullptr ? finalise_kernel<true, true> : finalise_kernel<false, true>,
@@ -473,10 +521,10 @@ cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms,
   cudaError_t e = launch(R.z != nullptr ? finalise_kernel<true, false> : finalise_kernel<false, false>,
                          dim3(static_cast<unsigned>(R.tokens > 0 ? R.tokens : 1)), true, stream, R, C);
   if (e != cudaSuccess || C.g == nullptr) return e;
-  const long long tasks = static_cast<long long>(R.padded) * runs;
+  const long long tasks = static_cast<long long>(R.tokens) * runs;
   const long long blocks = (tasks + kRowWarps - 1) / kRowWarps, many = 8ll * sms;
   return launch(convert_kernel, dim3(static_cast<unsigned>(blocks < many ? blocks : many)), true, stream, C,
-                static_cast<const Ctrl*>(R.ctrl));
+                static_cast<const Ctrl*>(R.ctrl), R.tokens);
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {

@@ -202,11 +202,11 @@ def test_vocabulary_in_pieces(knobs, codes, room, top):
     b = knobs
     T, D, V = 390, 72, 2500
     x, w, gen = make(T, D, V, 21)
-    b.muon_debug_set_head_piece_bytes(512 * 256 * 2 * 3)
+    b.muon_debug_set_head_piece_bytes(390 * 256 * 2 * 3)
     b.muon_debug_set_head_codes(codes)
     full = b.muon_head_workspace_bytes(T, D, V, top=top)
     least = b.muon_head_workspace_bytes(T, D, V, top=top, least=True)
-    piece = 512 * 256 * 2 * 3
+    piece = 390 * 256 * 2 * 3
     assert full - least == (3 * piece if codes == 2 else 0)
     ws = torch.full(({"full": full, "least": least, "between": least + piece}[room],), 255, dtype=torch.uint8, device="cuda")
     if top:
