@@ -34,7 +34,7 @@ __device__ __forceinline__ uint32_t encode_logit(float below) {
 // logits, in place, by one warp (8 columns a lane and tile, so that a tile is one
 // coalesced 512-byte access).  rq: the row's coefficient of q and log2 softmax
 // denominator; ids, entry_g: its sparse entries, ascending.
-constexpr int kConvertTiles = 8;  // independent loads in flight
+constexpr int kConvertTiles = 4;  // independent loads in flight
 
 struct Codes {
   uint4 v[kConvertTiles];

@@ -417,57 +417,63 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         // past the vocabulary that no piece buffer holds
         const bool codes = kMode == kModeStats && tl.ni < P.code_tiles;
         const bool idle = kMode == kModeStats && (row0 >= n_valid || (limit <= 0 && !codes));
-        uint32_t v[4][32];
-        if (!idle) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(taddr + half * kStatN + 32 * i, v[i]);
-          ptx::tmem_ld_wait();
-        }
-        release();
         if (idle) {
+          release();
           if (row_ok) P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * 2 + half] = make_float2(-INFINITY, 0.f);
           continue;
         }
-        float m = -INFINITY, base = 0.f, sum = 0.f;
+        taddr += half * kStatN;
+        uint32_t v[32];
+        float base = 0.f, m = -INFINITY, sum = 0.f;
+        // loops of 32 columns, not unrolled further: in a short launch the first pass
+        // through the code costs more than its loops do
         if (kMode == kModeStats) {
-          // logits of the sparse entries
+          // the row's maximum first, then exponentials and codes against it
+#pragma unroll 1
+          for (int c = 0; c < kStatN && c < limit; c += 32) {
+            ptx::tmem_ld_32x32(taddr + c, v);
+            ptx::tmem_ld_wait();
+            if (limit < c + 32) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            while (__any_sync(0xFFFFFFFFu, en.col - 32 * i < 32)) {
-              if (en.col - 32 * i < 32) {
-                P.entry_logit[static_cast<long long>(row) * P.top + en.next] = pick(v[i], en.col - 32 * i);
+              for (int j = 0; j < 32; ++j)
+                if (c + j >= limit) v[j] = 0xFF800000u;  // -inf
+            }
+            float a = __uint_as_float(v[0]), b = __uint_as_float(v[1]);
+#pragma unroll
+            for (int j = 2; j < 32; j += 2) {
+              a = fmaxf(a, __uint_as_float(v[j]));
+              b = fmaxf(b, __uint_as_float(v[j + 1]));
+            }
+            m = fmaxf(m, fmaxf(a, b));
+          }
+          m *= P.scale2;
+          base = m == -INFINITY ? 0.f : m;  // nothing but -inf
+        }
+#pragma unroll 1
+        for (int c = 0; c < kStatN; c += 32) {
+          ptx::tmem_ld_32x32(taddr + c, v);
+          ptx::tmem_ld_wait();
+          if (c == kStatN - 32) release();
+          uint32_t w[16];
+          if (kMode == kModeStats) {
+            // logits of the sparse entries
+            while (__any_sync(0xFFFFFFFFu, en.col - c < 32)) {
+              if (en.col - c < 32) {
+                P.entry_logit[static_cast<long long>(row) * P.top + en.next] = pick(v, en.col - c);
                 ++en.next;
                 en.fetch(c0);
               }
             }
-          }
-          if (limit < kStatN) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
+            if (limit < c + 32) {
 #pragma unroll
               for (int j = 0; j < 32; ++j)
-                if (32 * i + j >= limit) v[i][j] = 0xFF800000u;  // -inf
-          }
-          // the row's maximum first, then exponentials and codes against it
-          float mm[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            mm[i] = __uint_as_float(v[i][0]);
-#pragma unroll
-            for (int j = 1; j < 32; ++j) mm[i] = fmaxf(mm[i], __uint_as_float(v[i][j]));
-          }
-          m = fmaxf(fmaxf(mm[0], mm[1]), fmaxf(mm[2], mm[3])) * P.scale2;
-          base = m == -INFINITY ? 0.f : m;  // nothing but -inf
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {  // 64 columns: one staged row of 128 bytes
-          uint32_t w[32];
-          if (kMode == kModeStats) {
+                if (c + j >= limit) v[j] = 0xFF800000u;  // -inf
+            }
             float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 64; j += 2) {
-              const float y0 = fmaf(__uint_as_float(v[2 * h + (j >> 5)][j & 31]), P.scale2, -base);
-              const float y1 = fmaf(__uint_as_float(v[2 * h + (j >> 5)][(j & 31) + 1]), P.scale2, -base);
+            for (int j = 0; j < 32; j += 2) {
+              const float y0 = fmaf(__uint_as_float(v[j]), P.scale2, -base);
+              const float y1 = fmaf(__uint_as_float(v[j + 1]), P.scale2, -base);
               s[j & 2] += ex2_fast(y0);
               s[(j & 2) + 1] += ex2_fast(y1);
               w[j >> 1] = __byte_perm(encode_logit(y0), encode_logit(y1), 0x5410);
@@ -475,40 +481,46 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             sum += (s[0] + s[1]) + (s[2] + s[3]);
           } else {
 #pragma unroll
-            for (int j = 0; j < 64; j += 2) {
-              float y0 = rq.x * ex2_fast(fmaf(__uint_as_float(v[2 * h + (j >> 5)][j & 31]), P.scale2, -rq.y));
-              float y1 = rq.x * ex2_fast(fmaf(__uint_as_float(v[2 * h + (j >> 5)][(j & 31) + 1]), P.scale2, -rq.y));
+            for (int j = 0; j < 32; j += 2) {
+              const float y0 = rq.x * ex2_fast(fmaf(__uint_as_float(v[j]), P.scale2, -rq.y));
+              const float y1 = rq.x * ex2_fast(fmaf(__uint_as_float(v[j + 1]), P.scale2, -rq.y));
               w[j >> 1] = row_ok ? pack2(y0, y1) : 0u;
             }
-            if (limit < 64 * h + 64) {  // columns past the vocabulary
+            if (limit < c + 32) {  // columns past the vocabulary
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                w[j] &= (64 * h + 2 * j < limit ? 0x0000FFFFu : 0u) | (64 * h + 2 * j + 1 < limit ? 0xFFFF0000u : 0u);
+              for (int j = 0; j < 16; ++j)
+                w[j] &= (c + 2 * j < limit ? 0x0000FFFFu : 0u) | (c + 2 * j + 1 < limit ? 0xFFFF0000u : 0u);
             }
           }
           if (kMode == kModeGrad || codes) {
-            if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
-            __syncwarp();
+            const int piece16 = (c & 32) >> 3;  // a staged row of 128 bytes takes two rounds
+            if (piece16 == 0) {
+              if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
+              __syncwarp();
+            }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) sts128(staged(buf, lane, c), w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+            for (int i = 0; i < 4; ++i)
+              sts128(staged(buf, lane, piece16 + i), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
             if (kMode == kModeGrad) {
               // the entries' gradients replace what the same thread just wrote
-              while (en.col < 64 * h + 64) {
-                const int c = en.col - 64 * h;
+              while (en.col < c + 32) {
+                const int at = en.col & 63;
                 const __nv_bfloat16 e = __float2bfloat16_rn(P.entry_g[static_cast<long long>(row) * P.top + en.next]);
-                asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane, c >> 3) + 2u * (c & 7)),
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane, at >> 3) + 2u * (at & 7)),
                              "h"(*reinterpret_cast<const unsigned short*>(&e))
                              : "memory");
                 ++en.next;
                 en.fetch(c0);
               }
             }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
-              ptx::tma_store_3d(&P.map_g, g0 + 64 * h - piece * P.piece_tiles * kTileN, row0, piece, buf);
-              ptx::tma_store_commit();
+            if (piece16 != 0) {
+              ptx::fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
+                ptx::tma_store_3d(&P.map_g, g0 + c - 32 - piece * P.piece_tiles * kTileN, row0, piece, buf);
+                ptx::tma_store_commit();
+              }
             }
           }
         }

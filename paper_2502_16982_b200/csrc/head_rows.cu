@@ -336,19 +336,28 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     // softmax sum with them in place of the tensor cores' values: the tensor cores
     // truncate at every step of 16 products, which shifts a logit of 15 over 2048
     // columns by about 1e-5.
-    for (int e = warp; e < K; e += kRowWarps)
-      if (s_p[e] >= kExactMass) {
-        const float exact = warp_dot(R.xc + static_cast<long long>(row) * R.ld_xc,
-                                     R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
-        if (lane == 0) s_exact[e] = exact;
-      }
+    unsigned heavy[kDistill ? kMaxTop / 32 : 1];  // entries with their own dot product
+    int nth = 0;
+#pragma unroll
+    for (int i = 0; i < (kDistill ? kMaxTop / 32 : 1); ++i) {
+      heavy[i] = __ballot_sync(0xFFFFFFFFu, 32 * i + lane < K && s_p[32 * i + lane] >= kExactMass);
+      for (unsigned todo = heavy[i]; todo; todo &= todo - 1, ++nth)
+        if (nth % kRowWarps == warp) {
+          const int e = 32 * i + __ffs(todo) - 1;
+          const float exact = warp_dot(R.xc + static_cast<long long>(row) * R.ld_xc,
+                                       R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
+          if (lane == 0) s_exact[e] = exact;
+        }
+    }
     float mx = s_max[0];
 #pragma unroll
     for (int i = 1; i < kRowWarps; ++i) mx = fmaxf(mx, s_max[i]);
     const float base = mx == -INFINITY ? 0.f : mx;
     s = block_sum(s * exp2f(m - base), s_f);
-    for (int e = 0; e < K; ++e)
-      if (s_p[e] >= kExactMass) {
+#pragma unroll
+    for (int i = 0; i < (kDistill ? kMaxTop / 32 : 1); ++i)
+      for (unsigned todo = heavy[i]; todo; todo &= todo - 1) {
+        const int e = 32 * i + __ffs(todo) - 1;
         bool again = false;  // an index listed more than once is one logit
         for (int j = e - 1; j >= 0 && s_id[j] == s_id[e]; --j) again |= s_p[j] >= kExactMass;
         if (!again) s += exp2f(fmaf(s_exact[e], R.scale2, -base)) - exp2f(fmaf(s_raw[e], R.scale2, -base));
