@@ -205,12 +205,17 @@ class Hyper:
         return hp
 
 
+_dtype_codes = {}
+
+
 def _dtype_code(t):
+    code = _dtype_codes.get(t.dtype)
+    if code is not None:
+        return code
     import torch
-    if t.dtype == torch.bfloat16:
-        return MUON_DTYPE_BF16
-    if t.dtype == torch.float32:
-        return MUON_DTYPE_FP32
+    _dtype_codes.update({torch.bfloat16: MUON_DTYPE_BF16, torch.float32: MUON_DTYPE_FP32})
+    if t.dtype in _dtype_codes:
+        return _dtype_codes[t.dtype]
     raise MuonError(MUON_ERR_UNSUPPORTED, "dtype %s" % t.dtype)
 
 
@@ -341,6 +346,8 @@ def _raw_stream(stream, dev):
 
 def _head_vector(t, what, n, dev):
     import torch
+    if t is None:
+        return torch.empty(n, dtype=torch.float32, device=dev)
     if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != dev:
         raise MuonError(MUON_ERR_INVALID_ARG, "%s must be %d contiguous fp32 values on x's device" % (what, n))
     return t
@@ -367,12 +374,15 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
         raise MuonError(MUON_ERR_INVALID_ARG, "x and w must have contiguous rows")
     if accumulate_dw and not isinstance(dw, torch.Tensor):
         raise MuonError(MUON_ERR_INVALID_ARG, "accumulate_dw needs the dw to add to")
-    empty, f32 = torch.empty, torch.float32
+    empty = torch.empty
     # allocated for the stream the kernels run on
     with torch.cuda.stream(stream) if stream is not None else _no_context:
-        loss = empty(tokens, dtype=f32, device=dev) if loss is None else _head_vector(loss, "loss", tokens, dev)
-        lse = empty(tokens, dtype=f32, device=dev) if lse is None else _head_vector(lse, "lse", tokens, dev)
-        total = empty(1, dtype=f32, device=dev) if total is None else _head_vector(total, "total", 1, dev)
+        if loss is None and lse is None and total is None:
+            loss, lse, total = empty(2 * tokens + 1, dtype=torch.float32, device=dev).split_with_sizes((tokens, tokens, 1))
+        else:
+            loss = _head_vector(loss, "loss", tokens, dev)
+            lse = _head_vector(lse, "lse", tokens, dev)
+            total = _head_vector(total, "total", 1, dev)
         if dx is False:
             dx = None
         elif dx is not None:

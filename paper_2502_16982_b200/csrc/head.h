@@ -95,6 +95,15 @@ struct GemmParams {
   CUtensorMap map_part;
   int part_cols;
   int part_add;       // add to what an earlier piece left
+  // dX itself straight from the accumulator: the last piece's launch, where a tile is
+  // one run of K blocks
+  int dx_final;
+  const float* part;
+  long long part_ld;
+  const int* row_of;
+  void* dx;
+  long long ld_dx;
+  int dx_fp32;
   // product 1 of kModeOut: dW, box {64, 32} bf16 or {32, 32} fp32
   CUtensorMap map_dw;
   void* dw;
@@ -125,7 +134,6 @@ struct RowParams {
   float scale;
   int mean;
   unsigned char* flags;  // [tokens] token counts (distillation)
-  int* pos_of;           // [tokens]: row of the token, -1 if it does not count
   int* row_of;           // [token]
   int* ids;              // [token][top]
   float* p;              // [token][top]
@@ -145,13 +153,13 @@ struct RowParams {
   float* loss;           // [tokens]
   float* lse;            // [tokens] or NULL
   float* total;          // [1] or NULL
-  // dX
-  const float* part;
-  long long part_ld, part_stride;
-  int splits;
+  // dX: rows of tokens that do not count become zeros
   void* dx;
   long long ld_dx;
   int dx_fp32, dx_vec;
+  const float* part;     // partial dX, several runs of K blocks
+  long long part_ld, part_stride;
+  int splits;
 };
 
 cudaError_t gemm_configure();

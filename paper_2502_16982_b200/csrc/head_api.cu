@@ -48,7 +48,7 @@ struct Plan {
   int n_stored, n_buffers;   // pieces kept as codes; piece buffers in the workspace
   int splits, dx_n_tile, dx_n_tiles;
   long long ld_xc, ld_wc, part_ld, part_stride;
-  size_t ctrl, xc, wc, flags, pos_of, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
+  size_t ctrl, xc, wc, flags, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
       part, bytes, least;
 };
 
@@ -56,8 +56,10 @@ struct Plan {
 // a long axis (the vocabulary piece), dW many with a short one; both are dealt
 // out to the CTA pairs in turn, dX first.  The split with the smallest load of
 // the fullest pair is taken, a tile counted as its K blocks plus kTileCost for
-// its epilogue, and `split_cost` K blocks for joining one more partial sum.
+// its epilogue, kJoinCost for the launch that joins partial sums (4 us) and
+// `split_cost` for each of them.
 constexpr int kTileCost = 6;
+constexpr int kJoinCost = 15;
 int choose_splits(long long dx_tiles, int dx_kb, long long dw_tiles, int dw_kb, int pairs, int most, double split_cost) {
   int best = 1;
   double best_load = -1;
@@ -73,7 +75,7 @@ int choose_splits(long long dx_tiles, int dx_kb, long long dw_tiles, int dw_kb, 
                        static_cast<double>(all - x) * (dw_kb + kTileCost);
       if (l > load) load = l;
     }
-    load += s * split_cost;
+    if (s > 1) load += kJoinCost + s * split_cost;
     if (best_load < 0 || load < best_load) {
       best_load = load;
       best = s;
@@ -122,7 +124,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     long long most = kPartBytes / (P->part_stride * 4);
     most = most < 1 ? 1 : (most > 64 ? 64 : most);
     // a partial sum costs its bytes (1.7 MB in the time of a K block, 0.27 us) once a call
-    // and its place in the loop of dx_kernel
+    // and its place in the loop that joins them
     const double split_cost = 1.0 + static_cast<double>(P->part_stride) * 4 / 1.7e6 / P->n_pieces;
     P->splits = choose_splits(static_cast<long long>(P->m_tiles) * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
                               P->want_dw ? static_cast<long long>(P->piece_tiles) * P->dx_n_tiles : 0,
@@ -138,7 +140,6 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   };
   P->ctrl = take(sizeof(Ctrl));
   P->xc = take(rows * P->ld_xc * 2);
-  P->pos_of = take(rows * 4);
   P->row_of = take(rows * 4);
   P->ids = take(entries * 4);
   P->entry_logit = take(entries * 4);
@@ -155,7 +156,9 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     P->starts = take(rows * (P->v_tiles + 1));
   }
   if (P->pack) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
-  if (P->want_dx) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
+  // one run over the whole vocabulary needs no partial sums
+  const bool partial = P->splits > 1 || P->n_pieces > 1;
+  if (P->want_dx && partial) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
   P->n_stored = P->n_buffers = 0;
   P->least = off;
   if (P->grads) {
@@ -324,7 +327,6 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.scale = a->scale;
   R.mean = a->mean;
   R.flags = nullptr;
-  R.pos_of = reinterpret_cast<int*>(ws + P.pos_of);
   R.row_of = reinterpret_cast<int*>(ws + P.row_of);
   R.ids = reinterpret_cast<int*>(ws + P.ids);
   R.p = reinterpret_cast<float*>(ws + P.p);
@@ -344,14 +346,14 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.loss = a->loss;
   R.lse = a->lse;
   R.total = a->total;
+  R.dx = P.want_dx ? a->dx : nullptr;
+  R.ld_dx = a->ld_dx;
+  R.dx_fp32 = a->dx_dtype == MUON_DTYPE_FP32;
+  R.dx_vec = !misaligned(a->dx, 16) && (a->ld_dx & (R.dx_fp32 ? 3 : 7)) == 0;
   R.part = reinterpret_cast<const float*>(ws + P.part);
   R.part_ld = P.part_ld;
   R.part_stride = P.part_stride;
   R.splits = P.splits;
-  R.dx = a->dx;
-  R.ld_dx = a->ld_dx;
-  R.dx_fp32 = a->dx_dtype == MUON_DTYPE_FP32;
-  R.dx_vec = !misaligned(a->dx, 16) && (a->ld_dx & (R.dx_fp32 ? 3 : 7)) == 0;
 
   GemmParams S = {};
   S.n_prod = 1;
@@ -408,7 +410,13 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     W.swap_order = 1;
     O.n_prod = P.want_dw ? 2 : 1;
     O.part_cols = static_cast<int>(P.part_ld);
-    if (P.want_dx)
+    O.part = reinterpret_cast<const float*>(ws + P.part);
+    O.part_ld = P.part_ld;
+    O.row_of = R.row_of;
+    O.dx = R.dx;
+    O.ld_dx = R.ld_dx;
+    O.dx_fp32 = R.dx_fp32;
+    if (P.part)
       HEAD_TRY(encode(&O.map_part, ws + P.part, P.splits, P.rows, P.part_ld, P.part_ld, 32, true));
     O.dw = a->dw;
     O.ld_dw = a->ld_dw;
@@ -473,6 +481,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;
       O.part_add = i > 0;
+      O.dx_final = P.splits == 1 && i + 1 == P.n_pieces;
       O.row_l = R.row_l;
       O.total = i == 0 ? a->total : nullptr;
       O.prod[1].m_tiles = tiles;
@@ -482,7 +491,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
                                   (P.want_dw ? static_cast<long long>(tiles) * P.dx_n_tiles : 0);
       HEAD_CUDA(launch_gemm(kModeOut, O, out_tiles, pairs, stream));
     }
-    if (P.want_dx) HEAD_CUDA(launch_dx(R, stream));
+    if (P.want_dx && P.splits > 1) HEAD_CUDA(launch_dx(R, stream));
   }
   return MUON_OK;
 }

@@ -71,6 +71,16 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t w0, uint32_t w1, 
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w0), "r"(w1), "r"(w2), "r"(w3) : "memory");
 }
 
+__device__ __forceinline__ void sts32(uint32_t addr, uint32_t w) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(w) : "memory");
+}
+
+__device__ __forceinline__ float lds32(uint32_t addr) {
+  float y;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=f"(y) : "r"(addr));
+  return y;
+}
+
 // Address of 16-byte chunk `c` of row `lane` in a 32-row staging buffer, 128-byte swizzle.
 __device__ __forceinline__ uint32_t staged(uint32_t buf, int lane, int c) {
   return buf + static_cast<uint32_t>(lane * 128 + ((c ^ (lane & 7)) << 4));
@@ -557,7 +567,35 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             for (int i = 0; i < 32; ++i) v[i] = 0u;
           }
         };
-        if (rows_ok && (is_dx || (P.dw_fp32 && P.dw_tma))) {
+        if (is_dx && rows_ok && P.dx_final) {
+          // dX itself: 32 columns at a time through shared memory, so that stores run along a row
+          const int rows = min(32, n_valid - row0);
+          const int token = row < n_valid ? P.row_of[row] : 0;
+#pragma unroll 1
+          for (int c = 0; c < limit; c += 32) {
+            uint32_t v[32];
+            load(v, c);
+            ptx::tmem_ld_wait();
+            if (lane == 0) ptx::tma_store_wait_read();
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sts32(buf0 + 4u * (lane * 32 + (i ^ lane)), v[i]);
+            __syncwarp();
+            const int col = c0 + c + lane;
+            const float* part = P.part + static_cast<long long>(row0) * P.part_ld + col;
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r, part += P.part_ld) {
+              const int t = __shfl_sync(0xFFFFFFFFu, token, r);
+              if (col >= P.dw_cols) continue;  // dim
+              float y = lds32(buf0 + 4u * (r * 32 + (lane ^ r)));
+              if (P.part_add) y += *part;
+              const long long off = static_cast<long long>(t) * P.ld_dx + col;
+              if (P.dx_fp32) static_cast<float*>(P.dx)[off] = y;
+              else static_cast<__nv_bfloat16*>(P.dx)[off] = __float2bfloat16_rn(y);
+            }
+            __syncwarp();
+          }
+        } else if (rows_ok && (is_dx || (P.dw_fp32 && P.dw_tma))) {
           const CUtensorMap* map = is_dx ? &P.map_part : &P.map_dw;
           const int y = is_dx ? row0 : P.dw_row0 + row0, z = is_dx ? tl.split : 0;
           const bool add = is_dx ? P.part_add != 0 : P.dw_add != 0;
@@ -604,15 +642,14 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(buf0 + 4u * (lane * 32 + (i ^ lane))), "r"(v[i]) : "memory");
+              sts32(buf0 + 4u * (lane * 32 + (i ^ lane)), v[i]);
             __syncwarp();
             const int rows = min(32, P.dw_rows - row0);
             if (c + lane < limit) {
               long long off = static_cast<long long>(P.dw_row0 + row0) * P.ld_dw + c0 + c + lane;
 #pragma unroll 4
               for (int r = 0; r < rows; ++r, off += P.ld_dw) {
-                float y;
-                asm volatile("ld.shared.b32 %0, [%1];" : "=f"(y) : "r"(buf0 + 4u * (r * 32 + (lane ^ r))));
+                const float y = lds32(buf0 + 4u * (r * 32 + (lane ^ r)));
                 if (P.dw_fp32) {
                   float* d = static_cast<float*>(P.dw) + off;
                   *d = P.dw_add ? *d + y : y;

@@ -1,7 +1,7 @@
 // Row kernels around the products of the LM-head losses: which tokens count and
 // their rows gathered (prepare), the softmax statistics joined into losses and
-// gradient coefficients (finalise), partial dX joined and put back in token
-// order (dx).  All of them are short streaming kernels, one warp per token.
+// gradient coefficients (finalise), partial dX joined (dx).  All of them are short
+// streaming kernels.
 #include <cuda_bf16.h>
 
 #include "head_codes.cuh"
@@ -129,12 +129,18 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   const unsigned ahead = __ballot_sync(0xFFFFFFFFu, lane < warp && peer < R.tokens && counts<kDistill>(R, flags, peer));
   const int pos = before + __popc(ahead);
   if (t < R.tokens && lane == 0) {
-    R.pos_of[t] = mine ? pos : -1;
     if (mine) {
       R.row_of[pos] = t;
     } else {
       R.loss[t] = 0.f;
       if (R.lse != nullptr) R.lse[t] = 0.f;
+    }
+  }
+  if (t < R.tokens && !mine && R.dx != nullptr) {
+    const long long at = static_cast<long long>(t) * R.ld_dx;
+    for (int c = lane; c < R.dim; c += 32) {
+      if (R.dx_fp32) static_cast<float*>(R.dx)[at + c] = 0.f;
+      else static_cast<__nv_bfloat16*>(R.dx)[at + c] = __float2bfloat16_rn(0.f);
     }
   }
   if (mine) {
@@ -421,27 +427,24 @@ __global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParam
                 static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
 }
 
-// dX in token order: the partial sums of the token's row joined, zeros for a
-// token that does not count.  Eight columns a thread.
+// dX of the tokens that count, in token order, where its long axis was split: the
+// partial sums joined in the order of the runs.  Eight columns a thread.
 __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int per_row = (R.dim + 7) >> 3;
-  const long long n = static_cast<long long>(R.tokens) * per_row;
   const long long i = static_cast<long long>(blockIdx.x) * kRowThreads + threadIdx.x;
-  if (i >= n) return;
-  const int t = static_cast<int>(i / per_row);
-  const int c = static_cast<int>(i - static_cast<long long>(t) * per_row) * 8;
-  const int pos = R.pos_of[t];
+  const int row = static_cast<int>(i / per_row);
+  if (row >= R.ctrl->n_valid) return;
+  const int c = static_cast<int>(i - static_cast<long long>(row) * per_row) * 8;
+  const int t = R.row_of[row];
   float v[8] = {};
-  if (pos >= 0) {
-    const float* src = R.part + static_cast<long long>(pos) * R.part_ld + c;
+  const float* src = R.part + static_cast<long long>(row) * R.part_ld + c;
 #pragma unroll 8
-    for (int s = 0; s < R.splits; ++s, src += R.part_stride) {
-      const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
-      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-      v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-    }
+  for (int s = 0; s < R.splits; ++s, src += R.part_stride) {
+    const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
   }
   const long long off = static_cast<long long>(t) * R.ld_dx + c;
   if (R.dx_fp32) {
@@ -538,7 +541,6 @@ cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms,
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
   const long long n = static_cast<long long>(R.tokens) * ((R.dim + 7) >> 3);
-  if (n == 0) return cudaSuccess;
   return launch(dx_kernel, dim3(static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads)), true, stream, R);
 }
 
