@@ -386,11 +386,11 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
         if dx is False:
             dx = None
         elif dx is not None:
-            dx = empty(x.shape, dtype=x.dtype, device=dev) if dx is True else _head_matrix(dx, "dx", x.shape, dev)
+            dx = torch.empty_like(x) if dx is True else _head_matrix(dx, "dx", x.shape, dev)
         if dw is False:
             dw = None
         elif dw is not None:
-            dw = empty(w.shape, dtype=w.dtype, device=dev) if dw is True else _head_matrix(dw, "dw", w.shape, dev)
+            dw = torch.empty_like(w) if dw is True else _head_matrix(dw, "dw", w.shape, dev)
         ld_w, w_ptr = _row_stride(w), w.data_ptr()
         a = muon_head_args(tokens, dim, vocab, 1 if mean else 0, x.data_ptr(), w_ptr, _row_stride(x) if tokens else dim, ld_w,
                            _dtype_code(x), _dtype_code(w),

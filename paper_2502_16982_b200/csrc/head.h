@@ -14,6 +14,7 @@ constexpr int kTileM = 256;   // output rows of a CTA pair's tile (128 per CTA)
 constexpr int kTileN = 256;   // widest output tile
 constexpr int kStatN = 128;   // vocabulary columns of one statistics entry: what one epilogue warp sees of a row
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
+constexpr int kFusedRows = 296;  // fewer tokens: finalisation and conversion in one launch
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
 
@@ -95,15 +96,6 @@ struct GemmParams {
   CUtensorMap map_part;
   int part_cols;
   int part_add;       // add to what an earlier piece left
-  // dX itself straight from the accumulator: the last piece's launch, where a tile is
-  // one run of K blocks
-  int dx_final;
-  const float* part;
-  long long part_ld;
-  const int* row_of;
-  void* dx;
-  long long ld_dx;
-  int dx_fp32;
   // product 1 of kModeOut: dW, box {64, 32} bf16 or {32, 32} fp32
   CUtensorMap map_dw;
   void* dw;
@@ -157,7 +149,7 @@ struct RowParams {
   void* dx;
   long long ld_dx;
   int dx_fp32, dx_vec;
-  const float* part;     // partial dX, several runs of K blocks
+  const float* part;     // partial dX of each run of K blocks
   long long part_ld, part_stride;
   int splits;
 };

@@ -53,29 +53,28 @@ struct Plan {
 };
 
 // How many runs the K blocks of dX's tiles are cut into.  dX has few tiles with
-// a long axis (the vocabulary piece), dW many with a short one; both are dealt
-// out to the CTA pairs in turn, dX first.  The split with the smallest load of
-// the fullest pair is taken, a tile counted as its K blocks plus kTileCost for
-// its epilogue, kJoinCost for the launch that joins partial sums (4 us) and
-// `split_cost` for each of them.
+// a long axis (the vocabulary piece), dW many with a short one; the launch deals
+// them out evenly (head_gemm.cu).  The number with the smallest load of the fullest
+// CTA pair is taken, a tile counted as its K blocks plus kTileCost for its
+// epilogue, dX's long tiles a quarter dearer where a pair waits for them alone -
+// three times as dear with one row tile, whose w comes from memory and is not shared,
+// so that all pairs should read - and `split_cost` for each partial sum that is joined.
+// Measured at 1024 x 2560 x 65536 (1 split chosen): 769 us with 1, 799 with 2, 837
+// with 4; at 1 x 512 x 8192: 39 us with 8, 35 with 16 and with 32.
 constexpr int kTileCost = 6;
-constexpr int kJoinCost = 15;
-int choose_splits(long long dx_tiles, int dx_kb, long long dw_tiles, int dw_kb, int pairs, int most, double split_cost) {
+int choose_splits(int m_tiles, int n_tiles, int dx_kb, long long dw_tiles, int dw_kb, int pairs, int most, double split_cost) {
+  const long long dx_tiles = static_cast<long long>(m_tiles) * n_tiles;
+  const double wait = m_tiles == 1 ? 3.0 : 1.25;
   int best = 1;
   double best_load = -1;
   for (int s = 1; s <= most; ++s) {
     if (s > 1 && dx_kb / s < 4) break;
-    const long long nx = dx_tiles * s, n = nx + dw_tiles;
-    const int rx = static_cast<int>(nx % pairs), rn = static_cast<int>(n % pairs);
-    double load = 0;
-    // the load is one of these pairs' at its largest: it changes after pair rx - 1 and rn - 1
-    for (int w : {0, rx % pairs, rn % pairs, pairs - 1}) {
-      const long long x = nx / pairs + (w < rx), all = n / pairs + (w < rn);
-      const double l = static_cast<double>(x) * ((dx_kb + s - 1) / s + kTileCost) +
-                       static_cast<double>(all - x) * (dw_kb + kTileCost);
-      if (l > load) load = l;
-    }
-    if (s > 1) load += kJoinCost + s * split_cost;
+    const long long nx = dx_tiles * s;
+    const int cx = (dx_kb + s - 1) / s + kTileCost, cw = dw_kb + kTileCost;
+    const double even = (static_cast<double>(nx) * cx + static_cast<double>(dw_tiles) * cw) / pairs + (dw_tiles ? cw / 2 : 0);
+    const double fullest = wait * static_cast<double>((nx + pairs - 1) / pairs) * cx;
+    double load = even > fullest ? even : fullest;
+    load += s * split_cost;
     if (best_load < 0 || load < best_load) {
       best_load = load;
       best = s;
@@ -85,10 +84,15 @@ int choose_splits(long long dx_tiles, int dx_kb, long long dw_tiles, int dw_kb, 
 }
 
 // Codes or a second product x w^T?  The second product costs 2 dim FLOPs for every
-// logit, the codes 2 bytes written and 4 bytes of conversion.
-bool want_codes(int tokens, int dim) {
+// logit, the codes 2 bytes written and 4 bytes of conversion, which come cheap while
+// they stay in L2.  Measured, second product against codes: 1917 and 1686 us for
+// 2000 x 1024 x 163840, 1402 and 1396 at 768 columns, 1075 and 1282 at 512, 675
+// and 994 at 128; but 89 and 88 us for 500 x 128 x 50000, 54 and 52 for 2000 x 128
+// x 5000.
+constexpr long long kCodesInCache = 96ll << 20;
+bool want_codes(int tokens, int dim, int vocab) {
   if (g_codes != 0) return g_codes == 2;
-  return dim >= 768 || dim >= 2 * tokens;
+  return dim >= 768 || 2ll * tokens * vocab <= kCodesInCache;
 }
 
 // `room`: bytes of workspace to plan for; 0 plans for as many as are useful.
@@ -126,7 +130,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     // a partial sum costs its bytes (1.7 MB in the time of a K block, 0.27 us) once a call
     // and its place in the loop that joins them
     const double split_cost = 1.0 + static_cast<double>(P->part_stride) * 4 / 1.7e6 / P->n_pieces;
-    P->splits = choose_splits(static_cast<long long>(P->m_tiles) * P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
+    P->splits = choose_splits(P->m_tiles, P->dx_n_tiles, P->piece_tiles * (kTileN / kBK),
                               P->want_dw ? static_cast<long long>(P->piece_tiles) * P->dx_n_tiles : 0,
                               (P->tokens + kBK - 1) / kBK, pairs, static_cast<int>(most), split_cost);
   }
@@ -156,15 +160,13 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     P->starts = take(rows * (P->v_tiles + 1));
   }
   if (P->pack) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
-  // one run over the whole vocabulary needs no partial sums
-  const bool partial = P->splits > 1 || P->n_pieces > 1;
-  if (P->want_dx && partial) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
+  if (P->want_dx) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
   P->n_stored = P->n_buffers = 0;
   P->least = off;
   if (P->grads) {
     const long long one = static_cast<long long>(rows) * P->piece_tiles * kTileN * 2;
     P->n_buffers = 1;
-    if (want_codes(P->tokens, P->dim)) {
+    if (want_codes(P->tokens, P->dim, P->vocab)) {
       long long fit = (room ? static_cast<long long>(room) - static_cast<long long>(off) : kCodeBytes) / one;
       P->n_buffers = static_cast<int>(fit < 1 ? 1 : (fit > P->n_pieces ? P->n_pieces : fit));
       P->n_stored = P->n_buffers;
@@ -373,6 +375,10 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   __nv_bfloat16* const g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
   const long long g_ld = static_cast<long long>(P.piece_tiles) * kTileN;
   S.piece_tiles = P.piece_tiles;
+  auto tiles_of = [&](int piece) {
+    const int left = P.v_tiles - piece * P.piece_tiles;
+    return left < P.piece_tiles ? left : P.piece_tiles;
+  };
   S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
   if (P.grads) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, 32));
   Product& L = S.prod[0];  // logits: tokens x vocabulary
@@ -410,13 +416,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     W.swap_order = 1;
     O.n_prod = P.want_dw ? 2 : 1;
     O.part_cols = static_cast<int>(P.part_ld);
-    O.part = reinterpret_cast<const float*>(ws + P.part);
-    O.part_ld = P.part_ld;
-    O.row_of = R.row_of;
-    O.dx = R.dx;
-    O.ld_dx = R.ld_dx;
-    O.dx_fp32 = R.dx_fp32;
-    if (P.part)
+    if (P.want_dx)
       HEAD_TRY(encode(&O.map_part, ws + P.part, P.splits, P.rows, P.part_ld, P.part_ld, 32, true));
     O.dw = a->dw;
     O.ld_dw = a->ld_dw;
@@ -449,10 +449,6 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   C.entry_g = R.entry_g;
   C.starts = R.starts;
   C.n_starts = R.n_starts;
-  auto tiles_of = [&](int piece) {
-    const int left = P.v_tiles - piece * P.piece_tiles;
-    return left < P.piece_tiles ? left : P.piece_tiles;
-  };
   auto codes_of = [&](int piece) {
     ConvertParams D = C;
     if (piece < P.n_stored) D.g = g + piece * P.rows * g_ld;
@@ -481,7 +477,6 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;
       O.part_add = i > 0;
-      O.dx_final = P.splits == 1 && i + 1 == P.n_pieces;
       O.row_l = R.row_l;
       O.total = i == 0 ? a->total : nullptr;
       O.prod[1].m_tiles = tiles;
@@ -491,7 +486,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
                                   (P.want_dw ? static_cast<long long>(tiles) * P.dx_n_tiles : 0);
       HEAD_CUDA(launch_gemm(kModeOut, O, out_tiles, pairs, stream));
     }
-    if (P.want_dx && P.splits > 1) HEAD_CUDA(launch_dx(R, stream));
+    if (P.want_dx) HEAD_CUDA(launch_dx(R, stream));
   }
   return MUON_OK;
 }

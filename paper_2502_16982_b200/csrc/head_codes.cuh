@@ -30,31 +30,35 @@ __device__ __forceinline__ uint32_t encode_logit(float below) {
   return __float_as_uint(fminf(fmaf(below, -kCodeSteps, kCodeMagic), kCodeMagic + 65535.0f));
 }
 
-// Codes of up to kConvertTiles 256-column tiles of one row -> bf16 gradient of the
+// Codes of up to kTiles 256-column tiles of one row -> bf16 gradient of the
 // logits, in place, by one warp (8 columns a lane and tile, so that a tile is one
 // coalesced 512-byte access).  rq: the row's coefficient of q and log2 softmax
 // denominator; ids, entry_g: its sparse entries, ascending.
-constexpr int kConvertTiles = 4;  // independent loads in flight
+// kTiles: independent loads in flight.
+constexpr int kConvertTiles = 8;
 
+template <int kTiles>
 struct Codes {
-  uint4 v[kConvertTiles];
+  uint4 v[kTiles];
 };
 
 __device__ __forceinline__ uint4* code_cell(const ConvertParams& C, int row, int tile0, int lane) {
   return reinterpret_cast<uint4*>(C.g + static_cast<long long>(row) * C.ld + tile0 * kTileN) + lane;
 }
 
-__device__ __forceinline__ void load_codes(const ConvertParams& C, int row, int tile0, int lane, Codes& c) {
-  const int tiles = min(kConvertTiles, C.tiles - tile0);
+template <int kTiles>
+__device__ __forceinline__ void load_codes(const ConvertParams& C, int row, int tile0, int lane, Codes<kTiles>& c) {
+  const int tiles = min(kTiles, C.tiles - tile0);
   const uint4* cell = code_cell(C, row, tile0, lane);
 #pragma unroll
-  for (int i = 0; i < kConvertTiles; ++i)
+  for (int i = 0; i < kTiles; ++i)
     if (i < tiles) c.v[i] = __ldcs(cell + i * 32);
 }
 
+template <int kTiles>
 __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, int tile0, float2 rq, const int* ids,
-                                              const float* entry_g, int lane, const Codes& c) {
-  const int tiles = min(kConvertTiles, C.tiles - tile0);
+                                              const float* entry_g, int lane, const Codes<kTiles>& c) {
+  const int tiles = min(kTiles, C.tiles - tile0);
   uint4* cell = code_cell(C, row, tile0, lane);
   // lane i: what the i-th 128 columns of the run add to the exponent
   float shift = 0.f;
@@ -68,7 +72,7 @@ __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, i
   int id = next < end ? ids[next] - (C.v_tile0 + tile0) * kTileN : kNoId;
   if (id < 0) id = kNoId;
 #pragma unroll
-  for (int i = 0; i < kConvertTiles; ++i) {
+  for (int i = 0; i < kTiles; ++i) {
     if (i < tiles) {
       const float a = __shfl_sync(0xFFFFFFFFu, shift, 2 * i + (lane >> 4));
       uint32_t w[4] = {c.v[i].x, c.v[i].y, c.v[i].z, c.v[i].w};
@@ -101,8 +105,9 @@ __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, i
 }
 
 // A row past the tokens that count becomes zeros.
+template <int kTiles>
 __device__ __forceinline__ void clear_row(const ConvertParams& C, int row, int tile0, int lane) {
-  const int tiles = min(kConvertTiles, C.tiles - tile0);
+  const int tiles = min(kTiles, C.tiles - tile0);
   uint4* cell = code_cell(C, row, tile0, lane);
   for (int i = 0; i < tiles; ++i) cell[i * 32] = make_uint4(0u, 0u, 0u, 0u);
 }
@@ -117,11 +122,11 @@ __device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_vali
     const int tile0 = static_cast<int>(t - static_cast<long long>(row) * runs) * kConvertTiles;
     const long long at = static_cast<long long>(row) * C.top;
     if (row < n_valid) {
-      Codes c;
+      Codes<kConvertTiles> c;
       load_codes(C, row, tile0, lane, c);
       convert_codes(C, row, tile0, C.row_q[row], C.ids + at, C.entry_g + at, lane, c);
     } else {
-      clear_row(C, row, tile0, lane);
+      clear_row<kConvertTiles>(C, row, tile0, lane);
     }
   }
 }

@@ -120,13 +120,54 @@ struct Tile {
   int prod, mi, ni, split, kb0, kb1;
 };
 
-// Row tiles are walked in groups of `group` for each column tile (or the columns
-// innermost, swap_order), one split after the other, so that the CTA pairs that
-// run at the same time share operand tiles in L2.
-__device__ __forceinline__ Tile locate(const GemmParams& P, const Shape& s0, const Shape& s1, int t) {
-  Tile r;
-  r.prod = t < s0.tiles ? 0 : 1;
-  if (r.prod) t -= s0.tiles;
+// Which tiles a CTA pair takes, one after the other.  Product 0's tiles are dealt out
+// in turn.  Where that leaves some pairs with one more than others, product 1's go
+// to the others first, `extra` each - dX has few long tiles, dW many short ones -
+// and then to all in turn.
+constexpr int kTileCost = 6;  // K blocks that a tile's epilogue and start are worth
+
+struct Deal {
+  int pairs, pair;
+  int mine0;  // this pair's tiles of product 0
+  int more;   // pairs that have one more than the others
+  int extra;
+};
+
+__device__ __forceinline__ Deal deal_out(const Shape& s0, const Shape& s1, int pair, int pairs) {
+  Deal d;
+  d.pairs = pairs;
+  d.pair = pair;
+  const int each = s0.tiles / pairs;
+  d.more = s0.tiles - each * pairs;
+  d.mine0 = each + (pair < d.more);
+  d.extra = 0;
+  if (s1.tiles > 0 && d.more > 0) {
+    const int cost0 = (s0.k_blocks + s0.splits - 1) / s0.splits + kTileCost, cost1 = s1.k_blocks + kTileCost;
+    d.extra = min((cost0 + cost1 / 2) / cost1, s1.tiles / (pairs - d.more));
+  }
+  return d;
+}
+
+// The pair's k-th tile; false past the last.  Row tiles are walked in groups of
+// `group` for each column tile (or the columns innermost, swap_order), one split
+// after the other, so that the CTA pairs that run at the same time share operand
+// tiles in L2.
+__device__ __forceinline__ bool locate(const GemmParams& P, const Shape& s0, const Shape& s1, const Deal& d, int k, Tile& r) {
+  int t;
+  if (k < d.mine0) {
+    r.prod = 0;
+    t = d.pair + k * d.pairs;
+  } else {
+    r.prod = 1;
+    k -= d.mine0;
+    const int few = d.pairs - d.more;
+    if (d.pair >= d.more) {
+      t = k < d.extra ? k * few + d.pair - d.more : d.extra * few + (k - d.extra) * d.pairs + d.pair;
+    } else {
+      t = d.extra * few + k * d.pairs + d.pair;
+    }
+    if (t >= s1.tiles) return false;
+  }
   const Shape& s = r.prod ? s1 : s0;
   const Product& p = P.prod[r.prod];
   r.split = 0;
@@ -150,7 +191,7 @@ __device__ __forceinline__ Tile locate(const GemmParams& P, const Shape& s0, con
     r.ni = quotient(t, rows, __frcp_rn(static_cast<float>(rows)));
     r.mi = grp * p.group + (t - r.ni * rows);
   }
-  return r;
+  return true;
 }
 
 // Picks v[i] for a run-time i without putting v in local memory.
@@ -235,9 +276,9 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
 
   const int n_valid = *reinterpret_cast<volatile int*>(&P.ctrl->n_valid);
   const Shape s0 = shape_of(P, 0, n_valid);
-  Shape s1 = {0, 0, 0, 1, 0};
+  Shape s1 = {};
   if (kMode == kModeOut && P.n_prod == 2) s1 = shape_of(P, 1, n_valid);
-  const int total_tiles = s0.tiles + s1.tiles;
+  const Deal deal = deal_out(s0, s1, cluster, num_clusters);
 
   if (warp == 0) {
     // ------------------------------------------------------ TMA producer ----
@@ -248,8 +289,8 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
     const uint32_t full0 = ptx::smem_u32(&bars->full[0]);
     const uint32_t empty0 = ptx::smem_u32(&bars->empty[0]);
     const uint32_t leader_full0 = ptx::map_to_cta(full0, 0);
-    for (int t = cluster; t < total_tiles && ok; t += num_clusters) {
-      const Tile tl = locate(P, s0, s1, t);
+    Tile tl;
+    for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
       const Product& pr = P.prod[tl.prod];
       const int half_n = pr.n_tile >> 1;
       // rows past the tokens that count are asked for outside the tensor: zeros, without traffic
@@ -308,8 +349,8 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);  // SBO 1024, version 1, 128B swizzle
       constexpr uint32_t kLboK = (16u >> 4) << 16;
       constexpr uint32_t kLboMN = (8192u >> 4) << 16;  // next 64-element chunk of an MN-major operand
-      for (int t = cluster; t < total_tiles && ok; t += num_clusters) {
-        const Tile tl = locate(P, s0, s1, t);
+      Tile tl;
+    for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
         if (tl.kb0 == tl.kb1) continue;  // no token counts: the epilogue writes zeros by itself
         const Product& pr = P.prod[tl.prod];
         const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
@@ -393,8 +434,8 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         acc_phase ^= 1u;
       }
     };
-    for (int t = cluster; t < total_tiles && ok; t += num_clusters) {
-      const Tile tl = locate(P, s0, s1, t);
+    Tile tl;
+    for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
       const int row0 = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32;
       const int row = row0 + lane;
       const bool have_acc = tl.kb0 != tl.kb1;
@@ -567,35 +608,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             for (int i = 0; i < 32; ++i) v[i] = 0u;
           }
         };
-        if (is_dx && rows_ok && P.dx_final) {
-          // dX itself: 32 columns at a time through shared memory, so that stores run along a row
-          const int rows = min(32, n_valid - row0);
-          const int token = row < n_valid ? P.row_of[row] : 0;
-#pragma unroll 1
-          for (int c = 0; c < limit; c += 32) {
-            uint32_t v[32];
-            load(v, c);
-            ptx::tmem_ld_wait();
-            if (lane == 0) ptx::tma_store_wait_read();
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) sts32(buf0 + 4u * (lane * 32 + (i ^ lane)), v[i]);
-            __syncwarp();
-            const int col = c0 + c + lane;
-            const float* part = P.part + static_cast<long long>(row0) * P.part_ld + col;
-#pragma unroll 8
-            for (int r = 0; r < rows; ++r, part += P.part_ld) {
-              const int t = __shfl_sync(0xFFFFFFFFu, token, r);
-              if (col >= P.dw_cols) continue;  // dim
-              float y = lds32(buf0 + 4u * (r * 32 + (lane ^ r)));
-              if (P.part_add) y += *part;
-              const long long off = static_cast<long long>(t) * P.ld_dx + col;
-              if (P.dx_fp32) static_cast<float*>(P.dx)[off] = y;
-              else static_cast<__nv_bfloat16*>(P.dx)[off] = __float2bfloat16_rn(y);
-            }
-            __syncwarp();
-          }
-        } else if (rows_ok && (is_dx || (P.dw_fp32 && P.dw_tma))) {
+        if (rows_ok && (is_dx || (P.dw_fp32 && P.dw_tma))) {
           const CUtensorMap* map = is_dx ? &P.map_part : &P.map_dw;
           const int y = is_dx ? row0 : P.dw_row0 + row0, z = is_dx ? tl.split : 0;
           const bool add = is_dx ? P.part_add != 0 : P.dw_add != 0;

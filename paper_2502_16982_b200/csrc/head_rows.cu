@@ -28,8 +28,8 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
-// Sum over the block in a fixed order; every thread gets it.
-template <typename T>
+// Sum over a block of kWarps warps in a fixed order; every thread gets it.
+template <int kWarps = kRowWarps, typename T>
 __device__ __forceinline__ T block_sum(T v, T* scratch) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
@@ -37,7 +37,8 @@ __device__ __forceinline__ T block_sum(T v, T* scratch) {
   if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
   __syncthreads();
   T s = scratch[0];
-  for (int i = 1; i < kRowWarps; ++i) s += scratch[i];
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) s += scratch[i];
   return s;
 }
 
@@ -277,10 +278,15 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 // One block per row.  kConvert: for few rows, where a launch counts, gridDim.y blocks
 // per row, each joining the statistics by itself in the same order, and each then
 // turning its share of the first stored piece's codes into gradients.
+constexpr int kFusedTiles = 4;
+// Many rows: small blocks, so that a thousand are in flight at a time.
+__host__ __device__ constexpr int finalise_threads(bool convert) { return convert ? 256 : 128; }
+
 template <bool kDistill, bool kConvert>
-__global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R, const ConvertParams C) {
-  __shared__ float s_f[kRowWarps];
-  __shared__ float s_max[kRowWarps];
+__global__ void __launch_bounds__(finalise_threads(kConvert)) finalise_kernel(const RowParams R, const ConvertParams C) {
+  constexpr int kThreads = finalise_threads(kConvert), kWarps = kThreads / 32;
+  __shared__ float s_f[kWarps];
+  __shared__ float s_max[kWarps];
   __shared__ int s_id[kMaxTop];
   __shared__ float s_p[kMaxTop], s_raw[kMaxTop], s_exact[kMaxTop], s_g[kMaxTop];
   __shared__ bool s_last;
@@ -289,22 +295,22 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x;
   const bool writes = blockIdx.y == 0;
-  const int runs = kConvert ? (C.tiles + kConvertTiles - 1) / kConvertTiles : 0;
-  const int run0 = static_cast<int>(blockIdx.y) * kRowWarps + warp, run_step = static_cast<int>(gridDim.y) * kRowWarps;
+  const int runs = kConvert ? (C.tiles + kFusedTiles - 1) / kFusedTiles : 0;
+  const int run0 = static_cast<int>(blockIdx.y) * kWarps + warp, run_step = static_cast<int>(gridDim.y) * kWarps;
   // Everything whose address is known is asked for at once (rows past the tokens that
   // count hold no news, but they are there), so that one memory latency covers it.
   const int K = kDistill ? R.top : 1;
   const long long at = static_cast<long long>(row) * K;
-  constexpr int kAhead = 5;  // statistics of 163840 columns
+  constexpr int kAhead = 1280 / kThreads;  // statistics of 163840 columns
   const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
   float2 ahead[kAhead];
   int my_id = kNoId, t = 0;
   float my_p = 1.0f, my_raw = 0.f, row_c = 1.0f, row_h = 0.f;
-  Codes codes;
+  Codes<kFusedTiles> codes;
   if (row < R.tokens) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      ahead[i] = tid + i * kRowThreads < R.stats_n ? st[tid + i * kRowThreads] : make_float2(-INFINITY, 0.f);
+      ahead[i] = tid + i * kThreads < R.stats_n ? st[tid + i * kThreads] : make_float2(-INFINITY, 0.f);
     if (tid < K) {
       my_id = R.ids[at + tid];
       my_raw = R.entry_logit[at + tid];
@@ -315,7 +321,7 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
       row_c = R.row_c[row];
       row_h = R.row_h[row];
     }
-    if (kConvert && run0 < runs) load_codes(C, row, run0 * kConvertTiles, lane, codes);
+    if (kConvert && run0 < runs) load_codes(C, row, run0 * kFusedTiles, lane, codes);
   }
   const int n_valid = R.ctrl->n_valid;
   const float coef = R.ctrl->coef;
@@ -334,7 +340,7 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) join(ahead[i]);
-    for (int i = tid + kAhead * kRowThreads; i < R.stats_n; i += kRowThreads) join(st[i]);
+    for (int i = tid + kAhead * kThreads; i < R.stats_n; i += kThreads) join(st[i]);
     const float wm = warp_max(m);
     if (lane == 0) s_max[warp] = wm;
     __syncthreads();
@@ -348,7 +354,7 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     for (int i = 0; i < (kDistill ? kMaxTop / 32 : 1); ++i) {
       heavy[i] = __ballot_sync(0xFFFFFFFFu, 32 * i + lane < K && s_p[32 * i + lane] >= kExactMass);
       for (unsigned todo = heavy[i]; todo; todo &= todo - 1, ++nth)
-        if (nth % kRowWarps == warp) {
+        if (nth % kWarps == warp) {
           const int e = 32 * i + __ffs(todo) - 1;
           const float exact = warp_dot(R.xc + static_cast<long long>(row) * R.ld_xc,
                                        R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
@@ -357,9 +363,9 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     }
     float mx = s_max[0];
 #pragma unroll
-    for (int i = 1; i < kRowWarps; ++i) mx = fmaxf(mx, s_max[i]);
+    for (int i = 1; i < kWarps; ++i) mx = fmaxf(mx, s_max[i]);
     const float base = mx == -INFINITY ? 0.f : mx;
-    s = block_sum(s * exp2f(m - base), s_f);
+    s = block_sum<kWarps>(s * exp2f(m - base), s_f);
 #pragma unroll
     for (int i = 0; i < (kDistill ? kMaxTop / 32 : 1); ++i)
       for (unsigned todo = heavy[i]; todo; todo &= todo - 1) {
@@ -385,7 +391,7 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
       s_g[tid] = ga * (cq * exp2f(lq2) - pj);
       if (writes) R.entry_g[at + tid] = s_g[tid];
     }
-    ce = block_sum(ce, s_f);  // a barrier, too: s_g is complete
+    ce = block_sum<kWarps>(ce, s_f);  // a barrier, too: s_g is complete
     const float2 rq = make_float2(ga * cq, lse2);
     if (writes && tid == 0) {
       const float loss = ce + row_h + R.z_loss * lse * lse;
@@ -396,11 +402,11 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
     }
     if (kConvert)
       for (int r = run0; r < runs; r += run_step) {
-        if (r != run0) load_codes(C, row, r * kConvertTiles, lane, codes);
-        convert_codes(C, row, r * kConvertTiles, rq, s_id, s_g, lane, codes);
+        if (r != run0) load_codes(C, row, r * kFusedTiles, lane, codes);
+        convert_codes(C, row, r * kFusedTiles, rq, s_id, s_g, lane, codes);
       }
   } else if (kConvert && row < min(R.tokens, (n_valid + kBK - 1) / kBK * kBK)) {
-    for (int r = run0; r < runs; r += run_step) clear_row(C, row, r * kConvertTiles, lane);
+    for (int r = run0; r < runs; r += run_step) clear_row<kFusedTiles>(C, row, r * kFusedTiles, lane);
   }
   if (R.total == nullptr || !writes) return;
   // no gradients: the last row's block adds the tokens up, always in the same order
@@ -412,8 +418,8 @@ __global__ void __launch_bounds__(kRowThreads) finalise_kernel(const RowParams R
   if (s_last) {
     __threadfence();
     float sum = 0.f;
-    for (int i = tid; i < n_valid; i += kRowThreads) sum += __ldcg(R.row_l + i);
-    sum = block_sum(sum, s_f);
+    for (int i = tid; i < n_valid; i += kThreads) sum += __ldcg(R.row_l + i);
+    sum = block_sum<kWarps>(sum, s_f);
     if (tid == 0) *R.total = sum;
   }
 }
@@ -427,8 +433,10 @@ __global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParam
                 static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
 }
 
-// dX of the tokens that count, in token order, where its long axis was split: the
-// partial sums joined in the order of the runs.  Eight columns a thread.
+// dX of the tokens that count, in token order: the partial sums joined in the order
+// of the runs.  Eight columns a thread.  (Rows of dX written by the last product's
+// epilogue itself, 64 bytes at a time and to scattered tokens, cost that launch
+// 120 us at 8192 x 2048; this pass costs 28.)
 __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
@@ -491,10 +499,10 @@ __global__ void __launch_bounds__(kRowThreads) pack_kernel(const __nv_bfloat16* 
 }
 
 template <typename... Args>
-cudaError_t launch(void (*kernel)(Args...), dim3 blocks, bool overlap, cudaStream_t stream, Args... args) {
+cudaError_t launch_of(int threads, void (*kernel)(Args...), dim3 blocks, bool overlap, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = blocks;
-  cfg.blockDim = dim3(kRowThreads, 1, 1);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -502,6 +510,11 @@ cudaError_t launch(void (*kernel)(Args...), dim3 blocks, bool overlap, cudaStrea
   cfg.attrs = &attr;
   cfg.numAttrs = overlap ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <typename... Args>
+cudaError_t launch(void (*kernel)(Args...), dim3 blocks, bool overlap, cudaStream_t stream, Args... args) {
+  return launch_of(kRowThreads, kernel, blocks, overlap, stream, args...);
 }
 
 unsigned row_blocks(int tokens) { return tokens > 0 ? static_cast<unsigned>((tokens + kRowWarps - 1) / kRowWarps) : 1u; }
@@ -521,18 +534,19 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
 }
 
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
-  const int runs = C.g != nullptr ? (C.tiles + kConvertTiles - 1) / kConvertTiles : 0;
-  if (C.g != nullptr && R.tokens < 2 * sms) {
+  if (C.g != nullptr && R.tokens < kFusedRows) {
     // enough blocks to spread the conversion over the device
     const int rows = R.tokens > 0 ? R.tokens : 1;
+    const int runs = (C.tiles + kFusedTiles - 1) / kFusedTiles;
     const int most = (runs + kRowWarps - 1) / kRowWarps, want = (2 * sms + R.tokens) / (R.tokens + 1);
     const unsigned parts = static_cast<unsigned>(want < most ? want : most);
     return launch(R.z != nullptr ? finalise_kernel<true, true> : finalise_kernel<false, true>,
                   dim3(static_cast<unsigned>(rows), parts), true, stream, R, C);
   }
-  cudaError_t e = launch(R.z != nullptr ? finalise_kernel<true, false> : finalise_kernel<false, false>,
-                         dim3(static_cast<unsigned>(R.tokens > 0 ? R.tokens : 1)), true, stream, R, C);
+  cudaError_t e = launch_of(finalise_threads(false), R.z != nullptr ? finalise_kernel<true, false> : finalise_kernel<false, false>,
+                            dim3(static_cast<unsigned>(R.tokens > 0 ? R.tokens : 1)), true, stream, R, C);
   if (e != cudaSuccess || C.g == nullptr) return e;
+  const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
   const long long tasks = static_cast<long long>(R.tokens) * runs;
   const long long blocks = (tasks + kRowWarps - 1) / kRowWarps, many = 8ll * sms;
   return launch(convert_kernel, dim3(static_cast<unsigned>(blocks < many ? blocks : many)), true, stream, C,
