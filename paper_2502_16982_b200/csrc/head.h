@@ -12,7 +12,8 @@ namespace head {
 
 constexpr int kTileM = 256;   // output rows of a CTA pair's tile (128 per CTA)
 constexpr int kTileN = 256;   // widest output tile
-constexpr int kStatN = 128;   // vocabulary columns of one statistics entry: what one epilogue warp sees of a row
+constexpr int kStatN = 64;    // vocabulary columns of one statistics entry: what an epilogue thread holds of a row
+constexpr int kUnits = kTileN / kStatN;
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
 constexpr int kFusedRows = 296;  // fewer tokens: finalisation and conversion in one launch
 constexpr int kMaxTop = 128;  // sparse target entries of one token
@@ -64,6 +65,7 @@ enum { kModeStats = 0, kModeGrad = 1, kModeOut = 2 };
 struct GemmParams {
   Product prod[2];
   int n_prod;
+  int by_tile;  // statistics, gradient: see the epilogue
   Ctrl* ctrl;
 
   int tokens;
@@ -77,7 +79,7 @@ struct GemmParams {
   const unsigned char* starts;  // [token][n_starts]: entries below each 256-column tile (top > 1)
   int n_starts;
   float* entry_logit; // [token][top] raw logit of each entry
-  float2* stats;      // [token][stats_ld]: maximum and sum of exponentials per 128 columns
+  float2* stats;      // [token][stats_ld]: maximum and sum of exponentials per kStatN columns
   int stats_ld;
   const float2* row_q;   // [token]: coefficient of q, log2 of the softmax denominator
   const float* entry_g;  // [token][top]: gradient of the logit at the entry

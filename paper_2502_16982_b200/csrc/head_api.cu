@@ -148,7 +148,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   P->ids = take(entries * 4);
   P->entry_logit = take(entries * 4);
   P->entry_g = take(entries * 4);
-  P->stats = take(rows * P->v_tiles * 2 * sizeof(float2));
+  P->stats = take(rows * P->v_tiles * kUnits * sizeof(float2));
   P->row_q = take(rows * sizeof(float2));
   P->row_l = take(rows * 4);
   P->flags = P->p = P->row_h = P->row_c = P->starts = P->wc = P->g = P->part = 0;
@@ -338,7 +338,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.n_starts = P.v_tiles + 1;
   R.entry_logit = reinterpret_cast<float*>(ws + P.entry_logit);
   R.stats = reinterpret_cast<float2*>(ws + P.stats);
-  R.stats_ld = R.stats_n = 2 * P.v_tiles;
+  R.stats_ld = R.stats_n = kUnits * P.v_tiles;
   R.scale2 = static_cast<float>(logit_scale * 1.4426950408889634);
   R.logit_scale = logit_scale;
   R.z_loss = z_loss;
@@ -438,6 +438,8 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   }
   HEAD_CUDA(launch_prepare(R, flags, stream));
   const long long m_tiles = P.m_tiles;
+  // more tiles than CTA pairs: the epilogue's warps share them out instead of their columns
+  S.by_tile = m_tiles * P.v_tiles > pairs;
   HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, stream));
   ConvertParams C = {};
   C.ld = g_ld;
@@ -470,6 +472,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
         S.v0 = v0;
         L.b_n0 = v0;
         L.n_tiles = tiles;
+        S.by_tile = m_tiles * tiles > pairs;
         HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
       }
       O.convert = i + 1 < P.n_stored ? codes_of(i + 1) : ConvertParams{};

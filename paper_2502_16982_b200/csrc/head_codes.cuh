@@ -1,5 +1,5 @@
 // 16-bit codes of logits.  Where the workspace has room, the statistics pass keeps
-// every logit as its distance below the largest one of its row in the same 128
+// every logit as its distance below the largest one of its row in the same 64
 // columns, in steps of 2^-11 on the log2 scale: code = round((max - y) 2^11), capped at
 // 65535, y = scale2 * logit.  Decoding gives q within 2^-12 ln 2 = 1.7e-4, a
 // twentieth of the bf16 rounding of the gradient that follows; what lies 2^-32
@@ -25,9 +25,10 @@ __device__ __forceinline__ float ex2_fast(float x) {
   return y;
 }
 
-// `below` = y - max, at most 0; the code is in the low 16 bits of the result.
-__device__ __forceinline__ uint32_t encode_logit(float below) {
-  return __float_as_uint(fminf(fmaf(below, -kCodeSteps, kCodeMagic), kCodeMagic + 65535.0f));
+// `steps` = (max - y) kCodeSteps + kCodeMagic, rounded to a whole number by the
+// addition; the code is in the low 16 bits of the result.
+__device__ __forceinline__ uint32_t clamp_code(float steps) {
+  return __float_as_uint(fminf(steps, kCodeMagic + 65535.0f));
 }
 
 // Codes of up to kTiles 256-column tiles of one row -> bf16 gradient of the
@@ -60,9 +61,11 @@ __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, i
                                               const float* entry_g, int lane, const Codes<kTiles>& c) {
   const int tiles = min(kTiles, C.tiles - tile0);
   uint4* cell = code_cell(C, row, tile0, lane);
-  // lane i: what the i-th 128 columns of the run add to the exponent
+  // lane i: what the i-th kStatN columns of the run add to the exponent
   float shift = 0.f;
-  if (lane < 2 * tiles) shift = C.stats[static_cast<long long>(row) * C.stats_ld + 2 * (C.v_tile0 + tile0) + lane].x - rq.y;
+  static_assert(kTiles * kUnits <= 32, "one lane per statistics entry");
+  if (lane < kUnits * tiles)
+    shift = C.stats[static_cast<long long>(row) * C.stats_ld + kUnits * (C.v_tile0 + tile0) + lane].x - rq.y;
   int next = 0, end = 1;
   if (C.top > 1) {
     const unsigned char* s = C.starts + static_cast<long long>(row) * C.n_starts + C.v_tile0 + tile0;
@@ -74,7 +77,7 @@ __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, i
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     if (i < tiles) {
-      const float a = __shfl_sync(0xFFFFFFFFu, shift, 2 * i + (lane >> 4));
+      const float a = __shfl_sync(0xFFFFFFFFu, shift, kUnits * i + lane * 8 / kStatN);
       uint32_t w[4] = {c.v[i].x, c.v[i].y, c.v[i].z, c.v[i].w};
       float g[8];
 #pragma unroll

@@ -11,9 +11,9 @@
 //   warp 0     TMA producer: this CTA's 128 rows of A and its half of B per K
 //              block, into a ring of kStages; no multicast
 //   warp 1     leader CTA only: UMMA issuer, two TMEM accumulator stages
-//   epilogue   statistics and gradient: warps 2-9, a lane per row and half of the
-//              tile's columns per warp, so that a row's maximum and sum over 128
-//              columns stay in one thread's registers; outputs: warps 2-5
+//   epilogue   statistics and gradient: warps 2-17, a lane per row and 64 columns at
+//              a time, so that a row's maximum and sum over them stay in one
+//              thread's registers; outputs: warps 2-5
 //   warps 6-9  outputs only: turn the next piece's codes (head_codes.cuh) into the
 //              gradient of its logits while the tensor cores work on this piece
 //
@@ -25,6 +25,8 @@
 // MUON_ERR_TIMEOUT, all roles drain and the kernel returns.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "head_codes.cuh"
 #include "ptx.cuh"
 
@@ -33,7 +35,6 @@ namespace head {
 
 namespace {
 
-constexpr int kStages = 6;
 constexpr int kTileABytes = 128 * kBK * 2;
 constexpr int kTileBBytes = 128 * kBK * 2;
 constexpr int kStageBytes = kTileABytes + kTileBBytes;
@@ -41,24 +42,29 @@ constexpr int kNumAcc = 2;
 constexpr int kAccCols = 256;
 constexpr int kTmemCols = kNumAcc * kAccCols;
 constexpr int kStageOut = 32 * 128;  // one warp's 32 rows x 128 bytes
-constexpr int kStaging = 8 * kStageOut;  // eight warps with one buffer each, or four with two
-__host__ __device__ constexpr int epi_warps(int mode) { return mode == kModeOut ? 4 : 8; }
+// Shared memory is split between the operand ring and the staging of stores: sixteen
+// warps with one buffer each, or four with two.
+__host__ __device__ constexpr int epi_warps(int mode) { return mode == kModeOut ? 4 : 16; }
+__host__ __device__ constexpr int stages_of(int mode) { return mode == kModeOut ? 6 : 5; }
+__host__ __device__ constexpr int staging_of(int mode) { return (mode == kModeOut ? 8 : 16) * kStageOut; }
+constexpr int kMaxStages = 6;
 constexpr int kConvertWarps = 4;
 __host__ __device__ constexpr int threads_of(int mode) { return 64 + 32 * (epi_warps(mode) + (mode == kModeOut ? kConvertWarps : 0)); }
 
 constexpr int kOutside = 1 << 30;  // a row coordinate past every tensor
 
 struct Barriers {
-  unsigned long long full[kStages];    // leader's copy is the live one
-  unsigned long long empty[kStages];
+  unsigned long long full[kMaxStages];    // leader's copy is the live one
+  unsigned long long empty[kMaxStages];
   unsigned long long acc_full[kNumAcc];
   unsigned long long acc_empty[kNumAcc];  // leader's copy is the live one
   uint32_t tmem_base;
   int abort_flag;
 };
 
-constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
-static_assert(sizeof(Barriers) <= 512 && kSmemBytes <= 232448, "exceeds the 227 KiB shared-memory limit");
+constexpr int smem_of(int mode) { return 1024 + stages_of(mode) * kStageBytes + staging_of(mode) + 512; }
+static_assert(sizeof(Barriers) <= 512 && smem_of(kModeOut) <= 232448 && smem_of(kModeStats) <= 232448,
+              "exceeds the 227 KiB shared-memory limit");
 
 __device__ __forceinline__ void report_timeout(const GemmParams& P) { atomicExch(&P.ctrl->status, -6); }
 
@@ -79,6 +85,36 @@ __device__ __forceinline__ float lds32(uint32_t addr) {
   float y;
   asm volatile("ld.shared.b32 %0, [%1];" : "=f"(y) : "r"(addr));
   return y;
+}
+
+// Pairs of floats in one instruction each.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Largest of three; a NaN shows.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 // Address of 16-byte chunk `c` of row `lane` in a 32-row staging buffer, 128-byte swizzle.
@@ -195,37 +231,62 @@ __device__ __forceinline__ bool locate(const GemmParams& P, const Shape& s0, con
 }
 
 // Picks v[i] for a run-time i without putting v in local memory.
-__device__ __forceinline__ float pick(const uint32_t (&v)[32], int i) {
+__device__ __forceinline__ float pick(const uint32_t (&v)[kStatN], int i) {
   uint32_t r = v[0];
 #pragma unroll
-  for (int j = 1; j < 32; ++j) r = i == j ? v[j] : r;
+  for (int j = 1; j < kStatN; ++j) r = i == j ? v[j] : r;
   return __uint_as_float(r);
 }
 
-// The sparse entries of one row that fall into 128 columns from `col0` on.
+// Where a row's sparse entries in one 256-column tile are found: asked for a tile
+// ahead, so that the loads wait for nothing.
+struct EntryHead {
+  int a, b;  // one target per token: its index; else positions in the row's list
+};
+
+__device__ __forceinline__ EntryHead entry_head(const GemmParams& P, int row, int tile, bool row_ok) {
+  EntryHead h = {kNoId, 0};
+  if (P.top == 1) {
+    if (row_ok) h.a = P.ids[row];
+  } else {
+    h.a = 0;
+    if (row_ok) {
+      const unsigned char* s = P.starts + static_cast<long long>(row) * P.n_starts + tile;
+      h.a = s[0];
+      h.b = s[1];
+    }
+  }
+  return h;
+}
+
+// The sparse entries of one row in kStatN columns from col0 on.
 struct Entries {
   int next, end;  // positions in the row's list
   int col;        // column of entry `next` from col0, or past every column
   const int* ids;
 
-  __device__ __forceinline__ void open(const GemmParams& P, int row, int col0, bool row_ok) {
-    next = end = 0;
-    ids = P.ids + static_cast<long long>(row) * P.top;
-    if (row_ok) {
-      if (P.top == 1) {
-        end = 1;
-      } else {
-        const unsigned char* s = P.starts + static_cast<long long>(row) * P.n_starts + col0 / kTileN;
-        next = s[0];
-        end = s[1];
-        while (next < end && ids[next] < col0) ++next;
-      }
+  __device__ __forceinline__ void open(const GemmParams& P, const EntryHead& h, int row, int col0) {
+    if (P.top == 1) {
+      next = 0;
+      end = 1;
+      col = h.a - col0;
+      if (col < 0 || col >= kStatN) col = kNoId;
+    } else {
+      next = h.a;
+      end = h.b;
+      ids = P.ids + static_cast<long long>(row) * P.top;
+      while (next < end && ids[next] < col0) ++next;
+      fetch(col0);
     }
-    fetch(col0);
   }
   __device__ __forceinline__ void fetch(int col0) {
     col = next < end ? ids[next] - col0 : kNoId;
-    if (col < 0 || col >= kStatN) col = kNoId;
+    if (col >= kStatN) col = kNoId;
+  }
+  __device__ __forceinline__ void pop(const GemmParams& P, int col0) {
+    ++next;
+    if (P.top == 1) col = kNoId;
+    else fetch(col0);
   }
 };
 
@@ -234,9 +295,9 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
+  constexpr int kStages = stages_of(kMode);
   uint8_t* staging = ring + kStages * kStageBytes;
-  Barriers* bars = reinterpret_cast<Barriers*>(staging + kStaging);
-  constexpr int kEpiWarps = epi_warps(kMode);
+  Barriers* bars = reinterpret_cast<Barriers*>(staging + staging_of(kMode));
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -252,7 +313,8 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
     }
     for (int s = 0; s < kNumAcc; ++s) {
       ptx::mbar_init(ptx::smem_u32(&bars->acc_full[s]), 1);
-      ptx::mbar_init(ptx::smem_u32(&bars->acc_empty[s]), 2 * kEpiWarps);
+      // warps of both CTAs that read one accumulator
+      ptx::mbar_init(ptx::smem_u32(&bars->acc_empty[s]), 2 * (kMode == kModeOut ? 4 : (P.by_tile ? 8 : 16)));
     }
     bars->abort_flag = 0;
     ptx::fence_barrier_init();
@@ -419,165 +481,177 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   } else {
     // ----------------------------------------------------------- epilogue ----
     const int q = warp & 3;  // TMEM lane quarter this warp may read
-    int acc = 0;
-    uint32_t acc_phase = 0;
-    int turn = 0;  // staging buffer last used (outputs)
+    const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
     bool ok = true;
+    auto wait_acc = [&](int acc, uint32_t acc_phase) {
+      ok = ptx::mbar_wait_relaxed(ptx::smem_u32(&bars->acc_full[acc]), acc_phase, abort_flag);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok && lane == 0) report_timeout(P);
+      if (ok) ptx::tc_fence_after();
+    };
     // accumulator fully read: hand the TMEM stage back to the leader's issuer
-    auto release = [&]() {
+    auto release = [&](int acc) {
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0)
         ptx::mbar_arrive_cluster_no_release(ptx::map_to_cta(ptx::smem_u32(&bars->acc_empty[acc]), 0));
-      if (++acc == kNumAcc) {
-        acc = 0;
-        acc_phase ^= 1u;
-      }
     };
-    Tile tl;
-    for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
-      const int row0 = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32;
-      const int row = row0 + lane;
-      const bool have_acc = tl.kb0 != tl.kb1;
-      const int half = (warp - 2) >> 2;  // logits: columns [128 half, 128 half + 128) of the tile
-      const int g0 = tl.ni * kTileN + half * kStatN;        // column within the launch
-      const int c0v = (kMode == kModeGrad ? P.v0 : 0) + g0;  // and in the vocabulary
-      Entries en;
+    if constexpr (kMode != kModeOut) {
+      // Four groups of four warps, a unit of work being 64 columns of a warp's 32 rows:
+      // all that a thread needs of its row then stays in registers.  Each group takes
+      // one unit of every tile or, where a pair has several tiles, two units of every
+      // other tile, so that the groups' waits and arithmetic overlap (a tile's
+      // accumulator is read and handed back at once in either case).  With two groups
+      // the schedulers issued in 45 % of the cycles, waiting for latencies.
+      const int group = (warp - 2) >> 2;
+      const bool by_tile = P.by_tile != 0;
+      const int step = by_tile ? 2 : 1;
+      const int unit0 = by_tile ? (group & 1) * 2 : group, unit1 = by_tile ? unit0 + 2 : unit0 + 1;
+      const uint32_t buf = ptx::smem_u32(staging + (warp - 2) * kStageOut);
+      const int row_in = static_cast<int>(rank) * 128 + q * 32;
+      const uint64_t scale = pair(P.scale2, P.scale2);
+      Tile tl;
+      int k = by_tile ? group >> 1 : 0;
+      bool more = locate(P, s0, s1, deal, k, tl);
+      EntryHead head = {kNoId, 0};
       float2 rq = make_float2(0.f, 0.f);
-      if (kMode != kModeOut) {  // these loads wait beside the accumulator
-        en.open(P, row, c0v, row < n_valid);
-        if (kMode == kModeGrad && row < n_valid) rq = P.row_q[row];
-      }
-      if (have_acc) {
-        ok = ptx::mbar_wait_relaxed(ptx::smem_u32(&bars->acc_full[acc]), acc_phase, abort_flag);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) {
-          if (lane == 0) report_timeout(P);
-          break;
-        }
-        ptx::tc_fence_after();
-      }
-      uint32_t taddr = tmem_base + static_cast<uint32_t>(acc * kAccCols) + (static_cast<uint32_t>(q * 32) << 16);
-
-      if (kMode != kModeOut) {
-        const uint32_t buf = ptx::smem_u32(staging + (warp - 2) * kStageOut);
-        const int c0 = c0v;
-        const int limit = P.vocab - c0;
+      const int first_tile = kMode == kModeGrad ? P.v0 / kTileN : 0;
+      auto ask = [&](const Tile& t, EntryHead& h, float2& r) {
+        const int row = t.mi * kTileM + row_in + lane;
+        h = entry_head(P, row, first_tile + t.ni, row < n_valid);
+        if (kMode == kModeGrad) r = row < n_valid ? P.row_q[row] : make_float2(0.f, 0.f);
+      };
+      if (more) ask(tl, head, rq);
+      while (more) {
+        Tile tl_next;
+        EntryHead head_next = {kNoId, 0};
+        float2 rq_next = make_float2(0.f, 0.f);
+        more = locate(P, s0, s1, deal, k + step, tl_next);
+        if (more) ask(tl_next, head_next, rq_next);
+        const int row0 = tl.mi * kTileM + row_in;
+        const int row = row0 + lane;
         const bool row_ok = row < n_valid;
-        // statistics: nothing is asked of rows past the tokens that count, or of columns
-        // past the vocabulary that no piece buffer holds
+        const int c0 = (first_tile + tl.ni) * kTileN;  // first vocabulary column of the tile
+        const int acc = k & 1;
+        wait_acc(acc, static_cast<uint32_t>(k >> 1) & 1u);
+        if (!ok) break;
+        // nothing is asked of the statistics of rows past the tokens that count
+        const bool idle = kMode == kModeStats && row0 >= n_valid;
         const bool codes = kMode == kModeStats && tl.ni < P.code_tiles;
-        const bool idle = kMode == kModeStats && (row0 >= n_valid || (limit <= 0 && !codes));
-        if (idle) {
-          release();
-          if (row_ok) P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * 2 + half] = make_float2(-INFINITY, 0.f);
-          continue;
-        }
-        taddr += half * kStatN;
-        uint32_t v[32];
-        float base = 0.f, m = -INFINITY, sum = 0.f;
-        // loops of 32 columns, not unrolled further: in a short launch the first pass
-        // through the code costs more than its loops do
-        if (kMode == kModeStats) {
-          // the row's maximum first, then exponentials and codes against it
+        if (idle) release(acc);
 #pragma unroll 1
-          for (int c = 0; c < kStatN && c < limit; c += 32) {
-            ptx::tmem_ld_32x32(taddr + c, v);
-            ptx::tmem_ld_wait();
-            if (limit < c + 32) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c + j >= limit) v[j] = 0xFF800000u;  // -inf
-            }
-            float a = __uint_as_float(v[0]), b = __uint_as_float(v[1]);
-#pragma unroll
-            for (int j = 2; j < 32; j += 2) {
-              a = fmaxf(a, __uint_as_float(v[j]));
-              b = fmaxf(b, __uint_as_float(v[j + 1]));
-            }
-            m = fmaxf(m, fmaxf(a, b));
-          }
-          m *= P.scale2;
-          base = m == -INFINITY ? 0.f : m;  // nothing but -inf
-        }
-#pragma unroll 1
-        for (int c = 0; c < kStatN; c += 32) {
-          ptx::tmem_ld_32x32(taddr + c, v);
+        for (int unit = unit0; unit < unit1 && !idle; ++unit) {
+          const int col0 = c0 + unit * kStatN;
+          const int limit = P.vocab - col0;  // columns of the unit in the vocabulary
+          uint32_t v[kStatN];
+          ptx::tmem_ld_32x64(tmem_row + static_cast<uint32_t>(acc * kAccCols + unit * kStatN), v);
+          Entries en;
+          en.open(P, head, row, col0);
           ptx::tmem_ld_wait();
-          if (c == kStatN - 32) release();
-          uint32_t w[16];
+          if (unit + 1 == unit1) release(acc);
+          float m = -INFINITY, base = 0.f;
           if (kMode == kModeStats) {
             // logits of the sparse entries
-            while (__any_sync(0xFFFFFFFFu, en.col - c < 32)) {
-              if (en.col - c < 32) {
-                P.entry_logit[static_cast<long long>(row) * P.top + en.next] = pick(v, en.col - c);
-                ++en.next;
-                en.fetch(c0);
+            while (__any_sync(0xFFFFFFFFu, en.col < kStatN)) {
+              if (en.col < kStatN) {
+                P.entry_logit[static_cast<long long>(row) * P.top + en.next] = pick(v, en.col);
+                en.pop(P, col0);
               }
             }
-            if (limit < c + 32) {
+            if (limit < kStatN) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c + j >= limit) v[j] = 0xFF800000u;  // -inf
+              for (int j = 0; j < kStatN; ++j)
+                if (j >= limit) v[j] = 0xFF800000u;  // -inf
             }
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            // the row's maximum first, then exponentials and codes against it
+            float a = __uint_as_float(v[0]), b = __uint_as_float(v[1]);
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float y0 = fmaf(__uint_as_float(v[j]), P.scale2, -base);
-              const float y1 = fmaf(__uint_as_float(v[j + 1]), P.scale2, -base);
-              s[j & 2] += ex2_fast(y0);
-              s[(j & 2) + 1] += ex2_fast(y1);
-              w[j >> 1] = __byte_perm(encode_logit(y0), encode_logit(y1), 0x5410);
+            for (int j = 2; j < kStatN - 2; j += 4) {
+              a = max3(a, __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
+              b = max3(b, __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
             }
-            sum += (s[0] + s[1]) + (s[2] + s[3]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float y0 = rq.x * ex2_fast(fmaf(__uint_as_float(v[j]), P.scale2, -rq.y));
-              const float y1 = rq.x * ex2_fast(fmaf(__uint_as_float(v[j + 1]), P.scale2, -rq.y));
-              w[j >> 1] = row_ok ? pack2(y0, y1) : 0u;
-            }
-            if (limit < c + 32) {  // columns past the vocabulary
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-                w[j] &= (c + 2 * j < limit ? 0x0000FFFFu : 0u) | (c + 2 * j + 1 < limit ? 0xFFFF0000u : 0u);
-            }
+            m = max3(max3(a, __uint_as_float(v[kStatN - 2]), __uint_as_float(v[kStatN - 1])), b, b) * P.scale2;
+            base = m == -INFINITY ? 0.f : m;  // nothing but -inf
           }
-          if (kMode == kModeGrad || codes) {
-            const int piece16 = (c & 32) >> 3;  // a staged row of 128 bytes takes two rounds
-            if (piece16 == 0) {
-              if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
-              __syncwarp();
-            }
+          const uint64_t shift = kMode == kModeStats ? pair(-base, -base) : pair(-rq.y, -rq.y);
+          auto work = [&](auto store) {
+            constexpr bool kStore = decltype(store)::value;
+            const uint64_t steps = pair(-kCodeSteps, -kCodeSteps), magic = pair(kCodeMagic, kCodeMagic);
+            uint64_t sum[2] = {0, 0};  // pairs of zeros
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              sts128(staged(buf, lane, piece16 + i), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            for (int j = 0; j < kStatN; j += 2) {
+              const uint64_t y = fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale, shift);
+              float y0, y1;
+              unpair(y, y0, y1);
+              y0 = ex2_fast(y0);
+              y1 = ex2_fast(y1);
+              if (kMode == kModeStats) {
+                sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pair(y0, y1));
+                if (kStore) {
+                  float d0, d1;
+                  unpair(fma2(y, steps, magic), d0, d1);
+                  v[j >> 1] = __byte_perm(clamp_code(d0), clamp_code(d1), 0x5410);
+                }
+              } else {
+                v[j >> 1] = row_ok ? pack2(rq.x * y0, rq.x * y1) : 0u;
+              }
+            }
+            if (kMode == kModeStats && row_ok) {
+              float s0_, s1_;
+              unpair(add2(sum[0], sum[1]), s0_, s1_);
+              P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * kUnits + unit] = make_float2(m, s0_ + s1_);
+            }
+          };
+          if (kMode == kModeGrad || codes) {
+            work(std::true_type{});
+            if (kMode == kModeGrad && limit < kStatN) {  // columns past the vocabulary
+#pragma unroll
+              for (int j = 0; j < kStatN / 2; ++j)
+                v[j] &= (2 * j < limit ? 0x0000FFFFu : 0u) | (2 * j + 1 < limit ? 0xFFFF0000u : 0u);
+            }
+            if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sts128(staged(buf, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             if (kMode == kModeGrad) {
               // the entries' gradients replace what the same thread just wrote
-              while (en.col < c + 32) {
-                const int at = en.col & 63;
+              while (en.col < kStatN) {
                 const __nv_bfloat16 e = __float2bfloat16_rn(P.entry_g[static_cast<long long>(row) * P.top + en.next]);
-                asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane, at >> 3) + 2u * (at & 7)),
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane, en.col >> 3) + 2u * (en.col & 7)),
                              "h"(*reinterpret_cast<const unsigned short*>(&e))
                              : "memory");
-                ++en.next;
-                en.fetch(c0);
+                en.pop(P, col0);
               }
             }
-            if (piece16 != 0) {
-              ptx::fence_proxy_async_smem();
-              __syncwarp();
-              if (lane == 0) {
-                const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
-                ptx::tma_store_3d(&P.map_g, g0 + c - 32 - piece * P.piece_tiles * kTileN, row0, piece, buf);
-                ptx::tma_store_commit();
-              }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
+              ptx::tma_store_3d(&P.map_g, (tl.ni - piece * P.piece_tiles) * kTileN + unit * kStatN, row0, piece, buf);
+              ptx::tma_store_commit();
             }
+          } else {
+            work(std::false_type{});
           }
         }
-        if (kMode == kModeStats && row_ok)
-          P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * 2 + half] = make_float2(m, sum);
-      } else {
+        tl = tl_next;
+        head = head_next;
+        rq = rq_next;
+        k += step;
+      }
+    } else {
+      int acc = 0;
+      uint32_t acc_phase = 0;
+      int turn = 0;  // staging buffer last used
+      Tile tl;
+      for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
+        const int row0 = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32;
+        const bool have_acc = tl.kb0 != tl.kb1;
+        if (have_acc) {
+          wait_acc(acc, acc_phase);
+          if (!ok) break;
+        }
+        const uint32_t taddr = tmem_row + static_cast<uint32_t>(acc * kAccCols);
         const uint32_t buf0 = ptx::smem_u32(staging + (warp - 2) * 2 * kStageOut);
         const bool is_dx = tl.prod == 0;
         const int n_tile = P.prod[tl.prod].n_tile;
@@ -675,7 +749,13 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
             __syncwarp();
           }
         }
-        if (have_acc) release();
+        if (have_acc) {
+          release(acc);
+          if (++acc == kNumAcc) {
+            acc = 0;
+            acc_phase ^= 1u;
+          }
+        }
       }
     }
     if (lane == 0) ptx::tma_store_wait_all();
@@ -693,7 +773,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
 
 template <int kMode>
 cudaError_t configure_one() {
-  return cudaFuncSetAttribute(head_gemm_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  return cudaFuncSetAttribute(head_gemm_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kMode));
 }
 
 template <int kMode>
@@ -701,7 +781,7 @@ cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stre
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * clusters, 1, 1);
   cfg.blockDim = dim3(threads_of(kMode), 1, 1);
-  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.dynamicSmemBytes = smem_of(kMode);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -729,7 +809,7 @@ cudaError_t gemm_max_clusters(int* out) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2, 1, 1);
   cfg.blockDim = dim3(threads_of(kModeOut), 1, 1);
-  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.dynamicSmemBytes = smem_of(kModeOut);
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = 2;

@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(finalise_threads(kConvert)) finalise_kernel(co
   // count hold no news, but they are there), so that one memory latency covers it.
   const int K = kDistill ? R.top : 1;
   const long long at = static_cast<long long>(row) * K;
-  constexpr int kAhead = 1280 / kThreads;  // statistics of 163840 columns
+  constexpr int kAhead = 10;  // statistics of 163840 columns with 256 threads, of half as many with 128
   const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
   float2 ahead[kAhead];
   int my_id = kNoId, t = 0;
