@@ -83,7 +83,8 @@ struct GemmParams {
   int stats_ld;
   const float2* row_q;   // [token]: coefficient of q, log2 of the softmax denominator
   const float* entry_g;  // [token][top]: gradient of the logit at the entry
-  // Piece buffers [buffer][token][piece columns], box {64, 32}: where the
+  // Piece buffers [buffer][token][piece columns], box {64, stats_rows} or
+  // {64, 32}: where the
   // gradient of one piece's logits is stored, or the codes of the logits of the
   // first `code_tiles` tiles, in pieces of piece_tiles tiles.
   CUtensorMap map_g;
@@ -158,6 +159,7 @@ struct RowParams {
 
 cudaError_t gemm_configure();
 cudaError_t gemm_max_clusters(int* out);
+int stats_rows(int tokens);
 cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, cudaStream_t stream);
 
 bool flags_needed(const RowParams& R);

@@ -380,7 +380,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     return left < P.piece_tiles ? left : P.piece_tiles;
   };
   S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
-  if (P.grads) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, 32));
+  if (P.grads) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, stats_rows(P.tokens)));
   Product& L = S.prod[0];  // logits: tokens x vocabulary
   HEAD_TRY(encode(&L.map_a, R.xc, 1, P.rows, P.dim, P.ld_xc, 128));
   HEAD_TRY(encode(&L.map_b, w, 1, P.vocab, P.dim, ld_w, 128));
@@ -470,6 +470,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       const int cols = P.vocab - v0 < tiles * kTileN ? P.vocab - v0 : tiles * kTileN;
       if (!stored) {
         S.v0 = v0;
+        HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, 32));
         L.b_n0 = v0;
         L.n_tiles = tiles;
         S.by_tile = m_tiles * tiles > pairs;

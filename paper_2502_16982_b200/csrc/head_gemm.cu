@@ -42,12 +42,18 @@ constexpr int kNumAcc = 2;
 constexpr int kAccCols = 256;
 constexpr int kTmemCols = kNumAcc * kAccCols;
 constexpr int kStageOut = 32 * 128;  // one warp's 32 rows x 128 bytes
-// Shared memory is split between the operand ring and the staging of stores: sixteen
-// warps with one buffer each, or four with two.
-__host__ __device__ constexpr int epi_warps(int mode) { return mode == kModeOut ? 4 : 16; }
-__host__ __device__ constexpr int stages_of(int mode) { return mode == kModeOut ? 6 : 5; }
-__host__ __device__ constexpr int staging_of(int mode) { return (mode == kModeOut ? 8 : 16) * kStageOut; }
+// Shared memory is split between the operand ring and the staging of stores: four
+// warps with two buffers each, or sixteen with one or with half of one (`rows` of a
+// warp's 32 at a time).  A whole buffer and five stages: 896 us against 1015 at 8192 x
+// 256 x 50000.  Half a buffer and six stages: 154 us against 165 for the statistics of
+// 100 x 2048 x 163840, where w streams from memory.
 constexpr int kMaxStages = 6;
+__host__ __device__ constexpr int staging_of(int mode, int rows) {
+  return (mode == kModeOut ? 8 : 16) * kStageOut * rows / 32;
+}
+__host__ __device__ constexpr int stages_of(int mode, int rows) { return mode == kModeOut || rows == 16 ? 6 : 5; }
+__host__ __device__ constexpr int epi_warps(int mode) { return mode == kModeOut ? 4 : 16; }
+
 constexpr int kConvertWarps = 4;
 __host__ __device__ constexpr int threads_of(int mode) { return 64 + 32 * (epi_warps(mode) + (mode == kModeOut ? kConvertWarps : 0)); }
 
@@ -62,8 +68,11 @@ struct Barriers {
   int abort_flag;
 };
 
-constexpr int smem_of(int mode) { return 1024 + stages_of(mode) * kStageBytes + staging_of(mode) + 512; }
-static_assert(sizeof(Barriers) <= 512 && smem_of(kModeOut) <= 232448 && smem_of(kModeStats) <= 232448,
+constexpr int smem_of(int mode, int rows) {
+  return 1024 + stages_of(mode, rows) * kStageBytes + staging_of(mode, rows) + 512;
+}
+static_assert(sizeof(Barriers) <= 512 && smem_of(kModeOut, 32) <= 232448 && smem_of(kModeStats, 32) <= 232448 &&
+                  smem_of(kModeStats, 16) <= 232448,
               "exceeds the 227 KiB shared-memory limit");
 
 __device__ __forceinline__ void report_timeout(const GemmParams& P) { atomicExch(&P.ctrl->status, -6); }
@@ -290,14 +299,14 @@ struct Entries {
   }
 };
 
-template <int kMode>
+template <int kMode, int kRows>
 __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const __grid_constant__ GemmParams P) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  constexpr int kStages = stages_of(kMode);
+  constexpr int kStages = stages_of(kMode, kRows);
   uint8_t* staging = ring + kStages * kStageBytes;
-  Barriers* bars = reinterpret_cast<Barriers*>(staging + staging_of(kMode));
+  Barriers* bars = reinterpret_cast<Barriers*>(staging + staging_of(kMode, kRows));
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -507,7 +516,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       const bool by_tile = P.by_tile != 0;
       const int step = by_tile ? 2 : 1;
       const int unit0 = by_tile ? (group & 1) * 2 : group, unit1 = by_tile ? unit0 + 2 : unit0 + 1;
-      const uint32_t buf = ptx::smem_u32(staging + (warp - 2) * kStageOut);
+      const uint32_t buf = ptx::smem_u32(staging + (warp - 2) * (kStageOut * kRows / 32));
       const int row_in = static_cast<int>(rank) * 128 + q * 32;
       const uint64_t scale = pair(P.scale2, P.scale2);
       Tile tl;
@@ -609,26 +618,33 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
               for (int j = 0; j < kStatN / 2; ++j)
                 v[j] &= (2 * j < limit ? 0x0000FFFFu : 0u) | (2 * j + 1 < limit ? 0xFFFF0000u : 0u);
             }
-            if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
-            __syncwarp();
+            const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
+            const int x = (tl.ni - piece * P.piece_tiles) * kTileN + unit * kStatN;
+#pragma unroll 1
+            for (int r = 0; r < 32 && row0 + r < P.tokens; r += kRows) {
+              if (lane == 0) ptx::tma_store_wait_read();  // the previous store has left the buffer
+              __syncwarp();
+              if ((lane & (32 - kRows)) == r) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sts128(staged(buf, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            if (kMode == kModeGrad) {
-              // the entries' gradients replace what the same thread just wrote
-              while (en.col < kStatN) {
-                const __nv_bfloat16 e = __float2bfloat16_rn(P.entry_g[static_cast<long long>(row) * P.top + en.next]);
-                asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane, en.col >> 3) + 2u * (en.col & 7)),
-                             "h"(*reinterpret_cast<const unsigned short*>(&e))
-                             : "memory");
-                en.pop(P, col0);
+                for (int i = 0; i < 8; ++i)
+                  sts128(staged(buf, lane & (kRows - 1), i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                if (kMode == kModeGrad) {
+                  // the entries' gradients replace what the same thread just wrote
+                  while (en.col < kStatN) {
+                    const __nv_bfloat16 e = __float2bfloat16_rn(P.entry_g[static_cast<long long>(row) * P.top + en.next]);
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged(buf, lane & (kRows - 1), en.col >> 3) + 2u * (en.col & 7)),
+                                 "h"(*reinterpret_cast<const unsigned short*>(&e))
+                                 : "memory");
+                    en.pop(P, col0);
+                  }
+                }
               }
-            }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              const int piece = kMode == kModeStats ? tl.ni / P.piece_tiles : 0;
-              ptx::tma_store_3d(&P.map_g, (tl.ni - piece * P.piece_tiles) * kTileN + unit * kStatN, row0, piece, buf);
-              ptx::tma_store_commit();
+              ptx::fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                ptx::tma_store_3d(&P.map_g, x, row0 + r, piece, buf);
+                ptx::tma_store_commit();
+              }
             }
           } else {
             work(std::false_type{});
@@ -771,17 +787,18 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   }
 }
 
-template <int kMode>
+template <int kMode, int kRows = 32>
 cudaError_t configure_one() {
-  return cudaFuncSetAttribute(head_gemm_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kMode));
+  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              smem_of(kMode, kRows));
 }
 
-template <int kMode>
+template <int kMode, int kRows = 32>
 cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * clusters, 1, 1);
   cfg.blockDim = dim3(threads_of(kMode), 1, 1);
-  cfg.dynamicSmemBytes = smem_of(kMode);
+  cfg.dynamicSmemBytes = smem_of(kMode, kRows);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -792,13 +809,14 @@ cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stre
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode>, P);
+  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kRows>, P);
 }
 
 }  // namespace
 
 cudaError_t gemm_configure() {
   cudaError_t e = configure_one<kModeStats>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, 16>();
   if (e == cudaSuccess) e = configure_one<kModeGrad>();
   if (e == cudaSuccess) e = configure_one<kModeOut>();
   return e;
@@ -809,7 +827,7 @@ cudaError_t gemm_max_clusters(int* out) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2, 1, 1);
   cfg.blockDim = dim3(threads_of(kModeOut), 1, 1);
-  cfg.dynamicSmemBytes = smem_of(kModeOut);
+  cfg.dynamicSmemBytes = smem_of(kModeOut, 32);
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = 2;
@@ -817,14 +835,20 @@ cudaError_t gemm_max_clusters(int* out) {
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut>, &cfg);
+  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, 32>, &cfg);
 }
+
+// Rows of a box in which the statistics' codes are stored: one row tile reads w from
+// memory once, more share it in L2.
+int stats_rows(int tokens) { return tokens <= kTileM ? 16 : 32; }
 
 // `tiles`: an upper bound on the launch's tiles (every token counts).
 cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, cudaStream_t stream) {
   if (tiles <= 0) return cudaSuccess;
   const unsigned clusters = static_cast<unsigned>(tiles < max_clusters ? tiles : max_clusters);
-  if (mode == kModeStats) return launch_one<kModeStats>(P, clusters, stream);
+  if (mode == kModeStats)
+    return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, 16>(P, clusters, stream)
+                                      : launch_one<kModeStats>(P, clusters, stream);
   if (mode == kModeGrad) return launch_one<kModeGrad>(P, clusters, stream);
   return launch_one<kModeOut>(P, clusters, stream);
 }
