@@ -15,7 +15,8 @@ constexpr int kTileN = 256;   // widest output tile
 constexpr int kStatN = 64;    // vocabulary columns of one statistics entry: what an epilogue thread holds of a row
 constexpr int kUnits = kTileN / kStatN;
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
-constexpr int kFusedRows = 296;  // fewer tokens: finalisation and conversion in one launch
+constexpr int kFusedRows = 296;  // fewer tokens than this count as few
+constexpr long long kCodesInCache = 96ll << 20;  // bytes of codes that stay in L2 (126 MB)
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
 

@@ -89,7 +89,6 @@ int choose_splits(int m_tiles, int n_tiles, int dx_kb, long long dw_tiles, int d
 // 2000 x 1024 x 163840, 1402 and 1396 at 768 columns, 1075 and 1282 at 512, 675
 // and 994 at 128; but 89 and 88 us for 500 x 128 x 50000, 54 and 52 for 2000 x 128
 // x 5000.
-constexpr long long kCodesInCache = 96ll << 20;
 bool want_codes(int tokens, int dim, int vocab) {
   if (g_codes != 0) return g_codes == 2;
   return dim >= 768 || 2ll * tokens * vocab <= kCodesInCache;

@@ -275,16 +275,13 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 // Exponents are taken from one fused multiply-add on the raw logit, so that a
 // large logit costs a single rounding.
 //
-// One block per row.  kConvert: for few rows, where a launch counts, gridDim.y blocks
-// per row, each joining the statistics by itself in the same order, and each then
-// turning its share of the first stored piece's codes into gradients.
+// One block per row; where there are few rows, gridDim.y blocks per row, each joining
+// the statistics by itself in the same order.  kConvert: the block then turns its
+// share of the first stored piece's codes into gradients.
 constexpr int kFusedTiles = 4;
-// Many rows: small blocks, so that a thousand are in flight at a time.
-__host__ __device__ constexpr int finalise_threads(bool convert) { return convert ? 256 : 128; }
-
-template <bool kDistill, bool kConvert>
-__global__ void __launch_bounds__(finalise_threads(kConvert)) finalise_kernel(const RowParams R, const ConvertParams C) {
-  constexpr int kThreads = finalise_threads(kConvert), kWarps = kThreads / 32;
+template <bool kDistill, bool kConvert, int kThreads>
+__global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, const ConvertParams C) {
+  constexpr int kWarps = kThreads / 32;
   __shared__ float s_f[kWarps];
   __shared__ float s_max[kWarps];
   __shared__ int s_id[kMaxTop];
@@ -533,18 +530,27 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
   return launch(R.z != nullptr ? prepare_kernel<true> : prepare_kernel<false>, dim3(row_blocks(R.tokens)), overlap, stream, R);
 }
 
+// Few rows: large blocks, several a row, that convert the first piece's codes as
+// well.  More rows: small blocks, so that a thousand are in flight, that still convert
+// while the codes lie in L2 (62 us in place of 65 for a call of 500 x 1024 x 13000); a
+// pass of its own above that (1576 us in place of 1609 at 4097 x 1536 x 50021).
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
+  const bool distill = R.z != nullptr;
+  const int rows = R.tokens > 0 ? R.tokens : 1;
   if (C.g != nullptr && R.tokens < kFusedRows) {
     // enough blocks to spread the conversion over the device
-    const int rows = R.tokens > 0 ? R.tokens : 1;
     const int runs = (C.tiles + kFusedTiles - 1) / kFusedTiles;
     const int most = (runs + kRowWarps - 1) / kRowWarps, want = (2 * sms + R.tokens) / (R.tokens + 1);
-    const unsigned parts = static_cast<unsigned>(want < most ? want : most);
-    return launch(R.z != nullptr ? finalise_kernel<true, true> : finalise_kernel<false, true>,
-                  dim3(static_cast<unsigned>(rows), parts), true, stream, R, C);
+    const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(want < most ? want : most));
+    return launch_of(256, distill ? finalise_kernel<true, true, 256> : finalise_kernel<false, true, 256>, grid, true,
+                     stream, R, C);
   }
-  cudaError_t e = launch_of(finalise_threads(false), R.z != nullptr ? finalise_kernel<true, false> : finalise_kernel<false, false>,
-                            dim3(static_cast<unsigned>(R.tokens > 0 ? R.tokens : 1)), true, stream, R, C);
+  const dim3 grid(static_cast<unsigned>(rows));
+  if (C.g != nullptr && static_cast<long long>(R.tokens) * C.tiles * kTileN * 2 <= kCodesInCache)
+    return launch_of(128, distill ? finalise_kernel<true, true, 128> : finalise_kernel<false, true, 128>, grid, true,
+                     stream, R, C);
+  cudaError_t e = launch_of(128, distill ? finalise_kernel<true, false, 128> : finalise_kernel<false, false, 128>, grid,
+                            true, stream, R, C);
   if (e != cudaSuccess || C.g == nullptr) return e;
   const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
   const long long tasks = static_cast<long long>(R.tokens) * runs;
