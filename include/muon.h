@@ -627,6 +627,7 @@ int muon_head_xent(const muon_head_args* args, const int64_t* targets, float z_l
  *   with teacher_lse:    p = exp(top_logits / temperature - teacher_lse), where
  *                        teacher_lse is the log-sum-exp of ALL of the teacher's
  *                        logits / temperature; the mass it did not keep adds nothing
+ *                        (what is left of the divergence can then be negative)
  *   loss = sum_k p_k (log p_k - (l_k - lse)),  gradient of l: c q - p
  *
  * The usual factor temperature^2 is the caller's (`scale`).
