@@ -16,6 +16,8 @@ constexpr int kStatN = 64;    // vocabulary columns of one statistics entry: wha
 constexpr int kUnits = kTileN / kStatN;
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
 constexpr int kFusedRows = 296;  // fewer tokens than this count as few
+constexpr int kInPlaceRows = 256;     // most tokens whose rows are not gathered
+constexpr int kInPlaceEntries = 4096; // and most of a teacher's entries in all
 constexpr long long kCodesInCache = 96ll << 20;  // bytes of codes that stay in L2 (126 MB)
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
@@ -70,6 +72,11 @@ struct GemmParams {
   Ctrl* ctrl;
 
   int tokens;
+  // Few tokens: the statistics run on x as it is, before anything else, every token a
+  // row, and find the sparse entries in the caller's list; otherwise ids64 is NULL
+  const int64_t* ids64;  // [token][top], row stride ld_ids64
+  long long ld_ids64;
+  int in_place;          // rows are tokens (few tokens), not the gathered ones
 
   // statistics and gradient of the logits
   int vocab;          // columns of the whole problem
@@ -118,6 +125,7 @@ struct RowParams {
   __nv_bfloat16* xc;     // [token][ld_xc] rows of the tokens that count, then zeros to the next K block
   long long ld_xc;
   int x_vec;             // rows can be copied in 16-byte pieces
+  int in_place;          // few tokens: rows are tokens, nothing is gathered
   const int64_t* ids_in; // [tokens][top]
   long long ld_ids;
   const void* z;         // teacher logits [tokens][top], NULL: one target per token
@@ -161,9 +169,9 @@ struct RowParams {
 cudaError_t gemm_configure();
 cudaError_t gemm_max_clusters(int* out);
 int stats_rows(int tokens);
-cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, cudaStream_t stream);
+cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, bool overlap,
+                        cudaStream_t stream);
 
-bool flags_needed(const RowParams& R);
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);

@@ -42,7 +42,7 @@ constexpr long long kPartBytes = 1ll << 28;
 
 struct Plan {
   int tokens, rows, m_tiles, dim, vocab, top;  // rows: tokens, at least 1
-  bool want_dx, want_dw, grads, distill, pack;
+  bool want_dx, want_dw, grads, distill, pack, in_place;
   int v_tiles;               // 256-column tiles of the vocabulary
   int piece_tiles, n_pieces;
   int n_stored, n_buffers;   // pieces kept as codes; piece buffers in the workspace
@@ -173,6 +173,10 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     P->least = off + static_cast<size_t>(round_up(one, 1024));
     P->g = take(static_cast<size_t>(one) * P->n_buffers);
   }
+  // few tokens with rows that TMA can address, and nothing but codes between the passes
+  P->in_place = a->tokens > 0 && a->tokens <= kInPlaceRows && static_cast<long long>(a->tokens) * top <= kInPlaceEntries &&
+                (reinterpret_cast<uintptr_t>(a->x) & 15) == 0 && (a->ld_x & 7) == 0 &&
+                (!P->grads || (P->n_pieces == 1 && P->n_stored == 1));
   P->bytes = off;
   return MUON_OK;
 }
@@ -381,7 +385,15 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
   if (P.grads) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, stats_rows(P.tokens)));
   Product& L = S.prod[0];  // logits: tokens x vocabulary
-  HEAD_TRY(encode(&L.map_a, R.xc, 1, P.rows, P.dim, P.ld_xc, 128));
+  if (P.in_place) {
+    S.ids64 = R.ids_in;
+    S.ld_ids64 = R.ld_ids;
+    S.in_place = 1;
+    R.in_place = 1;
+    HEAD_TRY(encode(&L.map_a, a->x, 1, P.rows, P.dim, a->ld_x, 128));
+  } else {
+    HEAD_TRY(encode(&L.map_a, R.xc, 1, P.rows, P.dim, P.ld_xc, 128));
+  }
   HEAD_TRY(encode(&L.map_b, w, 1, P.vocab, P.dim, ld_w, 128));
   L.n_tile = kTileN;
   L.m_tiles = -1;
@@ -430,16 +442,18 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   if (P.pack)
     HEAD_CUDA(launch_pack(static_cast<const __nv_bfloat16*>(a->w), a->ld_w, reinterpret_cast<__nv_bfloat16*>(ws + P.wc),
                           P.ld_wc, P.vocab, P.dim, stream));
-  const bool flags = flags_needed(R);
-  if (flags) {
-    R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
-    HEAD_CUDA(launch_flags(R, stream));
+  if (!P.in_place) {
+    const bool flags = distill && P.tokens > 0;
+    if (flags) {
+      R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
+      HEAD_CUDA(launch_flags(R, stream));
+    }
+    HEAD_CUDA(launch_prepare(R, flags, stream));
   }
-  HEAD_CUDA(launch_prepare(R, flags, stream));
   const long long m_tiles = P.m_tiles;
   // more tiles than CTA pairs: the epilogue's warps share them out instead of their columns
   S.by_tile = m_tiles * P.v_tiles > pairs;
-  HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, stream));
+  HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, !P.in_place, stream));
   ConvertParams C = {};
   C.ld = g_ld;
   C.row_q = R.row_q;
@@ -448,7 +462,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   C.top = top;
   C.ids = R.ids;
   C.entry_g = R.entry_g;
-  C.starts = R.starts;
+  C.starts = P.in_place ? nullptr : R.starts;
   C.n_starts = R.n_starts;
   auto codes_of = [&](int piece) {
     ConvertParams D = C;
@@ -473,7 +487,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
         L.b_n0 = v0;
         L.n_tiles = tiles;
         S.by_tile = m_tiles * tiles > pairs;
-        HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, stream));
+        HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, true, stream));
       }
       O.convert = i + 1 < P.n_stored ? codes_of(i + 1) : ConvertParams{};
       O.prod[0].a_z = O.prod[1].a_z = buffer;
@@ -487,7 +501,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       O.dw_rows = cols;
       const long long out_tiles = (P.want_dx ? m_tiles * P.dx_n_tiles * P.splits : 0) +
                                   (P.want_dw ? static_cast<long long>(tiles) * P.dx_n_tiles : 0);
-      HEAD_CUDA(launch_gemm(kModeOut, O, out_tiles, pairs, stream));
+      HEAD_CUDA(launch_gemm(kModeOut, O, out_tiles, pairs, true, stream));
     }
     if (P.want_dx) HEAD_CUDA(launch_dx(R, stream));
   }

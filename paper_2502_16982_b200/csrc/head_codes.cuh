@@ -67,7 +67,15 @@ __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, i
   if (lane < kUnits * tiles)
     shift = C.stats[static_cast<long long>(row) * C.stats_ld + kUnits * (C.v_tile0 + tile0) + lane].x - rq.y;
   int next = 0, end = 1;
-  if (C.top > 1) {
+  if (C.top > 1 && C.starts == nullptr) {  // the list lies in shared memory: count
+    const int lo = (C.v_tile0 + tile0) * kTileN, hi = lo + tiles * kTileN;
+    end = 0;
+    for (int k = 0; k < C.top; k += 32) {
+      const int id = k + lane < C.top ? ids[k + lane] : kNoId;
+      next += __popc(__ballot_sync(0xFFFFFFFFu, id < lo));
+      end += __popc(__ballot_sync(0xFFFFFFFFu, id < hi));
+    }
+  } else if (C.top > 1) {
     const unsigned char* s = C.starts + static_cast<long long>(row) * C.n_starts + C.v_tile0 + tile0;
     next = s[0];
     end = s[tiles];

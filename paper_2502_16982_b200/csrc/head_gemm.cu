@@ -299,7 +299,74 @@ struct Entries {
   }
 };
 
-template <int kMode, int kRows>
+// The same from the caller's list, as it is: 64-bit indices in any order, few enough to
+// look at all of a row's for every tile.  mask: entries that fall into the tile.
+struct ListHead {
+  int id;
+  unsigned long long mask[2];
+};
+
+__device__ __forceinline__ int list_id(const GemmParams& P, int row, int k) {
+  const int64_t id = P.ids64[row * P.ld_ids64 + k];
+  return id >= 0 && id < P.vocab ? static_cast<int>(id) : kNoId;
+}
+
+__device__ __forceinline__ ListHead list_head(const GemmParams& P, int row, int tile, bool row_ok) {
+  ListHead h = {kNoId, {0, 0}};
+  if (row_ok) {
+    if (P.top == 1) {
+      h.id = list_id(P, row, 0);
+    } else {
+#pragma unroll 8
+      for (int k = 0; k < P.top; ++k) {
+        const unsigned long long in = list_id(P, row, k) / kTileN == tile;
+        h.mask[0] |= k < 64 ? in << k : 0;
+        h.mask[1] |= k < 64 ? 0 : in << (k - 64);
+      }
+    }
+  }
+  return h;
+}
+
+struct ListEntries {
+  int next, col;
+  unsigned long long left[2];
+  int row;
+
+  __device__ __forceinline__ void open(const GemmParams& P, const ListHead& h, int r, int col0) {
+    row = r;
+    if (P.top == 1) {
+      next = 0;
+      col = h.id - col0;
+      if (col < 0 || col >= kStatN) col = kNoId;
+    } else {
+      left[0] = h.mask[0];
+      left[1] = h.mask[1];
+      fetch(P, col0);
+    }
+  }
+  __device__ __forceinline__ void fetch(const GemmParams& P, int col0) {
+    col = kNoId;
+    while (col == kNoId && (left[0] | left[1])) {
+      if (left[0]) {
+        next = __ffsll(static_cast<long long>(left[0])) - 1;
+        left[0] &= left[0] - 1;
+      } else {
+        next = 63 + __ffsll(static_cast<long long>(left[1]));
+        left[1] &= left[1] - 1;
+      }
+      const int c = list_id(P, row, next) - col0;
+      if (c >= 0 && c < kStatN) col = c;
+    }
+  }
+  __device__ __forceinline__ void pop(const GemmParams& P, int col0) {
+    if (P.top == 1) col = kNoId;
+    else fetch(P, col0);
+  }
+};
+
+// kList: the sparse entries come from the caller's list.
+template <int kMode, int kRows, bool kList>
 __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const __grid_constant__ GemmParams P) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -345,7 +412,11 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
 
-  const int n_valid = *reinterpret_cast<volatile int*>(&P.ctrl->n_valid);
+  if (kList && blockIdx.x == 0 && threadIdx.x == 0) {  // first of the call's kernels
+    P.ctrl->status = 0;
+    P.ctrl->ticket = 0;
+  }
+  const int n_valid = kList || P.in_place ? P.tokens : *reinterpret_cast<volatile int*>(&P.ctrl->n_valid);
   const Shape s0 = shape_of(P, 0, n_valid);
   Shape s1 = {};
   if (kMode == kModeOut && P.n_prod == 2) s1 = shape_of(P, 1, n_valid);
@@ -522,18 +593,21 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       Tile tl;
       int k = by_tile ? group >> 1 : 0;
       bool more = locate(P, s0, s1, deal, k, tl);
-      EntryHead head = {kNoId, 0};
+      using Head = std::conditional_t<kList, ListHead, EntryHead>;
+      using List = std::conditional_t<kList, ListEntries, Entries>;
+      Head head = {};
       float2 rq = make_float2(0.f, 0.f);
       const int first_tile = kMode == kModeGrad ? P.v0 / kTileN : 0;
-      auto ask = [&](const Tile& t, EntryHead& h, float2& r) {
+      auto ask = [&](const Tile& t, Head& h, float2& r) {
         const int row = t.mi * kTileM + row_in + lane;
-        h = entry_head(P, row, first_tile + t.ni, row < n_valid);
+        if constexpr (kList) h = list_head(P, row, first_tile + t.ni, row < n_valid);
+        else h = entry_head(P, row, first_tile + t.ni, row < n_valid);
         if (kMode == kModeGrad) r = row < n_valid ? P.row_q[row] : make_float2(0.f, 0.f);
       };
       if (more) ask(tl, head, rq);
       while (more) {
         Tile tl_next;
-        EntryHead head_next = {kNoId, 0};
+        Head head_next = {};
         float2 rq_next = make_float2(0.f, 0.f);
         more = locate(P, s0, s1, deal, k + step, tl_next);
         if (more) ask(tl_next, head_next, rq_next);
@@ -554,7 +628,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           const int limit = P.vocab - col0;  // columns of the unit in the vocabulary
           uint32_t v[kStatN];
           ptx::tmem_ld_32x64(tmem_row + static_cast<uint32_t>(acc * kAccCols + unit * kStatN), v);
-          Entries en;
+          List en;
           en.open(P, head, row, col0);
           ptx::tmem_ld_wait();
           if (unit + 1 == unit1) release(acc);
@@ -787,14 +861,14 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   }
 }
 
-template <int kMode, int kRows = 32>
+template <int kMode, int kRows = 32, bool kList = false>
 cudaError_t configure_one() {
-  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kRows, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               smem_of(kMode, kRows));
 }
 
-template <int kMode, int kRows = 32>
-cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stream) {
+template <int kMode, int kRows = 32, bool kList = false>
+cudaError_t launch_one(const GemmParams& P, unsigned clusters, bool overlap, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * clusters, 1, 1);
   cfg.blockDim = dim3(threads_of(kMode), 1, 1);
@@ -808,8 +882,8 @@ cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stre
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kRows>, P);
+  cfg.numAttrs = overlap ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kRows, kList>, P);
 }
 
 }  // namespace
@@ -817,6 +891,7 @@ cudaError_t launch_one(const GemmParams& P, unsigned clusters, cudaStream_t stre
 cudaError_t gemm_configure() {
   cudaError_t e = configure_one<kModeStats>();
   if (e == cudaSuccess) e = configure_one<kModeStats, 16>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, 16, true>();
   if (e == cudaSuccess) e = configure_one<kModeGrad>();
   if (e == cudaSuccess) e = configure_one<kModeOut>();
   return e;
@@ -835,22 +910,25 @@ cudaError_t gemm_max_clusters(int* out) {
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, 32>, &cfg);
+  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, 32, false>, &cfg);
 }
 
 // Rows of a box in which the statistics' codes are stored: one row tile reads w from
 // memory once, more share it in L2.
 int stats_rows(int tokens) { return tokens <= kTileM ? 16 : 32; }
 
-// `tiles`: an upper bound on the launch's tiles (every token counts).
-cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, cudaStream_t stream) {
+// `tiles`: an upper bound on the launch's tiles (every token counts).  overlap: an earlier
+// kernel of the call is what it waits for.
+cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, bool overlap, cudaStream_t stream) {
   if (tiles <= 0) return cudaSuccess;
   const unsigned clusters = static_cast<unsigned>(tiles < max_clusters ? tiles : max_clusters);
-  if (mode == kModeStats)
-    return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, 16>(P, clusters, stream)
-                                      : launch_one<kModeStats>(P, clusters, stream);
-  if (mode == kModeGrad) return launch_one<kModeGrad>(P, clusters, stream);
-  return launch_one<kModeOut>(P, clusters, stream);
+  if (mode == kModeStats) {
+    if (P.ids64 != nullptr) return launch_one<kModeStats, 16, true>(P, clusters, overlap, stream);
+    return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, 16>(P, clusters, overlap, stream)
+                                      : launch_one<kModeStats>(P, clusters, overlap, stream);
+  }
+  if (mode == kModeGrad) return launch_one<kModeGrad>(P, clusters, overlap, stream);
+  return launch_one<kModeOut>(P, clusters, overlap, stream);
 }
 
 }  // namespace head

@@ -69,10 +69,6 @@ __device__ __forceinline__ bool counts(const RowParams& R, const unsigned char* 
   return kDistill ? flags[t] != 0 : in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids]);
 }
 
-// Up to this many entries in all, every block looks at them by itself (4 KB out of
-// L2, about 1 us) instead of a launch before it (3 us).
-constexpr int kFewEntries = 2048;
-constexpr int kFewTokens = 128;
 
 // Gathers the rows of the tokens that count, in token order, so that masked
 // tokens cost nothing in the products and whatever they hold reaches no sum.
@@ -91,18 +87,6 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int first = blockIdx.x * kRowWarps;
   const unsigned char* flags = R.flags;
-  if (kDistill && flags == nullptr) {
-    __shared__ unsigned char s_flags[kFewTokens];
-    if (tid < kFewTokens) s_flags[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < R.tokens * R.top; i += kRowThreads) {
-      const int t = i / R.top, k = i - t * R.top;
-      if (in_vocab(R, R.ids_in[static_cast<long long>(t) * R.ld_ids + k]) && !(teacher_logit(R, t, k) == -INFINITY))
-        s_flags[t] = 1;
-    }
-    __syncthreads();
-    flags = s_flags;
-  }
 
   int before = 0, total = 0;
   float wsum = 0.f;
@@ -278,8 +262,12 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 // One block per row; where there are few rows, gridDim.y blocks per row, each joining
 // the statistics by itself in the same order.  kConvert: the block then turns its
 // share of the first stored piece's codes into gradients.
+//
+// kInPlace: few tokens, rows are tokens and nothing came before the statistics.  What
+// prepare_kernel does for more tokens is done here for one row, before the wait for
+// the statistics, while they run.
 constexpr int kFusedTiles = 4;
-template <bool kDistill, bool kConvert, int kThreads>
+template <bool kDistill, bool kConvert, int kThreads, bool kInPlace>
 __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, const ConvertParams C) {
   constexpr int kWarps = kThreads / 32;
   __shared__ float s_f[kWarps];
@@ -287,42 +275,123 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
   __shared__ int s_id[kMaxTop];
   __shared__ float s_p[kMaxTop], s_raw[kMaxTop], s_exact[kMaxTop], s_g[kMaxTop];
   __shared__ bool s_last;
-  ptx::grid_dependency_wait();
-  ptx::grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x;
   const bool writes = blockIdx.y == 0;
   const int runs = kConvert ? (C.tiles + kFusedTiles - 1) / kFusedTiles : 0;
   const int run0 = static_cast<int>(blockIdx.y) * kWarps + warp, run_step = static_cast<int>(gridDim.y) * kWarps;
-  // Everything whose address is known is asked for at once (rows past the tokens that
-  // count hold no news, but they are there), so that one memory latency covers it.
   const int K = kDistill ? R.top : 1;
   const long long at = static_cast<long long>(row) * K;
+  int my_id = kNoId, t = row;
+  float my_p = 1.0f, my_raw = 0.f, row_c = 1.0f, row_h = 0.f, coef = 0.f;
+  bool counted = true;
+  int source = tid;  // entry of the caller's list that thread `tid` < K holds
+  if constexpr (kInPlace) {
+    ptx::grid_launch_dependents();
+    __shared__ unsigned char s_flags[kInPlaceRows];
+    __shared__ int s_raw_id[kMaxTop], s_source[kMaxTop];
+    const bool known = tid < R.tokens;  // at most kThreads tokens
+    if (kDistill) {
+      s_flags[tid] = 0;
+      __syncthreads();
+      for (int i = tid; i < R.tokens * K; i += kThreads) {
+        const int r = i / K, k = i - r * K;
+        if (in_vocab(R, R.ids_in[static_cast<long long>(r) * R.ld_ids + k]) && !(teacher_logit(R, r, k) == -INFINITY))
+          s_flags[r] = 1;
+      }
+      __syncthreads();
+    }
+    const bool c = known && counts<kDistill>(R, s_flags, tid);
+    const float norm = block_sum<kWarps>(c ? (R.weight != nullptr ? R.weight[tid] : 1.0f) : 0.f, s_f);
+    coef = !R.mean ? R.scale : (norm == 0.f ? 0.f : R.scale / norm);
+    counted = counts<kDistill>(R, s_flags, row);
+    if (kConvert && writes) {  // operand of dW's product
+      const uint4* src = reinterpret_cast<const uint4*>(R.x + row * R.ld_x);
+      uint4* dst = reinterpret_cast<uint4*>(R.xc + row * R.ld_xc);
+      const int whole = R.dim >> 3;
+      for (int i = tid; i < whole; i += kThreads) dst[i] = counted ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+      const int i = whole * 8 + tid;
+      if (i < R.dim) R.xc[row * R.ld_xc + i] = counted ? R.x[row * R.ld_x + i] : __float2bfloat16_rn(0.f);
+    }
+    if (!kDistill) {
+      if (tid == 0 && counted) my_id = static_cast<int>(R.ids_in[static_cast<long long>(row) * R.ld_ids]);
+    } else if (counted) {
+      float z = -INFINITY;
+      int id = kNoId;
+      if (tid < K) {
+        const int64_t raw = R.ids_in[static_cast<long long>(row) * R.ld_ids + tid];
+        if (in_vocab(R, raw)) {
+          id = static_cast<int>(raw);
+          z = teacher_logit(R, row, tid) * R.inv_t;
+        }
+        s_raw_id[tid] = id;
+      }
+      const float wm = warp_max(z);
+      if (lane == 0) s_max[warp] = wm;
+      __syncthreads();
+      float ref = s_max[0];
+#pragma unroll
+      for (int i = 1; i < kWarps; ++i) ref = fmaxf(ref, s_max[i]);
+      if (R.teacher_lse != nullptr) ref = R.teacher_lse[row];
+      float p = id == kNoId ? 0.f : expf(z - ref);
+      row_c = block_sum<kWarps>(p, s_f);
+      float log_norm = ref;
+      if (R.teacher_lse == nullptr) {
+        log_norm = ref + logf(row_c);
+        p *= 1.0f / row_c;
+        row_c = row_c == row_c ? 1.0f : row_c;  // a NaN among the logits shows
+      }
+      row_h = block_sum<kWarps>(p > 0.f ? p * (z - log_norm) : (p == 0.f ? 0.f : p), s_f);
+      if (tid < K) {  // place of an entry = how many come before it by (index, position)
+        int place = 0;
+        for (int j = 0; j < K; ++j) {
+          const int other = s_raw_id[j];
+          place += other < id || (other == id && j < tid);
+        }
+        s_id[place] = id;
+        s_p[place] = p;
+        s_source[place] = tid;
+      }
+      __syncthreads();
+      if (tid < K) {
+        my_id = s_id[tid];
+        my_p = s_p[tid];
+        source = s_source[tid];
+      }
+      __syncthreads();
+    }
+  }
+  ptx::grid_dependency_wait();
+  if (!kInPlace) ptx::grid_launch_dependents();
+  // Everything whose address is known is asked for at once (rows past the tokens that
+  // count hold no news, but they are there), so that one memory latency covers it.
   constexpr int kAhead = 10;  // statistics of 163840 columns with 256 threads, of half as many with 128
   const float2* st = R.stats + static_cast<long long>(row) * R.stats_ld;
   float2 ahead[kAhead];
-  int my_id = kNoId, t = 0;
-  float my_p = 1.0f, my_raw = 0.f, row_c = 1.0f, row_h = 0.f;
   Codes<kFusedTiles> codes;
   if (row < R.tokens) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       ahead[i] = tid + i * kThreads < R.stats_n ? st[tid + i * kThreads] : make_float2(-INFINITY, 0.f);
     if (tid < K) {
-      my_id = R.ids[at + tid];
-      my_raw = R.entry_logit[at + tid];
-      if (kDistill) my_p = R.p[at + tid];
+      my_raw = R.entry_logit[at + source];
+      if (!kInPlace) {
+        my_id = R.ids[at + tid];
+        if (kDistill) my_p = R.p[at + tid];
+      }
     }
-    t = R.row_of[row];
-    if (kDistill) {
-      row_c = R.row_c[row];
-      row_h = R.row_h[row];
+    if (!kInPlace) {
+      t = R.row_of[row];
+      if (kDistill) {
+        row_c = R.row_c[row];
+        row_h = R.row_h[row];
+      }
     }
     if (kConvert && run0 < runs) load_codes(C, row, run0 * kFusedTiles, lane, codes);
   }
-  const int n_valid = R.ctrl->n_valid;
-  const float coef = R.ctrl->coef;
-  if (row < n_valid) {
+  const int n_valid = kInPlace ? R.tokens : R.ctrl->n_valid;
+  if (!kInPlace) coef = R.ctrl->coef;
+  if (row < n_valid && counted) {
     if (tid < K) {
       s_id[tid] = my_id;
       s_p[tid] = my_id == kNoId ? 0.f : my_p;
@@ -353,7 +422,7 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
       for (unsigned todo = heavy[i]; todo; todo &= todo - 1, ++nth)
         if (nth % kWarps == warp) {
           const int e = 32 * i + __ffs(todo) - 1;
-          const float exact = warp_dot(R.xc + static_cast<long long>(row) * R.ld_xc,
+          const float exact = warp_dot(kInPlace ? R.x + row * R.ld_x : R.xc + row * R.ld_xc,
                                        R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
           if (lane == 0) s_exact[e] = exact;
         }
@@ -386,7 +455,7 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
       for (int j = tid - 1; j >= 0 && s_id[j] == s_id[tid]; --j) pj += s_p[j];
       for (int j = tid + 1; j < K && s_id[j] == s_id[tid]; ++j) pj += s_p[j];
       s_g[tid] = ga * (cq * exp2f(lq2) - pj);
-      if (writes) R.entry_g[at + tid] = s_g[tid];
+      if (!kInPlace && writes) R.entry_g[at + tid] = s_g[tid];
     }
     ce = block_sum<kWarps>(ce, s_f);  // a barrier, too: s_g is complete
     const float2 rq = make_float2(ga * cq, lse2);
@@ -394,7 +463,7 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
       const float loss = ce + row_h + R.z_loss * lse * lse;
       R.loss[t] = loss;
       if (R.lse != nullptr) R.lse[t] = lse;
-      R.row_q[row] = rq;
+      if (!kInPlace) R.row_q[row] = rq;
       R.row_l[row] = g * loss;
     }
     if (kConvert)
@@ -402,8 +471,14 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
         if (r != run0) load_codes(C, row, r * kFusedTiles, lane, codes);
         convert_codes(C, row, r * kFusedTiles, rq, s_id, s_g, lane, codes);
       }
-  } else if (kConvert && row < min(R.tokens, (n_valid + kBK - 1) / kBK * kBK)) {
-    for (int r = run0; r < runs; r += run_step) clear_row<kFusedTiles>(C, row, r * kFusedTiles, lane);
+  } else if (row < min(R.tokens, (n_valid + kBK - 1) / kBK * kBK)) {
+    if (kInPlace && writes && tid == 0) {
+      R.loss[row] = 0.f;
+      if (R.lse != nullptr) R.lse[row] = 0.f;
+      R.row_l[row] = 0.f;
+    }
+    if (kConvert)
+      for (int r = run0; r < runs; r += run_step) clear_row<kFusedTiles>(C, row, r * kFusedTiles, lane);
   }
   if (R.total == nullptr || !writes) return;
   // no gradients: the last row's block adds the tokens up, always in the same order
@@ -440,9 +515,9 @@ __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   const int per_row = (R.dim + 7) >> 3;
   const long long i = static_cast<long long>(blockIdx.x) * kRowThreads + threadIdx.x;
   const int row = static_cast<int>(i / per_row);
-  if (row >= R.ctrl->n_valid) return;
+  if (row >= (R.in_place ? R.tokens : R.ctrl->n_valid)) return;
   const int c = static_cast<int>(i - static_cast<long long>(row) * per_row) * 8;
-  const int t = R.row_of[row];
+  const int t = R.in_place ? row : R.row_of[row];
   float v[8] = {};
   const float* src = R.part + static_cast<long long>(row) * R.part_ld + c;
 #pragma unroll 8
@@ -518,10 +593,6 @@ unsigned row_blocks(int tokens) { return tokens > 0 ? static_cast<unsigned>((tok
 
 }  // namespace
 
-bool flags_needed(const RowParams& R) {
-  return R.z != nullptr && (R.tokens > kFewTokens || static_cast<long long>(R.tokens) * R.top > kFewEntries);
-}
-
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream) {
   return launch(flags_kernel, dim3(row_blocks(R.tokens)), false, stream, R);
 }
@@ -534,23 +605,27 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
 // well.  More rows: small blocks, so that a thousand are in flight, that still convert
 // while the codes lie in L2 (62 us in place of 65 for a call of 500 x 1024 x 13000); a
 // pass of its own above that (1576 us in place of 1609 at 4097 x 1536 x 50021).
+template <int kThreads, bool kConvert, bool kInPlace>
+cudaError_t finalise_with(const RowParams& R, const ConvertParams& C, dim3 grid, cudaStream_t stream) {
+  return launch_of(kThreads, R.z != nullptr ? finalise_kernel<true, kConvert, kThreads, kInPlace>
+                                            : finalise_kernel<false, kConvert, kThreads, kInPlace>,
+                   grid, true, stream, R, C);
+}
+
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
-  const bool distill = R.z != nullptr;
   const int rows = R.tokens > 0 ? R.tokens : 1;
   if (C.g != nullptr && R.tokens < kFusedRows) {
     // enough blocks to spread the conversion over the device
     const int runs = (C.tiles + kFusedTiles - 1) / kFusedTiles;
     const int most = (runs + kRowWarps - 1) / kRowWarps, want = (2 * sms + R.tokens) / (R.tokens + 1);
     const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(want < most ? want : most));
-    return launch_of(256, distill ? finalise_kernel<true, true, 256> : finalise_kernel<false, true, 256>, grid, true,
-                     stream, R, C);
+    return R.in_place ? finalise_with<256, true, true>(R, C, grid, stream) : finalise_with<256, true, false>(R, C, grid, stream);
   }
   const dim3 grid(static_cast<unsigned>(rows));
+  if (R.in_place) return finalise_with<256, false, true>(R, C, grid, stream);
   if (C.g != nullptr && static_cast<long long>(R.tokens) * C.tiles * kTileN * 2 <= kCodesInCache)
-    return launch_of(128, distill ? finalise_kernel<true, true, 128> : finalise_kernel<false, true, 128>, grid, true,
-                     stream, R, C);
-  cudaError_t e = launch_of(128, distill ? finalise_kernel<true, false, 128> : finalise_kernel<false, false, 128>, grid,
-                            true, stream, R, C);
+    return finalise_with<128, true, false>(R, C, grid, stream);
+  cudaError_t e = finalise_with<128, false, false>(R, C, grid, stream);
   if (e != cudaSuccess || C.g == nullptr) return e;
   const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
   const long long tasks = static_cast<long long>(R.tokens) * runs;
