@@ -319,14 +319,12 @@ _no_context = contextlib.nullcontext()
 
 class HeadLoss(NamedTuple):
     """What a head loss gives: per-token ``loss`` and ``lse`` (fp32), ``total`` (one
-    fp32 element), the gradients of ``total`` (None where not asked for) and the
-    workspace that held the call's intermediates."""
+    fp32 element) and the gradients of ``total`` (None where not asked for)."""
     loss: "torch.Tensor"
     lse: "torch.Tensor"
     total: "torch.Tensor"
     dx: Optional["torch.Tensor"]
     dw: Optional["torch.Tensor"]
-    workspace: "torch.Tensor"
 
 
 def _row_stride(t):
@@ -415,7 +413,7 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
     first = workspace.data_ptr()
     base = (first + 1023) // 1024 * 1024
     _check(call(C.byref(a), base, max(first + workspace.numel() - base, 0), dev.index, _raw_stream(stream, dev.index)))
-    return HeadLoss(loss, lse, total, dx, dw, workspace)
+    return HeadLoss(loss, lse, total, dx, dw)
 
 
 def muon_head_workspace_bytes(tokens: int, dim: int, vocab: int, top: int = 0, dx: bool = True, dw: bool = True,
@@ -449,7 +447,8 @@ def muon_head_xent(x, w, targets, loss=None, lse=None, total=None, dx=None, dw=N
     ``targets`` int64 [tokens] (outside [0, vocab): the token is masked).
     ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True to allocate one like x / w,
     None to leave the gradient out.  Other outputs and the workspace are allocated
-    unless given.  Argument marshalling only; the formulas are in include/muon.h.
+    unless given; a workspace of :func:`muon_head_workspace_bytes` that is kept can be
+    asked for the call's status.  Argument marshalling only; the formulas are in include/muon.h.
     Tensors used on another stream than the one they were allocated on are the
     caller's to keep alive (``record_stream``)."""
     import torch
@@ -493,14 +492,13 @@ def muon_head_distill(x, w, top_ids, top_logits, temperature=1.0, teacher_lse=No
                       stream, call)
 
 
-def muon_head_status(result: HeadLoss, stream=None) -> int:
+def muon_head_status(workspace, stream=None) -> int:
     """Synchronises the stream; 0, or MUON_ERR_TIMEOUT if a device-side wait of the
-    last call on the result's workspace expired."""
+    last head-loss call that was given this workspace tensor expired."""
     import torch
-    ws = result.workspace
-    s = torch.cuda.current_stream(ws.device) if stream is None else stream
+    s = torch.cuda.current_stream(workspace.device) if stream is None else stream
     st = C.c_int(0)
-    _check(lib().muon_head_status(C.c_void_p((ws.data_ptr() + 1023) // 1024 * 1024), ws.device.index,
+    _check(lib().muon_head_status(C.c_void_p((workspace.data_ptr() + 1023) // 1024 * 1024), workspace.device.index,
                                   C.c_void_p(s.cuda_stream), C.byref(st)))
     return st.value
 

@@ -122,6 +122,11 @@ struct RowParams {
   long long ld_x;
   const __nv_bfloat16* w;  // head with 16-byte aligned rows
   long long ld_w;
+  // where the caller's has none: the copy that w points to, and what it is made from
+  __nv_bfloat16* pack_to;
+  const __nv_bfloat16* pack_from;
+  long long ld_pack;
+  int pack_blocks;
   __nv_bfloat16* xc;     // [token][ld_xc] rows of the tokens that count, then zeros to the next K block
   long long ld_xc;
   int x_vec;             // rows can be copied in 16-byte pieces
@@ -176,8 +181,8 @@ cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);
-cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
-                        int cols, cudaStream_t stream);
+cudaError_t launch_pack(const RowParams& R, cudaStream_t stream);
+int pack_blocks(int vocab);
 
 }  // namespace head
 }  // namespace muon

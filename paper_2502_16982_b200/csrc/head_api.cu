@@ -439,9 +439,13 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     if (O.dw_tma) HEAD_TRY(encode(&O.map_dw, a->dw, 1, P.vocab, P.dim, a->ld_dw, 32, O.dw_fp32 != 0));
   }
 
-  if (P.pack)
-    HEAD_CUDA(launch_pack(static_cast<const __nv_bfloat16*>(a->w), a->ld_w, reinterpret_cast<__nv_bfloat16*>(ws + P.wc),
-                          P.ld_wc, P.vocab, P.dim, stream));
+  if (P.pack) {
+    R.pack_to = reinterpret_cast<__nv_bfloat16*>(ws + P.wc);
+    R.pack_from = static_cast<const __nv_bfloat16*>(a->w);
+    R.ld_pack = a->ld_w;
+    R.pack_blocks = pack_blocks(P.vocab);
+    if (P.in_place) HEAD_CUDA(launch_pack(R, stream));
+  }
   if (!P.in_place) {
     const bool flags = distill && P.tokens > 0;
     if (flags) {
@@ -466,7 +470,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   C.n_starts = R.n_starts;
   auto codes_of = [&](int piece) {
     ConvertParams D = C;
-    if (piece < P.n_stored) D.g = g + piece * P.rows * g_ld;
+    if (piece < P.n_stored) D.g = g + static_cast<long long>(piece) * P.rows * g_ld;
     D.tiles = tiles_of(piece);
     D.v_tile0 = piece * P.piece_tiles;
     return D;

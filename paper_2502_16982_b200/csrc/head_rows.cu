@@ -70,6 +70,23 @@ __device__ __forceinline__ bool counts(const RowParams& R, const unsigned char* 
 }
 
 
+// Copy of a head whose rows TMA cannot address (16-byte aligned rows) into rows that it
+// can, by block `block` of `blocks`; one warp per row.
+__device__ __forceinline__ void pack_rows(const RowParams& R, int block, int blocks) {
+  const int lane = threadIdx.x & 31;
+  const long long step = static_cast<long long>(blocks) * kRowWarps;
+  for (long long r = static_cast<long long>(block) * kRowWarps + (threadIdx.x >> 5); r < R.vocab; r += step) {
+    const unsigned short* s = reinterpret_cast<const unsigned short*>(R.pack_from + r * R.ld_pack);
+    uint32_t* d = reinterpret_cast<uint32_t*>(R.pack_to + r * R.ld_w);
+    for (int c = lane * 2; c < R.dim; c += 64) {
+      const uint32_t lo = s[c], hi = c + 1 < R.dim ? s[c + 1] : 0u;
+      d[c >> 1] = lo | (hi << 16);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kRowThreads) pack_kernel(const RowParams R) { pack_rows(R, blockIdx.x, gridDim.x); }
+
 // Gathers the rows of the tokens that count, in token order, so that masked
 // tokens cost nothing in the products and whatever they hold reaches no sum.
 // Every block counts the tokens before its own by itself (8 bytes a token out of
@@ -85,6 +102,11 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int blocks = static_cast<int>(gridDim.x) - R.pack_blocks;  // the last ones copy the head
+  if (static_cast<int>(blockIdx.x) >= blocks) {
+    pack_rows(R, static_cast<int>(blockIdx.x) - blocks, R.pack_blocks);
+    return;
+  }
   const int first = blockIdx.x * kRowWarps;
   const unsigned char* flags = R.flags;
 
@@ -222,7 +244,7 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   }
   // zero rows up to the next K block of dW's product
   const int rows = min(R.tokens, (total + kBK - 1) / kBK * kBK);
-  for (int r = total + blockIdx.x * kRowWarps + warp; r < rows; r += gridDim.x * kRowWarps)
+  for (int r = total + blockIdx.x * kRowWarps + warp; r < rows; r += blocks * kRowWarps)
     for (int c = lane * 8; c < R.dim; c += 256)  // ld_xc is a multiple of 8
       *reinterpret_cast<uint4*>(R.xc + static_cast<long long>(r) * R.ld_xc + c) = make_uint4(0u, 0u, 0u, 0u);
 }
@@ -552,24 +574,6 @@ __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   }
 }
 
-// Copy of a head whose rows TMA cannot address (16-byte aligned rows) into rows
-// that it can; one warp per row.
-__global__ void __launch_bounds__(kRowThreads) pack_kernel(const __nv_bfloat16* src, long long ld_src,
-                                                           __nv_bfloat16* dst, long long ld_dst, int rows, int cols) {
-  ptx::grid_dependency_wait();
-  ptx::grid_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const long long step = static_cast<long long>(gridDim.x) * kRowWarps;
-  for (long long r = static_cast<long long>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5); r < rows; r += step) {
-    const unsigned short* s = reinterpret_cast<const unsigned short*>(src + r * ld_src);
-    uint32_t* d = reinterpret_cast<uint32_t*>(dst + r * ld_dst);
-    for (int c = lane * 2; c < cols; c += 64) {
-      const uint32_t lo = s[c], hi = c + 1 < cols ? s[c + 1] : 0u;
-      d[c >> 1] = lo | (hi << 16);
-    }
-  }
-}
-
 template <typename... Args>
 cudaError_t launch_of(int threads, void (*kernel)(Args...), dim3 blocks, bool overlap, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
@@ -598,7 +602,8 @@ cudaError_t launch_flags(const RowParams& R, cudaStream_t stream) {
 }
 
 cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream) {
-  return launch(R.z != nullptr ? prepare_kernel<true> : prepare_kernel<false>, dim3(row_blocks(R.tokens)), overlap, stream, R);
+  return launch(R.z != nullptr ? prepare_kernel<true> : prepare_kernel<false>, dim3(row_blocks(R.tokens) + static_cast<unsigned>(R.pack_blocks)),
+                overlap, stream, R);
 }
 
 // Few rows: large blocks, several a row, that convert the first piece's codes as
@@ -639,11 +644,13 @@ cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
   return launch(dx_kernel, dim3(static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads)), true, stream, R);
 }
 
-cudaError_t launch_pack(const __nv_bfloat16* src, long long ld_src, __nv_bfloat16* dst, long long ld_dst, int rows,
-                        int cols, cudaStream_t stream) {
-  const long long blocks = (rows + kRowWarps - 1) / kRowWarps;
-  return launch(pack_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), false, stream, src, ld_src, dst,
-                ld_dst, rows, cols);
+cudaError_t launch_pack(const RowParams& R, cudaStream_t stream) {
+  return launch(pack_kernel, dim3(static_cast<unsigned>(R.pack_blocks)), false, stream, R);
+}
+
+int pack_blocks(int vocab) {
+  const int blocks = (vocab + kRowWarps - 1) / kRowWarps;
+  return blocks < 4096 ? blocks : 4096;
 }
 
 }  // namespace head

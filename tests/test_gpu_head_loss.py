@@ -120,8 +120,9 @@ def test_cross_entropy_matches_the_oracle(T, D, V, masked, opts):
     dxt, dwt = o.pop("dx", BF), o.pop("dw", BF)
     dx = None if dxt is None else torch.full((T, D), 7.0, dtype=dxt, device="cuda")
     dw = None if dwt is None else torch.full((V, D), 7.0, dtype=dwt, device="cuda")
-    r = b.muon_head_xent(x, w, targets.cuda(), weight=weight, dx=dx, dw=dw, **o)
-    assert b.muon_head_status(r) == 0
+    ws = torch.full((b.muon_head_workspace_bytes(T, D, V, packed_head=False),), 255, dtype=torch.uint8, device="cuda")
+    r = b.muon_head_xent(x, w, targets.cuda(), weight=weight, dx=dx, dw=dw, workspace=ws, **o)
+    assert b.muon_head_status(ws) == 0
     rows = ho.target_rows(targets.numpy(), V)
     xr, wr = f64(x), f64(w)
     ref = ho.head_loss(np.where(rows[2].any(1)[:, None], xr, 0.0), wr, rows, weight=None if weight is None else f64(weight), **o)
@@ -177,8 +178,9 @@ def test_distillation_matches_the_oracle(T, D, V, K, opts):
         assert ids_d.stride(0) == K + 3 and z_d.stride(0) == K + 1
     dx = None if dxt is None else torch.full((T, D), 7.0, dtype=dxt, device="cuda")
     dw = None if dwt is None else torch.full((V, D), 7.0, dtype=dwt, device="cuda")
-    r = b.muon_head_distill(x, w, ids_d, z_d, teacher_lse=tlse, weight=weight, dx=dx, dw=dw, **o)
-    assert b.muon_head_status(r) == 0
+    ws = torch.full((b.muon_head_workspace_bytes(T, D, V, top=K, packed_head=False),), 255, dtype=torch.uint8, device="cuda")
+    r = b.muon_head_distill(x, w, ids_d, z_d, teacher_lse=tlse, weight=weight, dx=dx, dw=dw, workspace=ws, **o)
+    assert b.muon_head_status(ws) == 0
     rows = ho.teacher_rows(ids.numpy(), f64(z), V, tau, None if tlse is None else f64(tlse))
     xr, wr = np.where(rows[2].any(1)[:, None], f64(x), 0.0), f64(w)
     ref = ho.head_loss(xr, wr, rows, weight=None if weight is None else f64(weight), **o)
@@ -222,7 +224,7 @@ def test_vocabulary_in_pieces(knobs, codes, room, top):
         t[::5] = -100
         r = b.muon_head_xent(x, w, t.cuda(), dx=True, dw=True, workspace=ws)
         rows = ho.target_rows(t.numpy(), V)
-    assert b.muon_head_status(r) == 0
+    assert b.muon_head_status(ws) == 0
     ref = ho.head_loss(f64(x), f64(w), rows)
     check(r, ref, f64(x), f64(w), rows, 1.0, BF, BF, coefficients(ref["counts"], None, True, 1.0, 0.0))
     with pytest.raises(b.MuonError):
@@ -293,7 +295,8 @@ def test_results_are_the_same_bits_again_and_on_another_stream():
     ids = torch.stack([torch.randperm(5000, generator=gen)[:16] for _ in range(900)]).cuda()
     z = torch.randn(900, 16, generator=gen).cuda()
     a = b.muon_head_distill(x, w, ids, z, dx=True, dw=True)
-    again = b.muon_head_distill(x, w, ids, z, dx=True, dw=True, workspace=a.workspace.fill_(255))
+    ws = torch.full((b.muon_head_workspace_bytes(900, 256, 5000, top=16),), 255, dtype=torch.uint8, device="cuda")
+    again = b.muon_head_distill(x, w, ids, z, dx=True, dw=True, workspace=ws)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     other = b.muon_head_distill(x, w, ids, z, dx=True, dw=True, stream=s)
@@ -340,6 +343,44 @@ def test_margins_are_not_written():
         for m in (dx, dw):
             m[1:-1, 4:-8] = 5.0
             assert bool((m == 5.0).all())
+
+
+def test_rows_far_apart():
+    """Row strides that put the last rows past 2^31 elements, for w, dw and x, dx."""
+    from paper_2502_16982_b200 import binding as b
+
+    T, D, V, ld = 270, 64, 66000, 32768
+    x, w, gen = make(T, D, V, 12)
+    t = torch.randint(0, V, (T,), generator=gen).cuda()
+    t[-1] = V - 1
+    near = b.muon_head_xent(x, w, t, dx=True, dw=True)
+    far_w, far_dw = (torch.empty(V, ld, dtype=BF, device="cuda")[:, 64:64 + D] for _ in range(2))
+    far_w.copy_(w)
+    far = b.muon_head_xent(x, far_w, t, dx=True, dw=far_dw)
+    for k in ("loss", "lse", "total", "dx", "dw"):
+        assert torch.equal(getattr(near, k), getattr(far, k)), k
+    del far_w, far_dw, far
+    ld = (1 << 31) // (T - 1) // 8 * 8 + 8
+    far_x, far_dx = (torch.empty(T, ld, dtype=BF, device="cuda")[:, :D] for _ in range(2))
+    far_x.copy_(x)
+    far = b.muon_head_xent(far_x, w, t, dx=far_dx, dw=True)
+    for k in ("loss", "lse", "total", "dx", "dw"):
+        assert torch.equal(getattr(near, k), getattr(far, k)), k
+
+
+@pytest.mark.parametrize("T", [40, 400])
+def test_status_word(T):
+    """A status left by an earlier call is reported once and cleared by the next call."""
+    from paper_2502_16982_b200 import binding as b
+
+    x, w, gen = make(T, 64, 500, 13)
+    t = torch.randint(0, 500, (T,), generator=gen).cuda()
+    ws = torch.zeros(b.muon_head_workspace_bytes(T, 64, 500), dtype=torch.uint8, device="cuda")
+    at = -ws.data_ptr() % 1024
+    ws[at:at + 4].view(torch.int32).fill_(b.MUON_ERR_TIMEOUT)
+    assert b.muon_head_status(ws) == b.MUON_ERR_TIMEOUT
+    b.muon_head_xent(x, w, t, dx=True, dw=True, workspace=ws)
+    assert b.muon_head_status(ws) == 0
 
 
 def test_refusals_of_the_binding():
