@@ -308,6 +308,25 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
   float my_p = 1.0f, my_raw = 0.f, row_c = 1.0f, row_h = 0.f, coef = 0.f;
   bool counted = true;
   int source = tid;  // entry of the caller's list that thread `tid` < K holds
+  // The logits that carry the loss, again as plain fp32 dot products, for the softmax
+  // sum to hold them in place of the tensor cores' values: the tensor cores truncate at
+  // every step of 16 products, which shifts a logit of 15 over 2048 columns by about
+  // 1e-5.
+  unsigned heavy[kDistill ? kMaxTop / 32 : 1];  // entries with their own dot product
+  auto dots = [&]() {
+    int nth = 0;
+#pragma unroll
+    for (int i = 0; i < (kDistill ? kMaxTop / 32 : 1); ++i) {
+      heavy[i] = __ballot_sync(0xFFFFFFFFu, 32 * i + lane < K && s_p[32 * i + lane] >= kExactMass);
+      for (unsigned todo = heavy[i]; todo; todo &= todo - 1, ++nth)
+        if (nth % kWarps == warp) {
+          const int e = 32 * i + __ffs(todo) - 1;
+          const float exact = warp_dot(kInPlace ? R.x + row * R.ld_x : R.xc + row * R.ld_xc,
+                                       R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
+          if (lane == 0) s_exact[e] = exact;
+        }
+    }
+  };
   if constexpr (kInPlace) {
     ptx::grid_launch_dependents();
     __shared__ unsigned char s_flags[kInPlaceRows];
@@ -336,7 +355,12 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
       if (i < R.dim) R.xc[row * R.ld_xc + i] = counted ? R.x[row * R.ld_x + i] : __float2bfloat16_rn(0.f);
     }
     if (!kDistill) {
-      if (tid == 0 && counted) my_id = static_cast<int>(R.ids_in[static_cast<long long>(row) * R.ld_ids]);
+      if (tid == 0 && counted) {
+        my_id = static_cast<int>(R.ids_in[static_cast<long long>(row) * R.ld_ids]);
+        s_id[0] = my_id;
+        s_p[0] = 1.0f;
+      }
+      __syncthreads();
     } else if (counted) {
       float z = -INFINITY;
       int id = kNoId;
@@ -380,8 +404,8 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
         my_p = s_p[tid];
         source = s_source[tid];
       }
-      __syncthreads();
     }
+    if (counted) dots();
   }
   ptx::grid_dependency_wait();
   if (!kInPlace) ptx::grid_launch_dependents();
@@ -415,8 +439,10 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
   if (!kInPlace) coef = R.ctrl->coef;
   if (row < n_valid && counted) {
     if (tid < K) {
-      s_id[tid] = my_id;
-      s_p[tid] = my_id == kNoId ? 0.f : my_p;
+      if (!kInPlace) {
+        s_id[tid] = my_id;
+        s_p[tid] = my_id == kNoId ? 0.f : my_p;
+      }
       s_raw[tid] = my_id == kNoId ? 0.f : my_raw;
     }
     float m = -INFINITY, s = 0.f;
@@ -432,23 +458,7 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
     const float wm = warp_max(m);
     if (lane == 0) s_max[warp] = wm;
     __syncthreads();
-    // The logits that carry the loss, again as plain fp32 dot products, and the
-    // softmax sum with them in place of the tensor cores' values: the tensor cores
-    // truncate at every step of 16 products, which shifts a logit of 15 over 2048
-    // columns by about 1e-5.
-    unsigned heavy[kDistill ? kMaxTop / 32 : 1];  // entries with their own dot product
-    int nth = 0;
-#pragma unroll
-    for (int i = 0; i < (kDistill ? kMaxTop / 32 : 1); ++i) {
-      heavy[i] = __ballot_sync(0xFFFFFFFFu, 32 * i + lane < K && s_p[32 * i + lane] >= kExactMass);
-      for (unsigned todo = heavy[i]; todo; todo &= todo - 1, ++nth)
-        if (nth % kWarps == warp) {
-          const int e = 32 * i + __ffs(todo) - 1;
-          const float exact = warp_dot(kInPlace ? R.x + row * R.ld_x : R.xc + row * R.ld_xc,
-                                       R.w + static_cast<long long>(s_id[e]) * R.ld_w, R.dim, lane);
-          if (lane == 0) s_exact[e] = exact;
-        }
-    }
+    if (!kInPlace) dots();
     float mx = s_max[0];
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) mx = fmaxf(mx, s_max[i]);
@@ -527,48 +537,62 @@ __global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParam
                 static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
 }
 
-// dX of the tokens that count, in token order: the partial sums joined in the order
-// of the runs.  Eight columns a thread.  (Rows of dX written by the last product's
-// epilogue itself, 64 bytes at a time and to scattered tokens, cost that launch
-// 120 us at 8192 x 2048; this pass costs 28.)
+// dX of the tokens that count, in token order: the partial sums joined, always in the
+// same order.  Four columns a thread, or, kWays > 1, kWays neighbouring lanes that
+// take a stretch of the runs each: with the many runs of a small launch one memory
+// latency instead of several (13 us -> 3 for 60 x 512 x 50000).  (Rows of dX written by
+// the last product's epilogue itself, 64 bytes at a time and to scattered tokens,
+// cost that launch 120 us at 8192 x 2048; this pass costs 28.)
+template <int kWays>
 __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int per_row = (R.dim + 7) >> 3;
-  const long long i = static_cast<long long>(blockIdx.x) * kRowThreads + threadIdx.x;
+  const int per_row = (R.dim + 3) >> 2;
+  const long long thread = static_cast<long long>(blockIdx.x) * kRowThreads + threadIdx.x;
+  // lanes 0..31/kWays - 1 of a warp hold neighbouring columns, the next as many the next way
+  constexpr int kGroups = 32 / kWays;
+  const int lane = threadIdx.x & 31;
+  const long long i = (thread >> 5) * kGroups + lane % kGroups;
+  const int way = lane / kGroups;
   const int row = static_cast<int>(i / per_row);
-  if (row >= (R.in_place ? R.tokens : R.ctrl->n_valid)) return;
-  const int c = static_cast<int>(i - static_cast<long long>(row) * per_row) * 8;
-  const int t = R.in_place ? row : R.row_of[row];
-  float v[8] = {};
-  const float* src = R.part + static_cast<long long>(row) * R.part_ld + c;
+  const bool mine = row < (R.in_place ? R.tokens : R.ctrl->n_valid);
+  const int c = static_cast<int>(i - static_cast<long long>(row) * per_row) * 4;
+  float v[4] = {};
+  int t = 0;
+  if (mine) {
+    t = R.in_place ? row : R.row_of[row];
+    const int s0 = R.splits * way / kWays, s1 = R.splits * (way + 1) / kWays;
+    const float* src = R.part + static_cast<long long>(row) * R.part_ld + c + s0 * R.part_stride;
 #pragma unroll 8
-  for (int s = 0; s < R.splits; ++s, src += R.part_stride) {
-    const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
-    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    for (int s = s0; s < s1; ++s, src += R.part_stride) {
+      const float4 a = *reinterpret_cast<const float4*>(src);
+      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+    }
   }
+#pragma unroll
+  for (int o = kGroups; o < 32; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += __shfl_xor_sync(0xFFFFFFFFu, v[e], o);
+  if (!mine || way != 0) return;
   const long long off = static_cast<long long>(t) * R.ld_dx + c;
+  const bool whole = R.dx_vec && c + 4 <= R.dim;
   if (R.dx_fp32) {
     float* d = static_cast<float*>(R.dx) + off;
-    if (R.dx_vec && c + 8 <= R.dim) {
+    if (whole) {
       *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(d + 4) = make_float4(v[4], v[5], v[6], v[7]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < 4; ++e)
         if (c + e < R.dim) d[e] = v[e];
     }
   } else {
     __nv_bfloat16* d = static_cast<__nv_bfloat16*>(R.dx) + off;
-    if (R.dx_vec && c + 8 <= R.dim) {
-      __nv_bfloat162 h[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-      *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(h);
+    if (whole) {
+      __nv_bfloat162 h[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+      *reinterpret_cast<uint2*>(d) = *reinterpret_cast<const uint2*>(h);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < 4; ++e)
         if (c + e < R.dim) d[e] = __float2bfloat16_rn(v[e]);
     }
   }
@@ -640,8 +664,10 @@ cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms,
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
-  const long long n = static_cast<long long>(R.tokens) * ((R.dim + 7) >> 3);
-  return launch(dx_kernel, dim3(static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads)), true, stream, R);
+  const int ways = R.splits >= 8 ? 8 : 1;
+  const long long n = static_cast<long long>(R.tokens) * ((R.dim + 3) >> 2) * ways;
+  const dim3 grid(static_cast<unsigned>((n + kRowThreads - 1) / kRowThreads));
+  return launch(ways == 8 ? dx_kernel<8> : dx_kernel<1>, grid, true, stream, R);
 }
 
 cudaError_t launch_pack(const RowParams& R, cudaStream_t stream) {
