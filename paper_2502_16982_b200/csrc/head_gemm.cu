@@ -239,12 +239,16 @@ __device__ __forceinline__ bool locate(const GemmParams& P, const Shape& s0, con
   return true;
 }
 
-// Picks v[i] for a run-time i without putting v in local memory.
+// Picks v[i] for a run-time i without putting v in local memory: halves by the bits of i.
 __device__ __forceinline__ float pick(const uint32_t (&v)[kStatN], int i) {
-  uint32_t r = v[0];
+  uint32_t r[kStatN / 2];
 #pragma unroll
-  for (int j = 1; j < kStatN; ++j) r = i == j ? v[j] : r;
-  return __uint_as_float(r);
+  for (int j = 0; j < kStatN / 2; ++j) r[j] = i & (kStatN / 2) ? v[j + kStatN / 2] : v[j];
+#pragma unroll
+  for (int half = kStatN / 4; half > 0; half >>= 1)
+#pragma unroll
+    for (int j = 0; j < half; ++j) r[j] = i & half ? r[j + half] : r[j];
+  return __uint_as_float(r[0]);
 }
 
 // Where a row's sparse entries in one 256-column tile are found: asked for a tile
@@ -300,7 +304,8 @@ struct Entries {
 };
 
 // The same from the caller's list, as it is: 64-bit indices in any order, few enough to
-// look at all of a row's for every tile.  mask: entries that fall into the tile.
+// look at all of a row's for every tile.  mask: entries that fall into `cols` columns
+// from col0 on.
 struct ListHead {
   int id;
   unsigned long long mask[2];
@@ -311,7 +316,7 @@ __device__ __forceinline__ int list_id(const GemmParams& P, int row, int k) {
   return id >= 0 && id < P.vocab ? static_cast<int>(id) : kNoId;
 }
 
-__device__ __forceinline__ ListHead list_head(const GemmParams& P, int row, int tile, bool row_ok) {
+__device__ __forceinline__ ListHead list_head(const GemmParams& P, int row, int col0, int cols, bool row_ok) {
   ListHead h = {kNoId, {0, 0}};
   if (row_ok) {
     if (P.top == 1) {
@@ -319,7 +324,7 @@ __device__ __forceinline__ ListHead list_head(const GemmParams& P, int row, int 
     } else {
 #pragma unroll 8
       for (int k = 0; k < P.top; ++k) {
-        const unsigned long long in = list_id(P, row, k) / kTileN == tile;
+        const unsigned long long in = static_cast<unsigned>(list_id(P, row, k) - col0) < static_cast<unsigned>(cols);
         h.mask[0] |= k < 64 ? in << k : 0;
         h.mask[1] |= k < 64 ? 0 : in << (k - 64);
       }
@@ -600,7 +605,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
       const int first_tile = kMode == kModeGrad ? P.v0 / kTileN : 0;
       auto ask = [&](const Tile& t, Head& h, float2& r) {
         const int row = t.mi * kTileM + row_in + lane;
-        if constexpr (kList) h = list_head(P, row, first_tile + t.ni, row < n_valid);
+        if constexpr (kList) h = list_head(P, row, t.ni * kTileN + unit0 * kStatN, (unit1 - unit0) * kStatN, row < n_valid);
         else h = entry_head(P, row, first_tile + t.ni, row < n_valid);
         if (kMode == kModeGrad) r = row < n_valid ? P.row_q[row] : make_float2(0.f, 0.f);
       };

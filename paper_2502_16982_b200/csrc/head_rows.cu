@@ -288,10 +288,11 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 // kInPlace: few tokens, rows are tokens and nothing came before the statistics.  What
 // prepare_kernel does for more tokens is done here for one row, before the wait for
 // the statistics, while they run.
-constexpr int kFusedTiles = 4;
+// Tiles a warp converts at a time: few rows are spread thin, many rows want loads in flight.
+__host__ __device__ constexpr int fused_tiles(int threads) { return threads == 256 ? 2 : 4; }
 template <bool kDistill, bool kConvert, int kThreads, bool kInPlace>
 __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, const ConvertParams C) {
-  constexpr int kWarps = kThreads / 32;
+  constexpr int kWarps = kThreads / 32, kFusedTiles = fused_tiles(kThreads);
   __shared__ float s_f[kWarps];
   __shared__ float s_max[kWarps];
   __shared__ int s_id[kMaxTop];
@@ -645,8 +646,8 @@ cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms,
   const int rows = R.tokens > 0 ? R.tokens : 1;
   if (C.g != nullptr && R.tokens < kFusedRows) {
     // enough blocks to spread the conversion over the device
-    const int runs = (C.tiles + kFusedTiles - 1) / kFusedTiles;
-    const int most = (runs + kRowWarps - 1) / kRowWarps, want = (2 * sms + R.tokens) / (R.tokens + 1);
+    const int runs = (C.tiles + fused_tiles(256) - 1) / fused_tiles(256);
+    const int most = (runs + kRowWarps - 1) / kRowWarps, want = (3 * sms + rows - 1) / rows;
     const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(want < most ? want : most));
     return R.in_place ? finalise_with<256, true, true>(R, C, grid, stream) : finalise_with<256, true, false>(R, C, grid, stream);
   }
