@@ -14,8 +14,9 @@
 //   epilogue   statistics and gradient: warps 2-17, a lane per row and 64 columns at
 //              a time, so that a row's maximum and sum over them stay in one
 //              thread's registers; outputs: warps 2-5
-//   warps 6-9  outputs only: turn the next piece's codes (head_codes.cuh) into the
-//              gradient of its logits while the tensor cores work on this piece
+//   warps 6-9  outputs, several pieces: turn the next piece's codes (head_codes.cuh)
+//              into the gradient of its logits while the tensor cores work on this
+//              piece; with one piece they are four more epilogue warps
 //
 // Everything a tile stores goes through 4 KiB of shared memory per warp and leaves
 // as a TMA store (or a TMA reduction, where dX or dW is added to): 32 rows by 128
@@ -42,20 +43,26 @@ constexpr int kNumAcc = 2;
 constexpr int kAccCols = 256;
 constexpr int kTmemCols = kNumAcc * kAccCols;
 constexpr int kStageOut = 32 * 128;  // one warp's 32 rows x 128 bytes
-// Shared memory is split between the operand ring and the staging of stores: four
-// warps with two buffers each, or sixteen with one or with half of one (`rows` of a
-// warp's 32 at a time).  A whole buffer and five stages: 896 us against 1015 at 8192 x
-// 256 x 50000.  Half a buffer and six stages: 154 us against 165 for the statistics of
-// 100 x 2048 x 163840, where w streams from memory.
+// Shared memory is split between the operand ring and the staging of stores, six
+// stages and 32 KiB or five stages and 64 KiB:
+//   statistics  sixteen warps with one buffer each and five stages, or (kSpare) with half
+//               a buffer and six stages.  896 us against 1015 at 8192 x 256 x 50000; but
+//               165 us against 154 for 100 x 2048 x 163840, where w streams from memory
+//   outputs     four warps with two buffers each and six stages beside four that
+//               convert codes, or (kSpare) eight warps and five stages where nothing is
+//               left to convert
+template <int kMode, bool kSpare>
+struct Config {
+  static constexpr bool kDeep = kMode == kModeOut ? !kSpare : kSpare;
+  static constexpr int kStages = kDeep ? 6 : 5;
+  static constexpr int kStaging = (kDeep ? 8 : 16) * kStageOut;
+  static constexpr int kEpiWarps = kMode == kModeOut ? (kSpare ? 8 : 4) : 16;
+  static constexpr int kConvertWarps = kMode == kModeOut && !kSpare ? 4 : 0;
+  static constexpr int kThreads = 64 + 32 * (kEpiWarps + kConvertWarps);
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
+  static_assert(kSmemBytes <= 232448, "exceeds the 227 KiB shared-memory limit");
+};
 constexpr int kMaxStages = 6;
-__host__ __device__ constexpr int staging_of(int mode, int rows) {
-  return (mode == kModeOut ? 8 : 16) * kStageOut * rows / 32;
-}
-__host__ __device__ constexpr int stages_of(int mode, int rows) { return mode == kModeOut || rows == 16 ? 6 : 5; }
-__host__ __device__ constexpr int epi_warps(int mode) { return mode == kModeOut ? 4 : 16; }
-
-constexpr int kConvertWarps = 4;
-__host__ __device__ constexpr int threads_of(int mode) { return 64 + 32 * (epi_warps(mode) + (mode == kModeOut ? kConvertWarps : 0)); }
 
 constexpr int kOutside = 1 << 30;  // a row coordinate past every tensor
 
@@ -68,12 +75,7 @@ struct Barriers {
   int abort_flag;
 };
 
-constexpr int smem_of(int mode, int rows) {
-  return 1024 + stages_of(mode, rows) * kStageBytes + staging_of(mode, rows) + 512;
-}
-static_assert(sizeof(Barriers) <= 512 && smem_of(kModeOut, 32) <= 232448 && smem_of(kModeStats, 32) <= 232448 &&
-                  smem_of(kModeStats, 16) <= 232448,
-              "exceeds the 227 KiB shared-memory limit");
+static_assert(sizeof(Barriers) <= 512, "barrier block too large");
 
 __device__ __forceinline__ void report_timeout(const GemmParams& P) { atomicExch(&P.ctrl->status, -6); }
 
@@ -370,15 +372,30 @@ struct ListEntries {
   }
 };
 
+// The tokens' weighted losses added up, always in the same order, by one warp of the last
+// CTA beside its other work.
+__device__ __forceinline__ void add_losses(const GemmParams& P, int n_valid, int lane) {
+  if (P.total == nullptr || blockIdx.x != gridDim.x - 1) return;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int i = lane; i < n_valid; i += 32) sum += P.row_l[i];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if (lane == 0) *P.total = sum;
+}
+
 // kList: the sparse entries come from the caller's list.
-template <int kMode, int kRows, bool kList>
-__global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const __grid_constant__ GemmParams P) {
+template <int kMode, bool kSpare, bool kList>
+__global__ void __launch_bounds__(Config<kMode, kSpare>::kThreads, 1)
+head_gemm_kernel(const __grid_constant__ GemmParams P) {
+  using Cfg = Config<kMode, kSpare>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  constexpr int kStages = stages_of(kMode, kRows);
+  constexpr int kStages = Cfg::kStages;
+  constexpr int kRows = kSpare ? 16 : 32;  // logits: rows of a box that stores them
   uint8_t* staging = ring + kStages * kStageBytes;
-  Barriers* bars = reinterpret_cast<Barriers*>(staging + staging_of(kMode, kRows));
+  Barriers* bars = reinterpret_cast<Barriers*>(staging + Cfg::kStaging);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -395,7 +412,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
     for (int s = 0; s < kNumAcc; ++s) {
       ptx::mbar_init(ptx::smem_u32(&bars->acc_full[s]), 1);
       // warps of both CTAs that read one accumulator
-      ptx::mbar_init(ptx::smem_u32(&bars->acc_empty[s]), 2 * (kMode == kModeOut ? 4 : (P.by_tile ? 8 : 16)));
+      ptx::mbar_init(ptx::smem_u32(&bars->acc_empty[s]), 2 * (kMode == kModeOut ? Cfg::kEpiWarps : (P.by_tile ? 8 : 16)));
     }
     bars->abort_flag = 0;
     ptx::fence_barrier_init();
@@ -547,22 +564,13 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         }
       }
     }
-  } else if (kMode == kModeOut && warp >= 6) {
+  } else if (warp >= 2 + Cfg::kEpiWarps) {
     // ---------------------------------- codes of the next piece, meanwhile ----
+    const int convert = warp - 2 - Cfg::kEpiWarps;
     if (P.convert.g != nullptr)
-      convert_piece(P.convert, n_valid, P.tokens, static_cast<int>(blockIdx.x) * kConvertWarps + warp - 6,
-                    static_cast<int>(gridDim.x) * kConvertWarps, lane);
-    if (P.total != nullptr && blockIdx.x == gridDim.x - 1) {
-      // the tokens' weighted losses, always in the same order; one warp, so that no barrier is needed
-      if (warp == 6) {
-        float sum = 0.f;
-#pragma unroll 4
-        for (int i = lane; i < n_valid; i += 32) sum += P.row_l[i];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        if (lane == 0) *P.total = sum;
-      }
-    }
+      convert_piece(P.convert, n_valid, P.tokens, static_cast<int>(blockIdx.x) * Cfg::kConvertWarps + convert,
+                    static_cast<int>(gridDim.x) * Cfg::kConvertWarps, lane);
+    if (convert == 0) add_losses(P, n_valid, lane);
   } else {
     // ----------------------------------------------------------- epilogue ----
     const int q = warp & 3;  // TMEM lane quarter this warp may read
@@ -735,6 +743,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         k += step;
       }
     } else {
+      if (kSpare && warp == 2) add_losses(P, n_valid, lane);
       int acc = 0;
       uint32_t acc_phase = 0;
       int turn = 0;  // staging buffer last used
@@ -751,7 +760,9 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
         const bool is_dx = tl.prod == 0;
         const int n_tile = P.prod[tl.prod].n_tile;
         const int c0 = tl.ni * n_tile;
-        const int limit = min(n_tile, (is_dx ? P.part_cols : P.dw_cols) - c0);
+        // eight warps take half of the columns each
+        const int from = kSpare ? (warp - 2) / 4 * (n_tile / 2) : 0;
+        const int limit = min(kSpare ? from + n_tile / 2 : n_tile, (is_dx ? P.part_cols : P.dw_cols) - c0);
         const bool rows_ok = is_dx ? row0 < n_valid : row0 < P.dw_rows;
         // two buffers in turn: the store before last has been read
         auto next_buffer = [&]() {
@@ -782,7 +793,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           const int y = is_dx ? row0 : P.dw_row0 + row0, z = is_dx ? tl.split : 0;
           const bool add = is_dx ? P.part_add != 0 : P.dw_add != 0;
 #pragma unroll 1
-          for (int c = 0; c < limit; c += 32) {
+          for (int c = from; c < limit; c += 32) {
             uint32_t v[32];
             load(v, c);
             ptx::tmem_ld_wait();
@@ -793,7 +804,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           }
         } else if (rows_ok && P.dw_tma) {
 #pragma unroll 1
-          for (int c = 0; c < limit; c += 64) {
+          for (int c = from; c < limit; c += 64) {
             uint32_t v[32], u[32];
             load(v, c);
             load(u, c + 32);
@@ -816,7 +827,7 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
           // rows TMA cannot address, or sums into bf16: through shared memory, so that
           // a warp's accesses run along a row
 #pragma unroll 1
-          for (int c = 0; c < limit; c += 32) {
+          for (int c = from; c < limit; c += 32) {
             uint32_t v[32];
             load(v, c);
             ptx::tmem_ld_wait();
@@ -866,18 +877,18 @@ __global__ void __launch_bounds__(threads_of(kMode), 1) head_gemm_kernel(const _
   }
 }
 
-template <int kMode, int kRows = 32, bool kList = false>
+template <int kMode, bool kSpare = false, bool kList = false>
 cudaError_t configure_one() {
-  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kRows, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              smem_of(kMode, kRows));
+  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kSpare, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Config<kMode, kSpare>::kSmemBytes);
 }
 
-template <int kMode, int kRows = 32, bool kList = false>
+template <int kMode, bool kSpare = false, bool kList = false>
 cudaError_t launch_one(const GemmParams& P, unsigned clusters, bool overlap, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * clusters, 1, 1);
-  cfg.blockDim = dim3(threads_of(kMode), 1, 1);
-  cfg.dynamicSmemBytes = smem_of(kMode, kRows);
+  cfg.blockDim = dim3(Config<kMode, kSpare>::kThreads, 1, 1);
+  cfg.dynamicSmemBytes = Config<kMode, kSpare>::kSmemBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -888,17 +899,18 @@ cudaError_t launch_one(const GemmParams& P, unsigned clusters, bool overlap, cud
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = overlap ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kRows, kList>, P);
+  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kSpare, kList>, P);
 }
 
 }  // namespace
 
 cudaError_t gemm_configure() {
   cudaError_t e = configure_one<kModeStats>();
-  if (e == cudaSuccess) e = configure_one<kModeStats, 16>();
-  if (e == cudaSuccess) e = configure_one<kModeStats, 16, true>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, true>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, true, true>();
   if (e == cudaSuccess) e = configure_one<kModeGrad>();
   if (e == cudaSuccess) e = configure_one<kModeOut>();
+  if (e == cudaSuccess) e = configure_one<kModeOut, true>();
   return e;
 }
 
@@ -906,8 +918,8 @@ cudaError_t gemm_configure() {
 cudaError_t gemm_max_clusters(int* out) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2, 1, 1);
-  cfg.blockDim = dim3(threads_of(kModeOut), 1, 1);
-  cfg.dynamicSmemBytes = smem_of(kModeOut, 32);
+  cfg.blockDim = dim3(Config<kModeOut, false>::kThreads, 1, 1);
+  cfg.dynamicSmemBytes = Config<kModeOut, false>::kSmemBytes;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = 2;
@@ -915,7 +927,7 @@ cudaError_t gemm_max_clusters(int* out) {
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, 32, false>, &cfg);
+  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, false, false>, &cfg);
 }
 
 // Rows of a box in which the statistics' codes are stored: one row tile reads w from
@@ -928,12 +940,13 @@ cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_
   if (tiles <= 0) return cudaSuccess;
   const unsigned clusters = static_cast<unsigned>(tiles < max_clusters ? tiles : max_clusters);
   if (mode == kModeStats) {
-    if (P.ids64 != nullptr) return launch_one<kModeStats, 16, true>(P, clusters, overlap, stream);
-    return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, 16>(P, clusters, overlap, stream)
+    if (P.ids64 != nullptr) return launch_one<kModeStats, true, true>(P, clusters, overlap, stream);
+    return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, true>(P, clusters, overlap, stream)
                                       : launch_one<kModeStats>(P, clusters, overlap, stream);
   }
   if (mode == kModeGrad) return launch_one<kModeGrad>(P, clusters, overlap, stream);
-  return launch_one<kModeOut>(P, clusters, overlap, stream);
+  return P.spare ? launch_one<kModeOut, true>(P, clusters, overlap, stream)
+                 : launch_one<kModeOut>(P, clusters, overlap, stream);
 }
 
 }  // namespace head

@@ -288,11 +288,12 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 // kInPlace: few tokens, rows are tokens and nothing came before the statistics.  What
 // prepare_kernel does for more tokens is done here for one row, before the wait for
 // the statistics, while they run.
-// Tiles a warp converts at a time: few rows are spread thin, many rows want loads in flight.
-__host__ __device__ constexpr int fused_tiles(int threads) { return threads == 256 ? 2 : 4; }
-template <bool kDistill, bool kConvert, int kThreads, bool kInPlace>
+//
+// kFusedTiles: tiles a warp converts at a time, two with few rows (four: 482 us in place
+// of 466 at 100 x 2048 x 163840), four with many.
+template <bool kDistill, bool kConvert, int kThreads, bool kInPlace, int kFusedTiles>
 __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, const ConvertParams C) {
-  constexpr int kWarps = kThreads / 32, kFusedTiles = fused_tiles(kThreads);
+  constexpr int kWarps = kThreads / 32;
   __shared__ float s_f[kWarps];
   __shared__ float s_max[kWarps];
   __shared__ int s_id[kMaxTop];
@@ -635,27 +636,28 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
 // well.  More rows: small blocks, so that a thousand are in flight, that still convert
 // while the codes lie in L2 (62 us in place of 65 for a call of 500 x 1024 x 13000); a
 // pass of its own above that (1576 us in place of 1609 at 4097 x 1536 x 50021).
-template <int kThreads, bool kConvert, bool kInPlace>
+template <int kThreads, bool kConvert, bool kInPlace, int kFusedTiles>
 cudaError_t finalise_with(const RowParams& R, const ConvertParams& C, dim3 grid, cudaStream_t stream) {
-  return launch_of(kThreads, R.z != nullptr ? finalise_kernel<true, kConvert, kThreads, kInPlace>
-                                            : finalise_kernel<false, kConvert, kThreads, kInPlace>,
+  return launch_of(kThreads, R.z != nullptr ? finalise_kernel<true, kConvert, kThreads, kInPlace, kFusedTiles>
+                                            : finalise_kernel<false, kConvert, kThreads, kInPlace, kFusedTiles>,
                    grid, true, stream, R, C);
 }
 
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
   const int rows = R.tokens > 0 ? R.tokens : 1;
   if (C.g != nullptr && R.tokens < kFusedRows) {
-    // enough blocks to spread the conversion over the device
-    const int runs = (C.tiles + fused_tiles(256) - 1) / fused_tiles(256);
+    // blocks for three on every SM
+    const int runs = (C.tiles + 1) / 2;
     const int most = (runs + kRowWarps - 1) / kRowWarps, want = (3 * sms + rows - 1) / rows;
     const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(want < most ? want : most));
-    return R.in_place ? finalise_with<256, true, true>(R, C, grid, stream) : finalise_with<256, true, false>(R, C, grid, stream);
+    return R.in_place ? finalise_with<256, true, true, 2>(R, C, grid, stream)
+                      : finalise_with<256, true, false, 2>(R, C, grid, stream);
   }
   const dim3 grid(static_cast<unsigned>(rows));
-  if (R.in_place) return finalise_with<256, false, true>(R, C, grid, stream);
+  if (R.in_place) return finalise_with<256, false, true, 2>(R, C, grid, stream);
   if (C.g != nullptr && static_cast<long long>(R.tokens) * C.tiles * kTileN * 2 <= kCodesInCache)
-    return finalise_with<128, true, false>(R, C, grid, stream);
-  cudaError_t e = finalise_with<128, false, false>(R, C, grid, stream);
+    return finalise_with<128, true, false, 4>(R, C, grid, stream);
+  cudaError_t e = finalise_with<128, false, false, 2>(R, C, grid, stream);
   if (e != cudaSuccess || C.g == nullptr) return e;
   const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
   const long long tasks = static_cast<long long>(R.tokens) * runs;
