@@ -84,14 +84,16 @@ int choose_splits(int m_tiles, int n_tiles, int dx_kb, long long dw_tiles, int d
 }
 
 // Codes or a second product x w^T?  The second product costs 2 dim FLOPs for every
-// logit, the codes 2 bytes written and 4 bytes of conversion, which come cheap while
-// they stay in L2.  Measured, second product against codes: 1917 and 1686 us for
-// 2000 x 1024 x 163840, 1402 and 1396 at 768 columns, 1075 and 1282 at 512, 675
-// and 994 at 128; but 89 and 88 us for 500 x 128 x 50000, 54 and 52 for 2000 x 128
-// x 5000.
+// logit, the codes 2 bytes written and 4 bytes of conversion, and in a short call a
+// launch more against one fewer.  Measured, second product against codes, us: 4718 and
+// 3932 for 8192 x 1024 x 100000, 2711 and 2633 at 512 columns, 2442 and 2488 at 384;
+// 55.0 and 55.0 for 2000 x 256 x 5000, 47.0 and 43.0 for 500 x 256 x 13000; 85 and 80 for
+// 100 x 64 x 163840, whose tokens are not gathered.
+constexpr int kCodesDim = 448;
+constexpr long long kFewCodes = 20ll << 20;
 bool want_codes(int tokens, int dim, int vocab) {
   if (g_codes != 0) return g_codes == 2;
-  return dim >= 768 || 2ll * tokens * vocab <= kCodesInCache;
+  return dim >= kCodesDim || tokens <= kInPlaceRows || 2ll * tokens * vocab <= kFewCodes;
 }
 
 // `room`: bytes of workspace to plan for; 0 plans for as many as are useful.
