@@ -19,7 +19,6 @@ constexpr int kFusedRows = 296;  // fewer tokens than this count as few
 constexpr int kInPlaceRows = 256;     // most tokens whose rows are not gathered
 constexpr int kInPlaceEntries = 4096; // and most of a teacher's entries in all
 constexpr long long kHeadInCache = 96ll << 20;   // bytes of w that do, between its two readings
-constexpr long long kCodesInCache = 96ll << 20;  // bytes of codes that stay in L2 (126 MB)
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
 

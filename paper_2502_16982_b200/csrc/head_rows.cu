@@ -530,15 +530,6 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
   }
 }
 
-// The first stored piece's codes where there are many rows; those of the later
-// pieces are converted beside the products (head_gemm.cu).
-__global__ void __launch_bounds__(kRowThreads) convert_kernel(const ConvertParams C, const Ctrl* ctrl, int tokens) {
-  ptx::grid_dependency_wait();
-  ptx::grid_launch_dependents();
-  convert_piece(C, ctrl->n_valid, tokens, static_cast<int>(blockIdx.x) * kRowWarps + static_cast<int>(threadIdx.x >> 5),
-                static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
-}
-
 // dX of the tokens that count, in token order: the partial sums joined, always in the
 // same order.  Four columns a thread, or, kWays > 1, kWays neighbouring lanes that
 // take a stretch of the runs each: with the many runs of a small launch one memory
@@ -632,10 +623,11 @@ cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream
                 overlap, stream, R);
 }
 
-// Few rows: large blocks, several a row, that convert the first piece's codes as
-// well.  More rows: small blocks, so that a thousand are in flight, that still convert
-// while the codes lie in L2 (62 us in place of 65 for a call of 500 x 1024 x 13000); a
-// pass of its own above that (1576 us in place of 1609 at 4097 x 1536 x 50021).
+// Few rows: large blocks, several a row, to spread the conversion over the device.  More
+// rows: small blocks, so that a thousand are in flight (40 us in place of 85 for 8192 rows
+// without codes).  A conversion in a launch of its own is no faster at any size tried (375
+// us in place of 374 at 1777 x 1792 x 32003, 11.13 ms in place of 11.10 at 8192 x 2048 x
+// 163840) and slower at 500 x 1024 x 13000 (66 in place of 64).
 template <int kThreads, bool kConvert, bool kInPlace, int kFusedTiles>
 cudaError_t finalise_with(const RowParams& R, const ConvertParams& C, dim3 grid, cudaStream_t stream) {
   return launch_of(kThreads, R.z != nullptr ? finalise_kernel<true, kConvert, kThreads, kInPlace, kFusedTiles>
@@ -655,15 +647,8 @@ cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms,
   }
   const dim3 grid(static_cast<unsigned>(rows));
   if (R.in_place) return finalise_with<256, false, true, 2>(R, C, grid, stream);
-  if (C.g != nullptr && static_cast<long long>(R.tokens) * C.tiles * kTileN * 2 <= kCodesInCache)
-    return finalise_with<128, true, false, 4>(R, C, grid, stream);
-  cudaError_t e = finalise_with<128, false, false, 2>(R, C, grid, stream);
-  if (e != cudaSuccess || C.g == nullptr) return e;
-  const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
-  const long long tasks = static_cast<long long>(R.tokens) * runs;
-  const long long blocks = (tasks + kRowWarps - 1) / kRowWarps, many = 8ll * sms;
-  return launch(convert_kernel, dim3(static_cast<unsigned>(blocks < many ? blocks : many)), true, stream, C,
-                static_cast<const Ctrl*>(R.ctrl), R.tokens);
+  return C.g != nullptr ? finalise_with<128, true, false, 4>(R, C, grid, stream)
+                        : finalise_with<128, false, false, 2>(R, C, grid, stream);
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
