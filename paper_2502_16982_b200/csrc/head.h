@@ -16,6 +16,7 @@ constexpr int kStatN = 64;    // vocabulary columns of one statistics entry: wha
 constexpr int kUnits = kTileN / kStatN;
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
 constexpr int kFusedRows = 296;  // fewer tokens than this count as few
+constexpr int kManyTokens = 16384;    // from here on the tokens that count are counted in runs of 256 first
 constexpr int kInPlaceRows = 256;     // most tokens whose rows are not gathered
 constexpr int kInPlaceEntries = 4096; // and most of a teacher's entries in all
 constexpr long long kHeadInCache = 96ll << 20;   // bytes of w that do, between its two readings
@@ -144,6 +145,7 @@ struct RowParams {
   float scale;
   int mean;
   unsigned char* flags;  // [tokens] token counts (distillation)
+  int* run_counts;       // many tokens: how many count in every run of 256, else NULL
   int* row_of;           // [token]
   int* ids;              // [token][top]
   float* p;              // [token][top]
@@ -179,6 +181,7 @@ cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_
                         cudaStream_t stream);
 
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_count(const RowParams& R, bool overlap, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);

@@ -48,7 +48,7 @@ struct Plan {
   int n_stored, n_buffers;   // pieces kept as codes; piece buffers in the workspace
   int splits, dx_n_tile, dx_n_tiles;
   long long ld_xc, ld_wc, part_ld, part_stride;
-  size_t ctrl, xc, wc, flags, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
+  size_t ctrl, xc, wc, flags, run_counts, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
       part, bytes, least;
 };
 
@@ -146,6 +146,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   P->ctrl = take(sizeof(Ctrl));
   P->xc = take(rows * P->ld_xc * 2);
   P->row_of = take(rows * 4);
+  P->run_counts = take(P->tokens >= kManyTokens ? (rows / 256 + 1) * 4 : 0);
   P->ids = take(entries * 4);
   P->entry_logit = take(entries * 4);
   P->entry_g = take(entries * 4);
@@ -454,7 +455,12 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
       HEAD_CUDA(launch_flags(R, stream));
     }
-    HEAD_CUDA(launch_prepare(R, flags, stream));
+    const bool many = P.tokens >= kManyTokens;
+    if (many) {
+      R.run_counts = reinterpret_cast<int*>(ws + P.run_counts);
+      HEAD_CUDA(launch_count(R, flags, stream));
+    }
+    HEAD_CUDA(launch_prepare(R, flags || many, stream));
   }
   const long long m_tiles = P.m_tiles;
   // more tiles than CTA pairs: the epilogue's warps share them out instead of their columns

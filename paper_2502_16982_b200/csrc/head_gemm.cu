@@ -377,8 +377,13 @@ struct ListEntries {
 __device__ __forceinline__ void add_losses(const GemmParams& P, int n_valid, int lane) {
   if (P.total == nullptr || blockIdx.x != gridDim.x - 1) return;
   float sum = 0.f;
-#pragma unroll 4
-  for (int i = lane; i < n_valid; i += 32) sum += P.row_l[i];
+  const int whole = n_valid & ~127;
+#pragma unroll 8
+  for (int i = lane * 4; i < whole; i += 128) {
+    const float4 v = *reinterpret_cast<const float4*>(P.row_l + i);
+    sum += (v.x + v.y) + (v.z + v.w);
+  }
+  for (int i = whole + lane; i < n_valid; i += 32) sum += P.row_l[i];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if (lane == 0) *P.total = sum;

@@ -70,6 +70,16 @@ __device__ __forceinline__ bool counts(const RowParams& R, const unsigned char* 
 }
 
 
+// Many tokens: how many count in every run of kRowThreads, for prepare_kernel.
+template <bool kDistill>
+__global__ void __launch_bounds__(kRowThreads) count_kernel(const RowParams R) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int t = blockIdx.x * kRowThreads + threadIdx.x;
+  const int n = __syncthreads_count(t < R.tokens && counts<kDistill>(R, R.flags, t));
+  if (threadIdx.x == 0) R.run_counts[blockIdx.x] = n;
+}
+
 // Copy of a head whose rows TMA cannot address (16-byte aligned rows) into rows that it
 // can, by block `block` of `blocks`; one warp per row.
 __device__ __forceinline__ void pack_rows(const RowParams& R, int block, int blocks) {
@@ -90,7 +100,7 @@ __global__ void __launch_bounds__(kRowThreads) pack_kernel(const RowParams R) { 
 // Gathers the rows of the tokens that count, in token order, so that masked
 // tokens cost nothing in the products and whatever they hold reaches no sum.
 // Every block counts the tokens before its own by itself (8 bytes a token out of
-// L2) instead of waiting for a scan.  Distillation: the teacher's entries become
+// L2) instead of waiting for a scan; with many tokens it adds up the counts of whole runs.  Distillation: the teacher's entries become
 // probabilities, sorted by index, with the number of entries below every
 // 256-column tile, so that an epilogue finds its entries without a search.
 template <bool kDistill>
@@ -113,11 +123,25 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   int before = 0, total = 0;
   float wsum = 0.f;
   const bool sum_weights = blockIdx.x == 0 && R.weight != nullptr;
-  for (int t = tid; t < R.tokens; t += kRowThreads) {
-    const bool c = counts<kDistill>(R, flags, t);
-    total += c;
-    before += c && t < first;
-    if (sum_weights && c) wsum += R.weight[t];
+  if (R.run_counts == nullptr) {
+    for (int t = tid; t < R.tokens; t += kRowThreads) {
+      const bool c = counts<kDistill>(R, flags, t);
+      total += c;
+      before += c && t < first;
+      if (sum_weights && c) wsum += R.weight[t];
+    }
+  } else {
+    const int runs = (R.tokens + kRowThreads - 1) / kRowThreads, mine = first / kRowThreads;
+    for (int i = tid; i < runs; i += kRowThreads) {
+      const int n = R.run_counts[i];
+      total += n;
+      if (i < mine) before += n;
+    }
+    const int t = mine * kRowThreads + tid;
+    before += t < first && counts<kDistill>(R, flags, t);
+    if (sum_weights)
+      for (int u = tid; u < R.tokens; u += kRowThreads)
+        if (counts<kDistill>(R, flags, u)) wsum += R.weight[u];
   }
   total = block_sum(total, s_int);
   before = block_sum(before, s_int);
@@ -616,6 +640,11 @@ unsigned row_blocks(int tokens) { return tokens > 0 ? static_cast<unsigned>((tok
 
 cudaError_t launch_flags(const RowParams& R, cudaStream_t stream) {
   return launch(flags_kernel, dim3(row_blocks(R.tokens)), false, stream, R);
+}
+
+cudaError_t launch_count(const RowParams& R, bool overlap, cudaStream_t stream) {
+  return launch(R.z != nullptr ? count_kernel<true> : count_kernel<false>,
+                dim3(static_cast<unsigned>((R.tokens + kRowThreads - 1) / kRowThreads)), overlap, stream, R);
 }
 
 cudaError_t launch_prepare(const RowParams& R, bool overlap, cudaStream_t stream) {

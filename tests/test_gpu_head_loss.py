@@ -103,6 +103,7 @@ BF, FP = torch.bfloat16, torch.float32
     (200, 264, 4096, 0.0, dict(pad_x=3, pad_w=8, offset_x=1, offset_w=8)),
     (200, 264, 900, 0.2, dict(offset_w=1, pad_w=1, dw=FP)),
     (1100, 520, 3001, 0.4, {}),
+    (20011, 24, 300, 0.6, dict(weights=True)),           # tokens counted in runs first
     (1200, 776, 9100, 0.3, dict(dx=FP)),
 ])
 def test_cross_entropy_matches_the_oracle(T, D, V, masked, opts):
@@ -141,6 +142,7 @@ def test_cross_entropy_matches_the_oracle(T, D, V, masked, opts):
     (90, 64, 600, 8, dict(masked=1.0)),
     (700, 512, 2600, 5, dict(dx=None, tail=True, temperature=3.0)),
     (900, 768, 12000, 40, dict(masked=0.2)),
+    (16384, 16, 260, 3, dict(masked=0.5)),
 ])
 def test_distillation_matches_the_oracle(T, D, V, K, opts):
     from paper_2502_16982_b200 import binding as b
