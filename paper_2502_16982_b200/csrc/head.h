@@ -35,6 +35,7 @@ struct Ctrl {
 struct Product {
   CUtensorMap map_a, map_b;
   int a_mn, b_mn;    // operand stored with M (N) contiguous instead of K
+  int a_rows;        // rows of a box of operand A (K contiguous): 128, or what few tokens need
   int n_tile;        // 128 or 256
   int m_tiles;       // row tiles of 256; -1: from the number of tokens that count
   int n_tiles;

@@ -465,8 +465,9 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
       // rows past the tokens that count are asked for outside the tensor: zeros, without traffic
       const int m_row = tl.mi * kTileM + static_cast<int>(rank) * 128;
       const int a_row = pr.m_tiles < 0 && m_row >= n_valid ? kOutside : m_row;
+      const int a_rows = pr.a_mn ? 128 : pr.a_rows;
       const int b_row = pr.b_n0 + tl.ni * pr.n_tile + static_cast<int>(rank) * half_n;
-      const uint32_t stage_tx = 2u * static_cast<uint32_t>(kTileABytes + half_n * 128);
+      const uint32_t stage_tx = 2u * static_cast<uint32_t>((a_rows + half_n) * 128);
       const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
       for (int kb = tl.kb0; kb < tl.kb1; ++kb) {
         ok = ptx::mbar_wait(empty0 + stage * 8, phase ^ 1u, abort_flag);
@@ -481,11 +482,11 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
           const uint32_t sb = sa + kTileABytes;
           const int ka = kb * kBK, kbb = pr.b_k0 + kb * kBK;
           if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + stage * 8, stage_tx);
-          if (!a_mn) {
-            ptx::tma_load_3d_pair(sa, &pr.map_a, ka, a_row, pr.a_z, leader_full);
-          } else {
+          if (a_mn) {
             ptx::tma_load_3d_pair(sa, &pr.map_a, a_row, ka, pr.a_z, leader_full);
             ptx::tma_load_3d_pair(sa + 8192, &pr.map_a, a_row + 64, ka, pr.a_z, leader_full);
+          } else {
+            ptx::tma_load_3d_pair(sa, &pr.map_a, ka, a_row, pr.a_z, leader_full);
           }
           if (!b_mn) {
             ptx::tma_load_3d_pair(sb, &pr.map_b, kbb, b_row, 0, leader_full);
