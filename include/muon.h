@@ -595,9 +595,11 @@ typedef struct muon_head_args {
  * Bytes of DEVICE workspace (1024-byte aligned) of one call: pure host computation
  * on the sizes, the types, the alignment and stride of w, and which of dx and dw
  * are wanted.  top: teacher entries per token, 0 for cross entropy.
- *   *least_bytes: what the call cannot do without (either pointer may be NULL).  It
- *       holds the gradient of the logits of one piece of the vocabulary: at most
- *       256 MiB, or 256 vocabulary entries if that is more.
+ *   *least_bytes: what the call cannot do without (either pointer may be NULL): a
+ *       copy of x, the gradient of the logits of one piece of the vocabulary (at
+ *       most 256 MiB, or 256 vocabulary entries if that is more), partial sums of dX
+ *       (at most 256 MiB, or one fp32 dX) and the softmax statistics, one byte for
+ *       eight logits.
  *   *out_bytes: with up to 3 GiB more the call keeps the logits of as many pieces
  *       as 16-bit codes between the pass that forms the softmax sums and the one
  *       that forms the gradients, instead of computing them twice (a quarter of

@@ -32,7 +32,7 @@ long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 // Bytes of logit gradients (bf16) that one vocabulary piece takes, at most, and of
 // the pieces together whose logits are kept as codes in the workspace that
-// muon_head_workspace_bytes asks for.
+// muon_head_workspace_bytes asks for, their statistics (a sixteenth) included.
 constexpr long long kPieceBytes = 1ll << 28;
 constexpr long long kCodeBytes = 3ll << 30;
 long long g_piece_bytes = kPieceBytes;
@@ -162,18 +162,25 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     P->starts = take(rows * (P->v_tiles + 1));
   }
   if (P->pack) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
-  if (P->want_dx) P->part = take(static_cast<size_t>(P->splits) * P->part_stride * 4);
+  // Where no second piece is kept as codes nothing reads the statistics after the
+  // finalisation, and partial dX may lie in their place.
+  const size_t part_bytes = P->want_dx ? static_cast<size_t>(P->splits) * P->part_stride * 4 : 0;
+  const size_t stats_bytes = rows * P->v_tiles * kUnits * sizeof(float2);
+  const bool share = part_bytes > 0 && stats_bytes >= part_bytes;
+  const size_t apart = static_cast<size_t>(round_up(static_cast<long long>(part_bytes), 1024));
   P->n_stored = P->n_buffers = 0;
   P->least = off;
   if (P->grads) {
     const long long one = static_cast<long long>(rows) * P->piece_tiles * kTileN * 2;
     P->n_buffers = 1;
     if (want_codes(P->tokens, P->dim, P->vocab)) {
-      long long fit = (room ? static_cast<long long>(room) - static_cast<long long>(off) : kCodeBytes) / one;
+      long long fit = (room ? static_cast<long long>(room) - static_cast<long long>(off + apart)
+                            : kCodeBytes - static_cast<long long>(stats_bytes)) / one;
       P->n_buffers = static_cast<int>(fit < 1 ? 1 : (fit > P->n_pieces ? P->n_pieces : fit));
       P->n_stored = P->n_buffers;
     }
-    P->least = off + static_cast<size_t>(round_up(one, 1024));
+    P->least = off + (share ? 0 : apart) + static_cast<size_t>(round_up(one, 1024));
+    if (part_bytes) P->part = share && P->n_stored <= 1 ? P->stats : take(part_bytes);
     P->g = take(static_cast<size_t>(one) * P->n_buffers);
   }
   // few tokens with rows that TMA can address, and nothing but codes between the passes

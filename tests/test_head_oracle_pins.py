@@ -160,7 +160,8 @@ def test_workspace_stays_bounded_on_the_host():
     least = b.muon_head_workspace_bytes(65536, 2048, 163840, least=True)
     logits = 65536 * 163840 * 2
     assert least < full < logits / 4 and least < logits / 10
-    assert b.muon_head_workspace_bytes(8192, 2048, 163840, dx=False, dw=False) < 128 << 20
+    # without gradients: a copy of x, one byte of statistics for eight logits, a few words a token
+    assert b.muon_head_workspace_bytes(8192, 2048, 163840, dx=False, dw=False) < 8192 * (2 * 2048 + 163840 // 8) + (1 << 20)
     assert b.muon_head_workspace_bytes(0, 64, 1000) > 0
     with pytest.raises(b.MuonError):
         b.muon_head_workspace_bytes(16, 64, 1000, top=129)
