@@ -3,8 +3,11 @@
 // columns, in steps of 2^-11 on the log2 scale: code = round((max - y) 2^11), capped at
 // 65535, y = scale2 * logit.  Decoding gives q within 2^-12 ln 2 = 1.7e-4, a
 // twentieth of the bf16 rounding of the gradient that follows; what lies 2^-32
-// or more below its tile's largest becomes 0.  The gradient of the logits is then
-// a pass over the codes instead of a second product x w^T.
+// or more below its tile's largest becomes 0.  The maximum's product with scale2 is
+// rounded upwards, so that max - y is never negative (with the nearest value, a
+// largest logit of some thousands can lie above it, and its code would wrap to 65535).
+// The gradient of the logits is then a pass over the codes instead of a second
+// product x w^T.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -26,7 +29,7 @@ __device__ __forceinline__ float ex2_fast(float x) {
 }
 
 // `steps` = (max - y) kCodeSteps + kCodeMagic, rounded to a whole number by the
-// addition; the code is in the low 16 bits of the result.
+// addition; the code is in the low 16 bits of the result.  max - y >= 0.
 __device__ __forceinline__ uint32_t clamp_code(float steps) {
   return __float_as_uint(fminf(steps, kCodeMagic + 65535.0f));
 }

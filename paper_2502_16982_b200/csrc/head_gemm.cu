@@ -672,7 +672,8 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
               a = max3(a, __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
               b = max3(b, __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
             }
-            m = max3(max3(a, __uint_as_float(v[kStatN - 2]), __uint_as_float(v[kStatN - 1])), b, b) * P.scale2;
+            // rounded up: no exponent below comes out positive, which a code could not hold
+            m = __fmul_ru(max3(max3(a, __uint_as_float(v[kStatN - 2]), __uint_as_float(v[kStatN - 1])), b, b), P.scale2);
             base = m == -INFINITY ? 0.f : m;  // nothing but -inf
           }
           const uint64_t shift = kMode == kModeStats ? pair(-base, -base) : pair(-rq.y, -rq.y);

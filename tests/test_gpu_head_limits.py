@@ -1,0 +1,51 @@
+"""The LM-head losses where numbers, sizes or layouts are extreme.
+
+Tolerances are those of test_gpu_head_loss.py, derived there."""
+
+import pytest
+import torch
+
+from oracle import head_oracle as ho
+from test_gpu_head_loss import BF, check, coefficients, f64, knobs, make  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def shifted(T, D, V, seed, shift, spread):
+    """Logits of about `shift`, spread around it: one column of x and w carries the shift."""
+    x, w, gen = make(T, D, V, seed, gain=spread)
+    x[:, 0] = abs(shift) ** 0.5
+    w[:, 0] = abs(shift) ** 0.5 * (1 if shift > 0 else -1)
+    return x, w, gen
+
+
+@pytest.mark.parametrize("codes", [1, 2])
+@pytest.mark.parametrize("T", [70, 300])
+@pytest.mark.parametrize("shift,spread", [(3000, 3.0), (-3000, 3.0), (10000, 3.0), (-10000, 3.0), (0, 1000.0), (0, 4000.0)])
+def test_logits_of_thousands(knobs, codes, T, shift, spread):  # noqa: F811
+    """The rounding of a row's largest logit must not cost it its gradient; the largest is
+    hardly ever the target here.  Few tokens and gathered ones, codes and second product."""
+    b = knobs
+    b.muon_debug_set_head_codes(codes)
+    V = 1500
+    x, w, gen = shifted(T, 64, V, 41 + T, shift, spread) if shift else make(T, 64, V, 43 + T, gain=spread)
+    t = torch.randint(0, V, (T,), generator=gen)
+    r = b.muon_head_xent(x, w, t.cuda(), dx=True, dw=True)
+    rows = ho.target_rows(t.numpy(), V)
+    ref = ho.head_loss(f64(x), f64(w), rows)
+    check(r, ref, f64(x), f64(w), rows, 1.0, BF, BF, coefficients(ref["counts"], None, True, 1.0, 0.0))
+
+
+@pytest.mark.parametrize("codes", [1, 2])
+def test_low_temperature(knobs, codes):  # noqa: F811
+    """Logits of 30 - 40 at a temperature of 0.01."""
+    b = knobs
+    b.muon_debug_set_head_codes(codes)
+    T, V, K = 300, 1500, 8
+    x, w, gen = shifted(T, 64, V, 51, 36, 1.0)
+    ids = torch.stack([torch.randperm(V, generator=gen)[:K] for _ in range(T)])
+    z = torch.randn(T, K, generator=gen) * 0.02
+    r = b.muon_head_distill(x, w, ids.cuda(), z.cuda(), temperature=0.01, scale=1e-4, dx=True, dw=True)
+    rows = ho.teacher_rows(ids.numpy(), f64(z), V, 0.01)
+    ref = ho.head_loss(f64(x), f64(w), rows, temperature=0.01, scale=1e-4)
+    check(r, ref, f64(x), f64(w), rows, 100.0, BF, BF, coefficients(ref["counts"], None, True, 1e-4, 0.0))
