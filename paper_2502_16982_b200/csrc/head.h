@@ -147,7 +147,7 @@ struct RowParams {
   int mean;
   unsigned char* flags;  // [tokens] token counts (distillation)
   int* run_counts;       // many tokens: how many count in every run of 256, else NULL
-  int* row_of;           // [token]
+  int* row_of;           // [row]: its token; in_place: the row itself or, masked, -1
   int* ids;              // [token][top]
   float* p;              // [token][top]
   float* row_h;          // [token]: sum p log p

@@ -372,7 +372,8 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
     const float norm = block_sum<kWarps>(c ? (R.weight != nullptr ? R.weight[tid] : 1.0f) : 0.f, s_f);
     coef = !R.mean ? R.scale : (norm == 0.f ? 0.f : R.scale / norm);
     counted = counts<kDistill>(R, s_flags, row);
-    if (kConvert && writes) {  // operand of dW's product
+    if (kConvert && writes) {  // operand of dW's product, and which rows of dX stay 0
+      if (tid == 0) R.row_of[row] = counted ? row : -1;
       const uint4* src = reinterpret_cast<const uint4*>(R.x + row * R.ld_x);
       uint4* dst = reinterpret_cast<uint4*>(R.xc + row * R.ld_xc);
       const int whole = R.dim >> 3;
@@ -577,7 +578,7 @@ __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
   float v[4] = {};
   int t = 0;
   if (mine) {
-    t = R.in_place ? row : R.row_of[row];
+    t = R.row_of[row];
     const int s0 = R.splits * way / kWays, s1 = R.splits * (way + 1) / kWays;
     const float* src = R.part + static_cast<long long>(row) * R.part_ld + c + s0 * R.part_stride;
 #pragma unroll 8
@@ -591,6 +592,11 @@ __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += __shfl_xor_sync(0xFFFFFFFFu, v[e], o);
   if (!mine || way != 0) return;
+  if (t < 0) {  // a masked token among rows that are tokens: 0 whatever w holds
+    t = row;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = 0.f;
+  }
   const long long off = static_cast<long long>(t) * R.ld_dx + c;
   const bool whole = R.dx_vec && c + 4 <= R.dim;
   if (R.dx_fp32) {

@@ -49,3 +49,24 @@ def test_low_temperature(knobs, codes):  # noqa: F811
     rows = ho.teacher_rows(ids.numpy(), f64(z), V, 0.01)
     ref = ho.head_loss(f64(x), f64(w), rows, temperature=0.01, scale=1e-4)
     check(r, ref, f64(x), f64(w), rows, 100.0, BF, BF, coefficients(ref["counts"], None, True, 1e-4, 0.0))
+
+
+@pytest.mark.parametrize("bad", ["inf", "nan"])
+@pytest.mark.parametrize("T,pad", [(40, 0), (40, 1), (256, 0), (257, 0)])
+@pytest.mark.parametrize("top", [0, 3])
+def test_masked_rows_are_zero_whatever_the_head_holds(bad, T, pad, top):
+    from paper_2502_16982_b200 import binding as b
+
+    V = 600
+    x, w, gen = make(T, 64, V, 61, pad_x=pad)
+    w[5, 3] = float(bad)
+    if top:
+        ids = torch.randint(0, V, (T, top), generator=gen)
+        ids[::3] = -1
+        r = b.muon_head_distill(x, w, ids.cuda(), torch.randn(T, top, generator=gen).cuda(), dx=True, dw=True)
+    else:
+        t = torch.randint(0, V, (T,), generator=gen)
+        t[::3] = -100
+        r = b.muon_head_xent(x, w, t.cuda(), dx=True, dw=True)
+    assert not r.loss[::3].any() and not r.lse[::3].any() and not r.dx[::3].any()
+    assert not torch.isfinite(r.loss).all() and torch.isnan(r.dx[1::3]).any()  # the others show it
