@@ -70,3 +70,20 @@ def test_masked_rows_are_zero_whatever_the_head_holds(bad, T, pad, top):
         r = b.muon_head_xent(x, w, t.cuda(), dx=True, dw=True)
     assert not r.loss[::3].any() and not r.lse[::3].any() and not r.dx[::3].any()
     assert not torch.isfinite(r.loss).all() and torch.isnan(r.dx[1::3]).any()  # the others show it
+
+
+@pytest.mark.parametrize("D", [64, 2048])
+@pytest.mark.parametrize("T", [60, 300])
+def test_logits_without_fraction_bits_give_finite_results(D, T):
+    """Logits of about 2^24, where an fp32 value has no bits below 1: the target is the
+    largest, so that its two values stand against each other in the softmax sum."""
+    from paper_2502_16982_b200 import binding as b
+
+    scale = 1e6
+    x, w, _ = make(T, D, 3000, 71)
+    l = scale * (x.double() @ w.double().t())
+    r = b.muon_head_xent(x, w, l.argmax(1), dx=True, dw=True, logit_scale=scale)
+    for k in ("loss", "lse", "total", "dx", "dw"):
+        assert torch.isfinite(getattr(r, k)).all(), k
+    e_l = scale * (D / 16 + 8) * 2.0 ** -23 * float((x.double().abs() @ w.double().abs().t()).max())
+    assert float((r.lse.double() - torch.logsumexp(l, 1)).abs().max()) <= 2 * e_l
