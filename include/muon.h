@@ -563,6 +563,8 @@ int muon_momentum_norm_static(const void* g, float* m, int rows, int cols, int64
  *   dx, dw  : DEVICE, bf16 or fp32, [tokens, dim] and [vocab, dim], each NULL if not
  *             wanted.  dw_accumulate: dw is added to instead of written (several
  *             micro-batches into one fp32 gradient).
+ *   scale finite, logit_scale and temperature finite and positive, and
+ *   logit_scale / temperature neither 0 nor infinite in fp32.
  *   Every pointer aligned to its element size.  Outputs must not overlap inputs or
  *   one another.
  */

@@ -273,6 +273,20 @@ int check(const muon_head_args* a, int top, bool need_ptrs) {
   return MUON_OK;
 }
 
+// logit_scale / temperature, and the same times log2(e) for exponents of 2.
+float logit_scale_of(const muon_head_args* a, const muon_head_teacher* t) {
+  return t ? a->logit_scale / t->temperature : a->logit_scale;
+}
+float scale2_of(float logit_scale) { return static_cast<float>(logit_scale * 1.4426950408889634); }
+
+// As numbers that fp32 holds: with 0 or infinity in their place every row would be NaN.
+int check_scale(const muon_head_args* a, const muon_head_teacher* t) {
+  const float scale2 = scale2_of(logit_scale_of(a, t));
+  if (!std::isfinite(scale2) || scale2 == 0.f || (t && !std::isfinite(1.0f / t->temperature)))
+    return fail(MUON_ERR_INVALID_ARG, "logit_scale / temperature: 0 or infinite in fp32");
+  return MUON_OK;
+}
+
 struct DeviceGuard {
   int before = -1;
   cudaError_t set(int device) {
@@ -316,7 +330,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     w = ws + P.wc;
     ld_w = P.ld_wc;
   }
-  const float logit_scale = distill ? a->logit_scale / t->temperature : a->logit_scale;
+  const float logit_scale = logit_scale_of(a, t);
 
   RowParams R = {};
   R.ctrl = reinterpret_cast<Ctrl*>(ws + P.ctrl);
@@ -352,7 +366,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.entry_logit = reinterpret_cast<float*>(ws + P.entry_logit);
   R.stats = reinterpret_cast<float2*>(ws + P.stats);
   R.stats_ld = R.stats_n = kUnits * P.v_tiles;
-  R.scale2 = static_cast<float>(logit_scale * 1.4426950408889634);
+  R.scale2 = scale2_of(logit_scale);
   R.logit_scale = logit_scale;
   R.z_loss = z_loss;
   R.row_q = reinterpret_cast<float2*>(ws + P.row_q);
@@ -569,6 +583,7 @@ extern "C" int muon_head_xent(const muon_head_args* a, const int64_t* targets, f
   if (a->tokens > 0 && !targets) return fail(MUON_ERR_INVALID_ARG, "targets is null");
   if (misaligned(targets, 8)) return fail(MUON_ERR_ALIGNMENT, "targets not aligned to 8 bytes");
   if (!std::isfinite(z_loss)) return fail(MUON_ERR_INVALID_ARG, "z_loss must be finite");
+  HEAD_TRY(check_scale(a, nullptr));
   return run(a, nullptr, targets, z_loss, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
 }
 
@@ -583,6 +598,7 @@ extern "C" int muon_head_distill(const muon_head_args* a, const muon_head_teache
     return fail(MUON_ERR_UNSUPPORTED, "top_logits must be bf16 or fp32");
   if (!std::isfinite(t->temperature) || !(t->temperature > 0.f))
     return fail(MUON_ERR_INVALID_ARG, "temperature must be finite and positive");
+  HEAD_TRY(check_scale(a, t));
   if (misaligned(t->top_ids, 8) || misaligned(t->top_logits, t->logits_dtype == MUON_DTYPE_FP32 ? 4 : 2) ||
       misaligned(t->teacher_lse, 4))
     return fail(MUON_ERR_ALIGNMENT, "pointer not aligned to its element size");

@@ -1,0 +1,36 @@
+"""Limits of the LM-head losses that the host side checks; no GPU."""
+
+import ctypes as C
+
+import pytest
+
+
+def _call(b, logit_scale=1.0, temperature=None):
+    """Error code of a call that lacks nothing but its workspace."""
+    a = b.muon_head_args(16, 64, 1000, 1, 1 << 20, 1 << 20, 64, 64, b.MUON_DTYPE_BF16, b.MUON_DTYPE_BF16, None, 1.0,
+                         logit_scale, 1 << 20, None, None, None, None, 64, 64, b.MUON_DTYPE_BF16, b.MUON_DTYPE_BF16)
+    if temperature is None:
+        return b.lib().muon_head_xent(C.byref(a), 1 << 20, 0.0, None, 0, 0, None)
+    t = b.muon_head_teacher(1 << 20, 1 << 20, 8, 8, None, 8, b.MUON_DTYPE_FP32, temperature, 0)
+    return b.lib().muon_head_distill(C.byref(a), C.byref(t), None, 0, 0, None)
+
+
+@pytest.mark.parametrize("logit_scale,temperature", [
+    (3e38, None),      # times log2(e): infinite
+    (1e-45, 1e30),     # the quotient is 0
+    (1e30, 1e-30),     # the quotient is infinite
+    (1.0, 1e-40),      # 1 / temperature is infinite
+])
+def test_a_scale_that_fp32_cannot_hold_is_refused(logit_scale, temperature):
+    from paper_2502_16982_b200 import binding as b
+
+    assert _call(b, logit_scale, temperature) == b.MUON_ERR_INVALID_ARG
+    assert b"scale" in b.lib().muon_last_error() or b"temperature" in b.lib().muon_last_error()
+
+
+@pytest.mark.parametrize("logit_scale,temperature", [(1.0, None), (2e38, None), (2e-38, None), (1.0, 1e-6), (1.0, 1e6), (1e20, 1e20), (1e-40, None),
+                                                     (1.0, 3e38)])
+def test_scales_that_it_can_are_not(logit_scale, temperature):
+    from paper_2502_16982_b200 import binding as b
+
+    assert _call(b, logit_scale, temperature) == b.MUON_ERR_WORKSPACE
