@@ -524,7 +524,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
         if (tl.kb0 == tl.kb1) continue;  // no token counts: the epilogue writes zeros by itself
         const Product& pr = P.prod[tl.prod];
         const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
-        ok = ptx::mbar_wait(ptx::smem_u32(&bars->acc_empty[acc]), acc_phase ^ 1u, abort_flag);
+        ok = ptx::mbar_wait<true>(ptx::smem_u32(&bars->acc_empty[acc]), acc_phase ^ 1u, abort_flag);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) {
           if (elected) report_timeout(P);
@@ -593,7 +593,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0)
-        ptx::mbar_arrive_cluster_no_release(ptx::map_to_cta(ptx::smem_u32(&bars->acc_empty[acc]), 0));
+        ptx::mbar_arrive_cluster_relaxed(ptx::map_to_cta(ptx::smem_u32(&bars->acc_empty[acc]), 0));
     };
     if constexpr (kMode != kModeOut) {
       // Four groups of four warps, a unit of work being 64 columns of a warp's 32 rows:

@@ -46,15 +46,27 @@ __device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t byt
                : "memory");
 }
 
+// kCluster: of a barrier that threads of the peer CTA arrive on by themselves.
+template <bool kCluster = false>
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
+  if (kCluster) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+  }
   return ok != 0;
 }
 
@@ -66,12 +78,13 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 // Bounded wait on an mbarrier phase.  Returns false if the wait expired or
 // another role of this CTA already aborted; the caller must then leave its
 // loops and fall through to the kernel's teardown.
+template <bool kCluster = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                           uint64_t limit_ns = kWaitLimitNs) {
-  if (mbar_try_wait(bar, parity)) return true;
+  if (mbar_try_wait<kCluster>(bar, parity)) return true;
   uint64_t t0 = 0;
   for (uint32_t spin = 1;; ++spin) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (mbar_try_wait<kCluster>(bar, parity)) return true;
     if ((spin & 0xFFu) == 0) {
       if (*abort_flag) return false;
       uint64_t now = globaltimer_ns();
@@ -320,12 +333,17 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
                : "memory");
 }
 
-// The same without a cluster-wide release: for a signal that no memory write has to
-// be ordered before (a TMEM accumulator whose loads tcgen05.wait::ld has seen
-// complete).  The release form also waits for this thread's TMA stores: 2400 cycles
-// a tile in an epilogue that stores 64 KiB.
-__device__ __forceinline__ void mbar_arrive_cluster_no_release(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+// The same for handing over a TMEM accumulator, and nothing else.  What has to come
+// before the signal are tcgen05 loads, not memory writes: tcgen05.wait::ld has seen
+// them complete, tcgen05.fence::before_thread_sync orders them before the arrival as
+// an execution-ordering operation, and the waiting issuer's
+// fence::after_thread_sync orders its next tcgen05.mma after it.  For that the
+// arrival may be relaxed, at cluster scope like the wait.  The release form also waits
+// for what the SM has under way in stores (469 us in place of 425 for 100 tokens x
+// 2048 x 163840, 2470 in place of 2200 for 8192 x 64 x 163840; another lane than the
+// one that stores makes no difference).
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // Tiled 3-D load into this CTA's shared memory whose byte count is reported to

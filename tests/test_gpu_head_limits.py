@@ -87,3 +87,18 @@ def test_logits_without_fraction_bits_give_finite_results(D, T):
         assert torch.isfinite(getattr(r, k)).all(), k
     e_l = scale * (D / 16 + 8) * 2.0 ** -23 * float((x.double().abs() @ w.double().abs().t()).max())
     assert float((r.lse.double() - torch.logsumexp(l, 1)).abs().max()) <= 2 * e_l
+
+
+@pytest.mark.parametrize("T,D,V", [(100, 512, 40000), (2000, 64, 20000), (700, 1024, 20000)])
+def test_many_tiles_a_pair_give_the_same_bits(T, D, V):
+    """Both accumulators of every CTA pair are handed over many times, short products and
+    long ones, with the stores of codes, of dX and of dW in between."""
+    from paper_2502_16982_b200 import binding as b
+
+    x, w, gen = make(T, D, V, 81)
+    t = torch.randint(0, V, (T,), generator=gen).cuda()
+    first = b.muon_head_xent(x, w, t, dx=True, dw=True)
+    for _ in range(20):
+        again = b.muon_head_xent(x, w, t, dx=True, dw=True)
+        for k in ("loss", "lse", "total", "dx", "dw"):
+            assert torch.equal(getattr(first, k), getattr(again, k)), k
