@@ -526,11 +526,13 @@ int muon_momentum_norm_static(const void* g, float* m, int rows, int cols, int64
  * Losses at the LM head, with their gradients.  The head is the largest matrix
  * of a model and its logits [tokens, vocab] the largest activation; these calls
  * compute a loss over the whole vocabulary, and the gradients of the hidden
- * states and of the head, in pieces of the vocabulary and without an array of
- * logits: they stay in tensor memory, the workspace holds the bf16 gradient of one
- * piece at a time (and, where it has room, pieces of logits as 16-bit codes, see
- * muon_head_workspace_bytes).  dX goes on into the layers whose matrices muon_step
- * updates, dW to muon_adamw_step (Sec. 2.2: the LM head stays with AdamW).
+ * states and of the head, in pieces of the vocabulary.  No fp32 logits reach memory.
+ * With the least workspace it holds the bf16 gradient of one piece at a time, at most
+ * 256 MiB; with the larger one that muon_head_workspace_bytes recommends for speed
+ * it keeps up to 3 GiB of logits as 16-bit codes for the length of the call (all of
+ * them, in as much as a bf16 array of them takes, up to about 1.5 x 10^9 logits).
+ * Without gradients no logits are kept.  dX goes on into the layers whose matrices
+ * muon_step updates, dW to muon_adamw_step (Sec. 2.2: the LM head stays with AdamW).
  *
  *   l   = logit_scale * x w^T            (distillation: / temperature as well)
  *   lse = log sum_j exp(l_j),  q = exp(l - lse)
@@ -674,8 +676,9 @@ int muon_head_status(const void* workspace, int device, void* stream, int* devic
  * muon_debug_set_head_piece_bytes: bytes of logit gradients of one vocabulary
  * piece (0 restores the default of 256 MiB); tests lower it to run several pieces
  * on small sizes.  muon_debug_set_head_codes: 0 (default) keeps codes of logits
- * where that is faster, 1 never, 2 always; the ways agree to rounding, not bit
- * for bit.  Both return the previous value; a mode outside 0..2 only queries.
+ * where that is faster, 1 never, 2 always; the ways agree to rounding (a code adds
+ * 1.7e-4 relative to q, and what lies 2^-32 or more below the largest of its 64
+ * columns becomes 0), not bit for bit.  Both return the previous value; a mode outside 0..2 only queries.
  */
 size_t muon_debug_set_head_piece_bytes(size_t bytes);
 int muon_debug_set_head_codes(int mode);

@@ -363,7 +363,7 @@ def _head_matrix(t, what, shape, dev):
 
 
 def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace, stream,
-               call):
+               least_workspace, call):
     """Checks, outputs and workspace shared by the head losses; ``call(args,
     workspace address, bytes, device, stream)`` makes the C call."""
     import torch
@@ -405,11 +405,12 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
         if dw is not None:
             a.dw, a.ld_dw, a.dw_dtype, a.dw_accumulate = dw.data_ptr(), _row_stride(dw), _dtype_code(dw), 1 if accumulate_dw else 0
         if workspace is None:
-            key = (tokens, dim, vocab, top, dx is None, dw is None, ld_w & 7, w_ptr & 15)
+            key = (tokens, dim, vocab, top, dx is None, dw is None, ld_w & 7, w_ptr & 15, least_workspace)
             need = _head_bytes.get(key)
             if need is None:
                 out = C.c_size_t(0)
-                _check(lib().muon_head_workspace_bytes(C.byref(a), top, C.byref(out), None))
+                _check(lib().muon_head_workspace_bytes(C.byref(a), top, None if least_workspace else C.byref(out),
+                                                       C.byref(out) if least_workspace else None))
                 if len(_head_bytes) >= 1024:
                     _head_bytes.clear()
                 need = _head_bytes[key] = out.value + 1024
@@ -448,14 +449,18 @@ def muon_debug_set_head_codes(mode: int) -> int:
 
 
 def muon_head_xent(x, w, targets, loss=None, lse=None, total=None, dx=None, dw=None, weight=None, mean=True,
-                   scale=1.0, logit_scale=1.0, z_loss=0.0, accumulate_dw=False, workspace=None, stream=None) -> HeadLoss:
-    """Softmax cross entropy of ``x w^T`` over the vocabulary, with its gradients and
-    without the logits.  ``x`` [tokens, dim] and ``w`` [vocab, dim] are bf16,
-    ``targets`` int64 [tokens] (outside [0, vocab): the token is masked).
+                   scale=1.0, logit_scale=1.0, z_loss=0.0, accumulate_dw=False, workspace=None, stream=None,
+                   least_workspace=False) -> HeadLoss:
+    """Softmax cross entropy of ``x w^T`` over the vocabulary, with its gradients.
+    ``x`` [tokens, dim] and ``w`` [vocab, dim] are bf16, ``targets`` int64 [tokens]
+    (outside [0, vocab): the token is masked).
     ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True to allocate one like x / w,
     None to leave the gradient out.  Other outputs and the workspace are allocated
     unless given; a workspace of :func:`muon_head_workspace_bytes` that is kept can be
-    asked for the call's status.  Argument marshalling only; the formulas are in include/muon.h.
+    asked for the call's status.  By default a workspace with room for up to 3 GiB of
+    logits as 16-bit codes is allocated, for speed; ``least_workspace``: the smallest
+    that does, with one piece of the vocabulary's logits at a time.  Argument
+    marshalling only; the formulas are in include/muon.h.
     Tensors used on another stream than the one they were allocated on are the
     caller's to keep alive (``record_stream``)."""
     import torch
@@ -466,12 +471,12 @@ def muon_head_xent(x, w, targets, loss=None, lse=None, total=None, dx=None, dw=N
         return lib().muon_head_xent(a, targets.data_ptr(), z_loss, ws, nbytes, dev, s)
 
     return _head_call(x, w, 0, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace,
-                      stream, call)
+                      stream, bool(least_workspace), call)
 
 
 def muon_head_distill(x, w, top_ids, top_logits, temperature=1.0, teacher_lse=None, loss=None, lse=None, total=None,
                       dx=None, dw=None, weight=None, mean=True, scale=1.0, logit_scale=1.0, accumulate_dw=False,
-                      workspace=None, stream=None) -> HeadLoss:
+                      workspace=None, stream=None, least_workspace=False) -> HeadLoss:
     """Distillation from a teacher's top logits: ``top_ids`` int64 and ``top_logits``
     bf16 or fp32, both [tokens, top], ``teacher_lse`` fp32 [tokens] or None.
     Everything else as :func:`muon_head_xent`."""
@@ -496,7 +501,7 @@ def muon_head_distill(x, w, top_ids, top_logits, temperature=1.0, teacher_lse=No
         return lib().muon_head_distill(a, C.byref(t), ws, nbytes, dev, s)
 
     return _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_scale, accumulate_dw, workspace,
-                      stream, call)
+                      stream, bool(least_workspace), call)
 
 
 def muon_head_status(workspace, stream=None) -> int:

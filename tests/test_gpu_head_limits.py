@@ -102,3 +102,35 @@ def test_many_tiles_a_pair_give_the_same_bits(T, D, V):
         again = b.muon_head_xent(x, w, t, dx=True, dw=True)
         for k in ("loss", "lse", "total", "dx", "dw"):
             assert torch.equal(getattr(first, k), getattr(again, k)), k
+
+
+@pytest.mark.parametrize("top", [0, 20])
+def test_least_workspace(knobs, top):  # noqa: F811
+    """The argument takes the smallest workspace and changes nothing but its size and,
+    to rounding, how the gradient of the logits is formed."""
+    b = knobs
+    T, D, V = 600, 512, 4000
+    x, w, gen = make(T, D, V, 91)
+    b.muon_debug_set_head_piece_bytes(T * 256 * 2 * 2)  # eight pieces
+    if top:
+        ids = torch.stack([torch.randperm(V, generator=gen)[:top] for _ in range(T)])
+        z = torch.randn(T, top, generator=gen)
+        rows = ho.teacher_rows(ids.numpy(), f64(z), V, 1.0)
+        ids, z = ids.cuda(), z.cuda()
+    else:
+        t = torch.randint(0, V, (T,), generator=gen)
+        rows = ho.target_rows(t.numpy(), V)
+        t = t.cuda()
+    ref = ho.head_loss(f64(x), f64(w), rows)
+    for least in (False, True):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        r = (b.muon_head_distill(x, w, ids, z, dx=True, dw=True, least_workspace=least) if top else
+             b.muon_head_xent(x, w, t, dx=True, dw=True, least_workspace=least))
+        peak = torch.cuda.max_memory_allocated() - before
+        outputs = 2 * (T + V) * D + 8 * T + 4
+        need = b.muon_head_workspace_bytes(T, D, V, top=top, least=least)
+        assert need <= peak <= need + outputs + 4096
+        check(r, ref, f64(x), f64(w), rows, 1.0, BF, BF, coefficients(ref["counts"], None, True, 1.0, 0.0))

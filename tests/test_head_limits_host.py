@@ -51,3 +51,20 @@ def test_sizes_past_32_bits_are_refused(size):
         with pytest.raises(b.MuonError) as e:
             b.muon_head_xent(x, w, torch.empty(args["tokens"], dtype=torch.int64, device="meta"), dx=True, dw=True)
         assert e.value.code == b.MUON_ERR_UNSUPPORTED
+
+
+def test_workspace_against_an_array_of_logits():
+    """What the header says of both sizes: the recommended one may hold every logit as 16
+    bits, the least one a piece of 256 MiB; without gradients no logits at all."""
+    from paper_2502_16982_b200 import binding as b
+
+    for T in (1024, 4096, 8192, 65536):
+        logits = T * 163840 * 2
+        stats, rest = logits // 16, T * (2 * 2048 + 64) + (1 << 20)  # a copy of x, words per token
+        part = T * 2048 * 4
+        full, least, forward = (b.muon_head_workspace_bytes(T, 2048, 163840, **k)
+                                for k in ({}, dict(least=True), dict(dx=False, dw=False)))
+        assert least <= stats + rest + max(256 << 20, part) + (256 << 20)
+        assert full <= min(logits, 3 << 30) + stats + rest + max(256 << 20, part)
+        assert forward <= stats + rest
+        assert full >= min(logits, (3 << 30) - (256 << 20) - stats)
