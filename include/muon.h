@@ -601,11 +601,18 @@ typedef struct muon_head_args {
  * Bytes of DEVICE workspace (1024-byte aligned) of one call: pure host computation
  * on the sizes, the types, the alignment and stride of w, and which of dx and dw
  * are wanted.  top: teacher entries per token, 0 for cross entropy.
- *   *least_bytes: what the call cannot do without (either pointer may be NULL): a
- *       copy of x, the gradient of the logits of one piece of the vocabulary (at
- *       most 256 MiB, or 256 vocabulary entries if that is more), partial sums of dX
- *       (at most 256 MiB, or one fp32 dX) and the softmax statistics, one byte for
- *       eight logits.
+ *   *least_bytes: what the call cannot do without (either pointer may be NULL), every
+ *       array rounded up to 1024 bytes:
+ *         a copy of x, its rows rounded up to 8 columns;
+ *         the softmax statistics, 32 bytes for 256 columns of a token;
+ *         16 bytes per token and 12 per sparse entry; distillation: 9 more per token,
+ *           4 more per entry, and one byte per token and 256 columns;
+ *         where w is not 16-byte aligned or ld_w not a multiple of 8: a copy of w, its
+ *           rows rounded up to 8 columns;
+ *         with dx or dw: the bf16 gradient of the logits of one piece of the vocabulary,
+ *           at most 256 MiB, or 256 vocabulary entries if that is more;
+ *         with dx: 1 to 64 partial sums of dX in fp32, at most 256 MiB, or one - these
+ *           take no room where the statistics are as large, whose place they then use.
  *   *out_bytes: with up to 3 GiB more the call keeps the logits of as many pieces
  *       as 16-bit codes between the pass that forms the softmax sums and the one
  *       that forms the gradients, instead of computing them twice (a quarter of

@@ -68,3 +68,37 @@ def test_workspace_against_an_array_of_logits():
         assert full <= min(logits, 3 << 30) + stats + rest + max(256 << 20, part)
         assert forward <= stats + rest
         assert full >= min(logits, (3 << 30) - (256 << 20) - stats)
+
+
+@pytest.mark.parametrize("tokens,dim,vocab,top,packed,dx,dw", [
+    (8192, 2048, 163840, 0, True, True, True), (333, 203, 5003, 0, False, True, True), (4096, 2048, 163840, 64, True, True, True),
+    (1000, 64, 30000, 0, True, True, False), (2000, 1024, 20000, 33, False, False, True), (100, 2048, 163840, 0, False, True, True),
+    (300, 2560, 1000, 5, True, True, True), (4096, 2048, 163840, 0, True, False, False), (70000, 64, 5000, 8, True, False, False),
+])
+def test_least_workspace_is_the_sum_that_the_header_gives(tokens, dim, vocab, top, packed, dx, dw):
+    from paper_2502_16982_b200 import binding as b
+
+    def up(v, to):
+        return (v + to - 1) // to * to
+
+    entries, tiles, rows = tokens * max(top, 1), up(vocab, 256) // 256, up(dim, 8)
+    stats = up(tokens * tiles * 32, 1024)
+    least = up(tokens * rows * 2, 1024) + stats + tokens * 16 + entries * 12
+    if top:
+        least += tokens * (9 + tiles + 1) + entries * 4
+    if not packed:
+        least += up(vocab * rows * 2, 1024)
+    got = b.muon_head_workspace_bytes(tokens, dim, vocab, top=top, dx=dx, dw=dw, packed_head=packed, least=True)
+    slack = 16 * 1024 + tokens // 64  # arrays rounded up, the control block, tokens counted in runs
+    if not (dx or dw):
+        assert least <= got <= least + slack
+        return
+    # a piece: whole tiles, spread evenly over the pieces, so between half of the most and the most
+    most = max((256 << 20) // (tokens * 512), 1)
+    pieces = -(-tiles // min(most, tiles))
+    least += tokens * 512 * -(-tiles // pieces)
+    part = tokens * rows * 4
+    upto = max(256 << 20, part) if dx and stats < max(256 << 20, part) else 0
+    assert least <= got <= least + slack + upto
+    if dx and stats < part:
+        assert got >= least + part
