@@ -15,6 +15,7 @@ constexpr int kTileN = 256;   // widest output tile
 constexpr int kStatN = 64;    // vocabulary columns of one statistics entry: what an epilogue thread holds of a row
 constexpr int kUnits = kTileN / kStatN;
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
+constexpr int kTileCost = 6;  // K blocks that a tile's epilogue and start are worth, to the plan and to the dealing of tiles
 constexpr int kFusedRows = 296;  // fewer tokens than this count as few
 constexpr int kManyTokens = 16384;    // from here on the tokens that count are counted in runs of 256 first
 constexpr int kInPlaceRows = 256;     // most tokens whose rows are not gathered

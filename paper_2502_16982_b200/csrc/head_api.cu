@@ -61,7 +61,6 @@ struct Plan {
 // so that all pairs should read - and `split_cost` for each partial sum that is joined.
 // Measured at 1024 x 2560 x 65536 (1 split chosen): 769 us with 1, 799 with 2, 837
 // with 4; at 1 x 512 x 8192: 39 us with 8, 35 with 16 and with 32.
-constexpr int kTileCost = 6;
 int choose_splits(int m_tiles, int n_tiles, int dx_kb, long long dw_tiles, int dw_kb, int pairs, int most, double split_cost) {
   const long long dx_tiles = static_cast<long long>(m_tiles) * n_tiles;
   const double wait = m_tiles == 1 ? 3.0 : 1.25;

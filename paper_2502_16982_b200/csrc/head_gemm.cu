@@ -1,8 +1,9 @@
 // Products of the LM-head losses for sm_100a.  With hidden states x [T, D], head
 // w [V, D], logits l = a x w^T, q = softmax(l) and a sparse target distribution p:
 //
-//   statistics  max and sum of exponentials of every token over every 256
-//               columns of l, and l at the sparse entries (logits stay in TMEM)
+//   statistics  max and sum of exponentials of every token over every 64 columns
+//               of l, l at the sparse entries and, where they are kept, l as 16-bit
+//               codes (head_codes.cuh)
 //   gradient    G = g a (c q - p) for one piece of the vocabulary, in bf16
 //   outputs     dX += G w(piece)  and  dW(piece) = G^T x, one launch
 //
@@ -171,8 +172,6 @@ struct Tile {
 // in turn.  Where that leaves some pairs with one more than others, product 1's go
 // to the others first, `extra` each - dX has few long tiles, dW many short ones -
 // and then to all in turn.
-constexpr int kTileCost = 6;  // K blocks that a tile's epilogue and start are worth
-
 struct Deal {
   int pairs, pair;
   int mine0;  // this pair's tiles of product 0
@@ -520,7 +519,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
       constexpr uint32_t kLboK = (16u >> 4) << 16;
       constexpr uint32_t kLboMN = (8192u >> 4) << 16;  // next 64-element chunk of an MN-major operand
       Tile tl;
-    for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
+      for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
         if (tl.kb0 == tl.kb1) continue;  // no token counts: the epilogue writes zeros by itself
         const Product& pr = P.prod[tl.prod];
         const bool a_mn = pr.a_mn != 0, b_mn = pr.b_mn != 0;
