@@ -16,10 +16,15 @@ constexpr int kStatN = 64;    // vocabulary columns of one statistics entry: wha
 constexpr int kUnits = kTileN / kStatN;
 constexpr int kBK = 64;       // K elements per pipeline stage (128 bytes of bf16)
 constexpr int kTileCost = 6;  // K blocks that a tile's epilogue and start are worth, to the plan and to the dealing of tiles
-constexpr int kFusedRows = 296;  // fewer tokens than this count as few
+// Fewer tokens than this are finalised by several blocks a row, whose conversion spreads
+// over the device: two a SM, and more than are ever left in place.  (Whole calls, us, with
+// and without: 90 and 100 for 290 x 512 x 50000, 256 and 271 for 290 x 1024 x 100000; 131
+// and 130 for 400 x 2048 x 20000, 133 and 131 for 600 x 512 x 50000.)
+constexpr int kFusedRows = 296;
 constexpr int kManyTokens = 16384;    // from here on the tokens that count are counted in runs of 256 first
 constexpr int kInPlaceRows = 256;     // most tokens whose rows are not gathered
 constexpr int kInPlaceEntries = 4096; // and most of a teacher's entries in all
+static_assert(kInPlaceRows < kFusedRows, "rows in place are converted by the finalisation of few tokens");
 constexpr long long kHeadInCache = 96ll << 20;   // bytes of w that do, between its two readings
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
