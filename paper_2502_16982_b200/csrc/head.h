@@ -21,9 +21,16 @@ constexpr int kTileCost = 6;  // K blocks that a tile's epilogue and start are w
 // and without: 90 and 100 for 290 x 512 x 50000, 256 and 271 for 290 x 1024 x 100000; 131
 // and 130 for 400 x 2048 x 20000, 133 and 131 for 600 x 512 x 50000.)
 constexpr int kFusedRows = 296;
-constexpr int kManyTokens = 16384;    // from here on the tokens that count are counted in runs of 256 first
-constexpr int kInPlaceRows = 256;     // most tokens whose rows are not gathered
-constexpr int kInPlaceEntries = 4096; // and most of a teacher's entries in all
+// From here on the tokens that count are counted in runs of 256 first, a launch more.  (Whole
+// calls, us, with and without, x 64 x 2000: 30.7 and 30.9 for 1000 tokens, 146 and 169 for
+// 16384, 533 and 878 for 65536.)
+constexpr int kManyTokens = 16384;
+// Most tokens whose rows are not gathered (one thread of a block looks at each), and most of
+// a teacher's entries in all: every block looks at all of them.  (Whole calls, us, in place
+// and gathered, x 256 x 4096: 24.6 and 32.7 for 20 tokens with 16 entries, 41.0 and 40.9 for
+// 100 with 32, 54 and 49 for 100 with 64, 92 and 68 for 250 with 128.)
+constexpr int kInPlaceRows = 256;
+constexpr int kInPlaceEntries = 4096;
 static_assert(kInPlaceRows < kFusedRows, "rows in place are converted by the finalisation of few tokens");
 constexpr long long kHeadInCache = 96ll << 20;   // bytes of w that do, between its two readings
 constexpr int kMaxTop = 128;  // sparse target entries of one token
