@@ -342,9 +342,8 @@ def _raw_stream(stream, dev):
     return get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
-def _head_sizes(*sizes):
-    if min(sizes) < -1 << 31 or max(sizes) >= 1 << 31:  # ctypes would keep the low 32 bits
-        raise MuonError(MUON_ERR_UNSUPPORTED, "a size past 32 bits")
+def _past_32_bits():
+    raise MuonError(MUON_ERR_UNSUPPORTED, "a size past 32 bits")  # ctypes would keep its low 32 bits
 
 
 def _head_vector(t, what, n, dev):
@@ -370,7 +369,8 @@ def _head_call(x, w, top, loss, lse, total, dx, dw, weight, mean, scale, logit_s
     if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.shape[1] < 1 or w.shape[0] < 1:
         raise MuonError(MUON_ERR_INVALID_ARG, "x must be [tokens, dim] and w [vocab, dim]")
     (tokens, dim), vocab = x.shape, w.shape[0]
-    _head_sizes(tokens, dim, vocab, top)
+    if (tokens | dim | vocab | top) >> 31:
+        _past_32_bits()
     dev = x.device
     if dev.type != "cuda" or w.device != dev:
         raise MuonError(MUON_ERR_INVALID_ARG, "x and w must be on one CUDA device")
@@ -429,7 +429,8 @@ def muon_head_workspace_bytes(tokens: int, dim: int, vocab: int, top: int = 0, d
     for cross entropy), 1024 for aligning a tensor's start included.  ``least``: the
     smallest workspace a call accepts instead of the one it makes full use of.
     ``packed_head``: the head's rows are 16-byte aligned."""
-    _head_sizes(tokens, dim, vocab, top)
+    if any(C.c_int32(v).value != v for v in (tokens, dim, vocab, top)):
+        _past_32_bits()
     ld = (dim + 7) // 8 * 8 if packed_head else dim | 1
     a = muon_head_args(tokens, dim, vocab, 1, None, None, dim, ld, MUON_DTYPE_BF16, MUON_DTYPE_BF16)
     a.dx, a.dw = (1024 if dx else None), (1024 if dw else None)  # only whether they are there counts

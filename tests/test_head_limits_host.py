@@ -37,7 +37,8 @@ def test_scales_that_it_can_are_not(logit_scale, temperature):
     assert _call(b, logit_scale, temperature) == b.MUON_ERR_WORKSPACE
 
 
-@pytest.mark.parametrize("size", [dict(tokens=(1 << 32) + 4), dict(dim=(1 << 32) + 64), dict(vocab=(1 << 32) + 100), dict(top=(1 << 32) + 1)])
+@pytest.mark.parametrize("size", [dict(tokens=(1 << 32) + 4), dict(dim=(1 << 32) + 64), dict(vocab=(1 << 32) + 100), dict(top=(1 << 32) + 1),
+                                  dict(tokens=-(1 << 32) + 4)])
 def test_sizes_past_32_bits_are_refused(size):
     """They must not be cut to their low 32 bits on the way into the library."""
     from paper_2502_16982_b200 import binding as b
@@ -46,7 +47,7 @@ def test_sizes_past_32_bits_are_refused(size):
     with pytest.raises(b.MuonError) as e:
         b.muon_head_workspace_bytes(**args)
     assert e.value.code == b.MUON_ERR_UNSUPPORTED
-    if "top" not in size:
+    if "top" not in size and args["tokens"] > 0:
         x, w = (torch.empty(n, args["dim"], dtype=torch.bfloat16, device="meta") for n in (args["tokens"], args["vocab"]))
         with pytest.raises(b.MuonError) as e:
             b.muon_head_xent(x, w, torch.empty(args["tokens"], dtype=torch.int64, device="meta"), dx=True, dw=True)
