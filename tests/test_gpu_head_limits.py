@@ -127,10 +127,11 @@ def test_least_workspace(knobs, top):  # noqa: F811
         torch.cuda.synchronize()
         torch.cuda.empty_cache()
         torch.cuda.reset_peak_memory_stats()
-        before = torch.cuda.memory_allocated()
+        before = torch.cuda.memory_stats()["requested_bytes.all.current"]
         r = (b.muon_head_distill(x, w, ids, z, dx=True, dw=True, least_workspace=least) if top else
              b.muon_head_xent(x, w, t, dx=True, dw=True, least_workspace=least))
-        peak = torch.cuda.max_memory_allocated() - before
+        # what was asked for: the allocator's blocks may be larger, as its history has it
+        peak = torch.cuda.memory_stats()["requested_bytes.all.peak"] - before
         outputs = 2 * (T + V) * D + 8 * T + 4
         need = b.muon_head_workspace_bytes(T, D, V, top=top, least=least)
         assert need <= peak <= need + outputs + 4096
