@@ -534,12 +534,14 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;
       O.part_add = i > 0;
-      // One row tile of half a CTA pair or less, its products out of L2 (whole calls, us,
-      // with the four warps more against without, x 512 x 50000): 51.1 and 53.2 for 10
-      // tokens, 56.9 and 58.2 for 60, 62.1 and 63.3 for 128, 65.9 and 65.8 for 150, 72.3 and
-      // 71.5 for 200, 109.6 and 107.1 for 400; 24.8 and 26.6 for 1 x 512 x 8192.  With w out of
-      // memory 217 and 210 for 250 x 1024 x 100000.
-      O.spare = P.n_pieces == 1 && P.tokens <= kTileM / 2 && 2ll * P.vocab * P.dim <= kHeadInCache;
+      // Four epilogue warps more (whole calls, us, with and without).  Where dW leaves element
+      // by element: 37 and 42 for 333 x 203 x 5003, 86 and 90 for 4000 tokens of it, 212 and
+      // 288 for 100 x 2047 x 20000, 296 and 379 for 1000 tokens of it.  Else for one row tile of
+      // half a CTA pair or less with its products out of L2, x 512 x 50000: 51.1 and 53.2 for
+      // 10 tokens, 56.9 and 58.2 for 60, 62.1 and 63.3 for 128, 65.9 and 65.8 for 150, 72.3
+      // and 71.5 for 200, 109.6 and 107.1 for 400; 24.8 and 26.6 for 1 x 512 x 8192.  With w
+      // out of memory 217 and 210 for 250 x 1024 x 100000.
+      O.spare = P.n_pieces == 1 && ((P.want_dw && !O.dw_tma) || (P.tokens <= kTileM / 2 && 2ll * P.vocab * P.dim <= kHeadInCache));
       O.row_l = R.row_l;
       O.total = i == 0 ? a->total : nullptr;
       O.prod[1].m_tiles = tiles;
