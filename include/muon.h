@@ -549,8 +549,9 @@ int muon_momentum_norm_static(const void* g, float* m, int rows, int cols, int64
  *
  * Arithmetic: products of bf16 operands with fp32 sums; softmax statistics, losses
  * and sums in fp32; the gradient of the logits is rounded to bf16 once, as an
- * operand of the products that form dX and dW, those are summed in fp32 and
- * rounded once where the output is bf16.  Results are the same bits from call to
+ * operand of the products that form dX and dW (without the factor that all tokens
+ * share, scale, mean and logit_scale, which is multiplied into the sums), those are
+ * summed in fp32 and rounded once where the output is bf16.  Results are the same bits from call to
  * call with the same workspace size.  Exponents are fp32 numbers, l log2(e): from
  * magnitudes of 2^24 on they have no fraction, and from 2^28 on a loss or gradient may
  * come out as NaN or lose its largest term.

@@ -42,6 +42,7 @@ struct Ctrl {
   int n_valid;     // tokens that count
   unsigned ticket; // blocks of the finalisation that are done
   float coef;      // scale, divided by the sum of the weights where a mean is asked for
+  float rest;      // what dX and dW are still to be multiplied with, see finalise_kernel
 };
 
 // One product of a launch: D[m][n] = sum_k A[m][k] B[n][k].

@@ -5,7 +5,9 @@
 //               of l, l at the sparse entries and, where they are kept, l as 16-bit
 //               codes (head_codes.cuh)
 //   gradient    G = g a (c q - p) for one piece of the vocabulary, in bf16
-//   outputs     dX += G w(piece)  and  dW(piece) = G^T x, one launch
+//   outputs     dX += G w(piece)  and  dW(piece) = G^T x, one launch; G lacks a factor
+//               near 1 that all tokens share (Ctrl::rest), dW is given it here and dX
+//               where its partial sums are joined
 //
 // One persistent, warp-specialised kernel on CTA pairs (tcgen05.mma
 // cta_group::2, M = 256, N = 128 or 256), three instantiations by epilogue.
@@ -753,6 +755,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
       int acc = 0;
       uint32_t acc_phase = 0;
       int turn = 0;  // staging buffer last used
+      const float rest = *reinterpret_cast<volatile float*>(&P.ctrl->rest);
       Tile tl;
       for (int k = 0; ok && locate(P, s0, s1, deal, k, tl); ++k) {
         const int row0 = tl.mi * kTileM + static_cast<int>(rank) * 128 + q * 32;
@@ -786,6 +789,8 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
             ptx::tma_store_commit();
           }
         };
+        const float factor = is_dx ? 1.0f : rest;
+        auto scaled = [&](uint32_t v) { return __uint_as_float(v) * factor; };
         auto load = [&](uint32_t (&v)[32], int c) {
           if (have_acc) {
             ptx::tmem_ld_32x32(taddr + c, v);
@@ -805,6 +810,8 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
             ptx::tmem_ld_wait();
             const uint32_t buf = next_buffer();
 #pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(scaled(v[i]));
+#pragma unroll
             for (int i = 0; i < 8; ++i) sts128(staged(buf, lane, i), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             send(buf, map, c0 + c, y, z, add);
           }
@@ -821,8 +828,8 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
               uint32_t w[4], z[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                w[e] = pack2(__uint_as_float(v[8 * i + 2 * e]), __uint_as_float(v[8 * i + 2 * e + 1]));
-                z[e] = pack2(__uint_as_float(u[8 * i + 2 * e]), __uint_as_float(u[8 * i + 2 * e + 1]));
+                w[e] = pack2(scaled(v[8 * i + 2 * e]), scaled(v[8 * i + 2 * e + 1]));
+                z[e] = pack2(scaled(u[8 * i + 2 * e]), scaled(u[8 * i + 2 * e + 1]));
               }
               sts128(staged(buf, lane, i), w[0], w[1], w[2], w[3]);
               sts128(staged(buf, lane, i + 4), z[0], z[1], z[2], z[3]);
@@ -841,7 +848,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              sts32(buf0 + 4u * (lane * 32 + (i ^ lane)), v[i]);
+              sts32(buf0 + 4u * (lane * 32 + (i ^ lane)), __float_as_uint(scaled(v[i])));
             __syncwarp();
             const int rows = min(32, P.dw_rows - row0);
             if (c + lane < limit) {

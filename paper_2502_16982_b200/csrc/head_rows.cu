@@ -297,11 +297,24 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
   return warp_sum(a + b);
 }
 
+// v as power of two times a fraction in [1, 2); 0, subnormal, infinite and NaN stay as they
+// are, with fraction 1.
+__device__ __forceinline__ float fraction_of(float v, float& power) {
+  const uint32_t bits = __float_as_uint(v), exponent = bits & 0x7F800000u;
+  const bool normal = exponent != 0u && exponent != 0x7F800000u;
+  power = normal ? __uint_as_float(bits & 0xFF800000u) : v;
+  return normal ? __uint_as_float((bits & 0x007FFFFFu) | 0x3F800000u) : 1.0f;
+}
+
 // Joins a token's statistics over the vocabulary and forms, with l the scaled
 // logits, lse their log-sum-exp, p the sparse target distribution, c = sum p:
 //   loss = sum p log p - sum p (l - lse) + z_loss lse^2
 //   gradient of the raw logit: g a (c' q - p),  c' = c + 2 z_loss lse
-// row_q holds (g a c', log2-domain lse), entry_g the gradient at the entries.
+// row_q holds (g a c', log2-domain lse), entry_g the gradient at the entries, both
+// without the fraction of the factor that all tokens share, coef * logit_scale: in the
+// bf16 gradients of logits that fraction would be rounded with every -g a (1 - q) of a
+// q near 0 in the same way, and all of dX and dW come out up to 2^-9 too large or too
+// small.  The sums of dX and dW are multiplied with it in fp32 (Ctrl::rest).
 // Exponents are taken from one fused multiply-add on the raw logit, so that a
 // large logit costs a single rounding.
 //
@@ -466,6 +479,9 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
   }
   const int n_valid = kInPlace ? R.tokens : R.ctrl->n_valid;
   if (!kInPlace) coef = R.ctrl->coef;
+  float power;
+  const float rest = fraction_of(coef * R.logit_scale, power);
+  if (row == 0 && writes && tid == 0) R.ctrl->rest = rest;
   if (row < n_valid && counted) {
     if (tid < K) {
       if (!kInPlace) {
@@ -503,8 +519,8 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
       }
     const float lse2 = base + log2f(s);
     const float lse = lse2 * kLn2;
-    const float g = coef * (R.weight != nullptr ? R.weight[t] : 1.0f);
-    const float ga = g * R.logit_scale;
+    const float weight = R.weight != nullptr ? R.weight[t] : 1.0f;
+    const float g = coef * weight, ga = weight * power;
     const float cq = row_c + 2.0f * R.z_loss * lse;
     float ce = 0.f;
     if (tid < K && s_id[tid] != kNoId) {
@@ -589,10 +605,13 @@ __global__ void __launch_bounds__(kRowThreads) dx_kernel(const RowParams R) {
       v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
     }
   }
+  const float rest = R.ctrl->rest;
 #pragma unroll
   for (int o = kGroups; o < 32; o <<= 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += __shfl_xor_sync(0xFFFFFFFFu, v[e], o);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= rest;
   if (!mine || way != 0) return;
   if (t < 0) {  // a masked token among rows that are tokens: 0 whatever w holds
     t = row;

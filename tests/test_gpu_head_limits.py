@@ -291,3 +291,44 @@ def test_sizes_that_take_several_pieces(T, D, V, top, masked, z_loss):
     ref = head_loss64(x, w, ids.clamp(min=0).cuda(), p.cuda(), g, 1.0, z_loss)
     assert not r.dx[hide.cuda()].any()
     check64(r, ref, V, T, g, z_loss)
+
+
+@pytest.mark.parametrize("T,masked,opts", [
+    (40, 0, {}), (230, 1, {}), (367, 0, {}), (367, 2, dict(scale=0.37, mean=False)), (367, 0, dict(logit_scale=0.6, scale=-1.0)),
+    (1500, 30, {}), (367, 0, dict(distill=True)), (40, 0, dict(distill=True)),
+])
+@pytest.mark.parametrize("codes", [1, 2])
+def test_the_tokens_common_coefficient_is_not_rounded(knobs, codes, T, masked, opts):  # noqa: F811
+    """1 / tokens, scale and logit_scale are the same for every token.  Rounded to bf16 with
+    each gradient of a logit they would make all of dX and dW too large or too small,
+    by up to 2^-8.
+
+    The factor by which an output is too large is its projection on the oracle's, less 1.
+    The logits here are small and the vocabulary is large, q = 2^-14 on average: the
+    entries of a target distribution make up the gradient, and for cross entropy (p = 1)
+    what they lose is the rounding of 1 - q to 1, 2^-14 on average.  Distillation: of
+    p over four equal entries 1/4 - q, that is 2^-12.  The q's, rounded
+    independently, add less than 2^-8 / sqrt(T V) of a norm that is itself a small part;
+    outputs are fp32.  2^-11 in all."""
+    b = knobs
+    b.muon_debug_set_head_codes(codes)
+    o = dict(opts)
+    V, D = 20000, 64
+    x, w, gen = make(T, D, V, 121 + T, gain=0.5)
+    hide = torch.arange(T) < masked
+    dx, dw = torch.empty(T, D, device="cuda"), torch.empty(V, D, device="cuda")
+    if o.pop("distill", False):
+        ids = (torch.randint(0, V, (T, 1), generator=gen) + torch.arange(4) * (V // 4)) % V
+        ids[hide] = -1
+        z = torch.zeros(T, 4)
+        r = b.muon_head_distill(x, w, ids.cuda(), z.cuda(), dx=dx, dw=dw, **o)
+        rows = ho.teacher_rows(ids.numpy(), f64(z), V, 1.0)
+    else:
+        t = torch.randint(0, V, (T,), generator=gen)
+        t[hide] = -100
+        r = b.muon_head_xent(x, w, t.cuda(), dx=dx, dw=dw, **o)
+        rows = ho.target_rows(t.numpy(), V)
+    ref = ho.head_loss(f64(x), f64(w), rows, **o)
+    for name in ("dx", "dw"):
+        factor = float((f64(getattr(r, name)) * ref[name]).sum() / (ref[name] ** 2).sum())
+        assert abs(factor - 1) <= 2.0 ** -11, (name, factor - 1)
