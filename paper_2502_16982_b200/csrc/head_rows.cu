@@ -313,7 +313,7 @@ __device__ __forceinline__ float fraction_of(float v, float& power) {
 // row_q holds (g a c', log2-domain lse), entry_g the gradient at the entries, both
 // without the fraction of the factor that all tokens share, coef * logit_scale: in the
 // bf16 gradients of logits that fraction would be rounded with every -g a (1 - q) of a
-// q near 0 in the same way, and all of dX and dW come out up to 2^-9 too large or too
+// q near 0 in the same way, and all of dX and dW come out up to 2^-8 too large or too
 // small.  The sums of dX and dW are multiplied with it in fp32 (Ctrl::rest).
 // Exponents are taken from one fused multiply-add on the raw logit, so that a
 // large logit costs a single rounding.
