@@ -147,6 +147,10 @@ def prepare(case, seed):
             s["v_flat"], s["v"] = _flat(sizes, torch.float32, lambda i, n: (rand(n) + 0.1) * _STD**2)
         else:
             s["out_flat"], s["out"] = _flat(sizes, torch.float32 if case["out_fp32"] else torch.bfloat16)
+        if own:  # the handle that a program keeps beside its gradients
+            from paper_2502_16982_b200 import binding
+
+            s["handle"] = binding.MuonGrads(s["grads"], out=s.get("out"))
         return s
 
     T, V = case["tokens"], case["vocab"]
@@ -183,9 +187,9 @@ def run(s):
 
     if c["op"] == "clip":
         if not c["adamw"]:
-            r = binding.muon_clip_grads(s["grads"], s["max_norm"], eps=_NORM_EPS, out=s["out"])
+            r = s["handle"].muon_clip_grads(s["max_norm"], eps=_NORM_EPS)
             return {"norm": r.norm, "coef": r.coef, "grads": s["out_flat"]}
-        r = binding.muon_grad_norm(s["grads"], max_norm=s["max_norm"], eps=_NORM_EPS)
+        r = s["handle"].muon_grad_norm(s["max_norm"], eps=_NORM_EPS)
         binding.muon_adamw_step(s["params"], s["grads"], s["m"], s["v"], _STEP, coef=r.coef, **_HYPER)
         return {"norm": r.norm, "coef": r.coef, "params": s["params_flat"], "m": s["m_flat"], "v": s["v_flat"]}
     if c["op"] == "head":
