@@ -478,6 +478,61 @@ int muon_adamw_step(const muon_adamw_tensor* tensors, int n_tensors, const muon_
                     int device, void* stream);
 
 /*
+ * Global gradient norm over many tensors, and clipping by it, before muon_step and
+ * muon_adamw_step (the paper has no formula for it; this is the usual one):
+ *
+ *   sum_sq = sum over tensors and elements of g^2,   norm = sqrt(sum_sq)
+ *   coef   = min(1, max_norm / (norm + eps)),         out = coef * g
+ *
+ * `tensors` is a HOST array of descriptors with DEVICE pointers: `numel` elements each
+ * (0 is allowed), any shape, contiguous, bf16 or fp32, at any address aligned to the
+ * element.  `out` NULL or equal to `g`: in place.  Otherwise out, of its own dtype, does
+ * not overlap any g.  A tensor listed twice counts twice for the norm, and must not be
+ * listed twice where it is scaled.
+ *
+ * muon_grad_norm reads every gradient once and writes what is not NULL of sum_sq (one
+ * fp64), norm and coef (one fp32 each).  Squares are added in fp32 at most 64 at a time
+ * and in fp64 above that; the result is exact to fp32 for elements of any magnitude and
+ * the same bits from call to call.  An element that is not finite makes sum_sq and norm
+ * infinite or NaN.
+ *
+ * muon_clip_grads takes the coefficient from sum_sq, so that data-parallel ranks which
+ * hold different tensors can add theirs before it (Sec. 2.3).  Where coef is 1, tensors
+ * in place are not touched; a `coef` below 1 multiplies in fp32 and rounds once.  A norm
+ * that is not finite clips nothing: coef is then written as NaN and out holds g, so that
+ * muon_status finds the matrix and muon_adamw_step_clipped skips the step.  With
+ * n_tensors = 0 it only writes norm and coef.
+ *
+ * max_norm: 0 to infinity (infinity: never clipped).  Both are asynchronous on `stream`,
+ * allocate nothing and may be captured into a CUDA graph (the pointers are then those of
+ * the capture).  workspace: DEVICE, MUON_GRAD_NORM_WORKSPACE_BYTES, 8-byte aligned, not
+ * shared by calls that can overlap on the GPU.
+ */
+#define MUON_GRAD_NORM_WORKSPACE_BYTES 16384
+typedef struct muon_grad_tensor {
+  const void* g;
+  void* out;
+  int64_t numel;
+  int32_t g_dtype;
+  int32_t out_dtype;
+} muon_grad_tensor;
+
+int muon_grad_norm(const muon_grad_tensor* tensors, int n_tensors, float max_norm, float eps, double* sum_sq,
+                   float* norm, float* coef, void* workspace, size_t workspace_bytes, int device, void* stream);
+
+int muon_clip_grads(const muon_grad_tensor* tensors, int n_tensors, const double* sum_sq, float max_norm, float eps,
+                    float* norm, float* coef, int device, void* stream);
+
+/*
+ * muon_adamw_step with every gradient multiplied by *coef (DEVICE, one fp32, read when the
+ * step runs) as it is read: the clipped step without a pass that only scales.  The product
+ * is not rounded to the gradient's dtype.  Where *coef is NaN - the gradient norm was not
+ * finite - p, m and v stay as they are.
+ */
+int muon_adamw_step_clipped(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp,
+                            const float* coef, int device, void* stream);
+
+/*
  * Momentum update and Frobenius norm of ONE matrix with no workspace and no
  * allocation of any kind (the paper has no counterpart; this is a library
  * convenience, not a step of its method):

@@ -37,11 +37,12 @@ EXPORTED = [
     "muon_debug_keep", "muon_debug_read", "muon_debug_set_chunk_bytes", "muon_debug_set_pair_fold", "muon_debug_set_tile_mode",
     "muon_debug_wait_expiry",
     "muon_profile_enable", "muon_profile_read", "muon_debug_tmem_bases",
-    "muon_momentum_norm_static", "muon_adamw_step",
+    "muon_momentum_norm_static", "muon_adamw_step", "muon_adamw_step_clipped", "muon_grad_norm", "muon_clip_grads",
     "muon_head_workspace_bytes", "muon_head_xent", "muon_head_distill", "muon_head_status",
     "muon_debug_set_head_piece_bytes", "muon_debug_set_head_codes",
 ]
 MUON_STATIC_MAX_TILES = 65536
+MUON_GRAD_NORM_WORKSPACE_BYTES = 16384
 KERNEL_KINDS = ["momentum", "norm", "gram", "poly", "comb", "update"]
 
 
@@ -74,6 +75,11 @@ class muon_adamw_tensor(C.Structure):
 class muon_adamw_hparams(C.Structure):
     _fields_ = [("lr", C.c_float), ("wd", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
                 ("eps", C.c_float), ("step", C.c_int32)]
+
+
+class muon_grad_tensor(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("numel", C.c_int64), ("g_dtype", C.c_int32),
+                ("out_dtype", C.c_int32)]
 
 
 class muon_head_args(C.Structure):
@@ -147,6 +153,12 @@ def lib():
     L.muon_debug_wait_expiry.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_uint]
     L.muon_adamw_step.argtypes = [C.POINTER(muon_adamw_tensor), C.c_int, C.POINTER(muon_adamw_hparams), C.c_int,
                                   C.c_void_p]
+    L.muon_adamw_step_clipped.argtypes = [C.POINTER(muon_adamw_tensor), C.c_int, C.POINTER(muon_adamw_hparams), C.c_void_p,
+                                          C.c_int, C.c_void_p]
+    L.muon_grad_norm.argtypes = [C.POINTER(muon_grad_tensor), C.c_int, C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]
+    L.muon_clip_grads.argtypes = [C.POINTER(muon_grad_tensor), C.c_int, C.c_void_p, C.c_float, C.c_float, C.c_void_p, C.c_void_p,
+                                  C.c_int, C.c_void_p]
     L.muon_head_workspace_bytes.argtypes = [C.POINTER(muon_head_args), C.c_int, C.POINTER(C.c_size_t),
                                             C.POINTER(C.c_size_t)]
     L.muon_debug_set_head_piece_bytes.argtypes = [C.c_size_t]
@@ -294,9 +306,11 @@ def muon_momentum_norm_static(g, m, mu: float, nesterov: bool, norm_out, stream=
 
 
 def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, wd: float,
-                    beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, stream=None):
+                    beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, stream=None, coef=None):
     """AdamW step over lists of contiguous CUDA tensors (p bf16/fp32, g bf16/fp32,
-    m and v fp32), in place; argument marshalling only."""
+    m and v fp32), in place; argument marshalling only.  ``coef``: one fp32 CUDA
+    element that multiplies every gradient as it is read, as :class:`MuonGrads` gives
+    it (NaN: the step changes nothing)."""
     import torch
     n = len(params)
     arr = (muon_adamw_tensor * n)()
@@ -311,10 +325,116 @@ def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, 
     dev = params[0].device.index
     s = torch.cuda.current_stream(dev) if stream is None else stream
     hp = muon_adamw_hparams(lr, wd, beta1, beta2, eps, int(step))
-    _check(lib().muon_adamw_step(arr, n, C.byref(hp), dev, C.c_void_p(s.cuda_stream)))
+    if coef is None:
+        _check(lib().muon_adamw_step(arr, n, C.byref(hp), dev, C.c_void_p(s.cuda_stream)))
+        return
+    if coef.dtype != torch.float32 or coef.numel() != 1 or coef.device != params[0].device:
+        raise MuonError(MUON_ERR_INVALID_ARG, "coef must be one fp32 element on the parameters' device")
+    _check(lib().muon_adamw_step_clipped(arr, n, C.byref(hp), coef.data_ptr(), dev, s.cuda_stream))
 
 
 _no_context = contextlib.nullcontext()
+
+
+class GradNorm(NamedTuple):
+    """``norm`` and ``coef`` (one fp32 element each) and ``sum_sq`` (one fp64 element)."""
+    norm: "torch.Tensor"
+    coef: "torch.Tensor"
+    sum_sq: "torch.Tensor"
+
+
+class MuonGrads:
+    """The gradients of a training step, described once: their global norm, and
+    clipping by it.  ``grads``: contiguous CUDA tensors of any shapes, bf16 or fp32, on
+    one device; ``out``: tensors of the same sizes that get the clipped gradients
+    (default: in place).  Tensors must outlive the handle and keep their storage.  Calls
+    of one handle share its workspace and must be stream-ordered with respect to each
+    other; that holds for replays of graphs that captured them, too.  The formulas are
+    in include/muon.h; :func:`muon_grad_norm` and :func:`muon_clip_grads` are the same
+    for a list that is used once."""
+
+    def __init__(self, grads, out=None, workspace=None):
+        import torch
+        self.grads, self.out = list(grads), None if out is None else list(out)
+        n = len(self.grads)
+        if n == 0 or (self.out is not None and len(self.out) != n):
+            raise MuonError(MUON_ERR_INVALID_ARG, "at least one gradient, and an output for each")
+        dev = self.grads[0].device
+        if dev.type != "cuda":
+            raise MuonError(MUON_ERR_INVALID_ARG, "gradients must be on one CUDA device")
+        arr = (muon_grad_tensor * n)()
+        for i, g in enumerate(self.grads):
+            o = None if self.out is None else self.out[i]
+            if not g.is_contiguous() or g.device != dev:
+                raise MuonError(MUON_ERR_INVALID_ARG, "gradients must be contiguous and on one device")
+            if o is not None and (not o.is_contiguous() or o.device != dev or o.numel() != g.numel()):
+                raise MuonError(MUON_ERR_INVALID_ARG, "outputs must be contiguous, sized like their gradients, on their device")
+            arr[i] = muon_grad_tensor(g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), _dtype_code(g),
+                                      _dtype_code(g if o is None else o))
+        written = [t.data_ptr() for t in (self.grads if self.out is None else self.out) if t.numel()]
+        self._once = len(set(written)) == len(written)  # a norm may count a tensor twice, but not be clipped twice
+        if workspace is None:
+            workspace = torch.empty(MUON_GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
+        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise MuonError(MUON_ERR_WORKSPACE, "workspace must be a contiguous uint8 tensor on the gradients' device")
+        self.device, self.workspace = dev, workspace
+        self._arr, self._n = arr, n
+
+    def _results(self, norm, coef, sum_sq, stream):
+        import torch
+        with torch.cuda.stream(stream) if stream is not None else _no_context:
+            if norm is None and coef is None and sum_sq is None:
+                both = torch.empty(2, dtype=torch.float64, device=self.device)
+                sum_sq, pair = both.split_with_sizes((1, 1))
+                norm, coef = pair.view(torch.float32).split_with_sizes((1, 1))
+                return norm, coef, sum_sq
+            norm = torch.empty(1, dtype=torch.float32, device=self.device) if norm is None else norm
+            coef = torch.empty(1, dtype=torch.float32, device=self.device) if coef is None else coef
+            sum_sq = torch.empty(1, dtype=torch.float64, device=self.device) if sum_sq is None else sum_sq
+        for t, what, dtype in ((norm, "norm", torch.float32), (coef, "coef", torch.float32), (sum_sq, "sum_sq", torch.float64)):
+            if t.dtype != dtype or t.numel() != 1 or t.device != self.device:
+                raise MuonError(MUON_ERR_INVALID_ARG, "%s must be one %s element on the gradients' device" % (what, dtype))
+        return norm, coef, sum_sq
+
+    def muon_grad_norm(self, max_norm=float("inf"), eps=1e-6, norm=None, coef=None, sum_sq=None, stream=None) -> GradNorm:
+        """Norm, and the coefficient that ``max_norm`` gives."""
+        norm, coef, sum_sq = self._results(norm, coef, sum_sq, stream)
+        dev = self.device.index
+        _check(lib().muon_grad_norm(self._arr, self._n, max_norm, eps, sum_sq.data_ptr(), norm.data_ptr(), coef.data_ptr(),
+                                    self.workspace.data_ptr(), self.workspace.numel(), dev, _raw_stream(stream, dev)))
+        return GradNorm(norm, coef, sum_sq)
+
+    def muon_clip_grads(self, max_norm, eps=1e-6, sum_sq=None, norm=None, coef=None, stream=None) -> GradNorm:
+        """The gradients scaled to a global norm of at most ``max_norm``.  ``sum_sq``: the
+        sum of squares to take, as :meth:`muon_grad_norm` gives it and as ranks may have
+        added theirs; None: that of these gradients."""
+        if not self._once:
+            raise MuonError(MUON_ERR_INVALID_ARG, "a tensor is listed twice")
+        given = sum_sq is not None
+        norm, coef, sum_sq = self._results(norm, coef, sum_sq, stream)
+        dev = self.device.index
+        s = _raw_stream(stream, dev)
+        if not given:
+            _check(lib().muon_grad_norm(self._arr, self._n, max_norm, eps, sum_sq.data_ptr(), None, None,
+                                        self.workspace.data_ptr(), self.workspace.numel(), dev, s))
+        _check(lib().muon_clip_grads(self._arr, self._n, sum_sq.data_ptr(), max_norm, eps, norm.data_ptr(), coef.data_ptr(),
+                                     dev, s))
+        return GradNorm(norm, coef, sum_sq)
+
+
+def muon_grad_norm(grads, max_norm=float("inf"), eps=1e-6, stream=None) -> GradNorm:
+    """Global norm of a list of gradients; see :class:`MuonGrads`."""
+    import torch
+    with torch.cuda.stream(stream) if stream is not None else _no_context:  # the workspace is that stream's
+        return MuonGrads(grads).muon_grad_norm(max_norm, eps, stream=stream)
+
+
+def muon_clip_grads(grads, max_norm, eps=1e-6, out=None, sum_sq=None, stream=None) -> GradNorm:
+    """A list of gradients scaled to a global norm of at most ``max_norm``; see
+    :class:`MuonGrads`."""
+    import torch
+    with torch.cuda.stream(stream) if stream is not None else _no_context:
+        return MuonGrads(grads, out=out).muon_clip_grads(max_norm, eps, sum_sq=sum_sq, stream=stream)
 
 
 class HeadLoss(NamedTuple):

@@ -6,7 +6,9 @@
 //   p <- p - lr * ( (m / (1-beta1^t)) / (sqrt(v / (1-beta2^t)) + eps) + wd p )
 // One launch covers up to kMaxTensors tensors (their descriptors travel as
 // kernel parameters, so nothing is allocated); a pure HBM-streaming kernel:
-// 22 bytes per element with bf16 p and g (g 2, m 4+4, v 4+4, p 2+2).
+// 22 bytes per element with bf16 p and g (g 2, m 4+4, v 4+4, p 2+2).  Where the
+// gradients are clipped by their global norm, the coefficient multiplies them here as
+// they are read (a pass that scales them first would move 4 bytes more per bf16 element).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -39,6 +41,7 @@ struct LaunchArgs {
   int count;
   float lr, wd, beta1, beta2, eps;
   float inv_bc1, inv_bc2;  // 1 / (1 - beta^t)
+  const float* coef;       // clipped step: factor of every gradient
 };
 
 __device__ __forceinline__ void load8(const void* base, long long i, bool fp32, float (&out)[8]) {
@@ -66,8 +69,14 @@ __device__ __forceinline__ float adamw_one(float& p, float g, float& m, float& v
   return p;
 }
 
+template <bool kClip>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ LaunchArgs A) {
   const TensorArg T = A.t[blockIdx.y];
+  float coef = 1.0f;
+  if (kClip) {
+    coef = __ldg(A.coef);
+    if (!(coef == coef)) return;  // the norm was not finite
+  }
   const bool vec = ((reinterpret_cast<uintptr_t>(T.p) | reinterpret_cast<uintptr_t>(T.g) |
                      reinterpret_cast<uintptr_t>(T.m) | reinterpret_cast<uintptr_t>(T.v)) & 15) == 0;
   const long long n8 = vec ? T.numel / 8 : 0;
@@ -80,10 +89,10 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     load8(T.g, ia, T.g_fp32 != 0, ga); load8(T.m, ia, true, ma); load8(T.v, ia, true, va); load8(T.p, ia, T.p_fp32 != 0, pa);
     if (hb) { load8(T.g, ib, T.g_fp32 != 0, gb); load8(T.m, ib, true, mb); load8(T.v, ib, true, vb); load8(T.p, ib, T.p_fp32 != 0, pb); }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) adamw_one(pa[e], ga[e], ma[e], va[e], A);
+    for (int e = 0; e < 8; ++e) adamw_one(pa[e], kClip ? ga[e] * coef : ga[e], ma[e], va[e], A);
     if (hb) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) adamw_one(pb[e], gb[e], mb[e], vb[e], A);
+      for (int e = 0; e < 8; ++e) adamw_one(pb[e], kClip ? gb[e] * coef : gb[e], mb[e], vb[e], A);
     }
     for (int h = 0; h < (hb ? 2 : 1); ++h) {
       const long long i = h ? ib : ia;
@@ -110,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
                        : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(T.g)[i]);
     float p = T.p_fp32 ? reinterpret_cast<float*>(T.p)[i] : __bfloat162float(reinterpret_cast<__nv_bfloat16*>(T.p)[i]);
     float m = T.m[i], v = T.v[i];
-    adamw_one(p, g, m, v, A);
+    adamw_one(p, kClip ? g * coef : g, m, v, A);
     T.m[i] = m;
     T.v[i] = v;
     if (T.p_fp32) reinterpret_cast<float*>(T.p)[i] = p;
@@ -123,10 +132,8 @@ int fail(int code, const char* msg) {
   return code;
 }
 
-}  // namespace
-
-extern "C" int muon_adamw_step(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp,
-                               int device, void* stream_v) {
+int step(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp, const float* coef, int device,
+         void* stream_v) {
   if (!tensors || n_tensors <= 0 || !hp) return fail(MUON_ERR_INVALID_ARG, "tensors or hparams is null, or n_tensors <= 0");
   if (hp->step < 1) return fail(MUON_ERR_INVALID_ARG, "step counts from 1");
   if (!(hp->beta1 >= 0.f && hp->beta1 < 1.f && hp->beta2 >= 0.f && hp->beta2 < 1.f) || !(hp->eps >= 0.f) ||
@@ -163,13 +170,35 @@ extern "C" int muon_adamw_step(const muon_adamw_tensor* tensors, int n_tensors, 
     A.lr = hp->lr; A.wd = hp->wd; A.beta1 = hp->beta1; A.beta2 = hp->beta2; A.eps = hp->eps;
     A.inv_bc1 = static_cast<float>(1.0 / bc1);
     A.inv_bc2 = static_cast<float>(1.0 / bc2);
+    A.coef = coef;
     long long bx = (largest / 8 + kThreads - 1) / kThreads;
     const long long cap = static_cast<long long>(sms) * kCtasPerSm;
     if (bx > cap) bx = cap;
     if (bx < 1) bx = 1;
-    adamw_kernel<<<dim3(static_cast<unsigned>(bx), static_cast<unsigned>(A.count)), kThreads, 0, stream>>>(A);
+    const dim3 grid(static_cast<unsigned>(bx), static_cast<unsigned>(A.count));
+    if (coef) adamw_kernel<true><<<grid, kThreads, 0, stream>>>(A);
+    else adamw_kernel<false><<<grid, kThreads, 0, stream>>>(A);
     ce = cudaGetLastError();
     if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, cudaGetErrorString(ce));
   }
   return MUON_OK;
+}
+
+}  // namespace
+
+extern "C" int muon_adamw_step(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp,
+                               int device, void* stream) {
+  return step(tensors, n_tensors, hp, nullptr, device, stream);
+}
+
+extern "C" int muon_adamw_step_clipped(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp,
+                                       const float* coef, int device, void* stream) {
+  if (!coef) return fail(MUON_ERR_INVALID_ARG, "coef is null");
+  if (reinterpret_cast<uintptr_t>(coef) & 3) return fail(MUON_ERR_ALIGNMENT, "coef not aligned to its element size");
+  int before = -1;
+  cudaError_t ce = cudaGetDevice(&before);
+  if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, cudaGetErrorString(ce));
+  const int rc = step(tensors, n_tensors, hp, coef, device, stream);
+  cudaSetDevice(before);
+  return rc;
 }

@@ -1,0 +1,69 @@
+"""Refusals of the gradient norm and clipping that the host side checks; no GPU."""
+
+import ctypes as C
+
+import pytest
+
+P = 1 << 20  # an address that no call here reaches
+
+
+def _tensor(b, **more):
+    t = dict(g=P, out=None, numel=100, g_dtype=b.MUON_DTYPE_FP32, out_dtype=b.MUON_DTYPE_FP32)
+    t.update(more)
+    return b.muon_grad_tensor(t["g"], t["out"], t["numel"], t["g_dtype"], t["out_dtype"])
+
+
+def _norm(b, tensors, n=None, max_norm=1.0, eps=1e-6, sum_sq=P, norm=P, coef=P, workspace=P, nbytes=16384):
+    arr = (b.muon_grad_tensor * max(1, len(tensors)))(*tensors)
+    return b.lib().muon_grad_norm(arr, len(tensors) if n is None else n, max_norm, eps, sum_sq, norm, coef, workspace, nbytes, 0, None)
+
+
+def _clip(b, tensors, n=None, max_norm=1.0, eps=1e-6, sum_sq=P, norm=P, coef=P):
+    arr = (b.muon_grad_tensor * max(1, len(tensors)))(*tensors)
+    return b.lib().muon_clip_grads(arr, len(tensors) if n is None else n, sum_sq, max_norm, eps, norm, coef, 0, None)
+
+
+@pytest.mark.parametrize("code,more", [
+    ("INVALID_ARG", dict(g=None)), ("INVALID_ARG", dict(numel=-1)), ("UNSUPPORTED", dict(numel=1 << 42)),
+    ("UNSUPPORTED", dict(g_dtype=2)), ("ALIGNMENT", dict(g=P + 2)), ("ALIGNMENT", dict(g=P + 1, g_dtype=0, out_dtype=0)),
+])
+def test_tensors_that_are_refused(code, more):
+    from paper_2502_16982_b200 import binding as b
+
+    for call in (_norm, _clip):
+        assert call(b, [_tensor(b), _tensor(b, **more)]) == getattr(b, "MUON_ERR_" + code)
+
+
+@pytest.mark.parametrize("code,more", [
+    ("UNSUPPORTED", dict(out=P * 2, out_dtype=7)), ("ALIGNMENT", dict(out=P * 2 + 2)),
+    ("INVALID_ARG", dict(out=P, out_dtype=0)),
+])
+def test_outputs_that_are_refused(code, more):
+    from paper_2502_16982_b200 import binding as b
+
+    assert _clip(b, [_tensor(b, **more)]) == getattr(b, "MUON_ERR_" + code)
+
+
+@pytest.mark.parametrize("more", [dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(eps=-1.0), dict(eps=float("nan")),
+                                  dict(eps=float("inf")), dict(n=-1)])
+def test_limits_that_are_refused(more):
+    from paper_2502_16982_b200 import binding as b
+
+    for call in (_norm, _clip):
+        assert call(b, [_tensor(b)], **more) == b.MUON_ERR_INVALID_ARG
+
+
+def test_other_refusals():
+    from paper_2502_16982_b200 import binding as b
+
+    assert _norm(b, [_tensor(b)], sum_sq=None, norm=None, coef=None) == b.MUON_ERR_INVALID_ARG
+    assert _norm(b, [_tensor(b)], sum_sq=P + 4) == b.MUON_ERR_ALIGNMENT
+    assert _norm(b, [_tensor(b)], norm=P + 2) == b.MUON_ERR_ALIGNMENT
+    assert _norm(b, [_tensor(b)], workspace=None) == b.MUON_ERR_WORKSPACE
+    assert _norm(b, [_tensor(b)], nbytes=b.MUON_GRAD_NORM_WORKSPACE_BYTES - 1) == b.MUON_ERR_WORKSPACE
+    assert _norm(b, [_tensor(b)], workspace=P + 4) == b.MUON_ERR_WORKSPACE
+    assert _clip(b, [_tensor(b)], sum_sq=None) == b.MUON_ERR_INVALID_ARG
+    hp = b.muon_adamw_hparams(1e-3, 0.0, 0.9, 0.95, 1e-8, 1)
+    t = (b.muon_adamw_tensor * 1)(b.muon_adamw_tensor(P, P, P, P, 4, 1, 1))
+    assert b.lib().muon_adamw_step_clipped(t, 1, C.byref(hp), None, 0, None) == b.MUON_ERR_INVALID_ARG
+    assert b.lib().muon_adamw_step_clipped(t, 1, C.byref(hp), P + 2, 0, None) == b.MUON_ERR_ALIGNMENT
