@@ -735,6 +735,68 @@ int muon_head_distill(const muon_head_args* args, const muon_head_teacher* teach
 int muon_head_status(const void* workspace, int device, void* stream, int* device_status);
 
 /*
+ * Log probabilities of given tokens from stored logits - a decoder's, a teacher's, a
+ * policy's - with the entropy of their distribution, its log-sum-exp, and the best
+ * alternatives, in one pass over the logits; and the gradient of the logits.  (At the LM
+ * head itself, without logits in memory: muon_head_logprob.)
+ *
+ *   l = logit_scale * z,  lse = log sum_j exp(l_j),  q = exp(l - lse)
+ *   logprob = l_target - lse,   entropy = lse - sum_j q_j l_j
+ *   top_ids: the `top` entries with the largest logits, in falling order, equal logits by
+ *   rising index; top_logits: their z;  top_logprob = logit_scale * z - lse
+ *
+ *   gradient for upstream gradients r of logprob and h of entropy:
+ *   dlogits = logit_scale ( r ([j = target] - q_j) - h q_j (log q_j + entropy) )
+ *
+ * top_ids, top_logits and the lse of logit_scale = 1 / temperature are what
+ * muon_head_distill takes from a teacher.
+ *
+ *   tokens : rows; 0 is allowed.  vocab: columns.  top: 0 to 128, at most vocab.
+ *   logits : DEVICE, bf16 or fp32, row stride ld >= vocab, aligned to the element.
+ *   targets: DEVICE, one int64 per token, or NULL.  A token whose target lies outside
+ *            [0, vocab) (-100, say) is masked: its logprob, entropy, lse, top_logits and
+ *            top_logprob are 0, its top_ids -1, its row of dlogits 0, and nothing of its
+ *            logits is read.  Without targets no token is masked.
+ *   logprob (needs targets), entropy, lse: DEVICE, one fp32 per token;
+ *   top_ids (int64), top_logits, top_logprob (fp32): DEVICE, [tokens, top], contiguous.
+ *            Each NULL if not wanted, but one of them.
+ *
+ * A logit of minus infinity is probability 0; a row of nothing else has lse and logprob
+ * minus infinity, entropy 0, and a gradient of 0.  A NaN or plus infinity makes the
+ * statistics of its row NaN; among the alternatives a NaN counts as minus infinity.
+ * Exponents are l log2(e) in fp32 and sums are fp32.  Results are the same bits from call
+ * to call.  Asynchronous on `stream`; no workspace, allocates nothing, does not
+ * synchronise; may be captured into a CUDA graph.
+ *
+ * muon_logits_logprob_grad takes the same struct with lse, and entropy where g_entropy is
+ * given, as muon_logits_logprob wrote them.  g_logprob (needs targets) and g_entropy:
+ * DEVICE, one fp32 per token, or NULL for 0.  dlogits: of the logits' dtype, row stride
+ * ld_dlogits; it may be the logits themselves (same stride), and overlaps nothing else.
+ */
+typedef struct muon_logits_args {
+  int32_t tokens;
+  int32_t vocab;
+  const void* logits;
+  int64_t ld;
+  int32_t dtype;
+  int32_t top;
+  float logit_scale;
+  int32_t reserved;
+  const int64_t* targets;
+  float* logprob;
+  float* entropy;
+  float* lse;
+  int64_t* top_ids;
+  float* top_logits;
+  float* top_logprob;
+} muon_logits_args;
+
+int muon_logits_logprob(const muon_logits_args* args, int device, void* stream);
+
+int muon_logits_logprob_grad(const muon_logits_args* args, const float* g_logprob, const float* g_entropy, void* dlogits,
+                             int64_t ld_dlogits, int device, void* stream);
+
+/*
  * Knobs, process-wide, read by muon_head_workspace_bytes and by every call.
  * muon_debug_set_head_piece_bytes: bytes of logit gradients of one vocabulary
  * piece (0 restores the default of 256 MiB); tests lower it to run several pieces

@@ -39,6 +39,7 @@ EXPORTED = [
     "muon_profile_enable", "muon_profile_read", "muon_debug_tmem_bases",
     "muon_momentum_norm_static", "muon_adamw_step", "muon_adamw_step_clipped", "muon_grad_norm", "muon_clip_grads",
     "muon_head_workspace_bytes", "muon_head_xent", "muon_head_distill", "muon_head_status",
+    "muon_logits_logprob", "muon_logits_logprob_grad",
     "muon_debug_set_head_piece_bytes", "muon_debug_set_head_codes",
 ]
 MUON_STATIC_MAX_TILES = 65536
@@ -97,6 +98,13 @@ class muon_head_teacher(C.Structure):
     _fields_ = [("top_ids", C.c_void_p), ("top_logits", C.c_void_p), ("ld_ids", C.c_int64),
                 ("ld_logits", C.c_int64), ("teacher_lse", C.c_void_p), ("top", C.c_int32),
                 ("logits_dtype", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32)]
+
+
+class muon_logits_args(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("vocab", C.c_int32), ("logits", C.c_void_p), ("ld", C.c_int64), ("dtype", C.c_int32),
+                ("top", C.c_int32), ("logit_scale", C.c_float), ("reserved", C.c_int32), ("targets", C.c_void_p),
+                ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("lse", C.c_void_p), ("top_ids", C.c_void_p),
+                ("top_logits", C.c_void_p), ("top_logprob", C.c_void_p)]
 
 
 class MuonError(RuntimeError):
@@ -168,6 +176,9 @@ def lib():
     L.muon_head_distill.argtypes = [C.POINTER(muon_head_args), C.POINTER(muon_head_teacher), C.c_void_p, C.c_size_t,
                                     C.c_int, C.c_void_p]
     L.muon_head_status.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)]
+    L.muon_logits_logprob.argtypes = [C.POINTER(muon_logits_args), C.c_int, C.c_void_p]
+    L.muon_logits_logprob_grad.argtypes = [C.POINTER(muon_logits_args), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int,
+                                           C.c_void_p]
     for name in EXPORTED:
         if name in ("muon_debug_set_chunk_bytes", "muon_debug_set_head_piece_bytes"):
             getattr(L, name).restype = C.c_size_t
@@ -634,6 +645,103 @@ def muon_head_status(workspace, stream=None) -> int:
     _check(lib().muon_head_status(C.c_void_p((workspace.data_ptr() + 1023) // 1024 * 1024), workspace.device.index,
                                   C.c_void_p(s.cuda_stream), C.byref(st)))
     return st.value
+
+
+class LogitsLogprob(NamedTuple):
+    """Per token: ``logprob`` of the target (None without targets), ``entropy`` and ``lse``
+    (fp32), and the alternatives (None with ``top`` 0): ``top_ids`` int64, ``top_logits``
+    and ``top_logprob`` fp32, [tokens, top]."""
+    logprob: Optional["torch.Tensor"]
+    entropy: Optional["torch.Tensor"]
+    lse: Optional["torch.Tensor"]
+    top_ids: Optional["torch.Tensor"] = None
+    top_logits: Optional["torch.Tensor"] = None
+    top_logprob: Optional["torch.Tensor"] = None
+
+
+def _token_vector(t, what, n, dev, dtype):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != dev:
+        raise MuonError(MUON_ERR_INVALID_ARG, "%s must be %d contiguous %s values on one CUDA device" % (what, n, dtype))
+    return t.data_ptr()
+
+
+def _logits_args(logits, targets, logit_scale, top):
+    import torch
+    if logits.dim() != 2 or logits.device.type != "cuda" or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise MuonError(MUON_ERR_INVALID_ARG, "logits must be [tokens, vocab] on a CUDA device, with contiguous rows")
+    tokens, vocab = logits.shape
+    if (tokens | vocab | abs(top)) >> 31:
+        _past_32_bits()
+    a = muon_logits_args(tokens, vocab, logits.data_ptr(), _row_stride(logits) if tokens else vocab, _dtype_code(logits), top,
+                         logit_scale)
+    if targets is not None:
+        a.targets = _token_vector(targets, "targets", tokens, logits.device, torch.int64)
+    return a
+
+
+def muon_logits_logprob(logits, targets=None, top: int = 0, logit_scale: float = 1.0, out: Optional[LogitsLogprob] = None,
+                        stream=None) -> LogitsLogprob:
+    """Log probabilities of ``targets`` (int64 [tokens], outside [0, vocab): masked) under
+    ``logits`` [tokens, vocab], bf16 or fp32, with the entropies, the log-sum-exps and the
+    ``top`` best alternatives.  ``out``: tensors to write, None in place of what is not
+    wanted; by default all are allocated.  Argument marshalling only; the formulas are in
+    include/muon.h.  ``top_ids``, ``top_logits`` and ``lse`` at ``logit_scale`` = 1 /
+    temperature are what :func:`muon_head_distill` takes from a teacher."""
+    import torch
+    a = _logits_args(logits, targets, logit_scale, int(top))
+    tokens, dev = logits.shape[0], logits.device
+    if out is None:
+        with torch.cuda.stream(stream) if stream is not None else _no_context:
+            n = 3 if targets is not None else 2
+            rows = torch.empty(n * tokens, dtype=torch.float32, device=dev).split_with_sizes((tokens,) * n)
+            more = (None, None, None)
+            if top > 0:
+                pair = torch.empty((2, tokens, top), dtype=torch.float32, device=dev)
+                more = (torch.empty((tokens, top), dtype=torch.int64, device=dev), pair[0], pair[1])
+        out = LogitsLogprob(rows[2] if targets is not None else None, rows[0], rows[1], *more)
+        a.entropy, a.lse = rows[0].data_ptr(), rows[1].data_ptr()
+        if targets is not None:
+            a.logprob = rows[2].data_ptr()
+        if top > 0:
+            a.top_ids, a.top_logits, a.top_logprob = more[0].data_ptr(), more[1].data_ptr(), more[2].data_ptr()
+    else:
+        for name in ("logprob", "entropy", "lse"):
+            t = getattr(out, name)
+            if t is not None:
+                setattr(a, name, _token_vector(t, name, tokens, dev, torch.float32))
+        for name, dtype in (("top_ids", torch.int64), ("top_logits", torch.float32), ("top_logprob", torch.float32)):
+            t = getattr(out, name)
+            if t is not None:
+                if t.dtype != dtype or tuple(t.shape) != (tokens, top) or not t.is_contiguous() or t.device != dev:
+                    raise MuonError(MUON_ERR_INVALID_ARG, "%s must be contiguous %s [tokens, top] on the logits' device" % (name, dtype))
+                setattr(a, name, t.data_ptr())
+    _check(lib().muon_logits_logprob(C.byref(a), dev.index, _raw_stream(stream, dev.index)))
+    return out
+
+
+def muon_logits_logprob_grad(logits, targets, saved: LogitsLogprob, g_logprob=None, g_entropy=None, logit_scale: float = 1.0,
+                             dlogits=None, stream=None):
+    """Gradient of the logits for the gradients ``g_logprob`` and ``g_entropy`` (fp32
+    [tokens] or None) of what :func:`muon_logits_logprob` gave as ``saved``.  ``dlogits``:
+    a tensor like ``logits`` to write, or ``logits`` itself; allocated by default."""
+    import torch
+    a = _logits_args(logits, targets, logit_scale, 0)
+    tokens, dev = logits.shape[0], logits.device
+    if saved.lse is None or (g_entropy is not None and saved.entropy is None):
+        raise MuonError(MUON_ERR_INVALID_ARG, "the gradient needs lse, and entropy where g_entropy is given")
+    a.lse = _token_vector(saved.lse, "lse", tokens, dev, torch.float32)
+    if g_entropy is not None:
+        a.entropy = _token_vector(saved.entropy, "entropy", tokens, dev, torch.float32)
+    r = None if g_logprob is None else _token_vector(g_logprob, "g_logprob", tokens, dev, torch.float32)
+    h = None if g_entropy is None else _token_vector(g_entropy, "g_entropy", tokens, dev, torch.float32)
+    if dlogits is None:
+        with torch.cuda.stream(stream) if stream is not None else _no_context:
+            dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    elif dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or dlogits.device != dev or (dlogits.shape[1] > 1 and dlogits.stride(1) != 1):
+        raise MuonError(MUON_ERR_INVALID_ARG, "dlogits must be like the logits, with contiguous rows")
+    _check(lib().muon_logits_logprob_grad(C.byref(a), r, h, dlogits.data_ptr(), _row_stride(dlogits) if tokens else a.vocab,
+                                          dev.index, _raw_stream(stream, dev.index)))
+    return dlogits
 
 
 def muon_partition(shapes, world: int):

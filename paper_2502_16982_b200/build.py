@@ -13,7 +13,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuon_b200.so")
-SOURCES = ["muon_api.cu", "stream_kernels.cu", "stream_tma.cu", "ns_gemm.cu", "no_alloc.cu", "adamw.cu", "clip.cu",
+SOURCES = ["muon_api.cu", "stream_kernels.cu", "stream_tma.cu", "ns_gemm.cu", "no_alloc.cu", "adamw.cu", "clip.cu", "logits.cu",
            "head_api.cu", "head_gemm.cu", "head_rows.cu"]
 HEADERS = ["internal.h", "ptx.cuh", "head.h", "head_codes.cuh", os.path.join("..", "..", "include", "muon.h")]
 NVCC_FLAGS = [
