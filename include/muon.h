@@ -735,6 +735,75 @@ int muon_head_distill(const muon_head_args* args, const muon_head_teacher* teach
 int muon_head_status(const void* workspace, int device, void* stream, int* device_status);
 
 /*
+ * Log probabilities of given tokens at the LM head, with the entropy of their
+ * distribution, and the gradients of both: what training on a policy's own samples, or
+ * scoring text under a model, needs of the head.  Like the losses above, without fp32
+ * logits in memory.  Two calls, because the caller's objective stands between them (a
+ * ratio to an older policy, clipped; a penalty on the distance from a reference; a bonus
+ * on the entropy) and gives each token gradients of its own:
+ *
+ *   l = logit_scale * x w^T,  lse = log sum_j exp(l_j),  q = exp(l - lse)
+ *   logprob = l_target - lse,   entropy = - sum_j q_j log q_j
+ *   gradient, for upstream gradients r of logprob and h of entropy:
+ *     G_j = logit_scale ( r ([j = target] - q_j) - h q_j (log q_j + entropy) )
+ *     dx  = G w,   dw = G^T x
+ *
+ * muon_head_logprob writes logprob, and lse and entropy where they are not NULL.  It keeps
+ * no logits.  muon_head_logprob_grad reads logprob, lse and (with g_entropy) entropy as
+ * that call wrote them and forms the logits again, a piece of the vocabulary of at most
+ * 256 MiB of bf16 gradients at a time.
+ *
+ * Masked tokens (a target outside [0, vocab)), operands, types, strides, dx, dw and
+ * dw_accumulate, arithmetic, streams, workspace and errors: as for muon_head_xent.  A
+ * masked token's logprob, entropy and lse are 0, its row of dx is 0, and its g_logprob
+ * and g_entropy do not count.
+ *
+ *   g_logprob, g_entropy: DEVICE, one fp32 per token, or NULL for 0; finite.
+ *   workspace: DEVICE, 1024-byte aligned, of muon_head_logprob_workspace_bytes: with
+ *   grads NULL that of muon_head_logprob, else that of muon_head_logprob_grad.  Of the
+ *   pointers it looks at which of entropy, dx and dw are NULL and at the alignment of w.
+ *   muon_head_status reads the status of either call from its workspace.
+ */
+typedef struct muon_logprob_args {
+  int32_t tokens;
+  int32_t dim;
+  int32_t vocab;
+  int32_t reserved;
+  const void* x;
+  const void* w;
+  int64_t ld_x;
+  int64_t ld_w;
+  int32_t x_dtype; /* MUON_DTYPE_BF16 */
+  int32_t w_dtype; /* MUON_DTYPE_BF16 */
+  const int64_t* targets;
+  float logit_scale;
+  int32_t reserved2;
+  float* logprob;
+  float* entropy;
+  float* lse;
+} muon_logprob_args;
+
+typedef struct muon_logprob_grads {
+  const float* g_logprob;
+  const float* g_entropy;
+  void* dx;
+  void* dw;
+  int64_t ld_dx;
+  int64_t ld_dw;
+  int32_t dx_dtype;
+  int32_t dw_dtype;
+  int32_t dw_accumulate;
+  int32_t reserved;
+} muon_logprob_grads;
+
+int muon_head_logprob_workspace_bytes(const muon_logprob_args* args, const muon_logprob_grads* grads, size_t* out_bytes);
+
+int muon_head_logprob(const muon_logprob_args* args, void* workspace, size_t workspace_bytes, int device, void* stream);
+
+int muon_head_logprob_grad(const muon_logprob_args* args, const muon_logprob_grads* grads, void* workspace,
+                           size_t workspace_bytes, int device, void* stream);
+
+/*
  * Log probabilities of given tokens from stored logits - a decoder's, a teacher's, a
  * policy's - with the entropy of their distribution, its log-sum-exp, and the best
  * alternatives, in one pass over the logits; and the gradient of the logits.  (At the LM

@@ -39,6 +39,7 @@ EXPORTED = [
     "muon_profile_enable", "muon_profile_read", "muon_debug_tmem_bases",
     "muon_momentum_norm_static", "muon_adamw_step", "muon_adamw_step_clipped", "muon_grad_norm", "muon_clip_grads",
     "muon_head_workspace_bytes", "muon_head_xent", "muon_head_distill", "muon_head_status",
+    "muon_head_logprob_workspace_bytes", "muon_head_logprob", "muon_head_logprob_grad",
     "muon_logits_logprob", "muon_logits_logprob_grad",
     "muon_debug_set_head_piece_bytes", "muon_debug_set_head_codes",
 ]
@@ -98,6 +99,19 @@ class muon_head_teacher(C.Structure):
     _fields_ = [("top_ids", C.c_void_p), ("top_logits", C.c_void_p), ("ld_ids", C.c_int64),
                 ("ld_logits", C.c_int64), ("teacher_lse", C.c_void_p), ("top", C.c_int32),
                 ("logits_dtype", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32)]
+
+
+class muon_logprob_args(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("dim", C.c_int32), ("vocab", C.c_int32), ("reserved", C.c_int32),
+                ("x", C.c_void_p), ("w", C.c_void_p), ("ld_x", C.c_int64), ("ld_w", C.c_int64),
+                ("x_dtype", C.c_int32), ("w_dtype", C.c_int32), ("targets", C.c_void_p), ("logit_scale", C.c_float),
+                ("reserved2", C.c_int32), ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("lse", C.c_void_p)]
+
+
+class muon_logprob_grads(C.Structure):
+    _fields_ = [("g_logprob", C.c_void_p), ("g_entropy", C.c_void_p), ("dx", C.c_void_p), ("dw", C.c_void_p),
+                ("ld_dx", C.c_int64), ("ld_dw", C.c_int64), ("dx_dtype", C.c_int32), ("dw_dtype", C.c_int32),
+                ("dw_accumulate", C.c_int32), ("reserved", C.c_int32)]
 
 
 class muon_logits_args(C.Structure):
@@ -176,6 +190,11 @@ def lib():
     L.muon_head_distill.argtypes = [C.POINTER(muon_head_args), C.POINTER(muon_head_teacher), C.c_void_p, C.c_size_t,
                                     C.c_int, C.c_void_p]
     L.muon_head_status.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)]
+    L.muon_head_logprob_workspace_bytes.argtypes = [C.POINTER(muon_logprob_args), C.POINTER(muon_logprob_grads),
+                                                    C.POINTER(C.c_size_t)]
+    L.muon_head_logprob.argtypes = [C.POINTER(muon_logprob_args), C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]
+    L.muon_head_logprob_grad.argtypes = [C.POINTER(muon_logprob_args), C.POINTER(muon_logprob_grads), C.c_void_p, C.c_size_t,
+                                         C.c_int, C.c_void_p]
     L.muon_logits_logprob.argtypes = [C.POINTER(muon_logits_args), C.c_int, C.c_void_p]
     L.muon_logits_logprob_grad.argtypes = [C.POINTER(muon_logits_args), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int,
                                            C.c_void_p]
@@ -645,6 +664,141 @@ def muon_head_status(workspace, stream=None) -> int:
     _check(lib().muon_head_status(C.c_void_p((workspace.data_ptr() + 1023) // 1024 * 1024), workspace.device.index,
                                   C.c_void_p(s.cuda_stream), C.byref(st)))
     return st.value
+
+
+class HeadLogprob(NamedTuple):
+    """Per token, fp32: ``logprob`` of the target, ``entropy`` and ``lse`` (None where not wanted)."""
+    logprob: "torch.Tensor"
+    entropy: Optional["torch.Tensor"]
+    lse: Optional["torch.Tensor"]
+
+
+class HeadGrads(NamedTuple):
+    """Gradients of the hidden states and of the head (None where not wanted)."""
+    dx: Optional["torch.Tensor"]
+    dw: Optional["torch.Tensor"]
+
+
+def _logprob_args(x, w, targets, logit_scale):
+    """Checks of the operands, and the struct without its outputs."""
+    import torch
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.shape[1] < 1 or w.shape[0] < 1:
+        raise MuonError(MUON_ERR_INVALID_ARG, "x must be [tokens, dim] and w [vocab, dim]")
+    (tokens, dim), vocab = x.shape, w.shape[0]
+    if (tokens | dim | vocab) >> 31:
+        _past_32_bits()
+    dev = x.device
+    if dev.type != "cuda" or w.device != dev:
+        raise MuonError(MUON_ERR_INVALID_ARG, "x and w must be on one CUDA device")
+    if dim > 1 and (x.stride(1) != 1 or w.stride(1) != 1):
+        raise MuonError(MUON_ERR_INVALID_ARG, "x and w must have contiguous rows")
+    return muon_logprob_args(tokens, dim, vocab, 0, x.data_ptr(), w.data_ptr(), _row_stride(x) if tokens else dim, _row_stride(w),
+                             _dtype_code(x), _dtype_code(w), _token_vector(targets, "targets", tokens, dev, torch.int64),
+                             logit_scale)
+
+
+def _logprob_workspace(workspace, dev, a, d):
+    """(tensor, first address, bytes) of the workspace of one call."""
+    import torch
+    if workspace is None:
+        key = (a.tokens, a.dim, a.vocab, -1 if d is None else -2, not a.entropy, d is None or not d.dx, d is None or not d.dw,
+               a.ld_w & 7, (a.w or 0) & 15)
+        need = _head_bytes.get(key)
+        if need is None:
+            out = C.c_size_t(0)
+            _check(lib().muon_head_logprob_workspace_bytes(C.byref(a), None if d is None else C.byref(d), C.byref(out)))
+            if len(_head_bytes) >= 1024:
+                _head_bytes.clear()
+            need = _head_bytes[key] = out.value + 1024
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+        raise MuonError(MUON_ERR_WORKSPACE, "workspace must be a contiguous uint8 tensor on x's device")
+    first = workspace.data_ptr()
+    base = (first + 1023) // 1024 * 1024
+    return workspace, base, max(first + workspace.numel() - base, 0)
+
+
+def muon_head_logprob_workspace_bytes(tokens: int, dim: int, vocab: int, grads: bool, entropy: bool = True, dx: bool = True,
+                                      dw: bool = True, packed_head: bool = True) -> int:
+    """Workspace bytes of :func:`muon_head_logprob` or, with ``grads``, of
+    :func:`muon_head_logprob_grad`, 1024 for aligning a tensor's start included.
+    ``packed_head``: the head's rows are 16-byte aligned."""
+    if any(C.c_int32(v).value != v for v in (tokens, dim, vocab)):
+        _past_32_bits()
+    a = muon_logprob_args(tokens, dim, vocab, 0, None, None, dim, (dim + 7) // 8 * 8 if packed_head else dim | 1,
+                          MUON_DTYPE_BF16, MUON_DTYPE_BF16, None, 1.0, 0, None, 1024 if entropy else None)
+    d = muon_logprob_grads(None, None, 1024 if dx else None, 1024 if dw else None)  # only whether they are there counts
+    out = C.c_size_t(0)
+    _check(lib().muon_head_logprob_workspace_bytes(C.byref(a), C.byref(d) if grads else None, C.byref(out)))
+    return out.value + 1024
+
+
+def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out: Optional[HeadLogprob] = None, workspace=None,
+                      stream=None) -> HeadLogprob:
+    """Log probabilities of ``targets`` (int64 [tokens], outside [0, vocab): masked) under
+    ``x w^T``, bf16 [tokens, dim] and [vocab, dim], with log-sum-exps and, unless
+    ``entropy`` is False, entropies.  ``out``: tensors to write, None in place of what is
+    not wanted.  Argument marshalling only; the formulas are in include/muon.h."""
+    import torch
+    a = _logprob_args(x, w, targets, logit_scale)
+    tokens, dev = x.shape[0], x.device
+    with torch.cuda.stream(stream) if stream is not None else _no_context:
+        if out is None:
+            n = 3 if entropy else 2
+            rows = torch.empty(n * tokens, dtype=torch.float32, device=dev).split_with_sizes((tokens,) * n)
+            out = HeadLogprob(rows[0], rows[2] if entropy else None, rows[1])
+            a.logprob, a.lse = rows[0].data_ptr(), rows[1].data_ptr()
+            if entropy:
+                a.entropy = rows[2].data_ptr()
+        else:
+            for name in ("logprob", "entropy", "lse"):
+                t = getattr(out, name)
+                if t is not None:
+                    setattr(a, name, _token_vector(t, name, tokens, dev, torch.float32))
+        workspace, base, nbytes = _logprob_workspace(workspace, dev, a, None)
+    _check(lib().muon_head_logprob(C.byref(a), base, nbytes, dev.index, _raw_stream(stream, dev.index)))
+    return out
+
+
+def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_entropy=None, logit_scale: float = 1.0, dx=None,
+                           dw=None, accumulate_dw=False, workspace=None, stream=None) -> HeadGrads:
+    """Gradients of the hidden states and of the head for the gradients ``g_logprob`` and
+    ``g_entropy`` (fp32 [tokens] or None) of what :func:`muon_head_logprob` gave as
+    ``saved`` for the same operands.  ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True
+    to allocate one like x / w, None to leave the gradient out."""
+    import torch
+    a = _logprob_args(x, w, targets, logit_scale)
+    tokens, dev = x.shape[0], x.device
+    if saved.logprob is None or saved.lse is None or (g_entropy is not None and saved.entropy is None):
+        raise MuonError(MUON_ERR_INVALID_ARG, "the gradient needs logprob, lse, and entropy where g_entropy is given")
+    if accumulate_dw and not isinstance(dw, torch.Tensor):
+        raise MuonError(MUON_ERR_INVALID_ARG, "accumulate_dw needs the dw to add to")
+    a.logprob = _token_vector(saved.logprob, "logprob", tokens, dev, torch.float32)
+    a.lse = _token_vector(saved.lse, "lse", tokens, dev, torch.float32)
+    d = muon_logprob_grads()
+    if g_logprob is not None:
+        d.g_logprob = _token_vector(g_logprob, "g_logprob", tokens, dev, torch.float32)
+    if g_entropy is not None:
+        a.entropy = _token_vector(saved.entropy, "entropy", tokens, dev, torch.float32)
+        d.g_entropy = _token_vector(g_entropy, "g_entropy", tokens, dev, torch.float32)
+    with torch.cuda.stream(stream) if stream is not None else _no_context:
+        if dx is False:
+            dx = None
+        elif dx is not None:
+            dx = torch.empty_like(x) if dx is True else _head_matrix(dx, "dx", x.shape, dev)
+            d.dx, d.ld_dx, d.dx_dtype = dx.data_ptr(), _row_stride(dx) if tokens else a.dim, _dtype_code(dx)
+        if dw is False:
+            dw = None
+        elif dw is not None:
+            dw = torch.empty_like(w) if dw is True else _head_matrix(dw, "dw", w.shape, dev)
+            d.dw, d.ld_dw, d.dw_dtype, d.dw_accumulate = dw.data_ptr(), _row_stride(dw), _dtype_code(dw), 1 if accumulate_dw else 0
+        if dx is None and dw is None:
+            raise MuonError(MUON_ERR_INVALID_ARG, "no gradient wanted")
+        if tokens == 0 and dw is None:
+            return HeadGrads(dx, dw)
+        workspace, base, nbytes = _logprob_workspace(workspace, dev, a, d)
+    _check(lib().muon_head_logprob_grad(C.byref(a), C.byref(d), base, nbytes, dev.index, _raw_stream(stream, dev.index)))
+    return HeadGrads(dx, dw)
 
 
 class LogitsLogprob(NamedTuple):

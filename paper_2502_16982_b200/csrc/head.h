@@ -106,7 +106,9 @@ struct GemmParams {
   float* entry_logit; // [token][top] raw logit of each entry
   float2* stats;      // [token][stats_ld]: maximum and sum of exponentials per kStatN columns
   int stats_ld;
+  float* stats_e;        // [token][stats_ld] with entropies: sum of y 2^y; NULL without
   const float2* row_q;   // [token]: coefficient of q, log2 of the softmax denominator
+  const float* row_b;    // [token] gradients of log probabilities: coefficient of q log2 q; else NULL
   const float* entry_g;  // [token][top]: gradient of the logit at the entry
   // Piece buffers [buffer][token][piece columns], box {64, stats_rows} or
   // {64, 32}: where the
@@ -184,6 +186,16 @@ struct RowParams {
   void* dx;
   long long ld_dx;
   int dx_fp32, dx_vec;
+  // log probabilities: `loss` holds them.  Forward: entropy [tokens] or NULL, and the sums
+  // behind it; gradient: what the forward pass gave, and the gradients of it (or NULL)
+  float* entropy;
+  const float* stats_e;
+  const float* logprob_in;
+  const float* entropy_in;
+  const float* lse_in;
+  const float* g_logprob;
+  const float* g_entropy;
+  float* row_b;
   const float* part;     // partial dX of each run of K blocks
   long long part_ld, part_stride;
   int splits;
@@ -199,6 +211,8 @@ cudaError_t launch_flags(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_count(const RowParams& R, bool overlap, cudaStream_t stream);
 cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t stream);
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);
+cudaError_t launch_logprob(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_logprob_grad(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_pack(const RowParams& R, cudaStream_t stream);
 int pack_blocks(int vocab);

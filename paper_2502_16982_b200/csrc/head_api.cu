@@ -1,5 +1,5 @@
-// Host side of the LM-head losses: argument checks, the plan (vocabulary pieces,
-// splits, workspace layout) and the launch sequence.
+// Host side of the LM-head losses and of the log probabilities at the head: argument
+// checks, the plan (vocabulary pieces, splits, workspace layout) and the launch sequence.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -40,7 +40,12 @@ int g_codes = 0;
 // Bytes of partial dX that splitting its long axis may take.
 constexpr long long kPartBytes = 1ll << 28;
 
+// What a call computes: a loss, with or without its gradients; log probabilities; or the
+// gradients of log probabilities that an earlier call computed.
+enum Kind { kLoss, kLogprob, kLogprobGrad };
+
 struct Plan {
+  Kind kind;
   int tokens, rows, m_tiles, dim, vocab, top;  // rows: tokens, at least 1
   bool want_dx, want_dw, grads, distill, pack, in_place;
   int v_tiles;               // 256-column tiles of the vocabulary
@@ -48,7 +53,7 @@ struct Plan {
   int n_stored, n_buffers;   // pieces kept as codes; piece buffers in the workspace
   int splits, dx_n_tile, dx_n_tiles;
   long long ld_xc, ld_wc, part_ld, part_stride;
-  size_t ctrl, xc, wc, flags, run_counts, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, row_q, row_l, g,
+  size_t ctrl, xc, wc, flags, run_counts, row_of, ids, p, row_h, row_c, starts, entry_logit, entry_g, stats, stats_e, row_q, row_b, row_l, g,
       part, bytes, least;
 };
 
@@ -96,7 +101,9 @@ bool want_codes(int tokens, int dim, int vocab) {
 }
 
 // `room`: bytes of workspace to plan for; 0 plans for as many as are useful.
-int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t room, Plan* P) {
+int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t room, Plan* P, Kind kind = kLoss,
+              bool entropy = false) {
+  P->kind = kind;
   P->tokens = a->tokens;
   P->dim = a->dim;
   P->vocab = a->vocab;
@@ -147,10 +154,14 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   P->row_of = take(rows * 4);
   P->run_counts = take(P->tokens >= kManyTokens ? (rows / 256 + 1) * 4 : 0);
   P->ids = take(entries * 4);
+  // the gradient of log probabilities starts from what an earlier call left with the caller
+  const size_t units = kind == kLogprobGrad ? 0 : rows * P->v_tiles * kUnits;
   P->entry_logit = take(entries * 4);
   P->entry_g = take(entries * 4);
-  P->stats = take(rows * P->v_tiles * kUnits * sizeof(float2));
+  P->stats = take(units * sizeof(float2));
+  P->stats_e = take(entropy ? units * 4 : 0);
   P->row_q = take(rows * sizeof(float2));
+  P->row_b = take(kind == kLogprobGrad ? rows * 4 : 0);
   P->row_l = take(rows * 4);
   P->flags = P->p = P->row_h = P->row_c = P->starts = P->wc = P->g = P->part = 0;
   if (distill) {
@@ -164,7 +175,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   // Where no second piece is kept as codes nothing reads the statistics after the
   // finalisation, and partial dX may lie in their place.
   const size_t part_bytes = P->want_dx ? static_cast<size_t>(P->splits) * P->part_stride * 4 : 0;
-  const size_t stats_bytes = rows * P->v_tiles * kUnits * sizeof(float2);
+  const size_t stats_bytes = units * sizeof(float2);
   const bool share = part_bytes > 0 && stats_bytes >= part_bytes;
   const size_t apart = static_cast<size_t>(round_up(static_cast<long long>(part_bytes), 1024));
   P->n_stored = P->n_buffers = 0;
@@ -172,7 +183,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   if (P->grads) {
     const long long one = static_cast<long long>(rows) * P->piece_tiles * kTileN * 2;
     P->n_buffers = 1;
-    if (want_codes(P->tokens, P->dim, P->vocab)) {
+    if (kind == kLoss && want_codes(P->tokens, P->dim, P->vocab)) {
       long long fit = (room ? static_cast<long long>(room) - static_cast<long long>(off + apart)
                             : kCodeBytes - static_cast<long long>(stats_bytes)) / one;
       P->n_buffers = static_cast<int>(fit < 1 ? 1 : (fit > P->n_pieces ? P->n_pieces : fit));
@@ -309,12 +320,15 @@ struct DeviceGuard {
     if (rc_ != MUON_OK) return rc_; \
   } while (0)
 
-int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targets, float z_loss, void* workspace,
-        size_t workspace_bytes, int device, cudaStream_t stream) {
+// l, d: log probabilities, and their gradients; NULL for a loss.
+int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targets, float z_loss, const muon_logprob_args* l,
+        const muon_logprob_grads* d, void* workspace, size_t workspace_bytes, int device, cudaStream_t stream) {
   const bool distill = t != nullptr;
   const int top = distill ? t->top : 1;
+  const Kind kind = d ? kLogprobGrad : l ? kLogprob : kLoss;
+  const bool entropy = kind == kLogprob && l->entropy;
   Plan P;
-  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, workspace_bytes ? workspace_bytes : 1, &P));
+  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, workspace_bytes ? workspace_bytes : 1, &P, kind, entropy));
   if (!workspace || workspace_bytes < P.least || misaligned(workspace, 1024))
     return fail(MUON_ERR_WORKSPACE, "workspace: need at least %zu bytes, 1024-byte aligned", P.least);
   DeviceGuard guard;
@@ -374,6 +388,20 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.loss = a->loss;
   R.lse = a->lse;
   R.total = a->total;
+  if (l) {
+    R.row_b = reinterpret_cast<float*>(ws + P.row_b);
+    if (d) {
+      R.logprob_in = l->logprob;
+      R.entropy_in = l->entropy;
+      R.lse_in = l->lse;
+      R.g_logprob = d->g_logprob;
+      R.g_entropy = d->g_entropy;
+      R.loss = R.lse = nullptr;
+    } else if (entropy) {
+      R.entropy = l->entropy;
+      R.stats_e = reinterpret_cast<const float*>(ws + P.stats_e);
+    }
+  }
   R.dx = P.want_dx ? a->dx : nullptr;
   R.ld_dx = a->ld_dx;
   R.dx_fp32 = a->dx_dtype == MUON_DTYPE_FP32;
@@ -398,6 +426,8 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   S.stats_ld = R.stats_ld;
   S.row_q = R.row_q;
   S.entry_g = R.entry_g;
+  if (entropy) S.stats_e = reinterpret_cast<float*>(ws + P.stats_e);
+  if (d) S.row_b = R.row_b;
   __nv_bfloat16* const g = reinterpret_cast<__nv_bfloat16*>(ws + P.g);
   const long long g_ld = static_cast<long long>(P.piece_tiles) * kTileN;
   S.piece_tiles = P.piece_tiles;
@@ -493,7 +523,11 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   const long long m_tiles = P.m_tiles;
   // more tiles than CTA pairs: the epilogue's warps share them out instead of their columns
   S.by_tile = m_tiles * P.v_tiles > pairs;
-  HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, !P.in_place, stream));
+  if (!d) HEAD_CUDA(launch_gemm(kModeStats, S, m_tiles * P.v_tiles, pairs, !P.in_place, stream));
+  if (kind == kLogprob) {
+    if (P.tokens > 0) HEAD_CUDA(launch_logprob(R, stream));
+    return MUON_OK;
+  }
   ConvertParams C = {};
   C.ld = g_ld;
   C.row_q = R.row_q;
@@ -512,7 +546,8 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     return D;
   };
   if (P.grads) R.total = nullptr;  // the products' launch adds the losses up beside its work
-  HEAD_CUDA(launch_finalise(R, codes_of(0), 2 * pairs, stream));
+  if (d) HEAD_CUDA(launch_logprob_grad(R, stream));
+  else HEAD_CUDA(launch_finalise(R, codes_of(0), 2 * pairs, stream));
   if (P.grads) {
     for (int i = 0; i < P.n_pieces; ++i) {
       // stored pieces lie in a buffer each, the others use the first one after them
@@ -556,7 +591,72 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   return MUON_OK;
 }
 
+// The same call as a loss: sizes, operands and gradients, for the checks and the plan.
+muon_head_args as_head_args(const muon_logprob_args* l, const muon_logprob_grads* d) {
+  muon_head_args a = {};
+  a.tokens = l->tokens;
+  a.dim = l->dim;
+  a.vocab = l->vocab;
+  a.x = l->x;
+  a.w = l->w;
+  a.ld_x = l->ld_x;
+  a.ld_w = l->ld_w;
+  a.x_dtype = l->x_dtype;
+  a.w_dtype = l->w_dtype;
+  a.scale = 1.0f;
+  a.logit_scale = l->logit_scale;
+  a.loss = l->logprob;
+  a.lse = l->lse;
+  if (d) {
+    a.dx = d->dx;
+    a.dw = d->dw;
+    a.ld_dx = d->ld_dx;
+    a.ld_dw = d->ld_dw;
+    a.dx_dtype = d->dx_dtype;
+    a.dw_dtype = d->dw_dtype;
+    a.dw_accumulate = d->dw_accumulate;
+  }
+  return a;
+}
+
 }  // namespace
+
+extern "C" int muon_head_logprob_workspace_bytes(const muon_logprob_args* l, const muon_logprob_grads* d, size_t* out_bytes) {
+  if (!l || !out_bytes) return fail(MUON_ERR_INVALID_ARG, "args or out_bytes is null");
+  const muon_head_args a = as_head_args(l, d);
+  HEAD_TRY(check(&a, 1, false));
+  Plan P;
+  HEAD_TRY(make_plan(&a, 1, false, kPlanPairs, 0, &P, d ? kLogprobGrad : kLogprob, !d && l->entropy));
+  *out_bytes = P.bytes;
+  return MUON_OK;
+}
+
+static int check_logprob(const muon_logprob_args* l, const muon_head_args* a) {
+  HEAD_TRY(check(a, 1, true));
+  if (l->tokens > 0 && !l->targets) return fail(MUON_ERR_INVALID_ARG, "targets is null");
+  if (misaligned(l->targets, 8) || misaligned(l->entropy, 4)) return fail(MUON_ERR_ALIGNMENT, "pointer not aligned to its element size");
+  return check_scale(a, nullptr);
+}
+
+extern "C" int muon_head_logprob(const muon_logprob_args* l, void* workspace, size_t workspace_bytes, int device, void* stream) {
+  if (!l) return fail(MUON_ERR_INVALID_ARG, "args is null");
+  const muon_head_args a = as_head_args(l, nullptr);
+  HEAD_TRY(check_logprob(l, &a));
+  return run(&a, nullptr, l->targets, 0.f, l, nullptr, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int muon_head_logprob_grad(const muon_logprob_args* l, const muon_logprob_grads* d, void* workspace,
+                                      size_t workspace_bytes, int device, void* stream) {
+  if (!l || !d) return fail(MUON_ERR_INVALID_ARG, "args or grads is null");
+  const muon_head_args a = as_head_args(l, d);
+  HEAD_TRY(check_logprob(l, &a));
+  if (!d->dx && !d->dw) return fail(MUON_ERR_INVALID_ARG, "no gradient wanted");
+  if (l->tokens > 0 && (!l->lse || (d->g_entropy && !l->entropy)))
+    return fail(MUON_ERR_INVALID_ARG, "the gradient needs lse, and entropy where g_entropy is given");
+  if (misaligned(d->g_logprob, 4) || misaligned(d->g_entropy, 4))
+    return fail(MUON_ERR_ALIGNMENT, "pointer not aligned to its element size");
+  return run(&a, nullptr, l->targets, 0.f, l, d, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
+}
 
 extern "C" int muon_head_workspace_bytes(const muon_head_args* a, int top, size_t* out_bytes, size_t* least_bytes) {
   if (!out_bytes && !least_bytes) return fail(MUON_ERR_INVALID_ARG, "out_bytes and least_bytes are null");
@@ -588,7 +688,7 @@ extern "C" int muon_head_xent(const muon_head_args* a, const int64_t* targets, f
   if (misaligned(targets, 8)) return fail(MUON_ERR_ALIGNMENT, "targets not aligned to 8 bytes");
   if (!std::isfinite(z_loss)) return fail(MUON_ERR_INVALID_ARG, "z_loss must be finite");
   HEAD_TRY(check_scale(a, nullptr));
-  return run(a, nullptr, targets, z_loss, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
+  return run(a, nullptr, targets, z_loss, nullptr, nullptr, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int muon_head_distill(const muon_head_args* a, const muon_head_teacher* t, void* workspace,
@@ -606,7 +706,7 @@ extern "C" int muon_head_distill(const muon_head_args* a, const muon_head_teache
   if (misaligned(t->top_ids, 8) || misaligned(t->top_logits, t->logits_dtype == MUON_DTYPE_FP32 ? 4 : 2) ||
       misaligned(t->teacher_lse, 4))
     return fail(MUON_ERR_ALIGNMENT, "pointer not aligned to its element size");
-  return run(a, t, nullptr, 0.f, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
+  return run(a, t, nullptr, 0.f, nullptr, nullptr, workspace, workspace_bytes, device, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int muon_head_status(const void* workspace, int device, void* stream, int* device_status) {

@@ -67,6 +67,8 @@ struct Config {
 };
 constexpr int kMaxStages = 6;
 
+constexpr float kLogFloor = -200.0f;  // exponents from here down give 0
+
 constexpr int kOutside = 1 << 30;  // a row coordinate past every tensor
 
 struct Barriers {
@@ -121,6 +123,13 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Larger of two; a NaN shows.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
 
@@ -390,8 +399,10 @@ __device__ __forceinline__ void add_losses(const GemmParams& P, int n_valid, int
   if (lane == 0) *P.total = sum;
 }
 
-// kList: the sparse entries come from the caller's list.
-template <int kMode, bool kSpare, bool kList>
+// kList: the sparse entries come from the caller's list.  kLog, log probabilities with their
+// entropy: the statistics hold the sum of y 2^y beside that of 2^y, y a logit's distance from
+// the maximum in log2 units, and the gradient of a logit is q (row_q.x + row_b log2 q).
+template <int kMode, bool kSpare, bool kList, bool kLog>
 __global__ void __launch_bounds__(Config<kMode, kSpare>::kThreads, 1)
 head_gemm_kernel(const __grid_constant__ GemmParams P) {
   using Cfg = Config<kMode, kSpare>;
@@ -617,20 +628,23 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
       using List = std::conditional_t<kList, ListEntries, Entries>;
       Head head = {};
       float2 rq = make_float2(0.f, 0.f);
+      float rb = 0.f;
       const int first_tile = kMode == kModeGrad ? P.v0 / kTileN : 0;
-      auto ask = [&](const Tile& t, Head& h, float2& r) {
+      auto ask = [&](const Tile& t, Head& h, float2& r, float& b) {
         const int row = t.mi * kTileM + row_in + lane;
         if constexpr (kList) h = list_head(P, row, t.ni * kTileN + unit0 * kStatN, (unit1 - unit0) * kStatN, row < n_valid);
         else h = entry_head(P, row, first_tile + t.ni, row < n_valid);
         if (kMode == kModeGrad) r = row < n_valid ? P.row_q[row] : make_float2(0.f, 0.f);
+        if (kMode == kModeGrad && kLog) b = row < n_valid ? P.row_b[row] : 0.f;
       };
-      if (more) ask(tl, head, rq);
+      if (more) ask(tl, head, rq, rb);
       while (more) {
         Tile tl_next;
         Head head_next = {};
         float2 rq_next = make_float2(0.f, 0.f);
+        float rb_next = 0.f;
         more = locate(P, s0, s1, deal, k + step, tl_next);
-        if (more) ask(tl_next, head_next, rq_next);
+        if (more) ask(tl_next, head_next, rq_next, rb_next);
         const int row0 = tl.mi * kTileM + row_in;
         const int row = row0 + lane;
         const bool row_ok = row < n_valid;
@@ -682,14 +696,27 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
             constexpr bool kStore = decltype(store)::value;
             const uint64_t steps = pair(-kCodeSteps, -kCodeSteps), magic = pair(kCodeMagic, kCodeMagic);
             uint64_t sum[2] = {0, 0};  // pairs of zeros
+            uint64_t weighted[2] = {0, 0};
+            const uint64_t log_factor = pair(rb, rb), factor = pair(rq.x, rq.x);
 #pragma unroll
             for (int j = 0; j < kStatN; j += 2) {
               const uint64_t y = fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale, shift);
               float y0, y1;
               unpair(y, y0, y1);
+              uint64_t z = 0;
+              if (kLog) {  // finite where 2^y is 0, and for columns past the vocabulary
+                y0 = max_nan(y0, kLogFloor);
+                y1 = max_nan(y1, kLogFloor);
+                z = pair(y0, y1);
+              }
               y0 = ex2_fast(y0);
               y1 = ex2_fast(y1);
-              if (kMode == kModeStats) {
+              if (kLog && kMode == kModeStats) weighted[(j >> 1) & 1] = fma2(z, pair(y0, y1), weighted[(j >> 1) & 1]);
+              if (kLog && kMode == kModeGrad) {
+                float c0, c1;
+                unpair(fma2(z, log_factor, factor), c0, c1);
+                v[j >> 1] = row_ok ? pack2(c0 * y0, c1 * y1) : 0u;
+              } else if (kMode == kModeStats) {
                 sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pair(y0, y1));
                 if (kStore) {
                   float d0, d1;
@@ -703,7 +730,12 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
             if (kMode == kModeStats && row_ok) {
               float s0_, s1_;
               unpair(add2(sum[0], sum[1]), s0_, s1_);
-              P.stats[static_cast<long long>(row) * P.stats_ld + tl.ni * kUnits + unit] = make_float2(m, s0_ + s1_);
+              const long long at = static_cast<long long>(row) * P.stats_ld + tl.ni * kUnits + unit;
+              P.stats[at] = make_float2(m, s0_ + s1_);
+              if (kLog) {
+                unpair(add2(weighted[0], weighted[1]), s0_, s1_);
+                P.stats_e[at] = s0_ + s1_;
+              }
             }
           };
           if (kMode == kModeGrad || codes) {
@@ -748,6 +780,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
         tl = tl_next;
         head = head_next;
         rq = rq_next;
+        rb = rb_next;
         k += step;
       }
     } else {
@@ -890,13 +923,13 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
   }
 }
 
-template <int kMode, bool kSpare = false, bool kList = false>
+template <int kMode, bool kSpare = false, bool kList = false, bool kLog = false>
 cudaError_t configure_one() {
-  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kSpare, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(head_gemm_kernel<kMode, kSpare, kList, kLog>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               Config<kMode, kSpare>::kSmemBytes);
 }
 
-template <int kMode, bool kSpare = false, bool kList = false>
+template <int kMode, bool kSpare = false, bool kList = false, bool kLog = false>
 cudaError_t launch_one(const GemmParams& P, unsigned clusters, bool overlap, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * clusters, 1, 1);
@@ -912,7 +945,7 @@ cudaError_t launch_one(const GemmParams& P, unsigned clusters, bool overlap, cud
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = overlap ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kSpare, kList>, P);
+  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<kMode, kSpare, kList, kLog>, P);
 }
 
 }  // namespace
@@ -921,6 +954,10 @@ cudaError_t gemm_configure() {
   cudaError_t e = configure_one<kModeStats>();
   if (e == cudaSuccess) e = configure_one<kModeStats, true>();
   if (e == cudaSuccess) e = configure_one<kModeStats, true, true>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, false, false, true>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, true, false, true>();
+  if (e == cudaSuccess) e = configure_one<kModeStats, true, true, true>();
+  if (e == cudaSuccess) e = configure_one<kModeGrad, false, false, true>();
   if (e == cudaSuccess) e = configure_one<kModeGrad>();
   if (e == cudaSuccess) e = configure_one<kModeOut>();
   if (e == cudaSuccess) e = configure_one<kModeOut, true>();
@@ -940,7 +977,7 @@ cudaError_t gemm_max_clusters(int* out) {
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, false, false>, &cfg);
+  return cudaOccupancyMaxActiveClusters(out, head_gemm_kernel<kModeOut, false, false, false>, &cfg);
 }
 
 // Rows of a box in which the statistics' codes are stored: one row tile reads w from
@@ -952,6 +989,12 @@ int stats_rows(int tokens) { return tokens <= kTileM ? 16 : 32; }
 cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_clusters, bool overlap, cudaStream_t stream) {
   if (tiles <= 0) return cudaSuccess;
   const unsigned clusters = static_cast<unsigned>(tiles < max_clusters ? tiles : max_clusters);
+  if (mode == kModeStats && P.stats_e != nullptr) {
+    if (P.ids64 != nullptr) return launch_one<kModeStats, true, true, true>(P, clusters, overlap, stream);
+    return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, true, false, true>(P, clusters, overlap, stream)
+                                      : launch_one<kModeStats, false, false, true>(P, clusters, overlap, stream);
+  }
+  if (mode == kModeGrad && P.row_b != nullptr) return launch_one<kModeGrad, false, false, true>(P, clusters, overlap, stream);
   if (mode == kModeStats) {
     if (P.ids64 != nullptr) return launch_one<kModeStats, true, true>(P, clusters, overlap, stream);
     return stats_rows(P.tokens) == 16 ? launch_one<kModeStats, true>(P, clusters, overlap, stream)

@@ -162,9 +162,10 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
   if (t < R.tokens && lane == 0) {
     if (mine) {
       R.row_of[pos] = t;
-    } else {
+    } else if (R.loss != nullptr) {
       R.loss[t] = 0.f;
       if (R.lse != nullptr) R.lse[t] = 0.f;
+      if (R.entropy != nullptr) R.entropy[t] = 0.f;
     }
   }
   if (t < R.tokens && !mine && R.dx != nullptr) {
@@ -573,6 +574,106 @@ __global__ void __launch_bounds__(kThreads) finalise_kernel(const RowParams R, c
   }
 }
 
+// Log probability, entropy and log-sum-exp of one token from its statistics, all in units
+// of log2: y = l log2(e), M a row's largest y, S = sum 2^(y - M), E = sum (y - M) 2^(y - M),
+//   logprob = ln 2 (y_target - M - log2 S),  entropy = ln 2 (log2 S - E / S)
+// The target's logit is formed again as a plain fp32 sum and takes the tensor cores' place in
+// S and E, as in finalise_kernel.  One block a row; kInPlace: rows are tokens.
+template <bool kInPlace, bool kEntropy>
+__global__ void __launch_bounds__(kRowThreads) logprob_kernel(const RowParams R) {
+  __shared__ float s_f[kRowWarps], s_max[kRowWarps];
+  __shared__ float s_exact;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row = blockIdx.x;
+  int t = row, id = 0;
+  if (kInPlace) {
+    ptx::grid_launch_dependents();
+    const int64_t raw = R.ids_in[static_cast<long long>(row) * R.ld_ids];
+    if (!in_vocab(R, raw)) {
+      if (tid == 0) {
+        R.loss[row] = 0.f;
+        if (R.lse != nullptr) R.lse[row] = 0.f;
+        if (kEntropy) R.entropy[row] = 0.f;
+      }
+      return;
+    }
+    id = static_cast<int>(raw);
+  } else {
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    if (row >= R.ctrl->n_valid) return;
+    t = R.row_of[row];
+    id = R.ids[row];
+  }
+  if (warp == 0) {
+    const float exact = warp_dot(kInPlace ? R.x + static_cast<long long>(row) * R.ld_x : R.xc + static_cast<long long>(row) * R.ld_xc,
+                                 R.w + static_cast<long long>(id) * R.ld_w, R.dim, lane);
+    if (lane == 0) s_exact = exact;
+  }
+  if (kInPlace) ptx::grid_dependency_wait();
+  const long long at = static_cast<long long>(row) * R.stats_ld;
+  float m = -INFINITY, s = 0.f, e = 0.f;
+#pragma unroll 4
+  for (int i = tid; i < R.stats_n; i += kRowThreads) {
+    const float2 v = R.stats[at + i];
+    const float ve = kEntropy ? R.stats_e[at + i] : 0.f;
+    const float mx = fmaxf(m, v.x);
+    const float dm = m == mx ? 0.f : fmaxf(m - mx, -200.f), dv = v.x == mx ? 0.f : fmaxf(v.x - mx, -200.f);
+    const float fm = exp2f(dm), fv = exp2f(dv);
+    if (kEntropy) e = fm * fmaf(dm, s, e) + fv * fmaf(dv, v.y, ve);
+    s = s * fm + v.y * fv;
+    m = mx;
+  }
+  const float wm = warp_max(m);
+  if (lane == 0) s_max[warp] = wm;
+  __syncthreads();
+  float mx = s_max[0];
+#pragma unroll
+  for (int i = 1; i < kRowWarps; ++i) mx = fmaxf(mx, s_max[i]);
+  const float d = m == mx ? 0.f : fmaxf(m - mx, -200.f), f = exp2f(d);
+  if (kEntropy) e = block_sum(f * fmaf(d, s, e), s_f);
+  s = block_sum(s * f, s_f);
+  if (tid != 0) return;
+  const float y = fmaf(s_exact, R.scale2, -mx);
+  const float was = fmaf(R.entry_logit[row], R.scale2, -mx);
+  const float p = exp2f(y), p_was = exp2f(was);
+  s += p - p_was;
+  const float log2_s = log2f(s);
+  R.loss[t] = (y - log2_s) * kLn2;
+  if (R.lse != nullptr) R.lse[t] = fmaf(mx, kLn2, log2_s * kLn2);
+  if (kEntropy) {
+    e += (p > 0.f ? p * y : p) - (p_was > 0.f ? p_was * was : p_was);
+    R.entropy[t] = (log2_s - e / s) * kLn2;
+  }
+}
+
+// What the gradient of a logit is formed from, for upstream gradients r of a token's log
+// probability and h of its entropy H, a the logit scale:
+//   g_j = a ( r [j = y] - q (r + h H + h ln 2 log2 q) )
+// row_q = (coefficient of q, log2 of the softmax denominator), row_b = that of q log2 q,
+// entry_g = g at the target.  All of them lack the fraction of the first token's a r, which
+// is every token's where all share one coefficient: in bf16 it would be rounded with every
+// r (1 - q) of a q near 0 in the same way (see finalise_kernel; Ctrl::rest).
+__global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const RowParams R) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int row = blockIdx.x * kRowThreads + threadIdx.x;
+  const int n_valid = R.ctrl->n_valid;
+  if (n_valid == 0 && row == 0) R.ctrl->rest = 1.0f;
+  if (row >= n_valid) return;
+  const int first = R.row_of[0], t = R.row_of[row];
+  float power;
+  const float r0 = R.g_logprob != nullptr ? R.g_logprob[first] : 0.f;
+  const float rest = fraction_of((r0 != 0.f ? r0 : R.g_entropy != nullptr ? R.g_entropy[first] : 0.f) * R.logit_scale, power);
+  if (row == 0) R.ctrl->rest = rest;
+  const float scale = R.logit_scale / rest;
+  const float r = R.g_logprob != nullptr ? R.g_logprob[t] * scale : 0.f, h = R.g_entropy != nullptr ? R.g_entropy[t] * scale : 0.f;
+  const float entropy = R.g_entropy != nullptr ? R.entropy_in[t] : 0.f;
+  const float log_q = R.logprob_in[t], q = expf(log_q);
+  R.row_q[row] = make_float2(-fmaf(h, entropy, r), R.lse_in[t] * (1.0f / kLn2));
+  R.row_b[row] = -h * kLn2;
+  R.entry_g[row] = r * -expm1f(log_q) - (q > 0.f ? h * q * (log_q + entropy) : 0.f);
+}
+
 // dX of the tokens that count, in token order: the partial sums joined, always in the
 // same order.  Four columns a thread, or, kWays > 1, kWays neighbouring lanes that
 // take a stretch of the runs each: with the many runs of a small launch one memory
@@ -705,6 +806,17 @@ cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms,
   if (R.in_place) return finalise_with<256, false, true, 2>(R, C, grid, stream);
   return C.g != nullptr ? finalise_with<128, true, false, 4>(R, C, grid, stream)
                         : finalise_with<128, false, false, 2>(R, C, grid, stream);
+}
+
+cudaError_t launch_logprob(const RowParams& R, cudaStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(R.tokens));
+  if (R.in_place) return launch(R.entropy != nullptr ? logprob_kernel<true, true> : logprob_kernel<true, false>, grid, true, stream, R);
+  return launch(R.entropy != nullptr ? logprob_kernel<false, true> : logprob_kernel<false, false>, grid, true, stream, R);
+}
+
+cudaError_t launch_logprob_grad(const RowParams& R, cudaStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(R.tokens > 0 ? (R.tokens + kRowThreads - 1) / kRowThreads : 1));
+  return launch(logprob_grad_kernel, grid, true, stream, R);
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {
