@@ -9,10 +9,16 @@
 // Forward: one pass over the logits.  A block takes a row, or, where there are few rows,
 // the blocks of a cluster take a run of its columns each and join over distributed shared
 // memory.  A thread keeps the maximum, S and E of its elements in registers and rescales
-// once a tile.  The alternatives come out of the same pass: elements above the running
-// threshold go into a list in shared memory, and where the list is long its `top` best
-// raise the threshold.  A first threshold comes from the threads' maxima over the first
-// tile, of which the top-th largest is below top different elements.
+// once a tile.  The alternatives come out of the same pass: the numbers of 16-byte vectors
+// whose largest element reaches a threshold go into a list of the warp's, and when the row
+// has ended those vectors, a few times `top`, are read again (out of L2) and the best of
+// their elements kept.  (Elements or vectors put aside as they come cost as much as the
+// sums.)  The threshold comes from the threads' running maxima: of a warp's 32 the want-th
+// largest, and of those values the m-th largest over the warps, want * m >= top, is reached by
+// at least `top` different elements.  It is formed again after 1, 2, 4, 8, ... tiles.  After
+// the first tile the warps run without a barrier until the row ends; nothing is called within
+// the loop, because what lives across a call is stored with every tile.  A warp whose list
+// does not hold all (a row that ascends) reads its part again.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -34,12 +40,16 @@ namespace ptx = muon::ptx;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kVectors = 4;  // 16-byte loads of one tile a thread
+constexpr int kVectors = 4;  // 16-byte loads of one tile a thread (forward: Cells::kVectors)
 constexpr int kTileVectors = kThreads * kVectors;
-constexpr int kList = 2048;  // candidates in shared memory; a cluster's lists fit one
+// Blocks on an SM, which leaves a thread 64 registers.  (4096 x 163840 bf16 with 64
+// alternatives, us: 402 with 3 blocks, 375 with 4, 434 with 5, whose registers spill.)
+constexpr int kBlocksPerSm = 4;
+constexpr int kVectorList = 256;  // of a warp
 constexpr int kMaxTop = 128;
+constexpr int kKeys = kMaxTop + 32 * 8;  // candidates of a warp: the best, and a vector a lane
 constexpr int kMaxCluster = 8;
-static_assert(kMaxCluster * kMaxTop <= kList, "the joined lists");
+static_assert(kMaxCluster * kMaxTop <= kWarps * kKeys, "a cluster's best fit a block's candidates");
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kFloor = -200.0f;  // exponents of 2 from here down give 0, and stay finite in products
@@ -47,7 +57,7 @@ constexpr float kFloor = -200.0f;  // exponents of 2 from here down give 0, and 
 struct LogitsParams {
   const void* z;
   long long ld;
-  int tokens, vocab, top, mark;
+  int tokens, vocab, top;
   float scale2;  // logit_scale * log2(e)
   const int64_t* targets;
   float* logprob;
@@ -92,11 +102,38 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// Pairs of floats in one instruction each.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 // Elements of a 16-byte vector.
 template <bool kFp32>
 struct Cells {
   using T = std::conditional_t<kFp32, float, __nv_bfloat16>;
   static constexpr int kEach = kFp32 ? 4 : 8;
+  // Of one tile a thread: 32 elements, whose arithmetic covers the next tile's loads.  (2048 x
+  // 163840 fp32 without and with 64 alternatives, us: 223 and 391 with 4, 212 and 282 with 8.)
+  static constexpr int kVectors = kFp32 ? 8 : 4;
+  static constexpr int kTileVectors = kThreads * kVectors;
   static constexpr uint32_t kLowest = kFp32 ? 0xFF800000u : 0xFF80FF80u;  // -inf throughout
   static __device__ __forceinline__ float value(const uint4& v, int e) {
     if constexpr (kFp32) {
@@ -105,6 +142,28 @@ struct Cells {
       const uint32_t w = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
       return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
     }
+  }
+};
+
+// A vector's largest element (a NaN does not show): of bf16 as the larger of its even and of
+// its odd elements, without taking them apart.
+template <bool kFp32>
+struct Largest {
+  std::conditional_t<kFp32, float, __nv_bfloat162> x;
+  static __device__ __forceinline__ __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+  static __device__ __forceinline__ Largest of(const uint4& v) {
+    Largest l;
+    if constexpr (kFp32) l.x = fmaxf(max3(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z)), __uint_as_float(v.w));
+    else l.x = __hmax2(__hmax2(two(v.x), two(v.y)), __hmax2(two(v.z), two(v.w)));
+    return l;
+  }
+  __device__ __forceinline__ void join(const Largest& o) {
+    if constexpr (kFp32) x = fmaxf(x, o.x);
+    else x = __hmax2(x, o.x);
+  }
+  __device__ __forceinline__ float value() const {
+    if constexpr (kFp32) return x;
+    else return fmaxf(__low2float(x), __high2float(x));
   }
 };
 
@@ -144,10 +203,19 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 }
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 
+constexpr uint32_t kLowestOrdered = 0x007FFFFFu;  // of minus infinity
+
 // Value above, column counted down below: larger keys come first, equal logits by column.
+// The lower half of a bf16 logit's 32 bits says nothing and is left out.
 typedef unsigned long long Key;
+template <bool kFp32>
 __device__ __forceinline__ Key make_key(const LogitsParams& P, float x, int column) {
-  return (static_cast<Key>(ordered(x)) << P.index_bits) | static_cast<unsigned>(P.vocab - 1 - column);
+  return (static_cast<Key>(ordered(x) >> (kFp32 ? 0 : 16)) << P.index_bits) | static_cast<unsigned>(P.vocab - 1 - column);
+}
+template <bool kFp32>
+__device__ __forceinline__ float value_of(const LogitsParams& P, Key k) {
+  const uint32_t o = static_cast<uint32_t>(k >> P.index_bits);
+  return unordered(kFp32 ? o : (o << 16) | (o & 0x8000u ? 0u : 0xFFFFu));
 }
 
 // Running statistics in powers of 2: y = z scale2, reference m = the largest y, rounded,
@@ -173,38 +241,55 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
   return Sums{m, a.s + b.s, a.e + b.e};
 }
 
+// The sum of d 2^d over a thread's elements, read again, with exponents from kFloor on.
+template <bool kFp32>
+__device__ __noinline__ float weighted_again(const uint4* cells, int begin, int end, float scale2, float base) {
+  float sum = 0.f;
+#pragma unroll 1
+  for (int i = begin + static_cast<int>(threadIdx.x); i < end; i += kThreads) {
+    const uint4 v = cells[i];
+    float part = 0.f;
+#pragma unroll
+    for (int e = 0; e < Cells<kFp32>::kEach; ++e) {
+      const float d = max_nan(fmaf(Cells<kFp32>::value(v, e), scale2, base), kFloor);
+      part = fmaf(ex2(d), d, part);
+    }
+    sum += part;
+  }
+  return sum;
+}
+
+__device__ __forceinline__ Sums from_lane(const Sums& a, int lane) {
+  return Sums{__shfl_sync(0xFFFFFFFFu, a.m, lane), __shfl_sync(0xFFFFFFFFu, a.s, lane), __shfl_sync(0xFFFFFFFFu, a.e, lane)};
+}
+
 struct Shared {
-  Key list[kList];
-  Key kept_keys[kMaxTop];
-  int count;        // candidates appended, more than kList where some found no room
-  int kept;
+  Key list[kWarps * kKeys];  // candidates: kKeys a warp, at the end the block's first `count`
+  int vectors[kWarps][kVectorList + 32];  // the last 32 for what finds no room
+  int count, counts[kWarps];
+  uint32_t reached[kWarps];  // ordered
   Sums sums[kWarps];
   Sums all;
 };
 
-// Sum over the block.
-__device__ __forceinline__ int block_total(int n, int* scratch) {
-  n = __reduce_add_sync(0xFFFFFFFFu, n);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = n;
-  __syncthreads();
-  int t = 0;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) t += scratch[i];
-  return t;
-}
+// The `top` largest of the n > top candidates, to the front in their order, by one warp.
+// Two bisections, of 32-bit numbers: for the top-th largest logit, and, where others equal
+// it, for the column up to which they stay.
+struct Cut {
+  uint32_t value;   // candidates above it stay,
+  uint32_t behind;  // and those of this value from here on (columns are counted down)
+};
 
-// Largest key that at least `top` of the block's keys reach, by bisection; `count_from`
-// counts a thread's keys not below its argument.
+// The largest x that at least `top` of the lanes' numbers reach; fewer reach hi.
 template <typename Count>
-__device__ __forceinline__ Key best_from(int top, Key lo, Key hi, int* scratch, Count count_from) {
-  // at least `top` keys reach lo, fewer reach hi
+__device__ __forceinline__ uint32_t bisect(int top, uint32_t lo, uint32_t hi, int* reach, Count count_from) {
   while (hi - lo > 1) {
-    const Key mid = lo + (hi - lo) / 2;
-    const int n = block_total(count_from(mid), scratch);
-    if (n >= top) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    const int c = __reduce_add_sync(0xFFFFFFFFu, count_from(mid));
+    if (c >= top) {
       lo = mid;
-      if (n == top) break;
+      *reach = c;
+      if (c == top) break;
     } else {
       hi = mid;
     }
@@ -212,85 +297,163 @@ __device__ __forceinline__ Key best_from(int top, Key lo, Key hi, int* scratch, 
   return lo;
 }
 
-// Keeps the `top` largest of list[0, n), in any order.  All threads call.
-__device__ __noinline__ void keep_best(const LogitsParams& P, Shared& sh, int n, int* scratch) {
-  Key mine[kList / kThreads];
+template <int kEach>  // candidates a lane
+__device__ __forceinline__ Cut find_cut(const Key* list, int n, int top, int bits, int lane) {
+  uint32_t value[kEach], column[kEach], low = 0xFFFFFFFFu, high = 0u;
+  const uint32_t columns = (1u << bits) - 1u;
 #pragma unroll
-  for (int i = 0; i < kList / kThreads; ++i) {
-    const int at = i * kThreads + static_cast<int>(threadIdx.x);
-    mine[i] = at < n ? sh.list[at] : 0;
+  for (int i = 0; i < kEach; ++i) {
+    const bool there = i * 32 + lane < n;
+    const Key k = there ? list[i * 32 + lane] : 0;
+    value[i] = static_cast<uint32_t>(k >> bits);
+    column[i] = static_cast<uint32_t>(k) & columns;
+    low = min(low, there ? value[i] : 0xFFFFFFFFu);
+    high = max(high, value[i]);
   }
-  const Key from = best_from(P.top, 0, 1ull << (32 + P.index_bits), scratch, [&](Key k) {
+  low = __reduce_min_sync(0xFFFFFFFFu, low);
+  high = __reduce_max_sync(0xFFFFFFFFu, high);
+  Cut cut = {low, 0u};
+  int reach = n;
+  cut.value = bisect(top, low, high + 1u, &reach, [&](uint32_t x) {
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < kList / kThreads; ++i) c += mine[i] >= k;
+    for (int i = 0; i < kEach; ++i) c += value[i] >= x;
     return c;
   });
-  __syncthreads();
-  if (threadIdx.x == 0) sh.count = 0;
-  __syncthreads();
+  if (reach > top) {
+    int above = 0;
 #pragma unroll
-  for (int i = 0; i < kList / kThreads; ++i) {
-    const int at = i * kThreads + static_cast<int>(threadIdx.x);
-    if (at < n && mine[i] >= from) sh.list[atomicAdd(&sh.count, 1)] = mine[i];
+    for (int i = 0; i < kEach; ++i) above += value[i] > cut.value;
+    above = __reduce_add_sync(0xFFFFFFFFu, above);
+    cut.behind = bisect(top - above, 0u, columns + 1u, &reach, [&](uint32_t x) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) c += value[i] == cut.value && column[i] >= x;
+      return c;
+    });
   }
-  __syncthreads();
+  return cut;
 }
 
-// Where a tile has more candidates than the list holds (many equal logits, or a row that
-// ascends): of the list only what came before this tile counts, and the tile's elements
-// are read again.
-template <bool kFp32>
-__device__ __noinline__ void keep_best_of_tile(const LogitsParams& P, Shared& sh, const typename Cells<kFp32>::T* row, int shift,
-                                               int v0, int end, int* scratch) {
-  const int from = max(0, v0 * Cells<kFp32>::kEach - shift);
-  const int to = min(P.vocab, min(end, v0 + kTileVectors) * Cells<kFp32>::kEach - shift);
-  const Key columns = (1ull << P.index_bits) - 1;
-  int earlier = 0;
-  for (int i = threadIdx.x; i < kList; i += kThreads) earlier += P.vocab - 1 - static_cast<int>(sh.list[i] & columns) < from;
-  earlier = block_total(earlier, scratch);
-  auto each = [&](auto&& visit) {
-    for (int i = threadIdx.x; i < earlier; i += kThreads) visit(sh.list[i]);
-#pragma unroll 4
-    for (int c = from + static_cast<int>(threadIdx.x); c < to; c += kThreads) visit(make_key(P, static_cast<float>(row[c]), c));
-  };
-  const Key best = best_from(P.top, 0, 1ull << (32 + P.index_bits), scratch, [&](Key k) {
-    int n = 0;
-    each([&](Key x) { n += x >= k; });
-    return n;
-  });
-  __syncthreads();
-  if (threadIdx.x == 0) sh.count = 0;
-  __syncthreads();
-  each([&](Key x) {
-    if (x >= best) sh.kept_keys[atomicAdd(&sh.count, 1)] = x;
-  });
-  __syncthreads();
-  for (int i = threadIdx.x; i < P.top; i += kThreads) sh.list[i] = sh.kept_keys[i];
-  __syncthreads();
+__device__ __noinline__ void keep_best(Key* list, int n, int top, int bits, int lane) {
+  static_assert(kWarps * kMaxTop <= 32 * 32 && kKeys <= 32 * 32, "all candidates in registers");
+  __syncwarp();
+  const Cut cut = n <= 64 ? find_cut<2>(list, n, top, bits, lane)
+                  : n <= 192 ? find_cut<6>(list, n, top, bits, lane)
+                  : n <= 384 ? find_cut<12>(list, n, top, bits, lane) : find_cut<32>(list, n, top, bits, lane);
+  int kept = 0;
+  for (int i = 0; i < n; i += 32) {
+    const Key k = i + lane < n ? list[i + lane] : 0;
+    const uint32_t value = static_cast<uint32_t>(k >> bits), column = static_cast<uint32_t>(k) & ((1u << bits) - 1u);
+    const bool keep = i + lane < n && (value > cut.value || (value == cut.value && column >= cut.behind));
+    const unsigned who = __ballot_sync(0xFFFFFFFFu, keep);
+    if (keep) list[kept + __popc(who & ((1u << lane) - 1u))] = k;  // at or before its place: read already
+    kept += __popc(who);
+    __syncwarp();
+  }
 }
 
-// The smallest value among the list's first n keys, as a float.
-__device__ __forceinline__ float lowest(const LogitsParams& P, const Shared& sh, int n, int* scratch) {
-  uint32_t low = 0xFFFFFFFFu;
-  for (int i = threadIdx.x; i < n; i += kThreads) low = min(low, static_cast<uint32_t>(sh.list[i] >> P.index_bits));
-  low = __reduce_min_sync(0xFFFFFFFFu, low);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = static_cast<int>(low);
-  __syncthreads();
-  low = 0xFFFFFFFFu;
+// A value that at least `want` of the warp's 32 maxima reach: the largest such, but for a
+// 64th of their range.
+__device__ __forceinline__ uint32_t reached_by(uint32_t mine, int want) {
+  const uint32_t high = __reduce_max_sync(0xFFFFFFFFu, mine);
+  if (want == 1) return high;
+  uint32_t lo = __reduce_min_sync(0xFFFFFFFFu, mine), step = high - lo;
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) low = min(low, static_cast<uint32_t>(scratch[i]));
-  return unordered(low);
+  for (int i = 0; i < 6; ++i) {
+    step = (step + 1) >> 1;
+    if (__popc(__ballot_sync(0xFFFFFFFFu, mine >= lo + step)) >= want) lo += step;
+  }
+  return lo;
+}
+
+// The m-th largest of the warps' values.
+__device__ __forceinline__ uint32_t mth_of(const volatile uint32_t* v, int m, int lane) {
+  const uint32_t mine = v[lane & (kWarps - 1)];
+  int not_less = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) not_less += v[i] >= mine;
+  // of the values that at least m reach the largest
+  return __reduce_max_sync(0xFFFFFFFFu, not_less >= m ? mine : 0u);
+}
+
+// The elements from `threshold` on of a warp's vectors as candidates; at most kMaxTop stay,
+// the `top` largest where they are cut.
+template <bool kFp32>
+struct Collector {
+  const LogitsParams& P;
+  Key* keys;
+  const uint4* cells;
+  int shift, lane, count;
+  float threshold;
+
+  // a vector a lane, or none (negative)
+  __device__ __forceinline__ void take(int index) {
+    using C = Cells<kFp32>;
+    const bool all = !(threshold > -INFINITY);
+    unsigned keep = 0;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (index >= 0) {
+      v = cells[index];
+#pragma unroll
+      for (int e = 0; e < C::kEach; ++e) keep |= static_cast<unsigned>(C::value(v, e) >= threshold || all) << e;
+    }
+    // places in the order of the lanes
+    int at = __popc(keep);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int below = __shfl_up_sync(0xFFFFFFFFu, at, o);
+      if (lane >= o) at += below;
+    }
+    const int added = __shfl_sync(0xFFFFFFFFu, at, 31);
+    at += count - __popc(keep);
+    for (; keep != 0; keep &= keep - 1) {
+      const int e = __ffs(keep) - 1, word = kFp32 ? e : e >> 1;
+      const uint32_t bits = word == 0 ? v.x : word == 1 ? v.y : word == 2 ? v.z : v.w;
+      const float x = __uint_as_float(kFp32 ? bits : e & 1 ? bits & 0xFFFF0000u : bits << 16);
+      keys[at++] = make_key<kFp32>(P, x, index * C::kEach - shift + e);
+    }
+    __syncwarp();
+    count += added;
+    if (count > kMaxTop) {
+      keep_best(keys, count, P.top, P.index_bits, lane);
+      count = P.top;
+    }
+  }
+};
+
+// Of the vectors that the warp put in its list, or, where it did not hold all, of every one of
+// its part that qualifies.  `first`: threshold of the first tile, later elements equal to which
+// come after the top that there are.
+template <bool kFp32>
+__device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uint4* cells, int shift, int begin, int end, int listed,
+                                    float first, float threshold) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Collector<kFp32> c = {P, sh.list + warp * kKeys, cells, shift, lane, 0, threshold};
+  __syncwarp();
+  if (listed <= kVectorList) {
+    for (int i = 0; i < listed; i += 32) c.take(i + lane < listed ? sh.vectors[warp][i + lane] : -1);
+  } else {
+    for (int v0 = begin + static_cast<int>(threadIdx.x) - lane; v0 < end; v0 += kThreads) {
+      const int index = v0 + lane;
+      const bool early = v0 < begin + Cells<kFp32>::kTileVectors;
+      bool mark = false;
+      if (index < end) {
+        const float x = Largest<kFp32>::of(cells[index]).value();
+        mark = early ? x >= threshold || !(threshold > -INFINITY) : x >= threshold && x > first;
+      }
+      if (__any_sync(0xFFFFFFFFu, mark)) c.take(mark ? index : -1);
+    }
+  }
+  return c.count;
 }
 
 template <bool kFp32, bool kTop>
-__global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_constant__ LogitsParams P) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const __grid_constant__ LogitsParams P) {
   using C = Cells<kFp32>;
-  constexpr int kEach = C::kEach;
+  constexpr int kEach = C::kEach, kVectors = C::kVectors, kTileVectors = C::kTileVectors;
   extern __shared__ __align__(16) unsigned char raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);
-  __shared__ int scratch[kWarps];
   __shared__ float s_target;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int parts = static_cast<int>(gridDim.x), part = static_cast<int>(blockIdx.x);
@@ -320,152 +483,213 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
       else s_target = __bfloat162float(row[y]);
     }
   }
-  if (kTop) {
-    if (tid == 0) sh.count = 0;
-    __syncthreads();
-  }
-
+  // vectors from the 16-byte boundary at or below the row's start; the ones that lie in the row
+  // as a whole are dealt out to the blocks, the elements before and behind them (at most two
+  // vectors less two elements) go to one lane each at the end
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(typename C::T));
-  const int vectors = static_cast<int>((static_cast<long long>(shift) + P.vocab + kEach - 1) / kEach);
-  const int begin = static_cast<int>(static_cast<long long>(vectors) * part / parts);
-  const int end = static_cast<int>(static_cast<long long>(vectors) * (part + 1) / parts);
+  const uint4* const cells = reinterpret_cast<const uint4*>(row - shift);
+  const int whole0 = shift > 0 ? 1 : 0, whole1 = max(whole0, static_cast<int>((static_cast<long long>(shift) + P.vocab) / kEach));
+  const int begin = whole0 + static_cast<int>(static_cast<long long>(whole1 - whole0) * part / parts);
+  const int end = whole0 + static_cast<int>(static_cast<long long>(whole1 - whole0) * (part + 1) / parts);
 
   Sums a = {-INFINITY, 0.f, 0.f};
-  float threshold = -INFINITY;
-  bool first = true;
-  uint4 next[kVectors];
+  float threshold = -INFINITY, most = -INFINITY;  // `most`: of the thread's elements so far
+  // `active` warps whose threads all have elements: m of them, and want maxima of each, make
+  // top; want > 32: everything is a candidate
+  const int active = min(kWarps, (end - begin) / 32), want = active > 0 ? (P.top + active - 1) / active : 33;
+  const int m = (P.top + want - 1) / want;
+  auto note_reached = [&]() {
+    const uint32_t t = want <= 32 && warp < active ? reached_by(ordered(most), want) : kLowestOrdered;
+    if (lane == 0) *const_cast<volatile uint32_t*>(&sh.reached[warp]) = t;
+  };
+  float bound = -INFINITY, first = -INFINITY;  // a vector is listed from `bound` on
+  int listed = 0;
+  const uint64_t scale = pair(P.scale2, P.scale2);
+  uint4 v[kVectors];
+  auto load = [&](int v0, int i, bool whole) {
+    const uint4* src = cells + v0 + i * kThreads + tid;
+    if (whole) return __ldcs(src);
+    return v0 + i * kThreads + tid < end ? __ldcs(src) : make_uint4(C::kLowest, C::kLowest, C::kLowest, C::kLowest);
+  };
 #pragma unroll
-  for (int i = 0; i < kVectors; ++i) next[i] = load_vector<kFp32>(row, P.vocab, shift, begin + i * kThreads + tid, end);
-  for (int v0 = begin; v0 < end; v0 += kTileVectors) {
-    uint4 v[kVectors];
+  for (int i = 0; i < kVectors; ++i) v[i] = load(begin, i, begin + kTileVectors <= end);
+  int tile = 0;
+  for (int v0 = begin; v0 < end; v0 += kTileVectors, ++tile) {
+    Largest<kFp32> largest[kVectors];
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i) v[i] = next[i];
-    if (v0 + kTileVectors < end) {
+    for (int i = 0; i < kVectors; ++i) largest[i] = Largest<kFp32>::of(v[i]);
+    Largest<kFp32> all_of = largest[0];
 #pragma unroll
-      for (int i = 0; i < kVectors; ++i)
-        next[i] = load_vector<kFp32>(row, P.vocab, shift, v0 + kTileVectors + i * kThreads + tid, end);
-    }
-    float top_of[kVectors], most = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kVectors; ++i) {
-      float x = C::value(v[i], 0);
-#pragma unroll
-      for (int e = 1; e + 1 < kEach; e += 2) x = max3(x, C::value(v[i], e), C::value(v[i], e + 1));
-      top_of[i] = fmaxf(x, C::value(v[i], kEach - 1));
-      most = fmaxf(most, top_of[i]);
+    for (int i = 1; i < kVectors; ++i) all_of.join(largest[i]);
+    const float here = all_of.value();
+    most = fmaxf(most, here);
+    if (kTop && (tile & (tile + 1)) == 0) {
+      note_reached();
+      if (tile == 0) __syncthreads();
+      // later others' may be of earlier tiles, and lower
+      threshold = fmaxf(threshold, unordered(mth_of(sh.reached, m, lane)));
+      bound = fmaxf(bound, threshold);
     }
     const float reference = most * P.scale2;
     if (reference > a.m) rescale(a, reference);
     const float base = a.m == -INFINITY ? 0.f : -a.m;
-    float s[2] = {0.f, 0.f}, w[2] = {0.f, 0.f};
+    const uint64_t from = pair(base, base);
+    uint64_t s = 0, w = 0;  // pairs of zeros
+    const int left = end - v0 - tid;
+    const bool more = v0 + kTileVectors < end, whole = v0 + 2 * kTileVectors <= end;
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i)
+    for (int i = 0; i < kVectors; ++i) {
+      if (i * kThreads < left) {
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const float d = max_nan(fmaf(C::value(v[i], e), P.scale2, base), kFloor);
-        const float p = ex2(d);
-        s[e & 1] += p;
-        w[e & 1] = fmaf(p, d, w[e & 1]);
+        for (int e = 0; e < kEach; e += 2) {
+          const uint64_t d = fma2(pair(C::value(v[i], e), C::value(v[i], e + 1)), scale, from);
+          float d0, d1;
+          unpair(d, d0, d1);
+          const uint64_t p = pair(ex2(d0), ex2(d1));
+          s = add2(s, p);
+          w = fma2(p, d, w);
+        }
       }
-    a.s += s[0] + s[1];
-    a.e += w[0] + w[1];
+      // the next tile's vector takes the place
+      if (more) v[i] = load(v0 + kTileVectors, i, whole);
+    }
+    float lo, hi;
+    unpair(w, lo, hi);
+    a.e += lo + hi;
+    unpair(s, lo, hi);
+    a.s += lo + hi;
 
     if constexpr (kTop) {
-      const int here = min(end - v0, kTileVectors);
-      if (first && here >= P.top) {
-        // the top-th largest of the threads' maxima, to 16 bits: as many elements reach it
-        const uint32_t mine = ordered(most) >> 16;
-        uint32_t lo = 0;
-        const bool some = tid < here;
-#pragma unroll 1
-        for (uint32_t b = 0x8000u; b > 0; b >>= 1)
-          if (__syncthreads_count(some && mine >= (lo | b)) >= P.top) lo |= b;
-        threshold = unordered(max(lo << 16, 0x007FFFFFu));
-      }
-      int last = -1;
-      const bool all = first && !(threshold > -INFINITY);
+      const bool every = tile == 0 && !(bound > -INFINITY);  // NaNs, too
+      if (__any_sync(0xFFFFFFFFu, here >= bound || every)) {
 #pragma unroll
-      for (int i = 0; i < kVectors; ++i) {
-        const int index = v0 + i * kThreads + tid;
-        if ((top_of[i] > threshold || (first && top_of[i] == threshold) || all) && index < end) {
-          const int column0 = index * kEach - shift;
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) {
-            const float x = C::value(v[i], e);
-            const int column = column0 + e;
-            if ((x > threshold || (first && x == threshold) || all) && column >= 0 && column < P.vocab) {
-              last = atomicAdd(&sh.count, 1);
-              if (last < kList) sh.list[last] = make_key(P, x, column);
-            }
-          }
+        for (int i = 0; i < kVectors; ++i) {
+          const bool in = (largest[i].value() >= bound || every) && i * kThreads < left;
+          const unsigned who = __ballot_sync(0xFFFFFFFFu, in);
+          if (in) sh.vectors[warp][min(listed, kVectorList) + __popc(who & ((1u << lane) - 1u))] = v0 + i * kThreads + tid;
+          listed += __popc(who);
         }
       }
-      // positions are given out one by one: one past the mark is seen by the thread that got it
-      if (__syncthreads_or(last >= P.mark)) {
-        const int n = sh.count;
-        if (n > kList) {
-          keep_best_of_tile<kFp32>(P, sh, row, shift, v0, end, scratch);
-        } else {
-          keep_best(P, sh, n, scratch);
-        }
-        threshold = lowest(P, sh, P.top, scratch);
-        __syncthreads();
+      // later elements have larger columns: one that equals the first tile's threshold comes
+      // after the top that there are
+      if (tile == 0) {
+        first = bound;
+        bound = unordered(ordered(bound) + 1u);
       }
-      first = false;
     }
+  }
+  // 0 times an exponent of minus infinity, most often
+  if (!(a.e == a.e)) a.e = weighted_again<kFp32>(cells, begin, end, P.scale2, a.m == -INFINITY ? 0.f : -a.m);
+
+  // elements outside whole vectors
+  float extra = 0.f;
+  int extra_at = -1;
+  if (part == 0 && warp == 0) {
+    const int head = whole0 * kEach - shift, behind = min(P.vocab, whole1 * kEach - shift);
+    const int column = lane < min(head, P.vocab) ? lane : behind + lane - min(head, P.vocab);
+    const bool mine = column < P.vocab;
+    const float x = mine ? static_cast<float>(row[column]) : -INFINITY;
+    const float y = x * P.scale2, m = fmaxf(a.m, y);
+    if (mine) {
+      rescale(a, m);
+      const float d = m == -INFINITY ? kFloor : max_nan(fmaf(x, P.scale2, -m), kFloor), p = ex2(d);
+      a.s += p;
+      a.e = fmaf(p, d, a.e);
+    }
+    extra = x;
+    extra_at = mine ? column : -1;
   }
 
   // statistics: warp, block, cluster
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const Sums b = {__shfl_xor_sync(0xFFFFFFFFu, a.m, o), __shfl_xor_sync(0xFFFFFFFFu, a.s, o),
-                    __shfl_xor_sync(0xFFFFFFFFu, a.e, o)};
-    a = join(a, b);
+    a = join(a, from_lane(a, lane ^ o));
   }
   if (lane == 0) sh.sums[warp] = a;
   if (kTop) {
+    int count = collect<kFp32>(P, sh, cells, shift, begin, end, listed, first, threshold);
+    if (warp == 0) {
+      const unsigned who = __ballot_sync(0xFFFFFFFFu, extra_at >= 0);
+      if (extra_at >= 0) sh.list[count + __popc(who & ((1u << lane) - 1u))] = make_key<kFp32>(P, extra, extra_at);
+      count += __popc(who);
+      __syncwarp();
+      if (count > kMaxTop) {
+        keep_best(sh.list, count, P.top, P.index_bits, lane);
+        count = P.top;
+      }
+    }
+    if (lane == 0) sh.counts[warp] = count;
+    // all warps' candidates one behind the other; what goes down is read first
     __syncthreads();
-    const int n = sh.count;
+    int before = 0, n = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const int c = sh.counts[i];
+      before += i < warp ? c : 0;
+      n += c;
+    }
+    Key mine[kMaxTop / 32];
+#pragma unroll
+    for (int i = 0; i < kMaxTop / 32; ++i)
+      if (i * 32 + lane < count) mine[i] = sh.list[warp * kKeys + i * 32 + lane];
     __syncthreads();
-    if (n > P.top) keep_best(P, sh, n, scratch);
+#pragma unroll
+    for (int i = 0; i < kMaxTop / 32; ++i)
+      if (i * 32 + lane < count) sh.list[before + i * 32 + lane] = mine[i];
+    __syncthreads();
+    // as many as are put in order with a thread each stay; in a cluster as many as its first block holds
+    const bool cut = n > (parts > 1 ? kMaxTop : kThreads);
+    if (warp == 0 && cut) keep_best(sh.list, n, P.top, P.index_bits, lane);
+    if (tid == 0) sh.count = cut ? P.top : n;
   }
   __syncthreads();
-  if (tid == 0) {
-    a = sh.sums[0];
-    for (int i = 1; i < kWarps; ++i) a = join(a, sh.sums[i]);
-    sh.all = a;
-    sh.kept = kTop ? sh.count : 0;
+  if (warp == 0) {
+    a = sh.sums[lane & (kWarps - 1)];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) a = join(a, from_lane(a, lane ^ o));
+    if (lane == 0) sh.all = a;
   }
   __syncthreads();
+  int candidates = kTop ? sh.count : 0;
   if (parts > 1) {
     ptx::cluster_sync_all();
     if (part == 0) {
-      // the other blocks' lists behind this one's, their sums into this one's
-      int n = sh.kept;
-      for (int r = 1; r < parts; ++r) {
-        const uint32_t theirs = ptx::map_to_cta(ptx::smem_u32(raw), static_cast<uint32_t>(r));
-        auto word = [&](size_t at) {
-          uint32_t x;
-          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(theirs + static_cast<uint32_t>(at)));
-          return x;
-        };
-        if (tid == 0) {
-          const Sums b = {__uint_as_float(word(offsetof(Shared, all))), __uint_as_float(word(offsetof(Shared, all) + 4)),
-                          __uint_as_float(word(offsetof(Shared, all) + 8))};
-          sh.all = join(sh.all, b);
+      // the other blocks' lists behind this one's, a warp for each block, and their sums into this one's
+      auto word = [&](int block, size_t at) {
+        uint32_t x;
+        const uint32_t theirs = ptx::map_to_cta(ptx::smem_u32(raw), static_cast<uint32_t>(block)) + static_cast<uint32_t>(at);
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(theirs));
+        return x;
+      };
+      if (kTop) {
+        const int theirs = lane < parts ? static_cast<int>(word(lane, offsetof(Shared, count))) : 0;
+        int before = 0, n = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) {
+          const int c = __shfl_sync(0xFFFFFFFFu, theirs, r);
+          if (r < warp) before += c;
+          if (r == warp) n = c;
+          if (r > 0) candidates += c;
         }
-        if (kTop) {
-          const int more = static_cast<int>(word(offsetof(Shared, kept)));
-          for (int i = tid; i < more; i += kThreads) {
-            const Key lo = word(8 * static_cast<size_t>(i)), hi = word(8 * static_cast<size_t>(i) + 4);
-            sh.list[n + i] = lo | (hi << 32);
+        if (warp > 0)
+          for (int i = lane; i < n; i += 32) {
+            const Key lo = word(warp, 8 * static_cast<size_t>(i)), hi = word(warp, 8 * static_cast<size_t>(i) + 4);
+            sh.list[before + i] = lo | (hi << 32);
           }
-          n += more;
-        }
+      }
+      if (warp == 0) {
+        a = Sums{-INFINITY, 0.f, 0.f};
+        if (lane < parts)
+          a = Sums{__uint_as_float(word(lane, offsetof(Shared, all))), __uint_as_float(word(lane, offsetof(Shared, all) + 4)),
+                   __uint_as_float(word(lane, offsetof(Shared, all) + 8))};
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) a = join(a, from_lane(a, lane ^ o));
+        if (lane == 0) sh.all = a;
       }
       __syncthreads();
-      if (kTop) {
-        if (n > P.top) keep_best(P, sh, n, scratch);
+      if (candidates > kThreads) {
+        if (kTop && warp == 0) keep_best(sh.list, candidates, P.top, P.index_bits, lane);
+        candidates = P.top;
       }
     }
     ptx::cluster_sync_all();  // lists stay until they are read
@@ -481,11 +705,13 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(const __grid_const
     if (P.entropy != nullptr) P.entropy[token] = nothing ? 0.f : (log2_s - all.e / all.s) * kLn2;
     if (P.lse != nullptr) P.lse[token] = nothing ? -INFINITY : fmaf(all.m, kLn2, log2_s * kLn2);
   }
-  if (kTop && tid < P.top) {
+  if (kTop && tid < candidates) {
     const Key mine = sh.list[tid];
-    int place = 0;
-    for (int i = 0; i < P.top; ++i) place += sh.list[i] > mine;
-    const float z = unordered(static_cast<uint32_t>(mine >> P.index_bits));
+    int place = 0;  // how many come before it
+#pragma unroll 4
+    for (int i = 0; i < candidates; ++i) place += sh.list[i] > mine;
+    if (place >= P.top) return;
+    const float z = value_of<kFp32>(P, mine);
     const long long at = token * P.top + place;
     if (P.top_ids != nullptr) P.top_ids[at] = P.vocab - 1 - static_cast<int>(mine & ((1ull << P.index_bits) - 1));
     if (P.top_logits != nullptr) P.top_logits[at] = z;
@@ -609,7 +835,7 @@ int check(const muon_logits_args* a) {
 // The grid's second dimension holds 65535 rows.
 constexpr int kRowsAtOnce = 65535;
 
-// Blocks that share a row: enough for a few on every SM, each with a tile at least.
+// Blocks that share a row: enough for a few on every SM, each with half a tile at least.
 int parts_for(int tokens, long long vectors, int sms) {
   int parts = 1;
   while (parts < kMaxCluster && static_cast<long long>(tokens) * parts * 2 <= 4ll * sms && vectors >= 2ll * parts * kTileVectors / 2) parts *= 2;
@@ -659,7 +885,6 @@ extern "C" int muon_logits_logprob(const muon_logits_args* a, int device, void* 
     P.tokens = rows;
     P.vocab = a->vocab;
     P.top = top ? a->top : 0;
-    P.mark = 8 * a->top < kList ? (8 * a->top > 256 ? 8 * a->top : 256) : kList;
     P.scale2 = a->logit_scale * kLog2e;
     P.targets = a->targets ? a->targets + first : nullptr;
     P.logprob = a->logprob ? a->logprob + first : nullptr;
