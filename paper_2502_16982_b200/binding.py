@@ -173,9 +173,9 @@ def lib():
     L.muon_debug_set_pair_fold.argtypes = [C.c_int]
     L.muon_debug_set_tile_mode.argtypes = [C.c_int]
     L.muon_debug_wait_expiry.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_uint]
-    L.muon_adamw_step.argtypes = [C.POINTER(muon_adamw_tensor), C.c_int, C.POINTER(muon_adamw_hparams), C.c_int,
+    L.muon_adamw_step.argtypes = [C.c_void_p, C.c_int, C.POINTER(muon_adamw_hparams), C.c_int,
                                   C.c_void_p]
-    L.muon_adamw_step_clipped.argtypes = [C.POINTER(muon_adamw_tensor), C.c_int, C.POINTER(muon_adamw_hparams), C.c_void_p,
+    L.muon_adamw_step_clipped.argtypes = [C.c_void_p, C.c_int, C.POINTER(muon_adamw_hparams), C.c_void_p,
                                           C.c_int, C.c_void_p]
     L.muon_grad_norm.argtypes = [C.POINTER(muon_grad_tensor), C.c_int, C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]
@@ -343,24 +343,27 @@ def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, 
     it (NaN: the step changes nothing)."""
     import torch
     n = len(params)
-    arr = (muon_adamw_tensor * n)()
-    for i, (p, g, m, v) in enumerate(zip(params, grads, exp_avgs, exp_avg_sqs)):
+    flat = []  # muon_adamw_tensor as six 64-bit words: four addresses, numel, both dtypes
+    for p, g, m, v in zip(params, grads, exp_avgs, exp_avg_sqs):
+        numel = p.numel()
         for t in (p, g, m, v):
-            if not t.is_contiguous() or t.numel() != p.numel():
+            if not t.is_contiguous() or t.numel() != numel:
                 raise MuonError(MUON_ERR_INVALID_ARG, "AdamW tensors must be contiguous and equally sized")
-        if m.dtype != torch.float32 or v.dtype != torch.float32:
+        if m.dtype is not torch.float32 or v.dtype is not torch.float32:
             raise MuonError(MUON_ERR_INVALID_ARG, "AdamW moments must be fp32")
-        arr[i] = muon_adamw_tensor(p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), p.numel(),
-                                   _dtype_code(p), _dtype_code(g))
+        flat += (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), numel, _dtype_code(p) | _dtype_code(g) << 32)
+    if len(flat) != 6 * n:
+        raise MuonError(MUON_ERR_INVALID_ARG, "as many gradients and moments as parameters")
+    arr = (C.c_int64 * len(flat))(*flat)
     dev = params[0].device.index
-    s = torch.cuda.current_stream(dev) if stream is None else stream
+    s = _raw_stream(stream, dev)
     hp = muon_adamw_hparams(lr, wd, beta1, beta2, eps, int(step))
     if coef is None:
-        _check(lib().muon_adamw_step(arr, n, C.byref(hp), dev, C.c_void_p(s.cuda_stream)))
+        _check(lib().muon_adamw_step(arr, n, C.byref(hp), dev, s))
         return
     if coef.dtype != torch.float32 or coef.numel() != 1 or coef.device != params[0].device:
         raise MuonError(MUON_ERR_INVALID_ARG, "coef must be one fp32 element on the parameters' device")
-    _check(lib().muon_adamw_step_clipped(arr, n, C.byref(hp), coef.data_ptr(), dev, s.cuda_stream))
+    _check(lib().muon_adamw_step_clipped(arr, n, C.byref(hp), coef.data_ptr(), dev, s))
 
 
 _no_context = contextlib.nullcontext()
@@ -814,7 +817,7 @@ class LogitsLogprob(NamedTuple):
 
 
 def _token_vector(t, what, n, dev, dtype):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != dev:
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or t.device != dev:
         raise MuonError(MUON_ERR_INVALID_ARG, "%s must be %d contiguous %s values on one CUDA device" % (what, n, dtype))
     return t.data_ptr()
 
@@ -824,8 +827,10 @@ def _logits_args(logits, targets, logit_scale, top):
     if logits.dim() != 2 or logits.device.type != "cuda" or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise MuonError(MUON_ERR_INVALID_ARG, "logits must be [tokens, vocab] on a CUDA device, with contiguous rows")
     tokens, vocab = logits.shape
-    if (tokens | vocab | abs(top)) >> 31:
+    if (tokens | vocab) >> 31:
         _past_32_bits()
+    if not 0 <= top <= 128:
+        raise MuonError(MUON_ERR_UNSUPPORTED, "0 to 128 alternatives per token")
     a = muon_logits_args(tokens, vocab, logits.data_ptr(), _row_stride(logits) if tokens else vocab, _dtype_code(logits), top,
                          logit_scale)
     if targets is not None:
@@ -842,22 +847,26 @@ def muon_logits_logprob(logits, targets=None, top: int = 0, logit_scale: float =
     include/muon.h.  ``top_ids``, ``top_logits`` and ``lse`` at ``logit_scale`` = 1 /
     temperature are what :func:`muon_head_distill` takes from a teacher."""
     import torch
-    a = _logits_args(logits, targets, logit_scale, int(top))
-    tokens, dev = logits.shape[0], logits.device
+    top = int(top)
+    a = _logits_args(logits, targets, logit_scale, top)
+    tokens, dev = a.tokens, logits.device
     if out is None:
         with torch.cuda.stream(stream) if stream is not None else _no_context:
-            n = 3 if targets is not None else 2
-            rows = torch.empty(n * tokens, dtype=torch.float32, device=dev).split_with_sizes((tokens,) * n)
-            more = (None, None, None)
+            # entropy, lse, logprob, top_logits and top_logprob are parts of one allocation
+            entries = tokens * top if top > 0 else 0
+            sizes = (tokens, tokens, tokens if targets is not None else 0, entries, entries)
+            flat = torch.empty(sum(sizes), dtype=torch.float32, device=dev)
+            entropy, lse, logprob, logits_, logprob_ = flat.split_with_sizes(sizes)
+            at = flat.data_ptr()
+            a.entropy, a.lse = at, at + 4 * tokens
+            if targets is not None:
+                a.logprob = at + 8 * tokens
+            more = ()
             if top > 0:
-                pair = torch.empty((2, tokens, top), dtype=torch.float32, device=dev)
-                more = (torch.empty((tokens, top), dtype=torch.int64, device=dev), pair[0], pair[1])
-        out = LogitsLogprob(rows[2] if targets is not None else None, rows[0], rows[1], *more)
-        a.entropy, a.lse = rows[0].data_ptr(), rows[1].data_ptr()
-        if targets is not None:
-            a.logprob = rows[2].data_ptr()
-        if top > 0:
-            a.top_ids, a.top_logits, a.top_logprob = more[0].data_ptr(), more[1].data_ptr(), more[2].data_ptr()
+                ids = torch.empty((tokens, top), dtype=torch.int64, device=dev)
+                a.top_ids, a.top_logits, a.top_logprob = ids.data_ptr(), at + 4 * sum(sizes[:3]), at + 4 * sum(sizes[:4])
+                more = (ids, logits_.view(tokens, top), logprob_.view(tokens, top))
+            out = LogitsLogprob(logprob if targets is not None else None, entropy, lse, *more)
     else:
         for name in ("logprob", "entropy", "lse"):
             t = getattr(out, name)
@@ -869,7 +878,8 @@ def muon_logits_logprob(logits, targets=None, top: int = 0, logit_scale: float =
                 if t.dtype != dtype or tuple(t.shape) != (tokens, top) or not t.is_contiguous() or t.device != dev:
                     raise MuonError(MUON_ERR_INVALID_ARG, "%s must be contiguous %s [tokens, top] on the logits' device" % (name, dtype))
                 setattr(a, name, t.data_ptr())
-    _check(lib().muon_logits_logprob(C.byref(a), dev.index, _raw_stream(stream, dev.index)))
+    index = dev.index
+    _check(lib().muon_logits_logprob(C.byref(a), index, _raw_stream(stream, index)))
     return out
 
 

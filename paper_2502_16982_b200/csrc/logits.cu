@@ -49,7 +49,8 @@ constexpr int kVectorList = 256;  // of a warp
 constexpr int kMaxTop = 128;
 constexpr int kKeys = kMaxTop + 32 * 8;  // candidates of a warp: the best, and a vector a lane
 constexpr int kMaxCluster = 8;
-static_assert(kMaxCluster * kMaxTop <= kWarps * kKeys, "a cluster's best fit a block's candidates");
+constexpr int kSorted = 2048;  // where a block of a cluster leaves its best in the list of candidates
+static_assert(kMaxCluster * kMaxTop <= kSorted && kSorted + kMaxTop <= kWarps * kKeys, "a cluster's best fit before a block's");
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kFloor = -200.0f;  // exponents of 2 from here down give 0, and stay finite in products
@@ -271,6 +272,14 @@ struct Shared {
   Sums sums[kWarps];
   Sums all;
 };
+
+// How many of the first n keys are larger.
+__device__ __forceinline__ int place_of(const Key* list, int n, Key mine) {
+  int place = 0;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) place += list[i] > mine;
+  return place;
+}
 
 // The `top` largest of the n > top candidates, to the front in their order, by one warp.
 // Two bisections, of 32-bit numbers: for the top-th largest logit, and, where others equal
@@ -637,10 +646,19 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
     for (int i = 0; i < kMaxTop / 32; ++i)
       if (i * 32 + lane < count) sh.list[before + i * 32 + lane] = mine[i];
     __syncthreads();
-    // as many as are put in order with a thread each stay; in a cluster as many as its first block holds
-    const bool cut = n > (parts > 1 ? kMaxTop : kThreads);
-    if (warp == 0 && cut) keep_best(sh.list, n, P.top, P.index_bits, lane);
-    if (tid == 0) sh.count = cut ? P.top : n;
+    // as many as are put in order with a thread each stay
+    const bool cut = n > kThreads;
+    if (cut) {
+      if (warp == 0) keep_best(sh.list, n, P.top, P.index_bits, lane);
+      n = P.top;
+      if (parts > 1) __syncthreads();
+    }
+    // a block of a cluster leaves its best in order
+    if (parts > 1 && tid < n) {
+      const int place = place_of(sh.list, n, sh.list[tid]);
+      if (place < P.top) sh.list[kSorted + place] = sh.list[tid];
+    }
+    if (tid == 0) sh.count = parts > 1 ? min(n, P.top) : n;
   }
   __syncthreads();
   if (warp == 0) {
@@ -669,13 +687,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
           const int c = __shfl_sync(0xFFFFFFFFu, theirs, r);
           if (r < warp) before += c;
           if (r == warp) n = c;
-          if (r > 0) candidates += c;
+          candidates += r > 0 ? c : 0;
         }
-        if (warp > 0)
-          for (int i = lane; i < n; i += 32) {
-            const Key lo = word(warp, 8 * static_cast<size_t>(i)), hi = word(warp, 8 * static_cast<size_t>(i) + 4);
-            sh.list[before + i] = lo | (hi << 32);
-          }
+        for (int i = lane; i < n; i += 32) {
+          const size_t at = 8 * static_cast<size_t>(kSorted + i);
+          const Key lo = word(warp, at), hi = word(warp, at + 4);
+          sh.list[before + i] = lo | (hi << 32);
+        }
       }
       if (warp == 0) {
         a = Sums{-INFINITY, 0.f, 0.f};
@@ -707,9 +725,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
   }
   if (kTop && tid < candidates) {
     const Key mine = sh.list[tid];
-    int place = 0;  // how many come before it
-#pragma unroll 4
-    for (int i = 0; i < candidates; ++i) place += sh.list[i] > mine;
+    const int place = place_of(sh.list, candidates, mine);
     if (place >= P.top) return;
     const float z = value_of<kFp32>(P, mine);
     const long long at = token * P.top + place;
