@@ -730,7 +730,9 @@ int muon_head_distill(const muon_head_args* args, const muon_head_teacher* teach
 /*
  * Synchronise `stream` and read the status of the last call that used this
  * workspace: 0, or MUON_ERR_TIMEOUT if a bounded device-side wait expired (its
- * outputs are then not valid).
+ * outputs are then not valid).  MUON_ERR_INVALID_ARG: muon_head_logprob_grad was
+ * given what a call with other pieces kept (muon_debug_set_head_piece_bytes was called
+ * in between); its gradients are 0.
  */
 int muon_head_status(const void* workspace, int device, void* stream, int* device_status);
 
@@ -748,10 +750,17 @@ int muon_head_status(const void* workspace, int device, void* stream, int* devic
  *     G_j = logit_scale ( r ([j = target] - q_j) - h q_j (log q_j + entropy) )
  *     dx  = G w,   dw = G^T x
  *
- * muon_head_logprob writes logprob, and lse and entropy where they are not NULL.  It keeps
- * no logits.  muon_head_logprob_grad reads logprob, lse and (with g_entropy) entropy as
- * that call wrote them and forms the logits again, a piece of the vocabulary of at most
- * 256 MiB of bf16 gradients at a time.
+ * muon_head_logprob writes logprob, and lse and entropy where they are not NULL.
+ * muon_head_logprob_grad reads logprob, lse and (with g_entropy) entropy as that call wrote
+ * them, and forms the gradient of the logits a piece of the vocabulary of at most 256 MiB of
+ * bf16 at a time.  Where does it have the logits from?
+ *   keep = 0: it forms them again, a third product.  The forward pass keeps none.
+ *   keep != 0: the forward pass leaves what it gathered and up to 3 GiB of logits as 16-bit
+ *     codes (as the losses' larger workspace does, where that is faster) in its workspace.
+ *     That workspace, given as `kept` with its size, is read by the gradient and not written
+ *     to, so that it may be asked for again; x, w, targets, logit_scale and the knobs below
+ *     must be the same and unchanged.  Codes add 2^-12 relative to q and as much absolutely
+ *     to log q, and what lies 2^-32 or more below the largest of its 64 columns counts as 0.
  *
  * Masked tokens (a target outside [0, vocab)), operands, types, strides, dx, dw and
  * dw_accumulate, arithmetic, streams, workspace and errors: as for muon_head_xent.  A
@@ -761,14 +770,14 @@ int muon_head_status(const void* workspace, int device, void* stream, int* devic
  *   g_logprob, g_entropy: DEVICE, one fp32 per token, or NULL for 0; finite.
  *   workspace: DEVICE, 1024-byte aligned, of muon_head_logprob_workspace_bytes: with
  *   grads NULL that of muon_head_logprob, else that of muon_head_logprob_grad.  Of the
- *   pointers it looks at which of entropy, dx and dw are NULL and at the alignment of w.
+ *   pointers it looks at which of entropy, dx, dw and kept are NULL and at the alignment of w.
  *   muon_head_status reads the status of either call from its workspace.
  */
 typedef struct muon_logprob_args {
   int32_t tokens;
   int32_t dim;
   int32_t vocab;
-  int32_t reserved;
+  int32_t keep; /* of muon_head_logprob */
   const void* x;
   const void* w;
   int64_t ld_x;
@@ -794,6 +803,8 @@ typedef struct muon_logprob_grads {
   int32_t dw_dtype;
   int32_t dw_accumulate;
   int32_t reserved;
+  const void* kept;
+  size_t kept_bytes;
 } muon_logprob_grads;
 
 int muon_head_logprob_workspace_bytes(const muon_logprob_args* args, const muon_logprob_grads* grads, size_t* out_bytes);

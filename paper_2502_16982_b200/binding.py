@@ -102,7 +102,7 @@ class muon_head_teacher(C.Structure):
 
 
 class muon_logprob_args(C.Structure):
-    _fields_ = [("tokens", C.c_int32), ("dim", C.c_int32), ("vocab", C.c_int32), ("reserved", C.c_int32),
+    _fields_ = [("tokens", C.c_int32), ("dim", C.c_int32), ("vocab", C.c_int32), ("keep", C.c_int32),
                 ("x", C.c_void_p), ("w", C.c_void_p), ("ld_x", C.c_int64), ("ld_w", C.c_int64),
                 ("x_dtype", C.c_int32), ("w_dtype", C.c_int32), ("targets", C.c_void_p), ("logit_scale", C.c_float),
                 ("reserved2", C.c_int32), ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("lse", C.c_void_p)]
@@ -111,7 +111,7 @@ class muon_logprob_args(C.Structure):
 class muon_logprob_grads(C.Structure):
     _fields_ = [("g_logprob", C.c_void_p), ("g_entropy", C.c_void_p), ("dx", C.c_void_p), ("dw", C.c_void_p),
                 ("ld_dx", C.c_int64), ("ld_dw", C.c_int64), ("dx_dtype", C.c_int32), ("dw_dtype", C.c_int32),
-                ("dw_accumulate", C.c_int32), ("reserved", C.c_int32)]
+                ("dw_accumulate", C.c_int32), ("reserved", C.c_int32), ("kept", C.c_void_p), ("kept_bytes", C.c_size_t)]
 
 
 class muon_logits_args(C.Structure):
@@ -669,11 +669,16 @@ def muon_head_status(workspace, stream=None) -> int:
     return st.value
 
 
-class HeadLogprob(NamedTuple):
-    """Per token, fp32: ``logprob`` of the target, ``entropy`` and ``lse`` (None where not wanted)."""
+class _HeadLogprob(NamedTuple):
     logprob: "torch.Tensor"
     entropy: Optional["torch.Tensor"]
     lse: Optional["torch.Tensor"]
+
+
+class HeadLogprob(_HeadLogprob):
+    """Per token, fp32: ``logprob`` of the target, ``entropy`` and ``lse`` (None where not
+    wanted); ``kept``: the workspace with the logits kept for the gradient, or None."""
+    kept: Optional["torch.Tensor"] = None
 
 
 class HeadGrads(NamedTuple):
@@ -704,8 +709,8 @@ def _logprob_workspace(workspace, dev, a, d):
     """(tensor, first address, bytes) of the workspace of one call."""
     import torch
     if workspace is None:
-        key = (a.tokens, a.dim, a.vocab, -1 if d is None else -2, not a.entropy, d is None or not d.dx, d is None or not d.dw,
-               a.ld_w & 7, (a.w or 0) & 15)
+        key = (a.tokens, a.dim, a.vocab, -1 if d is None else -2, not a.entropy, a.keep if d is None else not d.kept,
+               d is None or not d.dx, d is None or not d.dw, a.ld_w & 7, (a.w or 0) & 15)
         need = _head_bytes.get(key)
         if need is None:
             out = C.c_size_t(0)
@@ -722,28 +727,37 @@ def _logprob_workspace(workspace, dev, a, d):
 
 
 def muon_head_logprob_workspace_bytes(tokens: int, dim: int, vocab: int, grads: bool, entropy: bool = True, dx: bool = True,
-                                      dw: bool = True, packed_head: bool = True) -> int:
+                                      dw: bool = True, packed_head: bool = True, keep: bool = False) -> int:
     """Workspace bytes of :func:`muon_head_logprob` or, with ``grads``, of
     :func:`muon_head_logprob_grad`, 1024 for aligning a tensor's start included.
-    ``packed_head``: the head's rows are 16-byte aligned."""
+    ``packed_head``: the head's rows are 16-byte aligned.  ``keep``: of a forward pass that
+    keeps its logits, or of the gradient after one."""
     if any(C.c_int32(v).value != v for v in (tokens, dim, vocab)):
         _past_32_bits()
-    a = muon_logprob_args(tokens, dim, vocab, 0, None, None, dim, (dim + 7) // 8 * 8 if packed_head else dim | 1,
+    a = muon_logprob_args(tokens, dim, vocab, int(keep), None, None, dim, (dim + 7) // 8 * 8 if packed_head else dim | 1,
                           MUON_DTYPE_BF16, MUON_DTYPE_BF16, None, 1.0, 0, None, 1024 if entropy else None)
     d = muon_logprob_grads(None, None, 1024 if dx else None, 1024 if dw else None)  # only whether they are there counts
+    d.kept = 1024 if keep else None
     out = C.c_size_t(0)
     _check(lib().muon_head_logprob_workspace_bytes(C.byref(a), C.byref(d) if grads else None, C.byref(out)))
     return out.value + 1024
 
 
 def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out: Optional[HeadLogprob] = None, workspace=None,
-                      stream=None) -> HeadLogprob:
+                      stream=None, keep: Optional[bool] = None) -> HeadLogprob:
     """Log probabilities of ``targets`` (int64 [tokens], outside [0, vocab): masked) under
     ``x w^T``, bf16 [tokens, dim] and [vocab, dim], with log-sum-exps and, unless
     ``entropy`` is False, entropies.  ``out``: tensors to write, None in place of what is
-    not wanted.  Argument marshalling only; the formulas are in include/muon.h."""
+    not wanted.
+    ``keep``: up to 3 GiB of logits stay, as 16-bit codes, with the result until it is let go
+    of, and :func:`muon_head_logprob_grad` does not form them again.  By default as torch's
+    gradient mode says (not under ``torch.no_grad()``, for scoring) and not in a workspace of
+    the caller's.  Argument marshalling only; the formulas are in include/muon.h."""
     import torch
     a = _logprob_args(x, w, targets, logit_scale)
+    if keep is None:
+        keep = workspace is None and torch.is_grad_enabled()
+    a.keep = 1 if keep else 0
     tokens, dev = x.shape[0], x.device
     with torch.cuda.stream(stream) if stream is not None else _no_context:
         if out is None:
@@ -759,6 +773,9 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
                 if t is not None:
                     setattr(a, name, _token_vector(t, name, tokens, dev, torch.float32))
         workspace, base, nbytes = _logprob_workspace(workspace, dev, a, None)
+        if keep:
+            out = HeadLogprob(*out)
+            out.kept = workspace
     _check(lib().muon_head_logprob(C.byref(a), base, nbytes, dev.index, _raw_stream(stream, dev.index)))
     return out
 
@@ -767,7 +784,8 @@ def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_
                            dw=None, accumulate_dw=False, workspace=None, stream=None) -> HeadGrads:
     """Gradients of the hidden states and of the head for the gradients ``g_logprob`` and
     ``g_entropy`` (fp32 [tokens] or None) of what :func:`muon_head_logprob` gave as
-    ``saved`` for the same operands.  ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True
+    ``saved`` for the same operands, which must not have changed if it kept its logits; they
+    may be asked for again.  ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True
     to allocate one like x / w, None to leave the gradient out."""
     import torch
     a = _logprob_args(x, w, targets, logit_scale)
@@ -779,6 +797,12 @@ def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_
     a.logprob = _token_vector(saved.logprob, "logprob", tokens, dev, torch.float32)
     a.lse = _token_vector(saved.lse, "lse", tokens, dev, torch.float32)
     d = muon_logprob_grads()
+    kept = getattr(saved, "kept", None)
+    if kept is not None:
+        if kept.device != dev:
+            raise MuonError(MUON_ERR_WORKSPACE, "what the forward pass kept is not on x's device")
+        d.kept = (kept.data_ptr() + 1023) // 1024 * 1024
+        d.kept_bytes = kept.data_ptr() + kept.numel() - d.kept
     if g_logprob is not None:
         d.g_logprob = _token_vector(g_logprob, "g_logprob", tokens, dev, torch.float32)
     if g_entropy is not None:

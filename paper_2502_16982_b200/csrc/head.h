@@ -43,6 +43,7 @@ struct Ctrl {
   unsigned ticket; // blocks of the finalisation that are done
   float coef;      // scale, divided by the sum of the weights where a mean is asked for
   float rest;      // what dX and dW are still to be multiplied with, see finalise_kernel
+  int kept_tiles;  // log probabilities: tiles of the pieces whose codes are kept, for the gradient to compare
 };
 
 // One product of a launch: D[m][n] = sum_k A[m][k] B[n][k].
@@ -66,6 +67,8 @@ struct Product {
 // turned into the bf16 gradient of the logits in place.
 struct ConvertParams {
   __nv_bfloat16* g;  // [token][ld]; NULL: nothing to convert
+  const __nv_bfloat16* codes;  // gradients of log probabilities: the codes, which stay as they are
+  const float* row_b;          // and the coefficient of q log2 q
   long long ld;
   int tiles;         // 256-column tiles of the piece
   int v_tile0;       // its first tile in the vocabulary
@@ -196,6 +199,8 @@ struct RowParams {
   const float* g_logprob;
   const float* g_entropy;
   float* row_b;
+  int kept_tiles;        // see Ctrl
+  const Ctrl* kept;      // of the forward pass that kept its logits, else NULL
   const float* part;     // partial dX of each run of K blocks
   long long part_ld, part_stride;
   int splits;
@@ -213,6 +218,7 @@ cudaError_t launch_prepare(const RowParams& R, bool after_flags, cudaStream_t st
 cudaError_t launch_finalise(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);
 cudaError_t launch_logprob(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_logprob_grad(const RowParams& R, cudaStream_t stream);
+cudaError_t launch_convert_log(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream);
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream);
 cudaError_t launch_pack(const RowParams& R, cudaStream_t stream);
 int pack_blocks(int vocab);

@@ -102,7 +102,7 @@ bool want_codes(int tokens, int dim, int vocab) {
 
 // `room`: bytes of workspace to plan for; 0 plans for as many as are useful.
 int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t room, Plan* P, Kind kind = kLoss,
-              bool entropy = false) {
+              bool entropy = false, bool keep = false) {
   P->kind = kind;
   P->tokens = a->tokens;
   P->dim = a->dim;
@@ -150,16 +150,17 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     return at;
   };
   P->ctrl = take(sizeof(Ctrl));
-  P->xc = take(rows * P->ld_xc * 2);
-  P->row_of = take(rows * 4);
-  P->run_counts = take(P->tokens >= kManyTokens ? (rows / 256 + 1) * 4 : 0);
-  P->ids = take(entries * 4);
+  // `keep` of a gradient: what the forward pass kept is not formed again
+  const bool gather = !(kind == kLogprobGrad && keep);
+  P->xc = take(gather ? rows * P->ld_xc * 2 : 0);
+  P->row_of = take(gather ? rows * 4 : 0);
+  P->run_counts = take(gather && P->tokens >= kManyTokens ? (rows / 256 + 1) * 4 : 0);
+  P->ids = take(gather ? entries * 4 : 0);
   // the gradient of log probabilities starts from what an earlier call left with the caller
   const size_t units = kind == kLogprobGrad ? 0 : rows * P->v_tiles * kUnits;
   P->entry_logit = take(entries * 4);
   P->entry_g = take(entries * 4);
   P->stats = take(units * sizeof(float2));
-  P->stats_e = take(entropy ? units * 4 : 0);
   P->row_q = take(rows * sizeof(float2));
   P->row_b = take(kind == kLogprobGrad ? rows * 4 : 0);
   P->row_l = take(rows * 4);
@@ -171,7 +172,7 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
     P->row_c = take(rows * 4);
     P->starts = take(rows * (P->v_tiles + 1));
   }
-  if (P->pack) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
+  if (P->pack && gather) P->wc = take(static_cast<size_t>(a->vocab) * P->ld_wc * 2);
   // Where no second piece is kept as codes nothing reads the statistics after the
   // finalisation, and partial dX may lie in their place.
   const size_t part_bytes = P->want_dx ? static_cast<size_t>(P->splits) * P->part_stride * 4 : 0;
@@ -179,24 +180,32 @@ int make_plan(const muon_head_args* a, int top, bool distill, int pairs, size_t 
   const bool share = part_bytes > 0 && stats_bytes >= part_bytes;
   const size_t apart = static_cast<size_t>(round_up(static_cast<long long>(part_bytes), 1024));
   P->n_stored = P->n_buffers = 0;
+  const long long one = static_cast<long long>(rows) * P->piece_tiles * kTileN * 2;
+  if (kind == kLogprob && keep && want_codes(P->tokens, P->dim, P->vocab)) {
+    const long long fit = (kCodeBytes - static_cast<long long>(stats_bytes)) / one;
+    P->n_stored = static_cast<int>(fit < 0 ? 0 : (fit > P->n_pieces ? P->n_pieces : fit));
+    P->n_buffers = P->n_stored;
+    P->g = take(static_cast<size_t>(one) * P->n_stored);
+  }
+  P->stats_e = take(entropy ? units * 4 : 0);  // behind what is kept
   P->least = off;
   if (P->grads) {
-    const long long one = static_cast<long long>(rows) * P->piece_tiles * kTileN * 2;
-    P->n_buffers = 1;
+    // two in turn, where codes that stay are converted while the products of the other run
+    P->n_buffers = kind == kLogprobGrad && keep && P->n_pieces > 1 ? 2 : 1;
     if (kind == kLoss && want_codes(P->tokens, P->dim, P->vocab)) {
       long long fit = (room ? static_cast<long long>(room) - static_cast<long long>(off + apart)
                             : kCodeBytes - static_cast<long long>(stats_bytes)) / one;
       P->n_buffers = static_cast<int>(fit < 1 ? 1 : (fit > P->n_pieces ? P->n_pieces : fit));
       P->n_stored = P->n_buffers;
     }
-    P->least = off + (share ? 0 : apart) + static_cast<size_t>(round_up(one, 1024));
+    P->least = off + (share ? 0 : apart) + static_cast<size_t>(round_up(one * (kind == kLogprobGrad ? P->n_buffers : 1), 1024));
     if (part_bytes) P->part = share && P->n_stored <= 1 ? P->stats : take(part_bytes);
     P->g = take(static_cast<size_t>(one) * P->n_buffers);
   }
   // few tokens with rows that TMA can address, and nothing but codes between the passes
   P->in_place = a->tokens > 0 && a->tokens <= kInPlaceRows && static_cast<long long>(a->tokens) * top <= kInPlaceEntries &&
                 (reinterpret_cast<uintptr_t>(a->x) & 15) == 0 && (a->ld_x & 7) == 0 &&
-                (!P->grads || (P->n_pieces == 1 && P->n_stored == 1));
+                (!P->grads || (P->n_pieces == 1 && P->n_stored == 1)) && !keep;
   P->bytes = off;
   return MUON_OK;
 }
@@ -326,9 +335,9 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   const bool distill = t != nullptr;
   const int top = distill ? t->top : 1;
   const Kind kind = d ? kLogprobGrad : l ? kLogprob : kLoss;
-  const bool entropy = kind == kLogprob && l->entropy;
-  Plan P;
-  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, workspace_bytes ? workspace_bytes : 1, &P, kind, entropy));
+  const bool entropy = kind == kLogprob && l->entropy, keep = l && (d ? d->kept != nullptr : l->keep != 0);
+  Plan P, K = {};  // K: of the forward pass that kept its logits
+  HEAD_TRY(make_plan(a, top, distill, kPlanPairs, workspace_bytes ? workspace_bytes : 1, &P, kind, entropy, keep));
   if (!workspace || workspace_bytes < P.least || misaligned(workspace, 1024))
     return fail(MUON_ERR_WORKSPACE, "workspace: need at least %zu bytes, 1024-byte aligned", P.least);
   DeviceGuard guard;
@@ -337,10 +346,19 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   HEAD_TRY(device_pairs(device, &pairs));
 
   char* ws = static_cast<char*>(workspace);
+  char* kept = nullptr;
+  if (d && keep) {
+    muon_head_args forward = *a;
+    forward.dx = forward.dw = nullptr;
+    HEAD_TRY(make_plan(&forward, 1, false, kPlanPairs, 1, &K, kLogprob, false, true));
+    if (d->kept_bytes < K.least || misaligned(d->kept, 1024))
+      return fail(MUON_ERR_WORKSPACE, "kept: need the workspace of the forward pass, %zu bytes", K.least);
+    kept = static_cast<char*>(const_cast<void*>(d->kept));  // only read
+  }
   const void* w = a->w;
   long long ld_w = a->ld_w;
   if (P.pack) {
-    w = ws + P.wc;
+    w = kept ? kept + K.wc : ws + P.wc;
     ld_w = P.ld_wc;
   }
   const float logit_scale = logit_scale_of(a, t);
@@ -390,6 +408,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.total = a->total;
   if (l) {
     R.row_b = reinterpret_cast<float*>(ws + P.row_b);
+    R.kept_tiles = P.piece_tiles;
     if (d) {
       R.logprob_in = l->logprob;
       R.entropy_in = l->entropy;
@@ -397,6 +416,13 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
       R.g_logprob = d->g_logprob;
       R.g_entropy = d->g_entropy;
       R.loss = R.lse = nullptr;
+      if (kept) {
+        R.kept = reinterpret_cast<const Ctrl*>(kept + K.ctrl);
+        R.xc = reinterpret_cast<__nv_bfloat16*>(kept + K.xc);
+        R.row_of = reinterpret_cast<int*>(kept + K.row_of);
+        R.ids = reinterpret_cast<int*>(kept + K.ids);
+        R.stats = reinterpret_cast<float2*>(kept + K.stats);
+      }
     } else if (entropy) {
       R.entropy = l->entropy;
       R.stats_e = reinterpret_cast<const float*>(ws + P.stats_e);
@@ -436,7 +462,7 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     return left < P.piece_tiles ? left : P.piece_tiles;
   };
   S.code_tiles = P.n_stored * P.piece_tiles < P.v_tiles ? P.n_stored * P.piece_tiles : P.v_tiles;
-  if (P.grads) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, stats_rows(P.tokens)));
+  if (P.n_buffers > 0) HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, stats_rows(P.tokens)));
   // Fewer than 32 tokens: boxes of operand A that hold no more rows than there are; what a
   // slot holds past them reaches only rows of the accumulator that nothing reads.  (A box of
   // 128 rows over a tensor of fewer than 32 made the statistics of 10 x 2048 x 163840 take
@@ -500,14 +526,14 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     if (O.dw_tma) HEAD_TRY(encode(&O.map_dw, a->dw, 1, P.vocab, P.dim, a->ld_dw, 32, O.dw_fp32 != 0));
   }
 
-  if (P.pack) {
+  if (P.pack && !kept) {
     R.pack_to = reinterpret_cast<__nv_bfloat16*>(ws + P.wc);
     R.pack_from = static_cast<const __nv_bfloat16*>(a->w);
     R.ld_pack = a->ld_w;
     R.pack_blocks = pack_blocks(P.vocab);
     if (P.in_place) HEAD_CUDA(launch_pack(R, stream));
   }
-  if (!P.in_place) {
+  if (!P.in_place && !kept) {
     const bool flags = distill && P.tokens > 0;
     if (flags) {
       R.flags = reinterpret_cast<unsigned char*>(ws + P.flags);
@@ -538,6 +564,18 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   C.entry_g = R.entry_g;
   C.starts = P.in_place ? nullptr : R.starts;
   C.n_starts = R.n_starts;
+  // of log probabilities: kept codes, into the buffer that the piece's products read
+  const int n_kept = kept ? K.n_stored : 0;
+  auto log_codes_of = [&](int piece) {
+    ConvertParams D = C;
+    const long long one = P.rows * g_ld;
+    D.codes = reinterpret_cast<const __nv_bfloat16*>(kept + K.g) + piece * one;
+    D.row_b = R.row_b;
+    D.g = g + (piece % P.n_buffers) * one;
+    D.tiles = tiles_of(piece);
+    D.v_tile0 = piece * P.piece_tiles;
+    return D;
+  };
   auto codes_of = [&](int piece) {
     ConvertParams D = C;
     if (piece < P.n_stored) D.g = g + static_cast<long long>(piece) * P.rows * g_ld;
@@ -546,25 +584,28 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     return D;
   };
   if (P.grads) R.total = nullptr;  // the products' launch adds the losses up beside its work
-  if (d) HEAD_CUDA(launch_logprob_grad(R, stream));
-  else HEAD_CUDA(launch_finalise(R, codes_of(0), 2 * pairs, stream));
+  if (d) {
+    HEAD_CUDA(launch_logprob_grad(R, stream));
+    if (n_kept > 0) HEAD_CUDA(launch_convert_log(R, log_codes_of(0), 2 * pairs, stream));
+  } else HEAD_CUDA(launch_finalise(R, codes_of(0), 2 * pairs, stream));
   if (P.grads) {
     for (int i = 0; i < P.n_pieces; ++i) {
       // stored pieces lie in a buffer each, the others use the first one after them
-      const bool stored = i < P.n_stored;
-      const int buffer = stored ? i : 0;
+      const bool stored = d ? i < n_kept : i < P.n_stored;
+      const int buffer = d ? i % P.n_buffers : stored ? i : 0;
       const int tiles = tiles_of(i);
       const int v0 = i * P.piece_tiles * kTileN;
       const int cols = P.vocab - v0 < tiles * kTileN ? P.vocab - v0 : tiles * kTileN;
       if (!stored) {
         S.v0 = v0;
-        HEAD_TRY(encode(&S.map_g, g, P.n_buffers, P.rows, g_ld, g_ld, 32));
+        // the launch stores into the first buffer of its map
+        HEAD_TRY(encode(&S.map_g, g + buffer * P.rows * g_ld, 1, P.rows, g_ld, g_ld, 32));
         L.b_n0 = v0;
         L.n_tiles = tiles;
         S.by_tile = m_tiles * tiles > pairs;
         HEAD_CUDA(launch_gemm(kModeGrad, S, m_tiles * tiles, pairs, true, stream));
       }
-      O.convert = i + 1 < P.n_stored ? codes_of(i + 1) : ConvertParams{};
+      O.convert = i + 1 < n_kept ? log_codes_of(i + 1) : i + 1 < P.n_stored ? codes_of(i + 1) : ConvertParams{};
       O.prod[0].a_z = O.prod[1].a_z = buffer;
       O.prod[0].k_blocks = (cols + kBK - 1) / kBK;
       O.prod[0].b_k0 = v0;
@@ -626,7 +667,8 @@ extern "C" int muon_head_logprob_workspace_bytes(const muon_logprob_args* l, con
   const muon_head_args a = as_head_args(l, d);
   HEAD_TRY(check(&a, 1, false));
   Plan P;
-  HEAD_TRY(make_plan(&a, 1, false, kPlanPairs, 0, &P, d ? kLogprobGrad : kLogprob, !d && l->entropy));
+  HEAD_TRY(make_plan(&a, 1, false, kPlanPairs, 0, &P, d ? kLogprobGrad : kLogprob, !d && l->entropy,
+                     d ? d->kept != nullptr : l->keep != 0));
   *out_bytes = P.bytes;
   return MUON_OK;
 }
@@ -651,6 +693,7 @@ extern "C" int muon_head_logprob_grad(const muon_logprob_args* l, const muon_log
   const muon_head_args a = as_head_args(l, d);
   HEAD_TRY(check_logprob(l, &a));
   if (!d->dx && !d->dw) return fail(MUON_ERR_INVALID_ARG, "no gradient wanted");
+  if (misaligned(d->kept, 1024)) return fail(MUON_ERR_WORKSPACE, "kept is not 1024-byte aligned");
   if (l->tokens > 0 && (!l->lse || (d->g_entropy && !l->entropy)))
     return fail(MUON_ERR_INVALID_ARG, "the gradient needs lse, and entropy where g_entropy is given");
   if (misaligned(d->g_logprob, 4) || misaligned(d->g_entropy, 4))

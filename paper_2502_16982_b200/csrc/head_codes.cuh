@@ -118,6 +118,48 @@ __device__ __forceinline__ void convert_codes(const ConvertParams& C, int row, i
   }
 }
 
+// The same for the gradient of log probabilities, q (rq.x + rb log2 q), from codes that stay
+// as they are: a caller may ask for it again.  One entry a row: the target.
+template <int kTiles>
+__device__ __forceinline__ void convert_log(const ConvertParams& C, int row, int tile0, int lane) {
+  const int tiles = min(kTiles, C.tiles - tile0);
+  const long long at = static_cast<long long>(row) * C.ld + static_cast<long long>(tile0) * kTileN;
+  const uint4* src = reinterpret_cast<const uint4*>(C.codes + at) + lane;
+  uint4* dst = reinterpret_cast<uint4*>(C.g + at) + lane;
+  uint4 v[kTiles];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+    if (i < tiles) v[i] = __ldcs(src + i * 32);
+  const float2 rq = C.row_q[row];
+  const float rb = C.row_b[row];
+  float shift = 0.f;
+  static_assert(kTiles * kUnits <= 32, "one lane per statistics entry");
+  if (lane < kUnits * tiles)
+    shift = C.stats[static_cast<long long>(row) * C.stats_ld + kUnits * (C.v_tile0 + tile0) + lane].x - rq.y;
+  const int target = C.ids[row] - (C.v_tile0 + tile0) * kTileN - lane * 8;  // from this lane's first column
+  const float target_g = C.entry_g[row];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    if (i < tiles) {
+      const float a = __shfl_sync(0xFFFFFFFFu, shift, kUnits * i + lane * 8 / kStatN);
+      uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = w[e] & 0xFFFFu, hi = w[e] >> 16;
+        const float yl = fmaf(__uint_as_float(lo | 0x4B000000u) - kCodeMagic, -1.0f / kCodeSteps, a);
+        const float yh = fmaf(__uint_as_float(hi | 0x4B000000u) - kCodeMagic, -1.0f / kCodeSteps, a);
+        float gl = lo == kCodeMax ? 0.f : ex2_fast(yl) * fmaf(yl, rb, rq.x);
+        float gh = hi == kCodeMax ? 0.f : ex2_fast(yh) * fmaf(yh, rb, rq.x);
+        if (target == i * kTileN + 2 * e) gl = target_g;
+        if (target == i * kTileN + 2 * e + 1) gh = target_g;
+        const __nv_bfloat162 h = __floats2bfloat162_rn(gl, gh);
+        w[e] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      dst[i * 32] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
 // A row past the tokens that count becomes zeros.
 template <int kTiles>
 __device__ __forceinline__ void clear_row(const ConvertParams& C, int row, int tile0, int lane) {
@@ -127,6 +169,7 @@ __device__ __forceinline__ void clear_row(const ConvertParams& C, int row, int t
 }
 
 // All rows of a piece, dealt out to `warps` warps.
+template <bool kLog = false>
 __device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_valid, int tokens, int warp, int warps, int lane) {
   const int runs = (C.tiles + kConvertTiles - 1) / kConvertTiles;
   const int rows = min(tokens, (n_valid + kBK - 1) / kBK * kBK);  // dW's product reads whole K blocks of rows
@@ -135,7 +178,9 @@ __device__ __forceinline__ void convert_piece(const ConvertParams& C, int n_vali
     const int row = static_cast<int>(t / runs);
     const int tile0 = static_cast<int>(t - static_cast<long long>(row) * runs) * kConvertTiles;
     const long long at = static_cast<long long>(row) * C.top;
-    if (row < n_valid) {
+    if (kLog && row < n_valid) {
+      convert_log<kConvertTiles>(C, row, tile0, lane);
+    } else if (row < n_valid) {
       Codes<kConvertTiles> c;
       load_codes(C, row, tile0, lane, c);
       convert_codes(C, row, tile0, C.row_q[row], C.ids + at, C.entry_g + at, lane, c);

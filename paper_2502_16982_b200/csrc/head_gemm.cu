@@ -586,7 +586,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
     // ---------------------------------- codes of the next piece, meanwhile ----
     const int convert = warp - 2 - Cfg::kEpiWarps;
     if (P.convert.g != nullptr)
-      convert_piece(P.convert, n_valid, P.tokens, static_cast<int>(blockIdx.x) * Cfg::kConvertWarps + convert,
+      convert_piece<kLog>(P.convert, n_valid, P.tokens, static_cast<int>(blockIdx.x) * Cfg::kConvertWarps + convert,
                     static_cast<int>(gridDim.x) * Cfg::kConvertWarps, lane);
     if (convert == 0) add_losses(P, n_valid, lane);
   } else {
@@ -961,6 +961,7 @@ cudaError_t gemm_configure() {
   if (e == cudaSuccess) e = configure_one<kModeGrad>();
   if (e == cudaSuccess) e = configure_one<kModeOut>();
   if (e == cudaSuccess) e = configure_one<kModeOut, true>();
+  if (e == cudaSuccess) e = configure_one<kModeOut, false, false, true>();
   return e;
 }
 
@@ -1001,6 +1002,7 @@ cudaError_t launch_gemm(int mode, const GemmParams& P, long long tiles, int max_
                                       : launch_one<kModeStats>(P, clusters, overlap, stream);
   }
   if (mode == kModeGrad) return launch_one<kModeGrad>(P, clusters, overlap, stream);
+  if (P.convert.codes != nullptr) return launch_one<kModeOut, false, false, true>(P, clusters, overlap, stream);
   return P.spare ? launch_one<kModeOut, true>(P, clusters, overlap, stream)
                  : launch_one<kModeOut>(P, clusters, overlap, stream);
 }

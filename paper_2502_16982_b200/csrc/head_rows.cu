@@ -152,6 +152,7 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
     R.ctrl->n_valid = total;
     R.ctrl->ticket = 0;
     R.ctrl->coef = !R.mean ? R.scale : (norm == 0.f ? 0.f : R.scale / norm);
+    R.ctrl->kept_tiles = R.kept_tiles;
   }
 
   const int t = first + warp;
@@ -653,11 +654,31 @@ __global__ void __launch_bounds__(kRowThreads) logprob_kernel(const RowParams R)
 // entry_g = g at the target.  All of them lack the fraction of the first token's a r, which
 // is every token's where all share one coefficient: in bf16 it would be rounded with every
 // r (1 - q) of a q near 0 in the same way (see finalise_kernel; Ctrl::rest).
+//
+// A warp a token.  With a forward pass that kept its logits nothing else comes before the
+// products, and this pass also clears the rows of dX of the tokens that do not count.
 __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const RowParams R) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int row = blockIdx.x * kRowThreads + threadIdx.x;
-  const int n_valid = R.ctrl->n_valid;
+  const int row = blockIdx.x * kRowWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  int n_valid = R.kept != nullptr ? R.kept->n_valid : R.ctrl->n_valid;
+  if (R.kept != nullptr) {
+    // pieces of another size (the knob was turned in between): no gradient, and a status
+    const bool other = R.kept->kept_tiles != R.kept_tiles;
+    if (other) n_valid = 0;
+    if (row == 0 && lane == 0) {
+      R.ctrl->n_valid = n_valid;
+      R.ctrl->status = other ? -1 : R.kept->status;
+    }
+    if (R.dx != nullptr && row < R.tokens && (other || !in_vocab(R, R.ids_in[row]))) {
+      const long long at = static_cast<long long>(row) * R.ld_dx;
+      for (int c = lane; c < R.dim; c += 32) {
+        if (R.dx_fp32) static_cast<float*>(R.dx)[at + c] = 0.f;
+        else static_cast<__nv_bfloat16*>(R.dx)[at + c] = __float2bfloat16_rn(0.f);
+      }
+    }
+  }
+  if (lane != 0) return;
   if (n_valid == 0 && row == 0) R.ctrl->rest = 1.0f;
   if (row >= n_valid) return;
   const int first = R.row_of[0], t = R.row_of[row];
@@ -672,6 +693,14 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const RowPara
   R.row_q[row] = make_float2(-fmaf(h, entropy, r), R.lse_in[t] * (1.0f / kLn2));
   R.row_b[row] = -h * kLn2;
   R.entry_g[row] = r * -expm1f(log_q) - (q > 0.f ? h * q * (log_q + entropy) : 0.f);
+}
+
+// The first piece's codes into gradients; the others' are converted beside the products.
+__global__ void __launch_bounds__(kRowThreads) convert_log_kernel(const RowParams R, const ConvertParams C) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  convert_piece<true>(C, R.ctrl->n_valid, R.tokens, static_cast<int>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5),
+                      static_cast<int>(gridDim.x) * kRowWarps, threadIdx.x & 31);
 }
 
 // dX of the tokens that count, in token order: the partial sums joined, always in the
@@ -815,8 +844,13 @@ cudaError_t launch_logprob(const RowParams& R, cudaStream_t stream) {
 }
 
 cudaError_t launch_logprob_grad(const RowParams& R, cudaStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(R.tokens > 0 ? (R.tokens + kRowThreads - 1) / kRowThreads : 1));
-  return launch(logprob_grad_kernel, grid, true, stream, R);
+  return launch(logprob_grad_kernel, dim3(row_blocks(R.tokens)), R.kept == nullptr, stream, R);
+}
+
+cudaError_t launch_convert_log(const RowParams& R, const ConvertParams& C, int sms, cudaStream_t stream) {
+  const long long tasks = static_cast<long long>(R.tokens) * ((C.tiles + kConvertTiles - 1) / kConvertTiles);
+  const long long most = 4ll * sms, want = (tasks + kRowWarps - 1) / kRowWarps;
+  return launch(convert_log_kernel, dim3(static_cast<unsigned>(want < 1 ? 1 : want < most ? want : most)), true, stream, R, C);
 }
 
 cudaError_t launch_dx(const RowParams& R, cudaStream_t stream) {

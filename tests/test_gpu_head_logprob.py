@@ -13,7 +13,8 @@ The gradient of a logit is q (..): q is within e_q = 3 e_l + err(lse) + 2^-21 (1
 relative, the bracket r + h (log q + H) within |h| (2 e_l + err(lse) + err(H) + 2^-22 |log q|);
 it is rounded to bf16 once, 2^-8.  At the target r (1 - q) of fp32 values adds |r| (2 e_l +
 2^-20).  dx and dw are fp32 sums of those products (V/16 + 64 or T/16 + 16 steps of 2^-23)
-and rounded once where they are bf16."""
+and rounded once where they are bf16.  Logits kept as codes: q is within e_k = 2^-12 more and what
+lies 2^-32 below the largest of its columns is 0, log q within e_k absolutely."""
 
 import numpy as np
 import pytest
@@ -68,14 +69,17 @@ class Reference:
             assert np.all(err <= tol), (name, float((err / tol).max()))
             assert np.all(f64(got)[~self.counts] == 0)
 
-    def check_grads(self, d, r, h, before=None):
+    def check_grads(self, d, r, h, before=None, kept=False):
         T, V = self.log_q.shape
         G = lo.logprob_grad(self.log_q, self.entropy, self.counts, self.targets, r, h, self.scale)
         ra, ha = (np.zeros(T) if v is None else np.where(self.counts, np.abs(v), 0.0) for v in (r, h))
         t, u = np.abs(self.log_q), 2.0 ** -22
-        e_q = 3 * self.e_l + self.tol["lse"][:, None] + 2 * u * (1 + t)
+        e_k = 2.0 ** -12 if kept else 0.0
+        e_q = 3 * self.e_l + self.tol["lse"][:, None] + 2 * u * (1 + t) + e_k
         size = ra[:, None] + ha[:, None] * (t + self.entropy[:, None])
-        err = self.q * (size * e_q + ha[:, None] * (2 * self.e_l + (self.tol["lse"] + self.tol["entropy"])[:, None] + u * t))
+        err = self.q * (size * e_q + ha[:, None] * (2 * self.e_l + e_k + (self.tol["lse"] + self.tol["entropy"])[:, None] + u * t))
+        if kept:
+            err = err + 2.0 ** -31 * size
         for i in np.flatnonzero(self.counts):
             err[i, self.targets[i]] += ra[i] * (2 * self.e_l + 2.0 ** -20)
         err = self.scale * err
@@ -157,6 +161,83 @@ def test_values_and_gradients_match_the_oracle(T, D, V, masked, opts):
         ref.check_grads(d, zero(g), zero(e))
 
 
+@pytest.mark.parametrize("T,D,V,masked,opts", CASES + [(900, 512, 20000, 0.3, {}), (3000, 512, 9000, 0.1, dict(scale=0.8))])
+@pytest.mark.parametrize("tiles", [None, 2, 3])
+def test_gradients_from_kept_logits(T, D, V, masked, opts, tiles):
+    """Codes of all logits kept by the forward pass, in one piece or in several of them."""
+    from paper_2502_16982_b200 import binding as b
+
+    o = dict(opts)
+    scale = o.pop("scale", 1.0)
+    dxt, dwt = o.pop("dx", BF), o.pop("dw", BF)
+    x, w, gen = make(T, D, V, 2000 * T + D, **o)
+    targets = torch.randint(0, V, (T,), generator=gen)
+    hide = torch.rand(T, generator=gen) < masked
+    targets[hide] = -100
+    x[hide.cuda()] = float("nan")
+    y = targets.cuda()
+    ref = Reference(np.where(hide.numpy()[:, None], 0.0, f64(x)), f64(w), targets.numpy(), scale)
+    rr, hh = torch.randn(T, generator=gen) / T, torch.randn(T, generator=gen) * 0.1 / T
+    before, mode = b.muon_debug_set_head_piece_bytes(0 if tiles is None else tiles * T * 512), b.muon_debug_set_head_codes(2)
+    try:
+        n = b.muon_head_logprob_workspace_bytes(T, D, V, grads=False, packed_head=False, keep=True)
+        ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+        r = b.muon_head_logprob(x, w, y, logit_scale=scale, workspace=ws, keep=True)
+        assert r.kept is ws
+        ref.check(r)
+        held = ws.clone()
+        for g, e in ((rr, hh), (None, hh)):
+            dx = None if dxt is None else torch.full((T, D), 7.0, dtype=dxt, device="cuda")
+            dw = None if dwt is None else torch.full((V, D), 7.0, dtype=dwt, device="cuda")
+            n = b.muon_head_logprob_workspace_bytes(T, D, V, grads=True, dx=dxt is not None, dw=dwt is not None, packed_head=False, keep=True)
+            gs = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+            up = dict(g_logprob=None if g is None else g.cuda(), g_entropy=e.cuda(), logit_scale=scale)
+            d = b.muon_head_logprob_grad(x, w, y, r, dx=dx, dw=dw, workspace=gs, **up)
+            assert b.muon_head_status(gs) == 0
+            zero = lambda v: None if v is None else np.where(hide.numpy(), 0.0, v.double().numpy())
+            ref.check_grads(d, zero(g), zero(e), kept=True)
+        assert torch.equal(ws, held)  # only read: it may be asked for again
+        again = b.muon_head_logprob_grad(x, w, y, r, dx=dx is not None, dw=dw is not None, **up)
+        for p, q in zip(again, d):
+            assert p is None and q is None or p.dtype != q.dtype or torch.equal(p, q)
+    finally:
+        b.muon_debug_set_head_piece_bytes(before)
+        b.muon_debug_set_head_codes(mode)
+
+
+def test_what_other_pieces_kept_gives_no_gradient_but_a_status():
+    from paper_2502_16982_b200 import binding as b
+
+    x, w, gen = make(300, 512, 3000, 3)
+    y = torch.randint(0, 3000, (300,), generator=gen).cuda()
+    r = b.muon_head_logprob(x, w, y, keep=True)
+    before = b.muon_debug_set_head_piece_bytes(2 * 300 * 512)
+    try:
+        n = b.muon_head_logprob_workspace_bytes(300, 512, 3000, grads=True, keep=True)
+        ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+        d = b.muon_head_logprob_grad(x, w, y, r, g_logprob=torch.ones(300, device="cuda"), dx=True, dw=True, workspace=ws)
+        assert b.muon_head_status(ws) == b.MUON_ERR_INVALID_ARG
+        assert not d.dx.any() and not d.dw.any()
+    finally:
+        b.muon_debug_set_head_piece_bytes(before)
+    with pytest.raises(b.MuonError):
+        short = b.HeadLogprob(*r)
+        short.kept = r.kept[:4096]
+        b.muon_head_logprob_grad(x, w, y, short, g_logprob=torch.ones(300, device="cuda"), dx=True)
+
+
+def test_scoring_keeps_nothing():
+    from paper_2502_16982_b200 import binding as b
+
+    x, w, gen = make(300, 512, 3000, 4)
+    y = torch.randint(0, 3000, (300,), generator=gen).cuda()
+    with torch.no_grad():
+        assert b.muon_head_logprob(x, w, y).kept is None
+    r = b.muon_head_logprob(x, w, y)
+    assert r.kept is not None and r._replace(lse=r.lse).kept is None
+    assert b.muon_head_logprob(x, w, y, keep=False).kept is None
+
+
 @pytest.mark.parametrize("T,D,V", [(300, 136, 3000), (1100, 256, 2100), (70, 96, 5000)])
 def test_several_pieces_and_adding_to_dw(T, D, V):
     from paper_2502_16982_b200 import binding as b
@@ -165,7 +246,8 @@ def test_several_pieces_and_adding_to_dw(T, D, V):
     targets = torch.randint(0, V, (T,), generator=gen)
     targets[::9] = -100
     y = targets.cuda()
-    r = b.muon_head_logprob(x, w, y)
+    r = b.muon_head_logprob(x, w, y, keep=False)
+    assert r.kept is None
     ref = Reference(np.where(targets.numpy()[:, None] < 0, 0.0, f64(x)), f64(w), targets.numpy(), 1.0)
     ref.check(r)
     rr, hh = torch.randn(T, generator=gen), torch.randn(T, generator=gen) * 0.1
@@ -293,7 +375,7 @@ def test_a_policy_step():
 
     ref = Reference(np.where(counts.cpu().numpy()[:, None], f64(x), 0.0), f64(w), y.cpu().numpy(), 1.0)
     ref.check(r)
-    ref.check_grads(d, f64(g), f64(e))
+    ref.check_grads(d, f64(g), f64(e), kept=True)
     G = lo.logprob_grad(ref.log_q, ref.entropy, ref.counts, ref.targets, f64(upstream(torch.as_tensor(ref.logprob, device="cuda"))), f64(e))
     dx, dw = G @ ref.w, G.T @ ref.x
     coef = limit / (np.sqrt((dx ** 2).sum() + (dw ** 2).sum()) + 1e-6)
