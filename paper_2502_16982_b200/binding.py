@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import List, NamedTuple, Optional, Sequence
 
@@ -190,14 +191,12 @@ def lib():
     L.muon_head_distill.argtypes = [C.POINTER(muon_head_args), C.POINTER(muon_head_teacher), C.c_void_p, C.c_size_t,
                                     C.c_int, C.c_void_p]
     L.muon_head_status.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)]
-    L.muon_head_logprob_workspace_bytes.argtypes = [C.POINTER(muon_logprob_args), C.POINTER(muon_logprob_grads),
-                                                    C.POINTER(C.c_size_t)]
-    L.muon_head_logprob.argtypes = [C.POINTER(muon_logprob_args), C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]
-    L.muon_head_logprob_grad.argtypes = [C.POINTER(muon_logprob_args), C.POINTER(muon_logprob_grads), C.c_void_p, C.c_size_t,
-                                         C.c_int, C.c_void_p]
-    L.muon_logits_logprob.argtypes = [C.POINTER(muon_logits_args), C.c_int, C.c_void_p]
-    L.muon_logits_logprob_grad.argtypes = [C.POINTER(muon_logits_args), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int,
-                                           C.c_void_p]
+    # structs by their address or as bytes
+    L.muon_head_logprob_workspace_bytes.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
+    L.muon_head_logprob.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]
+    L.muon_head_logprob_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]
+    L.muon_logits_logprob.argtypes = [C.c_void_p, C.c_int, C.c_void_p]
+    L.muon_logits_logprob_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p]
     for name in EXPORTED:
         if name in ("muon_debug_set_chunk_bytes", "muon_debug_set_head_piece_bytes"):
             getattr(L, name).restype = C.c_size_t
@@ -417,8 +416,7 @@ class MuonGrads:
         import torch
         with torch.cuda.stream(stream) if stream is not None else _no_context:
             if norm is None and coef is None and sum_sq is None:
-                both = torch.empty(2, dtype=torch.float64, device=self.device)
-                sum_sq, pair = both.split_with_sizes((1, 1))
+                pair, sum_sq = torch.empty(2, dtype=torch.float64, device=self.device).split_with_sizes((1, 1))
                 norm, coef = pair.view(torch.float32).split_with_sizes((1, 1))
                 return norm, coef, sum_sq
             norm = torch.empty(1, dtype=torch.float32, device=self.device) if norm is None else norm
@@ -687,8 +685,8 @@ class HeadGrads(NamedTuple):
     dw: Optional["torch.Tensor"]
 
 
-def _logprob_args(x, w, targets, logit_scale):
-    """Checks of the operands, and the struct without its outputs."""
+def _logprob_operands(x, w, targets):
+    """Checks of the operands; (tokens, dim, vocab, device, address of the targets)."""
     import torch
     if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.shape[1] < 1 or w.shape[0] < 1:
         raise MuonError(MUON_ERR_INVALID_ARG, "x must be [tokens, dim] and w [vocab, dim]")
@@ -700,21 +698,18 @@ def _logprob_args(x, w, targets, logit_scale):
         raise MuonError(MUON_ERR_INVALID_ARG, "x and w must be on one CUDA device")
     if dim > 1 and (x.stride(1) != 1 or w.stride(1) != 1):
         raise MuonError(MUON_ERR_INVALID_ARG, "x and w must have contiguous rows")
-    return muon_logprob_args(tokens, dim, vocab, 0, x.data_ptr(), w.data_ptr(), _row_stride(x) if tokens else dim, _row_stride(w),
-                             _dtype_code(x), _dtype_code(w), _token_vector(targets, "targets", tokens, dev, torch.int64),
-                             logit_scale)
+    return tokens, dim, vocab, dev, _token_vector(targets, "targets", tokens, dev, torch.int64)
 
 
-def _logprob_workspace(workspace, dev, a, d):
-    """(tensor, first address, bytes) of the workspace of one call."""
+def _logprob_workspace(workspace, dev, key, args, grads):
+    """(tensor, first address, bytes) of the workspace of one call.  ``key``: all that its size
+    depends on; ``args`` and ``grads``: the structs as bytes (no gradients: None)."""
     import torch
     if workspace is None:
-        key = (a.tokens, a.dim, a.vocab, -1 if d is None else -2, not a.entropy, a.keep if d is None else not d.kept,
-               d is None or not d.dx, d is None or not d.dw, a.ld_w & 7, (a.w or 0) & 15)
         need = _head_bytes.get(key)
         if need is None:
             out = C.c_size_t(0)
-            _check(lib().muon_head_logprob_workspace_bytes(C.byref(a), None if d is None else C.byref(d), C.byref(out)))
+            _check(lib().muon_head_logprob_workspace_bytes(args, grads, C.byref(out)))
             if len(_head_bytes) >= 1024:
                 _head_bytes.clear()
             need = _head_bytes[key] = out.value + 1024
@@ -754,29 +749,29 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
     gradient mode says (not under ``torch.no_grad()``, for scoring) and not in a workspace of
     the caller's.  Argument marshalling only; the formulas are in include/muon.h."""
     import torch
-    a = _logprob_args(x, w, targets, logit_scale)
+    tokens, dim, vocab, dev, target_ptr = _logprob_operands(x, w, targets)
     if keep is None:
         keep = workspace is None and torch.is_grad_enabled()
-    a.keep = 1 if keep else 0
-    tokens, dev = x.shape[0], x.device
+    f32 = torch.float32
     with torch.cuda.stream(stream) if stream is not None else _no_context:
         if out is None:
-            n = 3 if entropy else 2
-            rows = torch.empty(n * tokens, dtype=torch.float32, device=dev).split_with_sizes((tokens,) * n)
-            out = HeadLogprob(rows[0], rows[2] if entropy else None, rows[1])
-            a.logprob, a.lse = rows[0].data_ptr(), rows[1].data_ptr()
-            if entropy:
-                a.entropy = rows[2].data_ptr()
+            flat = torch.empty((3 if entropy else 2) * tokens, dtype=f32, device=dev)
+            at = flat.data_ptr()
+            parts = flat.split_with_sizes((tokens,) * (3 if entropy else 2))
+            out = HeadLogprob(parts[0], parts[2] if entropy else None, parts[1])
+            ptrs = (at, at + 8 * tokens if entropy else 0, at + 4 * tokens)
         else:
-            for name in ("logprob", "entropy", "lse"):
-                t = getattr(out, name)
-                if t is not None:
-                    setattr(a, name, _token_vector(t, name, tokens, dev, torch.float32))
-        workspace, base, nbytes = _logprob_workspace(workspace, dev, a, None)
+            ptrs = [0 if t is None else _token_vector(t, name, tokens, dev, f32) for name, t in zip(("logprob", "entropy", "lse"), out[:3])]
+            out = HeadLogprob(*out[:3]) if keep else out
+        w_ptr, ld_w = w.data_ptr(), _row_stride(w)
+        a = _pack_logprob_args(tokens, dim, vocab, 1 if keep else 0, x.data_ptr(), w_ptr, _row_stride(x) if tokens else dim, ld_w,
+                               _dtype_code(x), _dtype_code(w), target_ptr, logit_scale, 0, *ptrs)
+        workspace, base, nbytes = _logprob_workspace(workspace, dev, (tokens, dim, vocab, -1, not ptrs[1], bool(keep), ld_w & 7, w_ptr & 15),
+                                                     a, None)
         if keep:
-            out = HeadLogprob(*out)
             out.kept = workspace
-    _check(lib().muon_head_logprob(C.byref(a), base, nbytes, dev.index, _raw_stream(stream, dev.index)))
+    index = dev.index
+    _check(lib().muon_head_logprob(a, base, nbytes, index, _raw_stream(stream, index)))
     return out
 
 
@@ -788,32 +783,33 @@ def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_
     may be asked for again.  ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True
     to allocate one like x / w, None to leave the gradient out."""
     import torch
-    a = _logprob_args(x, w, targets, logit_scale)
-    tokens, dev = x.shape[0], x.device
+    tokens, dim, vocab, dev, target_ptr = _logprob_operands(x, w, targets)
     if saved.logprob is None or saved.lse is None or (g_entropy is not None and saved.entropy is None):
         raise MuonError(MUON_ERR_INVALID_ARG, "the gradient needs logprob, lse, and entropy where g_entropy is given")
     if accumulate_dw and not isinstance(dw, torch.Tensor):
         raise MuonError(MUON_ERR_INVALID_ARG, "accumulate_dw needs the dw to add to")
-    a.logprob = _token_vector(saved.logprob, "logprob", tokens, dev, torch.float32)
-    a.lse = _token_vector(saved.lse, "lse", tokens, dev, torch.float32)
+    f32 = torch.float32
+    ptrs = (_token_vector(saved.logprob, "logprob", tokens, dev, f32),
+            0 if g_entropy is None else _token_vector(saved.entropy, "entropy", tokens, dev, f32),
+            _token_vector(saved.lse, "lse", tokens, dev, f32))
     d = muon_logprob_grads()
     kept = getattr(saved, "kept", None)
     if kept is not None:
         if kept.device != dev:
             raise MuonError(MUON_ERR_WORKSPACE, "what the forward pass kept is not on x's device")
-        d.kept = (kept.data_ptr() + 1023) // 1024 * 1024
-        d.kept_bytes = kept.data_ptr() + kept.numel() - d.kept
+        first = kept.data_ptr()
+        d.kept = base = (first + 1023) // 1024 * 1024
+        d.kept_bytes = max(first + kept.numel() - base, 0)
     if g_logprob is not None:
-        d.g_logprob = _token_vector(g_logprob, "g_logprob", tokens, dev, torch.float32)
+        d.g_logprob = _token_vector(g_logprob, "g_logprob", tokens, dev, f32)
     if g_entropy is not None:
-        a.entropy = _token_vector(saved.entropy, "entropy", tokens, dev, torch.float32)
-        d.g_entropy = _token_vector(g_entropy, "g_entropy", tokens, dev, torch.float32)
+        d.g_entropy = _token_vector(g_entropy, "g_entropy", tokens, dev, f32)
     with torch.cuda.stream(stream) if stream is not None else _no_context:
         if dx is False:
             dx = None
         elif dx is not None:
             dx = torch.empty_like(x) if dx is True else _head_matrix(dx, "dx", x.shape, dev)
-            d.dx, d.ld_dx, d.dx_dtype = dx.data_ptr(), _row_stride(dx) if tokens else a.dim, _dtype_code(dx)
+            d.dx, d.ld_dx, d.dx_dtype = dx.data_ptr(), _row_stride(dx) if tokens else dim, _dtype_code(dx)
         if dw is False:
             dw = None
         elif dw is not None:
@@ -823,8 +819,14 @@ def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_
             raise MuonError(MUON_ERR_INVALID_ARG, "no gradient wanted")
         if tokens == 0 and dw is None:
             return HeadGrads(dx, dw)
-        workspace, base, nbytes = _logprob_workspace(workspace, dev, a, d)
-    _check(lib().muon_head_logprob_grad(C.byref(a), C.byref(d), base, nbytes, dev.index, _raw_stream(stream, dev.index)))
+        w_ptr, ld_w = w.data_ptr(), _row_stride(w)
+        a = _pack_logprob_args(tokens, dim, vocab, 0, x.data_ptr(), w_ptr, _row_stride(x) if tokens else dim, ld_w,
+                               _dtype_code(x), _dtype_code(w), target_ptr, logit_scale, 0, *ptrs)
+        grads = bytes(d)
+        workspace, base, nbytes = _logprob_workspace(
+            workspace, dev, (tokens, dim, vocab, -2, kept is None, dx is None, dw is None, ld_w & 7, w_ptr & 15), a, grads)
+    index = dev.index
+    _check(lib().muon_head_logprob_grad(a, grads, base, nbytes, index, _raw_stream(stream, index)))
     return HeadGrads(dx, dw)
 
 
@@ -846,20 +848,25 @@ def _token_vector(t, what, n, dev, dtype):
     return t.data_ptr()
 
 
-def _logits_args(logits, targets, logit_scale, top):
+# muon_logits_args and muon_logprob_args as bytes: a tenth of the time that the ctypes structs take
+_pack_logits_args = struct.Struct("=iiqqiifiqqqqqqq").pack
+_pack_logprob_args = struct.Struct("=iiiiqqqqiiqfiqqq").pack
+
+
+def _logits_operand(logits, targets, top):
+    """Checks; (tokens, vocab, device, address of the targets or 0)."""
     import torch
-    if logits.dim() != 2 or logits.device.type != "cuda" or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    if logits.dim() != 2 or logits.device.type != "cuda":
         raise MuonError(MUON_ERR_INVALID_ARG, "logits must be [tokens, vocab] on a CUDA device, with contiguous rows")
     tokens, vocab = logits.shape
     if (tokens | vocab) >> 31:
         _past_32_bits()
+    if vocab > 1 and logits.stride(1) != 1:
+        raise MuonError(MUON_ERR_INVALID_ARG, "logits must be [tokens, vocab] on a CUDA device, with contiguous rows")
     if not 0 <= top <= 128:
         raise MuonError(MUON_ERR_UNSUPPORTED, "0 to 128 alternatives per token")
-    a = muon_logits_args(tokens, vocab, logits.data_ptr(), _row_stride(logits) if tokens else vocab, _dtype_code(logits), top,
-                         logit_scale)
-    if targets is not None:
-        a.targets = _token_vector(targets, "targets", tokens, logits.device, torch.int64)
-    return a
+    dev = logits.device
+    return tokens, vocab, dev, 0 if targets is None else _token_vector(targets, "targets", tokens, dev, torch.int64)
 
 
 def muon_logits_logprob(logits, targets=None, top: int = 0, logit_scale: float = 1.0, out: Optional[LogitsLogprob] = None,
@@ -871,39 +878,40 @@ def muon_logits_logprob(logits, targets=None, top: int = 0, logit_scale: float =
     include/muon.h.  ``top_ids``, ``top_logits`` and ``lse`` at ``logit_scale`` = 1 /
     temperature are what :func:`muon_head_distill` takes from a teacher."""
     import torch
-    top = int(top)
-    a = _logits_args(logits, targets, logit_scale, top)
-    tokens, dev = a.tokens, logits.device
+    tokens, vocab, dev, target_ptr = _logits_operand(logits, targets, top)
     if out is None:
         with torch.cuda.stream(stream) if stream is not None else _no_context:
             # entropy, lse, logprob, top_logits and top_logprob are parts of one allocation
-            entries = tokens * top if top > 0 else 0
-            sizes = (tokens, tokens, tokens if targets is not None else 0, entries, entries)
-            flat = torch.empty(sum(sizes), dtype=torch.float32, device=dev)
-            entropy, lse, logprob, logits_, logprob_ = flat.split_with_sizes(sizes)
+            entries, given = tokens * top, tokens if target_ptr else 0
+            flat = torch.empty(2 * tokens + given + 2 * entries, dtype=torch.float32, device=dev)
             at = flat.data_ptr()
-            a.entropy, a.lse = at, at + 4 * tokens
-            if targets is not None:
-                a.logprob = at + 8 * tokens
-            more = ()
+            third = at + 8 * tokens
             if top > 0:
+                entropy, lse, logprob, top_logits, top_logprob = flat.split_with_sizes((tokens, tokens, given, entries, entries))
                 ids = torch.empty((tokens, top), dtype=torch.int64, device=dev)
-                a.top_ids, a.top_logits, a.top_logprob = ids.data_ptr(), at + 4 * sum(sizes[:3]), at + 4 * sum(sizes[:4])
-                more = (ids, logits_.view(tokens, top), logprob_.view(tokens, top))
-            out = LogitsLogprob(logprob if targets is not None else None, entropy, lse, *more)
+                more = third + 4 * given
+                ptrs = (third if target_ptr else 0, at, at + 4 * tokens, ids.data_ptr(), more, more + 4 * entries)
+                shape = (tokens, top)
+                out = LogitsLogprob(logprob if targets is not None else None, entropy, lse, ids, top_logits.view(shape),
+                                    top_logprob.view(shape))
+            else:
+                entropy, lse, logprob = flat.split_with_sizes((tokens, tokens, given))
+                ptrs = (third if target_ptr else 0, at, at + 4 * tokens, 0, 0, 0)
+                out = LogitsLogprob(logprob if targets is not None else None, entropy, lse)
     else:
+        ptrs = []
         for name in ("logprob", "entropy", "lse"):
             t = getattr(out, name)
-            if t is not None:
-                setattr(a, name, _token_vector(t, name, tokens, dev, torch.float32))
+            ptrs.append(0 if t is None else _token_vector(t, name, tokens, dev, torch.float32))
         for name, dtype in (("top_ids", torch.int64), ("top_logits", torch.float32), ("top_logprob", torch.float32)):
             t = getattr(out, name)
-            if t is not None:
-                if t.dtype != dtype or tuple(t.shape) != (tokens, top) or not t.is_contiguous() or t.device != dev:
-                    raise MuonError(MUON_ERR_INVALID_ARG, "%s must be contiguous %s [tokens, top] on the logits' device" % (name, dtype))
-                setattr(a, name, t.data_ptr())
+            if t is not None and (t.dtype is not dtype or t.shape != (tokens, top) or not t.is_contiguous() or t.device != dev):
+                raise MuonError(MUON_ERR_INVALID_ARG, "%s must be contiguous %s [tokens, top] on the logits' device" % (name, dtype))
+            ptrs.append(0 if t is None else t.data_ptr())
     index = dev.index
-    _check(lib().muon_logits_logprob(C.byref(a), index, _raw_stream(stream, index)))
+    _check(lib().muon_logits_logprob(
+        _pack_logits_args(tokens, vocab, logits.data_ptr(), _row_stride(logits) if tokens else vocab, _dtype_code(logits), top,
+                          logit_scale, 0, target_ptr, *ptrs), index, _raw_stream(stream, index)))
     return out
 
 
@@ -913,22 +921,24 @@ def muon_logits_logprob_grad(logits, targets, saved: LogitsLogprob, g_logprob=No
     [tokens] or None) of what :func:`muon_logits_logprob` gave as ``saved``.  ``dlogits``:
     a tensor like ``logits`` to write, or ``logits`` itself; allocated by default."""
     import torch
-    a = _logits_args(logits, targets, logit_scale, 0)
-    tokens, dev = logits.shape[0], logits.device
+    tokens, vocab, dev, target_ptr = _logits_operand(logits, targets, 0)
     if saved.lse is None or (g_entropy is not None and saved.entropy is None):
         raise MuonError(MUON_ERR_INVALID_ARG, "the gradient needs lse, and entropy where g_entropy is given")
-    a.lse = _token_vector(saved.lse, "lse", tokens, dev, torch.float32)
-    if g_entropy is not None:
-        a.entropy = _token_vector(saved.entropy, "entropy", tokens, dev, torch.float32)
-    r = None if g_logprob is None else _token_vector(g_logprob, "g_logprob", tokens, dev, torch.float32)
-    h = None if g_entropy is None else _token_vector(g_entropy, "g_entropy", tokens, dev, torch.float32)
+    f32 = torch.float32
+    lse = _token_vector(saved.lse, "lse", tokens, dev, f32)
+    entropy = 0 if g_entropy is None else _token_vector(saved.entropy, "entropy", tokens, dev, f32)
+    r = None if g_logprob is None else _token_vector(g_logprob, "g_logprob", tokens, dev, f32)
+    h = None if g_entropy is None else _token_vector(g_entropy, "g_entropy", tokens, dev, f32)
     if dlogits is None:
         with torch.cuda.stream(stream) if stream is not None else _no_context:
             dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
-    elif dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or dlogits.device != dev or (dlogits.shape[1] > 1 and dlogits.stride(1) != 1):
+    elif dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or dlogits.device != dev or (vocab > 1 and dlogits.stride(1) != 1):
         raise MuonError(MUON_ERR_INVALID_ARG, "dlogits must be like the logits, with contiguous rows")
-    _check(lib().muon_logits_logprob_grad(C.byref(a), r, h, dlogits.data_ptr(), _row_stride(dlogits) if tokens else a.vocab,
-                                          dev.index, _raw_stream(stream, dev.index)))
+    index = dev.index
+    _check(lib().muon_logits_logprob_grad(
+        _pack_logits_args(tokens, vocab, logits.data_ptr(), _row_stride(logits) if tokens else vocab, _dtype_code(logits), 0,
+                          logit_scale, 0, target_ptr, 0, entropy, lse, 0, 0, 0),
+        r, h, dlogits.data_ptr(), _row_stride(dlogits) if tokens else vocab, index, _raw_stream(stream, index)))
     return dlogits
 
 

@@ -142,11 +142,21 @@ __device__ __forceinline__ double chunk_squares(const uint4 (&v)[kVectors]) {
   return d;
 }
 
-// One partial sum a block; blocks_before: partial sums that earlier launches of the call left.
-template <int kMost>
-__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Tensors<kMost> T, double* partials,
-                                                        int blocks_before) {
+// Sum over a block in a fixed order; thread 0 gets it.
+__device__ __forceinline__ double block_sum(double sum) {
   __shared__ double s_sum[kWarps];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  double t = s_sum[0];
+  for (int i = 1; i < kWarps; ++i) t += s_sum[i];
+  return t;
+}
+
+// A thread's squares of every gridDim.x-th chunk.
+template <int kMost>
+__device__ __forceinline__ double thread_squares(const Tensors<kMost>& T) {
   const unsigned chunks = T.count > 0 ? T.chunks_to[T.count - 1] : 0u;
   double sum = 0.0;
   for (unsigned c = blockIdx.x; c < chunks; c += gridDim.x) {
@@ -160,14 +170,17 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
       sum += chunk_squares<__nv_bfloat16>(v);
     }
   }
+  return sum;
+}
+
+// One partial sum a block; blocks_before: partial sums that earlier launches of the call left.
+template <int kMost>
+__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Tensors<kMost> T, double* partials,
+                                                        int blocks_before) {
+  const double sum = thread_squares(T);
   muon::ptx::grid_launch_dependents();
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-  __syncthreads();
+  double t = block_sum(sum);
   if (threadIdx.x == 0) {
-    double t = s_sum[0];
-    for (int i = 1; i < kWarps; ++i) t += s_sum[i];
     if (static_cast<int>(blockIdx.x) < blocks_before) t += partials[blockIdx.x];
     partials[blockIdx.x] = t;
   }
@@ -189,20 +202,37 @@ __device__ __forceinline__ void write_results(double sum, float max_norm, float 
 
 __global__ void __launch_bounds__(kThreads) join_kernel(const double* partials, int count, float max_norm, float eps,
                                                         double* sum_sq, float* norm, float* coef) {
-  __shared__ double s_sum[kWarps];
   muon::ptx::grid_dependency_wait();
   double sum = 0.0;
   for (int i = threadIdx.x; i < count; i += kThreads) sum += __ldcg(partials + i);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-  __syncthreads();
+  const double t = block_sum(sum);
   if (threadIdx.x == 0) {
-    double t = s_sum[0];
-    for (int i = 1; i < kWarps; ++i) t += s_sum[i];
     if (sum_sq != nullptr) *sum_sq = t;
     write_results(t, max_norm, eps, norm, coef);
   }
+}
+
+// Both in one launch, for few chunks: one cluster, whose first block adds up the others' sums.
+// (3 x 1408 + 65536 elements fp32: NORM_SMALL)
+constexpr int kClusterBlocks = 8;
+constexpr unsigned kClusterChunks = 64;
+__global__ void __launch_bounds__(kThreads) norm_cluster_kernel(const __grid_constant__ Tensors<kFewTensors> T, float max_norm, float eps,
+                                                                double* sum_sq, float* norm, float* coef) {
+  __shared__ double s_all;
+  const double mine = block_sum(thread_squares(T));
+  if (threadIdx.x == 0) s_all = mine;
+  muon::ptx::cluster_sync_all();
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    double t = mine;
+    for (int r = 1; r < kClusterBlocks; ++r) {
+      double theirs;
+      asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(theirs) : "r"(muon::ptx::map_to_cta(muon::ptx::smem_u32(&s_all), r)));
+      t += theirs;
+    }
+    if (sum_sq != nullptr) *sum_sq = t;
+    write_results(t, max_norm, eps, norm, coef);
+  }
+  muon::ptx::cluster_sync_all();  // sums stay until they are read
 }
 
 template <typename T, typename Out>
@@ -386,6 +416,23 @@ extern "C" int muon_grad_norm(const muon_grad_tensor* tensors, int n_tensors, fl
   CLIP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
   double* partials = static_cast<double*>(workspace);
+  if (n_tensors <= kFewTensors) {
+    Tensors<kFewTensors> T;
+    if (fill(tensors, 0, n_tensors, &T) == n_tensors && (T.count == 0 || T.chunks_to[T.count - 1] <= kClusterChunks)) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(kClusterBlocks);
+      cfg.blockDim = dim3(kThreads);
+      cfg.stream = stream;
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = kClusterBlocks;
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      CLIP_CUDA(cudaLaunchKernelEx(&cfg, norm_cluster_kernel, T, max_norm, eps, sum_sq, norm, coef));
+      return MUON_OK;
+    }
+  }
   int blocks = 0;  // partial sums so far
   auto launch = [&](const auto& T) {
     const int b = blocks_for(T.chunks_to[T.count - 1], sms);

@@ -79,3 +79,12 @@ def test_sizes_past_32_bits_are_refused(size):
     with pytest.raises(b.MuonError) as e:
         b.muon_logits_logprob(Fake(size.get("shape", (4, 10))), top=size.get("top", 0))
     assert e.value.code == b.MUON_ERR_UNSUPPORTED
+
+
+def test_structs_as_bytes_are_the_structs():
+    from paper_2502_16982_b200 import binding as b
+
+    v = (1, 2, 3, 4, 5, 6, 0.5, 8, 9, 10, 11, 12, 13, 14, 15)
+    assert bytes(b.muon_logits_args(*v)) == b._pack_logits_args(*v)
+    v = (1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 0.5, 13, 14, 15, 16)
+    assert bytes(b.muon_logprob_args(*v)) == b._pack_logprob_args(*v)
