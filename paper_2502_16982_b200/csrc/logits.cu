@@ -42,11 +42,16 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kVectors = 4;  // 16-byte loads of one tile a thread (forward: Cells::kVectors)
 constexpr int kTileVectors = kThreads * kVectors;
-// Blocks on an SM, which leaves a thread 64 registers.  (4096 x 163840 bf16 with 64
-// alternatives, us: 402 with 3 blocks, 375 with 4, 434 with 5, whose registers spill.)
-constexpr int kBlocksPerSm = 4;
+// Blocks on an SM: four leave a thread 64 registers, five 48.  (us, with 64 alternatives: 4096 x
+// 163840 bf16 402 with 3, 375 with 4, 434 with 5, whose registers spill; without: bf16 220 with
+// 4, 213 with 5, 229 with 6, 2048 x 163840 fp32 211 with 4, 214 with 5.)
+constexpr int blocks_per_sm(bool fp32, bool top) { return top || fp32 ? 4 : 5; }
+// Candidates up to which a thread each finds its place; of more, the best are found first.
+// (4096 x 163840 bf16 with 64: 357 us, with 256 in its place 363.)
+constexpr int kOrdered = 128;
 constexpr int kVectorList = 256;  // of a warp
 constexpr int kMaxTop = 128;
+static_assert(kMaxTop <= kOrdered && kOrdered <= kThreads, "what is left is put in order");
 constexpr int kKeys = kMaxTop + 32 * 8;  // candidates of a warp: the best, and a vector a lane
 constexpr int kMaxCluster = 8;
 constexpr int kSorted = 2048;  // where a block of a cluster leaves its best in the list of candidates
@@ -123,6 +128,12 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 
@@ -266,7 +277,8 @@ __device__ __forceinline__ Sums from_lane(const Sums& a, int lane) {
 
 struct Shared {
   Key list[kWarps * kKeys];  // candidates: kKeys a warp, at the end the block's first `count`
-  int vectors[kWarps][kVectorList + 32];  // the last 32 for what finds no room
+  int vectors[kWarps][kVectorList];
+  int listed[kWarps];  // more than kVectorList where some found no room
   int count, counts[kWarps];
   uint32_t reached[kWarps];  // ordered
   Sums sums[kWarps];
@@ -435,11 +447,12 @@ struct Collector {
 // its part that qualifies.  `first`: threshold of the first tile, later elements equal to which
 // come after the top that there are.
 template <bool kFp32>
-__device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uint4* cells, int shift, int begin, int end, int listed,
+__device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uint4* cells, int shift, int begin, int end,
                                     float first, float threshold) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Collector<kFp32> c = {P, sh.list + warp * kKeys, cells, shift, lane, 0, threshold};
   __syncwarp();
+  const int listed = sh.listed[warp];
   if (listed <= kVectorList) {
     for (int i = 0; i < listed; i += 32) c.take(i + lane < listed ? sh.vectors[warp][i + lane] : -1);
   } else {
@@ -458,7 +471,7 @@ __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uin
 }
 
 template <bool kFp32, bool kTop>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const __grid_constant__ LogitsParams P) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_kernel(const __grid_constant__ LogitsParams P) {
   using C = Cells<kFp32>;
   constexpr int kEach = C::kEach, kVectors = C::kVectors, kTileVectors = C::kTileVectors;
   extern __shared__ __align__(16) unsigned char raw[];
@@ -512,7 +525,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
     if (lane == 0) *const_cast<volatile uint32_t*>(&sh.reached[warp]) = t;
   };
   float bound = -INFINITY, first = -INFINITY;  // a vector is listed from `bound` on
-  int listed = 0;
+  if (kTop && lane == 0) sh.listed[warp] = 0;
+  __syncwarp();
   const uint64_t scale = pair(P.scale2, P.scale2);
   uint4 v[kVectors];
   auto load = [&](int v0, int i, bool whole) {
@@ -570,14 +584,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
 
     if constexpr (kTop) {
       const bool every = tile == 0 && !(bound > -INFINITY);  // NaNs, too
-      if (__any_sync(0xFFFFFFFFu, here >= bound || every)) {
+      if (here >= bound || every) {
 #pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-          const bool in = (largest[i].value() >= bound || every) && i * kThreads < left;
-          const unsigned who = __ballot_sync(0xFFFFFFFFu, in);
-          if (in) sh.vectors[warp][min(listed, kVectorList) + __popc(who & ((1u << lane) - 1u))] = v0 + i * kThreads + tid;
-          listed += __popc(who);
-        }
+        for (int i = 0; i < kVectors; ++i)
+          if ((largest[i].value() >= bound || every) && i * kThreads < left) {
+            const int at = atomicAdd(&sh.listed[warp], 1);
+            if (at < kVectorList) sh.vectors[warp][at] = v0 + i * kThreads + tid;
+          }
       }
       // later elements have larger columns: one that equals the first tile's threshold comes
       // after the top that there are
@@ -616,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
   }
   if (lane == 0) sh.sums[warp] = a;
   if (kTop) {
-    int count = collect<kFp32>(P, sh, cells, shift, begin, end, listed, first, threshold);
+    int count = collect<kFp32>(P, sh, cells, shift, begin, end, first, threshold);
     if (warp == 0) {
       const unsigned who = __ballot_sync(0xFFFFFFFFu, extra_at >= 0);
       if (extra_at >= 0) sh.list[count + __popc(who & ((1u << lane) - 1u))] = make_key<kFp32>(P, extra, extra_at);
@@ -646,8 +659,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
     for (int i = 0; i < kMaxTop / 32; ++i)
       if (i * 32 + lane < count) sh.list[before + i * 32 + lane] = mine[i];
     __syncthreads();
-    // as many as are put in order with a thread each stay
-    const bool cut = n > kThreads;
+    const bool cut = n > kOrdered;
     if (cut) {
       if (warp == 0) keep_best(sh.list, n, P.top, P.index_bits, lane);
       n = P.top;
@@ -705,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) logprob_kernel(const _
         if (lane == 0) sh.all = a;
       }
       __syncthreads();
-      if (candidates > kThreads) {
+      if (candidates > kOrdered) {
         if (kTop && warp == 0) keep_best(sh.list, candidates, P.top, P.index_bits, lane);
         candidates = P.top;
       }
@@ -766,6 +778,8 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
   const float c0 = -(r + h * entropy) * P.scale, c1 = -h * P.scale;
   const int target = static_cast<int>(y);
   const float at_target = r * P.scale;
+  const uint64_t scale = pair(P.scale, P.scale), minus_lse = pair(-lse, -lse), log2e = pair(kLog2e, kLog2e);
+  const uint64_t factor0 = pair(c0, c0), factor1 = pair(c1, c1);
   const bool vec = (reinterpret_cast<uintptr_t>(out - shift) & 15) == 0;
 #pragma unroll
   for (int i = 0; i < kVectors; ++i) {
@@ -773,13 +787,20 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
     if (index >= vectors) continue;
     float g[kEach];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      g[e] = 0.f;
+    for (int e = 0; e < kEach; e += 2) {
+      g[e] = g[e + 1] = 0.f;
       if (!nothing) {
-        const float log_q = max_nan(fmaf(C::value(v[i], e), P.scale, -lse), kFloor);
-        g[e] = ex2(log_q * kLog2e) * fmaf(c1, log_q, c0);
-        if (at + e == target) g[e] += at_target;
+        float l0, l1, x0, x1;
+        unpair(fma2(pair(C::value(v[i], e), C::value(v[i], e + 1)), scale, minus_lse), l0, l1);
+        const uint64_t log_q = pair(max_nan(l0, kFloor), max_nan(l1, kFloor));
+        unpair(mul2(log_q, log2e), x0, x1);
+        unpair(mul2(pair(ex2(x0), ex2(x1)), fma2(log_q, factor1, factor0)), g[e], g[e + 1]);
       }
+    }
+    if (!nothing && target >= at && target < at + kEach) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (at + e == target) g[e] += at_target;
     }
     if (vec && at >= 0 && at + kEach <= P.vocab) {
       uint32_t w[4];
