@@ -1,12 +1,15 @@
-"""Trains a small language model with the package's steps and losses, then distils it
-into a smaller one from its top logits.
+"""Trains a small language model with the package's steps and losses, distils it into a
+smaller one from its top logits, and trains that one on its own samples for a reward.
 
 The model is as small as shows every part in its place: token embedding, one residual
 matrix on the embedding of the last token and one on that of the token before,
-LM head.  The losses at the head give dX and dW (muon_head_xent, muon_head_distill);
-the two matrices are stepped by Muon (muon_step), embedding and head by AdamW
-(muon_adamw_step), in fp32 master weights with bf16 copies for the products.  The
-data is a synthetic second-order Markov chain.
+LM head.  The losses at the head give dX and dW (muon_head_xent, muon_head_distill, the
+log probabilities of muon_head_logprob with the gradient of an objective on them); all
+gradients are clipped by their global norm (MuonGrads), the two matrices stepped by Muon
+(muon_step), embedding and head by AdamW, which clips as it reads (muon_adamw_step), in
+fp32 master weights with bf16 copies for the products.  The teacher's entries come from
+its logits in one pass (muon_logits_logprob).  The data is a synthetic second-order
+Markov chain.
 
     python examples/train_and_distill.py [--steps 300] [--dim 256] [--vocab 4096]
 """
@@ -25,7 +28,7 @@ from paper_2502_16982_b200 import binding as mb  # noqa: E402
 class Model:
     """Master weights in fp32, bf16 copies for the products, optimizer state."""
 
-    def __init__(self, vocab, dim, seed):
+    def __init__(self, vocab, dim, seed, max_norm=float("inf")):
         g = torch.Generator(device="cuda").manual_seed(seed)
 
         def init(*shape, std):
@@ -44,6 +47,9 @@ class Model:
         self.moments = [torch.zeros_like(t) for t in (self.embed, self.embed, self.head, self.head)]
         self.embed_grad = torch.zeros_like(self.embed)
         self.head_grad = torch.empty_like(self.head16)
+        self.max_norm = max_norm
+        self.all_grads = mb.MuonGrads([self.mats_grad, self.embed_grad, self.head_grad])
+        self.mats_only = mb.MuonGrads([self.mats_grad])
         self.steps = 0
 
     def hidden(self, tokens):
@@ -63,9 +69,11 @@ class Model:
 
     def step(self, lr):
         self.steps += 1
+        total = self.all_grads.muon_grad_norm(self.max_norm)
+        self.mats_only.muon_clip_grads(self.max_norm, sum_sq=total.sum_sq)
         self.muon.muon_step(mb.Hyper(lr=lr, wd=0.0))
         mb.muon_adamw_step([self.embed, self.head], [self.embed_grad, self.head_grad], self.moments[0::2],
-                           self.moments[1::2], self.steps, lr=lr, wd=0.0)
+                           self.moments[1::2], self.steps, lr=lr, wd=0.0, coef=total.coef)
         self.embed16.copy_(self.embed)
         self.head16.copy_(self.head)
 
@@ -84,9 +92,11 @@ class Chain:
         t = torch.randint(0, self.vocab, (rows, length), generator=self.g, device="cuda")
         stray = torch.rand(rows, length, generator=self.g, device="cuda") < 0.125
         for i in range(2, length):
-            follow = (self.next1[t[:, i - 1]] + self.shift[t[:, i - 2]]) % self.vocab
-            t[:, i] = torch.where(stray[:, i], t[:, i], follow)
+            t[:, i] = torch.where(stray[:, i], t[:, i], self.follow(t[:, i - 1], t[:, i - 2]))
         return t
+
+    def follow(self, last, before):
+        return (self.next1[last] + self.shift[before]) % self.vocab
 
 
 def train(model, chain, steps, lr, rows, length):
@@ -109,16 +119,35 @@ def distil(student, teacher, chain, steps, lr, rows, length, top, temperature):
     losses = []
     for _ in range(steps):
         tokens = chain.batch(rows, length)
-        z = (teacher.hidden(tokens)[0] @ teacher.head16.t()).float()
-        lse = torch.logsumexp(z / temperature, dim=1)
-        z, ids = z.topk(top, dim=1)
+        best = mb.muon_logits_logprob(teacher.hidden(tokens)[0] @ teacher.head16.t(), top=top, logit_scale=1 / temperature)
         x, kept = student.hidden(tokens)
-        r = mb.muon_head_distill(x, student.head16, ids, z, temperature=temperature, teacher_lse=lse,
+        r = mb.muon_head_distill(x, student.head16, best.top_ids, best.top_logits, temperature=temperature, teacher_lse=best.lse,
                                  scale=temperature ** 2, dx=True, dw=student.head_grad)
         student.backward(r.dx, kept)
         student.step(lr)
         losses.append(r.total)
     return torch.cat(losses).tolist()
+
+
+def reinforce(model, chain, steps, lr, rows, length, bonus=1e-3):
+    """The model's own next tokens are rewarded where the chain would continue so: one
+    policy-gradient step a batch, the mean reward as baseline, with a bonus on the entropy."""
+    rewards = []
+    for _ in range(steps):
+        tokens = chain.batch(rows, length)
+        x, kept = model.hidden(tokens)
+        with torch.no_grad():
+            z = (x @ model.head16.t()).float()
+            sampled = torch.multinomial(torch.softmax(z, dim=1), 1, generator=chain.g)[:, 0]
+        reward = (sampled == chain.follow(tokens[:, 1:-1], tokens[:, :-2]).reshape(-1)).float()
+        r = mb.muon_head_logprob(x, model.head16, sampled)
+        n = reward.numel()
+        d = mb.muon_head_logprob_grad(x, model.head16, sampled, r, g_logprob=(reward.mean() - reward) / n,
+                                      g_entropy=torch.full_like(reward, -bonus / n), dx=True, dw=model.head_grad)
+        model.backward(d.dx, kept)
+        model.step(lr)
+        rewards.append(reward.mean())
+    return torch.stack(rewards).tolist() if rewards else []
 
 
 def perplexity_loss(model, chain, rows, length):
@@ -135,21 +164,26 @@ def main(argv=None):
     p.add_argument("--rows", type=int, default=64)
     p.add_argument("--length", type=int, default=66)
     p.add_argument("--lr", type=float, default=3e-3)
+    p.add_argument("--clip", type=float, default=float("inf"), help="largest global gradient norm")
+    p.add_argument("--policy-steps", type=int, default=40)
     a = p.parse_args(argv)
     chain = Chain(a.vocab, 1)
-    teacher = Model(a.vocab, a.dim, 2)
+    teacher = Model(a.vocab, a.dim, 2, a.clip)
     first = perplexity_loss(teacher, chain, a.rows, a.length)
     losses = train(teacher, chain, a.steps, a.lr, a.rows, a.length)
     taught = perplexity_loss(teacher, chain, a.rows, a.length)
     print("teacher: loss %.3f -> %.3f over %d steps, held out %.3f -> %.3f" % (losses[0], losses[-1], a.steps, first, taught))
-    student = Model(a.vocab, a.dim // 2, 3)
+    student = Model(a.vocab, a.dim // 2, 3, a.clip)
     kd = distil(student, teacher, chain, a.steps, a.lr, a.rows, a.length, 32, 2.0)
     final = perplexity_loss(student, chain, a.rows, a.length)
     print("student: distillation loss %.3f -> %.3f over %d steps, held-out loss %.3f" % (kd[0], kd[-1], a.steps, final))
+    reward = reinforce(student, chain, a.policy_steps, a.lr / 10, a.rows, a.length)
+    if reward:
+        print("student on its own samples: reward %.3f -> %.3f over %d steps" % (reward[0], reward[-1], a.policy_steps))
     for m in (teacher, student):
         status, which = m.muon.muon_status()
         assert status == 0, (status, which)
-    return {"teacher": losses, "first": first, "taught": taught, "student": kd, "final": final}
+    return {"teacher": losses, "first": first, "taught": taught, "student": kd, "final": final, "reward": reward}
 
 
 if __name__ == "__main__":

@@ -49,7 +49,7 @@ class DistributedMuon:
     partitioned as in ZeRO-1, and is half of AdamW's)."""
 
     def __init__(self, shapes: Sequence[Tuple[int, int, int, torch.dtype, torch.dtype]], device, dist=None,
-                 step_fn: Optional[Callable] = None):
+                 step_fn: Optional[Callable] = None, clip_fn: Optional[Callable] = None):
         self.dist = dist
         self.rank = dist.get_rank() if dist is not None else 0
         self.world = dist.get_world_size() if dist is not None else 1
@@ -118,6 +118,8 @@ class DistributedMuon:
                 self.unit_mats[u].append(triples[p])
 
         self._step_fn = step_fn
+        self._clip_fn = clip_fn
+        self._grads = None
         self._ctx = None
         if step_fn is None and self.local_groups:
             self._ctx = binding.MuonContext(self.local_groups)
@@ -235,6 +237,36 @@ class DistributedMuon:
             self._step_fn(self.unit_mats[u], hp)
         else:
             self._ctx.muon_step_bucket(hp, lb)
+
+    def clip_grads(self, max_norm: float, eps: float = 1e-6, others: Optional[torch.Tensor] = None, reduce_grads: bool = False):
+        """Before :meth:`step`: scales this rank's owned gradients so that the global norm of
+        all ranks' is at most ``max_norm``: the ranks add their sums of squares (one fp64
+        all-reduce) before the coefficient is formed.  ``others``: fp64 [1], this rank's share
+        of the sum of squares of parameters that are not Muon's, each counted by one rank.
+        ``reduce_grads``: the gradients are summed over the ranks first, and the step is then
+        called without (a norm needs all of them before the first matrix is stepped).
+        Returns what ``muon_clip_grads`` gives; its ``coef`` clips the others' AdamW step.
+        ``clip_fn(grads, max_norm, eps, sum_sq)``, with sum_sq None for the sum alone, replaces
+        the library call in tests on CPU ranks."""
+        if reduce_grads and self.world > 1:
+            for u in range(self.n_units):
+                self._reduce_scatter_unit(u)
+        grads = [t[1] for mats in self.unit_mats for t in mats]
+        clip = self._clip_fn or self._clip_library
+        total = clip(grads, None, eps, None)
+        if others is not None:
+            total = total + others
+        if self.world > 1:
+            self.dist.all_reduce(total)
+        return clip(grads, max_norm, eps, total)
+
+    def _clip_library(self, grads, max_norm, eps, sum_sq):
+        if self._grads is None:
+            # a rank may own nothing: an empty tensor has no elements to count or to scale
+            self._grads = binding.MuonGrads(grads or [torch.empty(0, device=self.device)])
+        if sum_sq is None:
+            return self._grads.muon_grad_norm().sum_sq
+        return self._grads.muon_clip_grads(max_norm, eps, sum_sq=sum_sq)
 
     def all_gather_weights(self) -> None:
         """Every rank ends with every owner's current weights (all buckets)."""

@@ -286,3 +286,29 @@ def test_refusals_of_the_handle():
     with pytest.raises(b.MuonError):
         b.muon_adamw_step([t], [t.clone()], [t.clone()], [t.clone()], 1, lr=0.1, wd=0.0, coef=torch.ones(1))
     assert float(t.sum()) == 100.0
+
+
+def test_owner_computes_step_clips_its_gradients():
+    from paper_2502_16982_b200 import binding as b
+    from paper_2502_16982_b200.distributed import DistributedMuon
+
+    m = DistributedMuon([(128, 192, 3, FP, FP), (64, 64, 2, BF, BF)], "cuda")
+    gen = torch.Generator().manual_seed(21)
+    for group in m.grads:
+        for g in group:
+            g.copy_(torch.randn(g.shape, generator=gen))
+    before = [g.clone() for group in m.grads for g in group]
+    other = torch.randn(1000, generator=gen).cuda()
+    want = norm64(before + [other])
+    r = m.clip_grads(0.5 * want, others=b.muon_grad_norm([other]).sum_sq)
+    assert abs(float(r.norm) - want) <= E_NORM * want
+    clipped = [g for group in m.grads for g in group]
+    for g, x in zip(clipped, before):
+        assert torch.equal(g, (x.float() * r.coef).to(x.dtype))
+    before = [g.clone() for g in clipped]
+    r = m.clip_grads(float("inf"))  # the handle is kept
+    assert float(r.coef) == 1.0 and abs(float(r.norm) - norm64(before)) <= E_NORM * norm64(before)
+    assert all(torch.equal(g, x) for g, x in zip(clipped, before))
+    m.step(b.Hyper(lr=1e-2))
+    assert m.status() == (0, -1)
+    m.close()
