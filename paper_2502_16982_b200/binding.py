@@ -849,8 +849,20 @@ def _token_vector(t, what, n, dev, dtype):
 
 
 # muon_logits_args and muon_logprob_args as bytes: a tenth of the time that the ctypes structs take
-_pack_logits_args = struct.Struct("=iiqqiifiqqqqqqq").pack
-_pack_logprob_args = struct.Struct("=iiiiqqqqiiqfiqqq").pack
+def _packer(form):
+    pack = struct.Struct(form).pack
+
+    def packed(*fields):
+        try:
+            return pack(*fields)
+        except (OverflowError, struct.error) as e:
+            raise MuonError(MUON_ERR_INVALID_ARG, "an argument that its field does not hold: %s" % e) from None
+
+    return packed
+
+
+_pack_logits_args = _packer("=iiqqiifiqqqqqqq")
+_pack_logprob_args = _packer("=iiiiqqqqiiqfiqqq")
 
 
 def _logits_operand(logits, targets, top):

@@ -417,3 +417,55 @@ def test_refusals_of_the_binding():
                 f(dx=torch.zeros(4, 63, device="cuda")), f(workspace=torch.zeros(1024, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(b.MuonError):
             b.muon_head_logprob_grad(**bad)
+
+
+@pytest.mark.parametrize("T,D,V", [(1100, 256, 2100), (300, 129, 3000)])
+def test_kept_without_codes_or_entropy(T, D, V):
+    """Where codes are not faster the forward pass keeps only what it gathered."""
+    from paper_2502_16982_b200 import binding as b
+
+    x, w, gen = make(T, D, V, 41)
+    targets = torch.randint(0, V, (T,), generator=gen)
+    targets[::5] = -100
+    y, z = targets.cuda(), np.where(targets.numpy() < 0, 0.0, 1.0)
+    ref = Reference(f64(x) * z[:, None], f64(w), targets.numpy(), 1.0)
+    rr = torch.randn(T, generator=gen)
+    for mode in (1, 2):
+        before, piece = b.muon_debug_set_head_codes(mode), b.muon_debug_set_head_piece_bytes(2 * T * 512)
+        try:
+            r = b.muon_head_logprob(x, w, y, keep=True, entropy=False)
+            assert r.kept is not None and r.entropy is None
+            d = b.muon_head_logprob_grad(x, w, y, r, g_logprob=rr.cuda(), dx=True, dw=True)
+        finally:
+            b.muon_debug_set_head_codes(before)
+            b.muon_debug_set_head_piece_bytes(piece)
+        ref.check(r)
+        ref.check_grads(d, rr.double().numpy() * z, None, kept=True)
+
+
+def test_more_logits_than_are_kept():
+    """3 GiB of codes, the rest of the logits formed again: REINFORCE with one advantage against
+    the cross entropy (both within 2^-8 of the sums, at most)."""
+    from paper_2502_16982_b200 import binding as b
+
+    T, D, V = 17000, 64, 110000
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    x = torch.randn(T, D, generator=gen, device="cuda").to(BF)
+    w = (torch.randn(V, D, generator=gen, device="cuda") * 0.3).to(BF)
+    y = torch.randint(0, V, (T,), generator=gen, device="cuda")
+    y[::11] = -1
+    before = b.muon_debug_set_head_codes(2)
+    try:
+        r = b.muon_head_logprob(x, w, y)
+        assert 3 << 30 > r.kept.numel() - T * V // 8 > (3 << 30) - (2 << 28)  # whole pieces beside the statistics
+        n = int((y >= 0).sum())
+        f32 = dict(device="cuda")
+        d = b.muon_head_logprob_grad(x, w, y, r, g_logprob=torch.full((T,), -1.0 / n, device="cuda"), dx=torch.empty(T, D, **f32),
+                                     dw=torch.empty(V, D, **f32))
+        del r
+        ref = b.muon_head_xent(x, w, y, dx=torch.empty(T, D, **f32), dw=torch.empty(V, D, **f32))
+    finally:
+        b.muon_debug_set_head_codes(before)
+    for p, q in zip(d, (ref.dx, ref.dw)):
+        assert float((p - q).norm()) <= 4e-3 * float(q.norm())
+    assert not d.dx[::11].any()

@@ -370,3 +370,52 @@ def test_refusals_of_the_binding():
                 f(dlogits=torch.zeros(4, 99, device="cuda"))):
         with pytest.raises(b.MuonError):
             b.muon_logits_logprob_grad(**bad)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("T", [6, 600])
+def test_masks_of_the_lowest_number(dtype, T):
+    """Entries masked with the dtype's lowest number are out, like those of minus infinity; a row
+    of them alone has nothing left."""
+    from paper_2502_16982_b200 import binding as b
+
+    V = 20003
+    gen = torch.Generator().manual_seed(31)
+    z = torch.randn(T, V, generator=gen).to(dtype)
+    masked = torch.rand(T, V, generator=gen) < 0.9
+    masked[:, 77] = False
+    masked[0] = True
+    low = torch.where(masked, torch.tensor(torch.finfo(dtype).min, dtype=dtype), z).cuda()
+    inf = torch.where(masked, torch.tensor(-float("inf"), dtype=dtype), z).cuda()
+    y = torch.full((T,), 77).cuda()
+    r, s = b.muon_logits_logprob(low, y, top=20), b.muon_logits_logprob(inf, y, top=20)
+    assert all(torch.equal(getattr(r, k), getattr(s, k)) for k in ("logprob", "entropy", "lse", "top_ids"))
+    assert float(r.lse[0]) == -float("inf") and float(r.entropy[0]) == 0.0
+    g = torch.ones(T, device="cuda")
+    d, e = (b.muon_logits_logprob_grad(q, y, v, g_logprob=g, g_entropy=g) for q, v in ((low, r), (inf, s)))
+    assert torch.equal(d, e) and not d[0].any() and not d[masked.cuda()].any()
+
+
+def test_calls_of_two_streams_at_once():
+    from paper_2502_16982_b200 import binding as b
+
+    gen = torch.Generator().manual_seed(32)
+    z = [(torch.randn(64, 50000, generator=gen) * 2).to(BF).cuda() for _ in range(2)]
+    y = torch.randint(0, 50000, (64,), generator=gen).cuda()
+    want = [b.muon_logits_logprob(v, y, top=32) for v in z]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[b.muon_logits_logprob(z[k], y, top=32, stream=streams[k]) for k in range(2)] for _ in range(20)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for r, w in zip(pair, want):
+            assert all(torch.equal(p, q) for p, q in zip(r, w))
+
+
+def test_a_scale_that_its_field_does_not_hold_is_refused():
+    from paper_2502_16982_b200 import binding as b
+
+    z, y = torch.zeros(4, 100, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    with pytest.raises(b.MuonError):
+        b.muon_logits_logprob(z, y, logit_scale=1e300)
