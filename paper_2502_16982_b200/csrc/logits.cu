@@ -536,8 +536,10 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
   };
 #pragma unroll
   for (int i = 0; i < kVectors; ++i) v[i] = load(begin, i, begin + kTileVectors <= end);
-  int tile = 0;
-  for (int v0 = begin; v0 < end; v0 += kTileVectors, ++tile) {
+  int tile = 0, v0 = begin;
+  // full: this tile and the next one lie in the part as a whole
+  auto take_tile = [&](auto full) {
+    constexpr bool kFull = decltype(full)::value;
     Largest<kFp32> largest[kVectors];
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) largest[i] = Largest<kFp32>::of(v[i]);
@@ -559,10 +561,10 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
     const uint64_t from = pair(base, base);
     uint64_t s = 0, w = 0;  // pairs of zeros
     const int left = end - v0 - tid;
-    const bool more = v0 + kTileVectors < end, whole = v0 + 2 * kTileVectors <= end;
+    const bool more = kFull || v0 + kTileVectors < end, whole = kFull || v0 + 2 * kTileVectors <= end;
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
-      if (i * kThreads < left) {
+      if (kFull || i * kThreads < left) {
 #pragma unroll
         for (int e = 0; e < kEach; e += 2) {
           const uint64_t d = fma2(pair(C::value(v[i], e), C::value(v[i], e + 1)), scale, from);
@@ -587,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
       if (here >= bound || every) {
 #pragma unroll
         for (int i = 0; i < kVectors; ++i)
-          if ((largest[i].value() >= bound || every) && i * kThreads < left) {
+          if ((largest[i].value() >= bound || every) && (kFull || i * kThreads < left)) {
             const int at = atomicAdd(&sh.listed[warp], 1);
             if (at < kVectorList) sh.vectors[warp][at] = v0 + i * kThreads + tid;
           }
@@ -599,7 +601,11 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
         bound = unordered(ordered(bound) + 1u);
       }
     }
-  }
+    ++tile;
+    v0 += kTileVectors;
+  };
+  while (v0 + 2 * kTileVectors <= end) take_tile(std::true_type{});
+  while (v0 < end) take_tile(std::false_type{});
   // 0 times an exponent of minus infinity, most often
   if (!(a.e == a.e)) a.e = weighted_again<kFp32>(cells, begin, end, P.scale2, a.m == -INFINITY ? 0.f : -a.m);
 
