@@ -15,7 +15,9 @@
 // their elements kept.  (Elements or vectors put aside as they come cost as much as the
 // sums.)  The threshold comes from the threads' running maxima: of a warp's 32 the want-th
 // largest, and of those values the m-th largest over the warps, want * m >= top, is reached by
-// at least `top` different elements.  It is formed again after 1, 2, 4, 8, ... tiles.  After
+// at least `top` different elements.  It is formed again with each of the first tiles and then
+// with every fourth (64 and 128 alternatives of 4096 x 163840, us: 307 and 367; with tiles 1, 2,
+// 4, 8, ... 325 and 517, with every tile 350 and 406).  After
 // the first tile the warps run without a barrier until the row ends; nothing is called within
 // the loop, because what lives across a call is stored with every tile.  A warp whose list
 // does not hold all (a row that ascends) reads its part again.
@@ -42,10 +44,11 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kVectors = 4;  // 16-byte loads of one tile a thread (forward: Cells::kVectors)
 constexpr int kTileVectors = kThreads * kVectors;
-// Blocks on an SM: four leave a thread 64 registers, five 48.  (us, with 64 alternatives: 4096 x
-// 163840 bf16 402 with 3, 375 with 4, 434 with 5, whose registers spill; without: bf16 220 with
-// 4, 213 with 5, 229 with 6, 2048 x 163840 fp32 211 with 4, 214 with 5.)
-constexpr int blocks_per_sm(bool fp32, bool top) { return top || fp32 ? 4 : 5; }
+// Blocks on an SM: five leave a thread 48 registers, four 64, three 80.  (us, with 64
+// alternatives: 4096 x 163840 bf16 380 with 3, 337 with 4, 325 with 5, 2048 x 163840 fp32 263,
+// 279 and 329, whose registers spill; without: bf16 220 with 4, 213 with 5, 229 with 6, fp32
+// 211 with 4, 214 with 5.)
+constexpr int blocks_per_sm(bool fp32, bool top) { return top ? (fp32 ? 3 : 5) : fp32 ? 4 : 5; }
 // Candidates up to which a thread each finds its place; of more, the best are found first.
 // (4096 x 163840 bf16 with 64: 357 us, with 256 in its place 363.)
 constexpr int kOrdered = 128;
@@ -408,14 +411,14 @@ struct Collector {
   int shift, lane, count;
   float threshold;
 
+  __device__ __forceinline__ uint4 read(int index) { return index >= 0 ? cells[index] : make_uint4(0u, 0u, 0u, 0u); }
+
   // a vector a lane, or none (negative)
-  __device__ __forceinline__ void take(int index) {
+  __device__ __forceinline__ void take(int index, const uint4& v) {
     using C = Cells<kFp32>;
     const bool all = !(threshold > -INFINITY);
     unsigned keep = 0;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
     if (index >= 0) {
-      v = cells[index];
 #pragma unroll
       for (int e = 0; e < C::kEach; ++e) keep |= static_cast<unsigned>(C::value(v, e) >= threshold || all) << e;
     }
@@ -454,7 +457,20 @@ __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uin
   __syncwarp();
   const int listed = sh.listed[warp];
   if (listed <= kVectorList) {
-    for (int i = 0; i < listed; i += 32) c.take(i + lane < listed ? sh.vectors[warp][i + lane] : -1);
+    constexpr int kAtOnce = 4;  // loads in flight
+    for (int first = 0; first < listed; first += 32 * kAtOnce) {
+      int index[kAtOnce];
+      uint4 v[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int at = first + i * 32 + lane;
+        index[i] = at < listed ? sh.vectors[warp][at] : -1;
+        v[i] = c.read(index[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (first + i * 32 < listed) c.take(index[i], v[i]);
+    }
   } else {
     for (int v0 = begin + static_cast<int>(threadIdx.x) - lane; v0 < end; v0 += kThreads) {
       const int index = v0 + lane;
@@ -464,7 +480,7 @@ __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uin
         const float x = Largest<kFp32>::of(cells[index]).value();
         mark = early ? x >= threshold || !(threshold > -INFINITY) : x >= threshold && x > first;
       }
-      if (__any_sync(0xFFFFFFFFu, mark)) c.take(mark ? index : -1);
+      if (__any_sync(0xFFFFFFFFu, mark)) c.take(mark ? index : -1, c.read(mark ? index : -1));
     }
   }
   return c.count;
@@ -548,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
     for (int i = 1; i < kVectors; ++i) all_of.join(largest[i]);
     const float here = all_of.value();
     most = fmaxf(most, here);
-    if (kTop && (tile & (tile + 1)) == 0) {
+    if (kTop && (tile < 4 || (tile & 3) == 3)) {
       note_reached();
       if (tile == 0) __syncthreads();
       // later others' may be of earlier tiles, and lower
