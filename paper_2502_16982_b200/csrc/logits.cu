@@ -58,6 +58,7 @@ static_assert(kMaxTop <= kOrdered && kOrdered <= kThreads, "what is left is put 
 constexpr int kKeys = kMaxTop + 32 * 8;  // candidates of a warp: the best, and a vector a lane
 constexpr int kMaxCluster = 8;
 constexpr int kSorted = 2048;  // where a block of a cluster leaves its best in the list of candidates
+static_assert(kMaxCluster == kWarps, "a warp reads a block's list");
 static_assert(kMaxCluster * kMaxTop <= kSorted && kSorted + kMaxTop <= kWarps * kKeys, "a cluster's best fit before a block's");
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2e = 1.44269504088896341f;
@@ -283,7 +284,7 @@ struct Shared {
   int vectors[kWarps][kVectorList];
   int listed[kWarps];  // more than kVectorList where some found no room
   int count, counts[kWarps];
-  uint32_t reached[kWarps];  // ordered
+  uint32_t reached[2][kWarps];  // ordered; of the first tile, and of all so far
   Sums sums[kWarps];
   Sums all;
 };
@@ -447,11 +448,11 @@ struct Collector {
 };
 
 // Of the vectors that the warp put in its list, or, where it did not hold all, of every one of
-// its part that qualifies.  `first`: threshold of the first tile, later elements equal to which
-// come after the top that there are.
+// its part that qualifies.  `first_tile`: threshold of the first tile, later elements equal to
+// which come after the top that there are.
 template <bool kFp32>
 __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uint4* cells, int shift, int begin, int end,
-                                    float first, float threshold) {
+                                    float first_tile, float threshold) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Collector<kFp32> c = {P, sh.list + warp * kKeys, cells, shift, lane, 0, threshold};
   __syncwarp();
@@ -478,7 +479,7 @@ __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uin
       bool mark = false;
       if (index < end) {
         const float x = Largest<kFp32>::of(cells[index]).value();
-        mark = early ? x >= threshold || !(threshold > -INFINITY) : x >= threshold && x > first;
+        mark = early ? x >= threshold || !(threshold > -INFINITY) : x >= threshold && x > first_tile;
       }
       if (__any_sync(0xFFFFFFFFu, mark)) c.take(mark ? index : -1, c.read(mark ? index : -1));
     }
@@ -536,9 +537,13 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
   // top; want > 32: everything is a candidate
   const int active = min(kWarps, (end - begin) / 32), want = active > 0 ? (P.top + active - 1) / active : 33;
   const int m = (P.top + want - 1) / want;
-  auto note_reached = [&]() {
+  auto note_reached = [&](int tile) {
     const uint32_t t = want <= 32 && warp < active ? reached_by(ordered(most), want) : kLowestOrdered;
-    if (lane == 0) *const_cast<volatile uint32_t*>(&sh.reached[warp]) = t;
+    if (lane == 0) {
+      volatile uint32_t* mine = &sh.reached[0][warp];
+      if (tile == 0) mine[0] = t;
+      mine[kWarps] = t;
+    }
   };
   float bound = -INFINITY, first = -INFINITY;  // a vector is listed from `bound` on
   if (kTop && lane == 0) sh.listed[warp] = 0;
@@ -565,10 +570,11 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
     const float here = all_of.value();
     most = fmaxf(most, here);
     if (kTop && (tile < 4 || (tile & 3) == 3)) {
-      note_reached();
+      note_reached(tile);
       if (tile == 0) __syncthreads();
-      // later others' may be of earlier tiles, and lower
-      threshold = fmaxf(threshold, unordered(mth_of(sh.reached, m, lane)));
+      // Of the first tile only its own: `first` has to be reached by elements that come before
+      // all later tiles'.  Afterwards others' may be of earlier tiles, and lower, or of later ones.
+      threshold = fmaxf(threshold, unordered(mth_of(sh.reached[tile > 0], m, lane)));
       bound = fmaxf(bound, threshold);
     }
     const float reference = most * P.scale2;
