@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const double* partials, 
 }
 
 // Both in one launch, for few chunks: one cluster, whose first block adds up the others' sums.
-// (3 x 1408 + 65536 elements fp32: NORM_SMALL)
+// (3 x 1408 + 65536 elements fp32: 3.4 us on the device either way, a call 4.5 us of the host's time, two
+// launches 6.8.)
 constexpr int kClusterBlocks = 8;
 constexpr unsigned kClusterChunks = 64;
 __global__ void __launch_bounds__(kThreads) norm_cluster_kernel(const __grid_constant__ Tensors<kFewTensors> T, float max_norm, float eps,
