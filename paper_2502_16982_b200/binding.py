@@ -12,7 +12,9 @@ import contextlib
 import ctypes as C
 import os
 import struct
+from array import array
 from dataclasses import dataclass
+from operator import attrgetter
 from typing import List, NamedTuple, Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -249,15 +251,23 @@ class Hyper:
 _dtype_codes = {}
 
 
-def _dtype_code(t):
-    code = _dtype_codes.get(t.dtype)
+_dtype_of = attrgetter("dtype")
+
+
+def _dtype_code_of(dtype):
+    code = _dtype_codes.get(dtype)
     if code is not None:
         return code
     import torch
     _dtype_codes.update({torch.bfloat16: MUON_DTYPE_BF16, torch.float32: MUON_DTYPE_FP32})
-    if t.dtype in _dtype_codes:
-        return _dtype_codes[t.dtype]
-    raise MuonError(MUON_ERR_UNSUPPORTED, "dtype %s" % t.dtype)
+    if dtype in _dtype_codes:
+        return _dtype_codes[dtype]
+    raise MuonError(MUON_ERR_UNSUPPORTED, "dtype %s" % dtype)
+
+
+def _dtype_code(t):
+    code = _dtype_codes.get(t.dtype)
+    return _dtype_code_of(t.dtype) if code is None else code
 
 
 class _GroupArrays:
@@ -341,19 +351,27 @@ def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, 
     element that multiplies every gradient as it is read, as :class:`MuonGrads` gives
     it (NaN: the step changes nothing)."""
     import torch
-    n = len(params)
-    flat = []  # muon_adamw_tensor as six 64-bit words: four addresses, numel, both dtypes
-    for p, g, m, v in zip(params, grads, exp_avgs, exp_avg_sqs):
-        numel = p.numel()
-        for t in (p, g, m, v):
-            if not t.is_contiguous() or t.numel() != numel:
-                raise MuonError(MUON_ERR_INVALID_ARG, "AdamW tensors must be contiguous and equally sized")
-        if m.dtype is not torch.float32 or v.dtype is not torch.float32:
-            raise MuonError(MUON_ERR_INVALID_ARG, "AdamW moments must be fp32")
-        flat += (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), numel, _dtype_code(p) | _dtype_code(g) << 32)
-    if len(flat) != 6 * n:
+    n, columns = len(params), (params, grads, exp_avgs, exp_avg_sqs)
+    if any(len(c) != n for c in columns):
         raise MuonError(MUON_ERR_INVALID_ARG, "as many gradients and moments as parameters")
-    arr = (C.c_int64 * len(flat))(*flat)
+    # column by column: a method's map costs half of a loop over the tensors
+    T = torch.Tensor
+    numels = list(map(T.numel, params))
+    for c in columns:
+        if not all(map(T.is_contiguous, c)) or list(map(T.numel, c)) != numels:
+            raise MuonError(MUON_ERR_INVALID_ARG, "AdamW tensors must be contiguous and equally sized")
+    if set(map(_dtype_of, exp_avgs)) | set(map(_dtype_of, exp_avg_sqs)) != {torch.float32}:
+        raise MuonError(MUON_ERR_INVALID_ARG, "AdamW moments must be fp32")
+    kinds = list(zip(map(_dtype_of, params), map(_dtype_of, grads)))
+    codes = {kind: _dtype_code_of(kind[0]) | _dtype_code_of(kind[1]) << 32 for kind in set(kinds)}
+    # muon_adamw_tensor as six 64-bit words: four addresses, numel, both dtypes
+    flat = [0] * (6 * n)
+    for k, c in enumerate(columns):
+        flat[k::6] = map(T.data_ptr, c)
+    flat[4::6] = numels
+    flat[5::6] = map(codes.__getitem__, kinds)
+    flat = array("q", flat)  # a sixth of the time of a ctypes array
+    arr = flat.buffer_info()[0]
     dev = params[0].device.index
     s = _raw_stream(stream, dev)
     hp = muon_adamw_hparams(lr, wd, beta1, beta2, eps, int(step))

@@ -4,7 +4,7 @@
 // decoupled weight decay:
 //   m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g^2
 //   p <- p - lr * ( (m / (1-beta1^t)) / (sqrt(v / (1-beta2^t)) + eps) + wd p )
-// One launch covers up to kMaxTensors tensors (their descriptors travel as
+// One launch covers up to kManyTensors tensors (their descriptors travel as
 // kernel parameters, so nothing is allocated); a pure HBM-streaming kernel:
 // 22 bytes per element with bf16 p and g (g 2, m 4+4, v 4+4, p 2+2).  Where the
 // gradients are clipped by their global norm, the coefficient multiplies them here as
@@ -23,7 +23,8 @@ void set_last_error(const char* msg);
 
 namespace {
 
-constexpr int kMaxTensors = 48;
+constexpr int kFewTensors = 48;    // fewer parameters take less time to pass
+constexpr int kManyTensors = 600;  // 52 bytes each, of 32764 bytes of parameters
 constexpr int kThreads = 128;
 // Two 8-element vectors in flight per thread; blocks of all tensors together, dealt out by
 // their sizes.  (2 x 335544320 + 55 x 2048 elements, fp32 with bf16
@@ -40,14 +41,19 @@ struct TensorArg {
   int p_fp32, g_fp32;
 };
 
-struct LaunchArgs {
-  TensorArg t[kMaxTensors];
-  int blocks_to[kMaxTensors];  // blocks of this tensor and of those before it
+struct Step {
   int count;
   float lr, wd, beta1, beta2, eps;
   float inv_bc1, inv_bc2;  // 1 / (1 - beta^t)
   const float* coef;       // clipped step: factor of every gradient
 };
+
+template <int kMost>
+struct LaunchArgs : Step {
+  TensorArg t[kMost];
+  int blocks_to[kMost];  // blocks of this tensor and of those before it
+};
+static_assert(sizeof(LaunchArgs<kManyTensors>) <= 32764, "kernel parameters");
 
 __device__ __forceinline__ void load8(const void* base, long long i, bool fp32, float (&out)[8]) {
   if (fp32) {
@@ -66,7 +72,7 @@ __device__ __forceinline__ void load8(const void* base, long long i, bool fp32, 
   }
 }
 
-__device__ __forceinline__ float adamw_one(float& p, float g, float& m, float& v, const LaunchArgs& A) {
+__device__ __forceinline__ float adamw_one(float& p, float g, float& m, float& v, const Step& A) {
   m = fmaf(A.beta1, m, (1.0f - A.beta1) * g);
   v = fmaf(A.beta2, v, (1.0f - A.beta2) * g * g);
   const float upd = (m * A.inv_bc1) / (sqrtf(v * A.inv_bc2) + A.eps);
@@ -74,10 +80,14 @@ __device__ __forceinline__ float adamw_one(float& p, float g, float& m, float& v
   return p;
 }
 
-template <bool kClip>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ LaunchArgs A) {
-  int which = 0;
-  while (A.blocks_to[which] <= static_cast<int>(blockIdx.x)) ++which;
+template <int kMost, bool kClip>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ LaunchArgs<kMost> A) {
+  int which = 0, last = A.count - 1;
+  while (which < last) {
+    const int mid = (which + last) >> 1;
+    if (A.blocks_to[mid] > static_cast<int>(blockIdx.x)) last = mid;
+    else which = mid + 1;
+  }
   const TensorArg T = A.t[which];
   const int before = which > 0 ? A.blocks_to[which - 1] : 0;
   const int block = static_cast<int>(blockIdx.x) - before, blocks = A.blocks_to[which] - before;
@@ -141,6 +151,34 @@ int fail(int code, const char* msg) {
   return code;
 }
 
+template <int kMost>
+int launch_all(const muon_adamw_tensor* tensors, int n_tensors, const Step& step, int sms, cudaStream_t stream) {
+  for (int first = 0; first < n_tensors; first += kMost) {
+    LaunchArgs<kMost> A;
+    static_cast<Step&>(A) = step;
+    A.count = n_tensors - first < kMost ? n_tensors - first : kMost;
+    double all = 0.0;
+    for (int i = 0; i < A.count; ++i) {
+      const muon_adamw_tensor& t = tensors[first + i];
+      A.t[i] = TensorArg{t.p, t.g, t.m, t.v, t.numel, t.p_dtype == MUON_DTYPE_FP32, t.g_dtype == MUON_DTYPE_FP32};
+      all += static_cast<double>(t.numel);
+    }
+    int grid = 0;
+    for (int i = 0; i < A.count; ++i) {
+      const long long most = (A.t[i].numel + kThreads * 16 - 1) / (kThreads * 16);  // a trip each
+      long long share = static_cast<long long>(static_cast<double>(sms) * kCtasPerSm * (A.t[i].numel / all)) + 1;
+      if (share > most) share = most;
+      grid += static_cast<int>(share);
+      A.blocks_to[i] = grid;
+    }
+    if (step.coef) adamw_kernel<kMost, true><<<grid, kThreads, 0, stream>>>(A);
+    else adamw_kernel<kMost, false><<<grid, kThreads, 0, stream>>>(A);
+    const cudaError_t ce = cudaGetLastError();
+    if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, cudaGetErrorString(ce));
+  }
+  return MUON_OK;
+}
+
 int step(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp, const float* coef, int device,
          void* stream_v) {
   if (!tensors || n_tensors <= 0 || !hp) return fail(MUON_ERR_INVALID_ARG, "tensors or hparams is null, or n_tensors <= 0");
@@ -167,33 +205,13 @@ int step(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hpara
   cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
   const double bc1 = 1.0 - std::pow(static_cast<double>(hp->beta1), hp->step);
   const double bc2 = 1.0 - std::pow(static_cast<double>(hp->beta2), hp->step);
-  for (int first = 0; first < n_tensors; first += kMaxTensors) {
-    LaunchArgs A{};
-    A.count = n_tensors - first < kMaxTensors ? n_tensors - first : kMaxTensors;
-    double all = 0.0;
-    for (int i = 0; i < A.count; ++i) {
-      const muon_adamw_tensor& t = tensors[first + i];
-      A.t[i] = TensorArg{t.p, t.g, t.m, t.v, t.numel, t.p_dtype == MUON_DTYPE_FP32, t.g_dtype == MUON_DTYPE_FP32};
-      all += static_cast<double>(t.numel);
-    }
-    int grid = 0;
-    for (int i = 0; i < A.count; ++i) {
-      const long long most = (A.t[i].numel + kThreads * 16 - 1) / (kThreads * 16);  // a trip each
-      long long share = static_cast<long long>(static_cast<double>(sms) * kCtasPerSm * (A.t[i].numel / all)) + 1;
-      if (share > most) share = most;
-      grid += static_cast<int>(share);
-      A.blocks_to[i] = grid;
-    }
-    A.lr = hp->lr; A.wd = hp->wd; A.beta1 = hp->beta1; A.beta2 = hp->beta2; A.eps = hp->eps;
-    A.inv_bc1 = static_cast<float>(1.0 / bc1);
-    A.inv_bc2 = static_cast<float>(1.0 / bc2);
-    A.coef = coef;
-    if (coef) adamw_kernel<true><<<grid, kThreads, 0, stream>>>(A);
-    else adamw_kernel<false><<<grid, kThreads, 0, stream>>>(A);
-    ce = cudaGetLastError();
-    if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, cudaGetErrorString(ce));
-  }
-  return MUON_OK;
+  Step s = {};
+  s.lr = hp->lr; s.wd = hp->wd; s.beta1 = hp->beta1; s.beta2 = hp->beta2; s.eps = hp->eps;
+  s.inv_bc1 = static_cast<float>(1.0 / bc1);
+  s.inv_bc2 = static_cast<float>(1.0 / bc2);
+  s.coef = coef;
+  return n_tensors <= kFewTensors ? launch_all<kFewTensors>(tensors, n_tensors, s, sms, stream)
+                                  : launch_all<kManyTensors>(tensors, n_tensors, s, sms, stream);
 }
 
 }  // namespace
