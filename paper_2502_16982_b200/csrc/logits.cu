@@ -40,26 +40,32 @@ namespace {
 
 namespace ptx = muon::ptx;
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kVectors = 4;  // 16-byte loads of one tile a thread (forward: Cells::kVectors)
+constexpr int kThreads = 256;  // forward: or kShortThreads
+constexpr int kVectors = 4;    // gradient: 16-byte loads a thread
 constexpr int kTileVectors = kThreads * kVectors;
 // Blocks on an SM: five leave a thread 48 registers, four 64, three 80.  (us, with 64
 // alternatives: 4096 x 163840 bf16 380 with 3, 337 with 4, 325 with 5, 2048 x 163840 fp32 263,
 // 279 and 329, whose registers spill; without: bf16 220 with 4, 213 with 5, 229 with 6, fp32
 // 211 with 4, 214 with 5.)
-constexpr int blocks_per_sm(bool fp32, bool top) { return top ? (fp32 ? 3 : 5) : fp32 ? 4 : 5; }
+constexpr int blocks_per_sm(bool fp32, bool top, int threads) { return (top ? (fp32 ? 3 : 5) : fp32 ? 4 : 5) * kThreads / threads; }
+// Short rows that a block takes alone: blocks of half the threads, twice as many, whose starts
+// and ends overlap.  (us, 4000 tokens, bf16, blocks of 256 and of 128 threads: 2000 columns 22.1
+// and 15.7, 16384 34.0 and 31.1, 50021 73.0 and 72.1; with 20 alternatives 2000 92.7 and 39.1,
+// 16384 75.3 and 62.4; with 64 50021 176 and 160, 100000 229 and 235; fp32 8192 32.0 and 25.9,
+// 32000 79.3 and 80.3, with 64 155 and 135.)  Twice the vectors where there are alternatives.
+constexpr int kShortThreads = 128;
+constexpr int kShortVectors = 4096;
 // Candidates up to which a thread each finds its place; of more, the best are found first.
 // (4096 x 163840 bf16 with 64: 357 us, with 256 in its place 363.)
 constexpr int kOrdered = 128;
 constexpr int kVectorList = 256;  // of a warp
 constexpr int kMaxTop = 128;
-static_assert(kMaxTop <= kOrdered && kOrdered <= kThreads, "what is left is put in order");
+static_assert(kMaxTop <= kOrdered && kOrdered <= kShortThreads, "what is left is put in order");
 constexpr int kKeys = kMaxTop + 32 * 8;  // candidates of a warp: the best, and a vector a lane
 constexpr int kMaxCluster = 8;
 constexpr int kSorted = 2048;  // where a block of a cluster leaves its best in the list of candidates
-static_assert(kMaxCluster == kWarps, "a warp reads a block's list");
-static_assert(kMaxCluster * kMaxTop <= kSorted && kSorted + kMaxTop <= kWarps * kKeys, "a cluster's best fit before a block's");
+static_assert(kMaxCluster == kThreads / 32, "a warp reads a block's list");
+static_assert(kMaxCluster * kMaxTop <= kSorted && kSorted + kMaxTop <= kThreads / 32 * kKeys, "a cluster's best fit before a block's");
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kFloor = -200.0f;  // exponents of 2 from here down give 0, and stay finite in products
@@ -149,7 +155,6 @@ struct Cells {
   // Of one tile a thread: 32 elements, whose arithmetic covers the next tile's loads.  (2048 x
   // 163840 fp32 without and with 64 alternatives, us: 223 and 391 with 4, 212 and 282 with 8.)
   static constexpr int kVectors = kFp32 ? 8 : 4;
-  static constexpr int kTileVectors = kThreads * kVectors;
   static constexpr uint32_t kLowest = kFp32 ? 0xFF800000u : 0xFF80FF80u;  // -inf throughout
   static __device__ __forceinline__ float value(const uint4& v, int e) {
     if constexpr (kFp32) {
@@ -258,7 +263,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
 }
 
 // The sum of d 2^d over a thread's elements, read again, with exponents from kFloor on.
-template <bool kFp32>
+template <bool kFp32, int kThreads>
 __device__ __noinline__ float weighted_again(const uint4* cells, int begin, int end, float scale2, float base) {
   float sum = 0.f;
 #pragma unroll 1
@@ -279,7 +284,9 @@ __device__ __forceinline__ Sums from_lane(const Sums& a, int lane) {
   return Sums{__shfl_sync(0xFFFFFFFFu, a.m, lane), __shfl_sync(0xFFFFFFFFu, a.s, lane), __shfl_sync(0xFFFFFFFFu, a.e, lane)};
 }
 
+template <int kThreads>
 struct Shared {
+  static constexpr int kWarps = kThreads / 32;
   Key list[kWarps * kKeys];  // candidates: kKeys a warp, at the end the block's first `count`
   int vectors[kWarps][kVectorList];
   int listed[kWarps];  // more than kVectorList where some found no room
@@ -361,7 +368,7 @@ __device__ __forceinline__ Cut find_cut(const Key* list, int n, int top, int bit
 }
 
 __device__ __noinline__ void keep_best(Key* list, int n, int top, int bits, int lane) {
-  static_assert(kWarps * kMaxTop <= 32 * 32 && kKeys <= 32 * 32, "all candidates in registers");
+  static_assert(kThreads / 32 * kMaxTop <= 32 * 32 && kKeys <= 32 * 32, "all candidates in registers");
   __syncwarp();
   const Cut cut = n <= 64 ? find_cut<2>(list, n, top, bits, lane)
                   : n <= 192 ? find_cut<6>(list, n, top, bits, lane)
@@ -393,6 +400,7 @@ __device__ __forceinline__ uint32_t reached_by(uint32_t mine, int want) {
 }
 
 // The m-th largest of the warps' values.
+template <int kWarps>
 __device__ __forceinline__ uint32_t mth_of(const volatile uint32_t* v, int m, int lane) {
   const uint32_t mine = v[lane & (kWarps - 1)];
   int not_less = 0;
@@ -450,8 +458,8 @@ struct Collector {
 // Of the vectors that the warp put in its list, or, where it did not hold all, of every one of
 // its part that qualifies.  `first_tile`: threshold of the first tile, later elements equal to
 // which come after the top that there are.
-template <bool kFp32>
-__device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uint4* cells, int shift, int begin, int end,
+template <bool kFp32, int kThreads>
+__device__ __noinline__ int collect(const LogitsParams& P, Shared<kThreads>& sh, const uint4* cells, int shift, int begin, int end,
                                     float first_tile, float threshold) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Collector<kFp32> c = {P, sh.list + warp * kKeys, cells, shift, lane, 0, threshold};
@@ -475,7 +483,7 @@ __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uin
   } else {
     for (int v0 = begin + static_cast<int>(threadIdx.x) - lane; v0 < end; v0 += kThreads) {
       const int index = v0 + lane;
-      const bool early = v0 < begin + Cells<kFp32>::kTileVectors;
+      const bool early = v0 < begin + kThreads * Cells<kFp32>::kVectors;
       bool mark = false;
       if (index < end) {
         const float x = Largest<kFp32>::of(cells[index]).value();
@@ -487,10 +495,11 @@ __device__ __noinline__ int collect(const LogitsParams& P, Shared& sh, const uin
   return c.count;
 }
 
-template <bool kFp32, bool kTop>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_kernel(const __grid_constant__ LogitsParams P) {
+template <bool kFp32, bool kTop, int kThreads>
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop, kThreads)) logprob_kernel(const __grid_constant__ LogitsParams P) {
   using C = Cells<kFp32>;
-  constexpr int kEach = C::kEach, kVectors = C::kVectors, kTileVectors = C::kTileVectors;
+  constexpr int kEach = C::kEach, kVectors = C::kVectors, kTileVectors = kThreads * kVectors, kWarps = kThreads / 32;
+  using Shared = Shared<kThreads>;
   extern __shared__ __align__(16) unsigned char raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);
   __shared__ float s_target;
@@ -574,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
       if (tile == 0) __syncthreads();
       // Of the first tile only its own: `first` has to be reached by elements that come before
       // all later tiles'.  Afterwards others' may be of earlier tiles, and lower, or of later ones.
-      threshold = fmaxf(threshold, unordered(mth_of(sh.reached[tile > 0], m, lane)));
+      threshold = fmaxf(threshold, unordered(mth_of<kWarps>(sh.reached[tile > 0], m, lane)));
       bound = fmaxf(bound, threshold);
     }
     const float reference = most * P.scale2;
@@ -629,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
   while (v0 + 2 * kTileVectors <= end) take_tile(std::true_type{});
   while (v0 < end) take_tile(std::false_type{});
   // 0 times an exponent of minus infinity, most often
-  if (!(a.e == a.e)) a.e = weighted_again<kFp32>(cells, begin, end, P.scale2, a.m == -INFINITY ? 0.f : -a.m);
+  if (!(a.e == a.e)) a.e = weighted_again<kFp32, kThreads>(cells, begin, end, P.scale2, a.m == -INFINITY ? 0.f : -a.m);
 
   // elements outside whole vectors
   float extra = 0.f;
@@ -657,7 +666,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop)) logprob_
   }
   if (lane == 0) sh.sums[warp] = a;
   if (kTop) {
-    int count = collect<kFp32>(P, sh, cells, shift, begin, end, first, threshold);
+    int count = collect<kFp32, kThreads>(P, sh, cells, shift, begin, end, first, threshold);
     if (warp == 0) {
       const unsigned who = __ballot_sync(0xFFFFFFFFu, extra_at >= 0);
       if (extra_at >= 0) sh.list[count + __popc(who & ((1u << lane) - 1u))] = make_key<kFp32>(P, extra, extra_at);
@@ -907,12 +916,12 @@ int parts_for(int tokens, long long vectors, int sms) {
   return parts;
 }
 
-template <bool kFp32, bool kTop>
-cudaError_t launch(const LogitsParams& P, int rows, int parts, cudaStream_t stream) {
+template <bool kFp32, bool kTop, int kThreads>
+cudaError_t launch_of(const LogitsParams& P, int rows, int parts, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Shared);
+  cfg.dynamicSmemBytes = sizeof(Shared<kThreads>);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -921,7 +930,14 @@ cudaError_t launch(const LogitsParams& P, int rows, int parts, cudaStream_t stre
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<kFp32, kTop>, P);
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<kFp32, kTop, kThreads>, P);
+}
+
+template <bool kFp32, bool kTop>
+cudaError_t launch(const LogitsParams& P, int rows, int parts, cudaStream_t stream) {
+  // (of its four warps each has 32 maxima for a fourth of `top`)
+  const bool brief = parts == 1 && P.vocab / Cells<kFp32>::kEach <= (kTop ? 2 : 1) * kShortVectors && P.top <= kMaxTop / 2;
+  return brief ? launch_of<kFp32, kTop, kShortThreads>(P, rows, parts, stream) : launch_of<kFp32, kTop, kThreads>(P, rows, parts, stream);
 }
 
 }  // namespace

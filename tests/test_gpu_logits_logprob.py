@@ -130,6 +130,13 @@ def check_rows(r, z, targets, scale, top):
     (40, 30000, 0, "normal", dict(masked=0.2)),
     (1000, 12345, 0, "spread", dict(pad=1)),
     (70001, 9, 3, "normal", {}),                          # more rows than a grid's dimension
+    (2000, 2003, 64, "ties", dict(pad=2, masked=0.1)),    # short rows: blocks of half the threads
+    (700, 3001, 64, "constant", dict(offset=3)),
+    (300, 1000, 64, "ascending", {}),
+    (620, 32768, 0, "normal", {}),                        # at the limits of short rows, and behind them
+    (620, 32776, 0, "normal", {}),
+    (310, 65536, 64, "ascending", {}),
+    (310, 65544, 64, "ties", {}),
     (1, 1 << 24, 128, "normal", {}),
 ])
 @pytest.mark.parametrize("dtype", [BF, FP])
