@@ -14,6 +14,7 @@ import os
 import struct
 from array import array
 from dataclasses import dataclass
+from itertools import islice
 from operator import attrgetter
 from typing import List, NamedTuple, Optional, Sequence
 
@@ -351,7 +352,11 @@ def muon_adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, 
     element that multiplies every gradient as it is read, as :class:`MuonGrads` gives
     it (NaN: the step changes nothing)."""
     import torch
-    n, columns = len(params), (params, grads, exp_avgs, exp_avg_sqs)
+    n = len(params)
+    if n == 0:
+        raise MuonError(MUON_ERR_INVALID_ARG, "no tensors")
+    # any iterables; what exceeds the parameters is left
+    params, grads, exp_avgs, exp_avg_sqs = columns = [list(islice(c, n)) for c in (params, grads, exp_avgs, exp_avg_sqs)]
     if any(len(c) != n for c in columns):
         raise MuonError(MUON_ERR_INVALID_ARG, "as many gradients and moments as parameters")
     # column by column: a method's map costs half of a loop over the tensors

@@ -67,3 +67,31 @@ def test_other_refusals():
     t = (b.muon_adamw_tensor * 1)(b.muon_adamw_tensor(P, P, P, P, 4, 1, 1))
     assert b.lib().muon_adamw_step_clipped(t, 1, C.byref(hp), None, 0, None) == b.MUON_ERR_INVALID_ARG
     assert b.lib().muon_adamw_step_clipped(t, 1, C.byref(hp), P + 2, 0, None) == b.MUON_ERR_ALIGNMENT
+
+
+def test_adamw_lists(monkeypatch):
+    """Any iterables, of which the parameters' number counts; shorter ones are refused."""
+    torch = pytest.importorskip("torch")
+    from paper_2502_16982_b200 import binding as b
+
+    seen = []
+
+    class Lib:
+        @staticmethod
+        def muon_adamw_step(arr, n, hp, dev, stream):
+            seen.append(list((C.c_int64 * (6 * n)).from_address(arr)))
+            return 0
+
+    monkeypatch.setattr(b, "lib", lambda: Lib)
+    monkeypatch.setattr(b, "_raw_stream", lambda stream, dev: None)
+    p, m, v = ([torch.zeros(k + 1) for k in range(3)] for _ in range(3))
+    g = [torch.zeros(k + 1, dtype=torch.bfloat16 if k else torch.float32) for k in range(4)]
+    b.muon_adamw_step(p, iter(g), tuple(m), (x for x in v), 1, 1e-3, 0.0)
+    words = [w for k in range(3) for w in (p[k].data_ptr(), g[k].data_ptr(), m[k].data_ptr(), v[k].data_ptr(), k + 1,
+                                           b.MUON_DTYPE_FP32 | (b.MUON_DTYPE_BF16 if k else b.MUON_DTYPE_FP32) << 32)]
+    assert seen == [words]
+    for bad in ((p, g, m[:2], v), ([], [], [], []), (p, g[:2], m, v), (p, g, v[::-1], m), (p, g, [x.half() for x in m], v),
+                ([x.half() for x in p], g, m, v)):
+        with pytest.raises(b.MuonError):
+            b.muon_adamw_step(*bad, 1, 1e-3, 0.0)
+    assert len(seen) == 1
