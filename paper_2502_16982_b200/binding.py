@@ -766,7 +766,7 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
     """Log probabilities of ``targets`` (int64 [tokens], outside [0, vocab): masked) under
     ``x w^T``, bf16 [tokens, dim] and [vocab, dim], with log-sum-exps and, unless
     ``entropy`` is False, entropies.  ``out``: tensors to write, None in place of what is
-    not wanted.
+    not wanted; an earlier result given so holds what this call gives, ``kept`` among it.
     ``keep``: up to 3 GiB of logits stay, as 16-bit codes, with the result until it is let go
     of, and :func:`muon_head_logprob_grad` does not form them again.  By default as torch's
     gradient mode says (not under ``torch.no_grad()``, for scoring) and not in a workspace of
@@ -775,7 +775,7 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
     tokens, dim, vocab, dev, target_ptr = _logprob_operands(x, w, targets)
     if keep is None:
         keep = workspace is None and torch.is_grad_enabled()
-    f32 = torch.float32
+    f32, given = torch.float32, out
     with torch.cuda.stream(stream) if stream is not None else _no_context:
         if out is None:
             flat = torch.empty((3 if entropy else 2) * tokens, dtype=f32, device=dev)
@@ -785,16 +785,18 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
             ptrs = (at, at + 8 * tokens if entropy else 0, at + 4 * tokens)
         else:
             ptrs = [0 if t is None else _token_vector(t, name, tokens, dev, f32) for name, t in zip(("logprob", "entropy", "lse"), out[:3])]
-            out = HeadLogprob(*out[:3]) if keep else out
+            out = HeadLogprob(*out[:3])
         w_ptr, ld_w = w.data_ptr(), _row_stride(w)
         a = _pack_logprob_args(tokens, dim, vocab, 1 if keep else 0, x.data_ptr(), w_ptr, _row_stride(x) if tokens else dim, ld_w,
                                _dtype_code(x), _dtype_code(w), target_ptr, logit_scale, 0, *ptrs)
         workspace, base, nbytes = _logprob_workspace(workspace, dev, (tokens, dim, vocab, -1, not ptrs[1], bool(keep), ld_w & 7, w_ptr & 15),
                                                      a, None)
-        if keep:
-            out.kept = workspace
     index = dev.index
     _check(lib().muon_head_logprob(a, base, nbytes, index, _raw_stream(stream, index)))
+    if keep:
+        out.kept = workspace
+    if isinstance(given, HeadLogprob):  # its tensors hold this call's results now: nothing of an earlier one stays
+        given.kept = out.kept
     return out
 
 

@@ -1,0 +1,58 @@
+"""Results of muon_head_logprob written into an earlier result, and then its gradients: nothing
+of the earlier pass reaches them.  Tolerances: those of test_gpu_head_logprob.py."""
+
+import contextlib
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_head_logprob import Reference, f64, make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("second", ["keep", "keep_false", "no_grad", "workspace"])
+@pytest.mark.parametrize("use", ["returned", "given"])
+@pytest.mark.parametrize("T,D,V", [(300, 136, 3000), (24, 512, 4096)])
+def test_an_earlier_result_written_again(second, use, T, D, V):
+    from paper_2502_16982_b200 import binding as b
+
+    x1, w1, _ = make(T, D, V, 51)
+    x2, w2, gen = make(T, D, V, 52)
+    y1, y2 = (torch.randint(0, V, (T,), generator=gen) for _ in range(2))
+    y1[::5] = -100
+    y2[::7] = -100
+    r = b.muon_head_logprob(x1, w1, y1.cuda())
+    assert r.kept is not None
+    more = {}
+    if second == "keep_false":
+        more["keep"] = False
+    elif second == "workspace":
+        n = b.muon_head_logprob_workspace_bytes(T, D, V, grads=False)
+        more["workspace"] = torch.empty(n, dtype=torch.uint8, device="cuda")
+    with torch.no_grad() if second == "no_grad" else contextlib.nullcontext():
+        again = b.muon_head_logprob(x2, w2, y2.cuda(), logit_scale=0.8, out=r, **more)
+    assert again.logprob is r.logprob and again.entropy is r.entropy and again.lse is r.lse
+    assert (again.kept is not None) == (second == "keep") and r.kept is again.kept
+    saved = again if use == "returned" else r
+    ref = Reference(f64(x2), f64(w2), y2.numpy(), 0.8)
+    ref.check(saved)
+    rr, hh = torch.randn(T, generator=gen) / T, torch.randn(T, generator=gen) * 0.1 / T
+    d = b.muon_head_logprob_grad(x2, w2, y2.cuda(), saved, g_logprob=rr.cuda(), g_entropy=hh.cuda(), logit_scale=0.8, dx=True, dw=True)
+    counted = lambda v: np.where(y2.numpy() < 0, 0.0, v.double().numpy())
+    ref.check_grads(d, counted(rr), counted(hh), kept=second == "keep")
+
+
+def test_a_call_that_is_refused_leaves_what_an_earlier_one_kept():
+    from paper_2502_16982_b200 import binding as b
+
+    x, w, gen = make(300, 136, 3000, 53)
+    y = torch.randint(0, 3000, (300,), generator=gen).cuda()
+    r = b.muon_head_logprob(x, w, y)
+    kept = r.kept
+    with pytest.raises(b.MuonError):
+        b.muon_head_logprob(x, w, y, out=r, workspace=torch.zeros(1024, dtype=torch.uint8, device="cuda"))
+    assert r.kept is kept
+    plain = b.muon_head_logprob(x, w, y, out=tuple(r), keep=False)
+    assert type(plain) is b.HeadLogprob and plain.kept is None and r.kept is kept
