@@ -758,7 +758,8 @@ int muon_head_status(const void* workspace, int device, void* stream, int* devic
  *   keep != 0: the forward pass leaves what it gathered and up to 3 GiB of logits as 16-bit
  *     codes (as the losses' larger workspace does, where that is faster) in its workspace.
  *     That workspace, given as `kept` with its size, is read by the gradient and not written
- *     to, so that it may be asked for again; x, w, targets, logit_scale and the knobs below
+ *     to, so that it may be asked for again (the gradient's own workspace must not overlap it:
+ *     MUON_ERR_WORKSPACE); x, w, targets, logit_scale and the knobs below
  *     must be the same and unchanged.  Codes add 2^-12 relative to q and as much absolutely
  *     to log q, and what lies 2^-32 or more below the largest of its 64 columns counts as 0.
  *

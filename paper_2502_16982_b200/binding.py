@@ -805,8 +805,9 @@ def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_
     """Gradients of the hidden states and of the head for the gradients ``g_logprob`` and
     ``g_entropy`` (fp32 [tokens] or None) of what :func:`muon_head_logprob` gave as
     ``saved`` for the same operands, which must not have changed if it kept its logits; they
-    may be asked for again.  Tensors of another stream, what was kept among them, are the
-    caller's to keep alive (``record_stream``).  ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True
+    may be asked for again; a ``workspace`` must not be the one in which they were kept.
+    Tensors of another stream, what was kept among them, are the caller's to keep alive
+    (``record_stream``).  ``dx`` / ``dw``: a bf16 or fp32 tensor to write, True
     to allocate one like x / w, None to leave the gradient out."""
     import torch
     tokens, dim, vocab, dev, target_ptr = _logprob_operands(x, w, targets)

@@ -340,11 +340,6 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   HEAD_TRY(make_plan(a, top, distill, kPlanPairs, workspace_bytes ? workspace_bytes : 1, &P, kind, entropy, keep));
   if (!workspace || workspace_bytes < P.least || misaligned(workspace, 1024))
     return fail(MUON_ERR_WORKSPACE, "workspace: need at least %zu bytes, 1024-byte aligned", P.least);
-  DeviceGuard guard;
-  HEAD_CUDA(guard.set(device));
-  int pairs = 0;
-  HEAD_TRY(device_pairs(device, &pairs));
-
   char* ws = static_cast<char*>(workspace);
   char* kept = nullptr;
   if (d && keep) {
@@ -354,7 +349,13 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
     if (d->kept_bytes < K.least || misaligned(d->kept, 1024))
       return fail(MUON_ERR_WORKSPACE, "kept: need the workspace of the forward pass, %zu bytes", K.least);
     kept = static_cast<char*>(const_cast<void*>(d->kept));  // only read
+    if (kept < ws + P.bytes && ws < kept + K.least) return fail(MUON_ERR_WORKSPACE, "workspace and kept overlap");
   }
+  DeviceGuard guard;
+  HEAD_CUDA(guard.set(device));
+  int pairs = 0;
+  HEAD_TRY(device_pairs(device, &pairs));
+
   const void* w = a->w;
   long long ld_w = a->ld_w;
   if (P.pack) {

@@ -56,3 +56,28 @@ def test_a_call_that_is_refused_leaves_what_an_earlier_one_kept():
     assert r.kept is kept
     plain = b.muon_head_logprob(x, w, y, out=tuple(r), keep=False)
     assert type(plain) is b.HeadLogprob and plain.kept is None and r.kept is kept
+
+
+def test_the_gradients_workspace_beside_what_was_kept():
+    """Both carved from one buffer, one behind the other in either order; overlapping is refused."""
+    from paper_2502_16982_b200 import binding as b
+
+    T, D, V = 300, 136, 3000
+    x, w, gen = make(T, D, V, 54)
+    y = torch.randint(0, V, (T,), generator=gen)
+    n = b.muon_head_logprob_workspace_bytes(T, D, V, grads=False, keep=True) - 1024
+    m = b.muon_head_logprob_workspace_bytes(T, D, V, grads=True, keep=True) - 1024
+    buffer = torch.zeros(n + m + 1024, dtype=torch.uint8, device="cuda")
+    buffer = buffer[-buffer.data_ptr() % 1024:]
+    rr = torch.randn(T, generator=gen) / T
+    ref = Reference(f64(x), f64(w), y.numpy(), 1.0)
+    for own in (buffer[n:n + m], buffer[:m]):
+        kept = buffer[:n] if own.data_ptr() != buffer.data_ptr() else buffer[m:m + n]
+        r = b.muon_head_logprob(x, w, y.cuda(), workspace=kept, keep=True)
+        ref.check(r)
+        for bad in (kept, buffer[1024:]):  # (the entropy's sums, behind what is kept, may be overwritten)
+            with pytest.raises(b.MuonError) as e:
+                b.muon_head_logprob_grad(x, w, y.cuda(), r, g_logprob=rr.cuda(), dx=True, dw=True, workspace=bad)
+            assert e.value.code == b.MUON_ERR_WORKSPACE
+        d = b.muon_head_logprob_grad(x, w, y.cuda(), r, g_logprob=rr.cuda(), dx=True, dw=True, workspace=own)
+        ref.check_grads(d, rr.double().numpy(), None, kept=True)
