@@ -730,9 +730,9 @@ int muon_head_distill(const muon_head_args* args, const muon_head_teacher* teach
 /*
  * Synchronise `stream` and read the status of the last call that used this
  * workspace: 0, or MUON_ERR_TIMEOUT if a bounded device-side wait expired (its
- * outputs are then not valid).  MUON_ERR_INVALID_ARG: muon_head_logprob_grad was
- * given what a call with other pieces kept (muon_debug_set_head_piece_bytes was called
- * in between); its gradients are 0.
+ * outputs are then not valid).  MUON_ERR_INVALID_ARG: what muon_head_logprob_grad was
+ * given as kept is not what a call with the same sizes, logit_scale, alignment of w and
+ * knobs left there last with keep; its gradients are 0 (with dw_accumulate, dw stays).
  */
 int muon_head_status(const void* workspace, int device, void* stream, int* device_status);
 

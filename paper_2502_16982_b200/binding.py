@@ -698,8 +698,10 @@ class _HeadLogprob(NamedTuple):
 
 class HeadLogprob(_HeadLogprob):
     """Per token, fp32: ``logprob`` of the target, ``entropy`` and ``lse`` (None where not
-    wanted); ``kept``: the workspace with the logits kept for the gradient, or None."""
+    wanted); ``kept``: the workspace with the logits kept for the gradient, or None;
+    ``kept_for``: their tokens, dimensions, vocabulary and logit scale."""
     kept: Optional["torch.Tensor"] = None
+    kept_for: Optional[tuple] = None
 
 
 class HeadGrads(NamedTuple):
@@ -794,9 +796,9 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
     index = dev.index
     _check(lib().muon_head_logprob(a, base, nbytes, index, _raw_stream(stream, index)))
     if keep:
-        out.kept = workspace
+        out.kept, out.kept_for = workspace, (tokens, dim, vocab, C.c_float(logit_scale).value)
     if isinstance(given, HeadLogprob):  # its tensors hold this call's results now: nothing of an earlier one stays
-        given.kept = out.kept
+        given.kept, given.kept_for = out.kept, out.kept_for
     return out
 
 
@@ -824,6 +826,9 @@ def muon_head_logprob_grad(x, w, targets, saved: HeadLogprob, g_logprob=None, g_
     if kept is not None:
         if kept.device != dev:
             raise MuonError(MUON_ERR_WORKSPACE, "what the forward pass kept is not on x's device")
+        made = getattr(saved, "kept_for", None)
+        if made is not None and made != (tokens, dim, vocab, C.c_float(logit_scale).value):
+            raise MuonError(MUON_ERR_INVALID_ARG, "logits kept for tokens, dim, vocab, logit_scale = %s, %s, %s, %s" % made)
         first = kept.data_ptr()
         d.kept = base = (first + 1023) // 1024 * 1024
         d.kept_bytes = max(first + kept.numel() - base, 0)

@@ -36,6 +36,16 @@ constexpr long long kHeadInCache = 96ll << 20;   // bytes of w that do, between 
 constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
 
+// What a forward pass that keeps its logits kept them of: all that the places in its
+// workspace depend on, and the scale.  Zeros where nothing was kept.
+struct Kept {
+  int tokens, dim, vocab;
+  int packed;         // a copy of w with aligned rows is kept, too
+  int piece_tiles;    // 256-column tiles of a piece,
+  int stored;         // pieces whose codes are kept
+  float scale2;
+};
+
 // Control block at the start of the workspace.
 struct Ctrl {
   int status;      // 0 or MUON_ERR_TIMEOUT
@@ -43,7 +53,7 @@ struct Ctrl {
   unsigned ticket; // blocks of the finalisation that are done
   float coef;      // scale, divided by the sum of the weights where a mean is asked for
   float rest;      // what dX and dW are still to be multiplied with, see finalise_kernel
-  int kept_tiles;  // log probabilities: tiles of the pieces whose codes are kept, for the gradient to compare
+  Kept kept;       // log probabilities, for the gradient to compare
 };
 
 // One product of a launch: D[m][n] = sum_k A[m][k] B[n][k].
@@ -199,7 +209,7 @@ struct RowParams {
   const float* g_logprob;
   const float* g_entropy;
   float* row_b;
-  int kept_tiles;        // see Ctrl
+  Kept keeps;            // what this call keeps, or, a gradient, what has to be there
   const Ctrl* kept;      // of the forward pass that kept its logits, else NULL
   const float* part;     // partial dX of each run of K blocks
   long long part_ld, part_stride;

@@ -409,7 +409,10 @@ int run(const muon_head_args* a, const muon_head_teacher* t, const int64_t* targ
   R.total = a->total;
   if (l) {
     R.row_b = reinterpret_cast<float*>(ws + P.row_b);
-    R.kept_tiles = P.piece_tiles;
+    if (keep) {
+      const Plan& F = d ? K : P;
+      R.keeps = Kept{F.tokens, F.dim, F.vocab, F.pack, F.piece_tiles, F.n_stored, R.scale2};
+    }
     if (d) {
       R.logprob_in = l->logprob;
       R.entropy_in = l->entropy;

@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kRowThreads) prepare_kernel(const RowParams R)
     R.ctrl->n_valid = total;
     R.ctrl->ticket = 0;
     R.ctrl->coef = !R.mean ? R.scale : (norm == 0.f ? 0.f : R.scale / norm);
-    R.ctrl->kept_tiles = R.kept_tiles;
+    R.ctrl->kept = R.keeps;
   }
 
   const int t = first + warp;
@@ -663,8 +663,11 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const RowPara
   const int row = blockIdx.x * kRowWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   int n_valid = R.kept != nullptr ? R.kept->n_valid : R.ctrl->n_valid;
   if (R.kept != nullptr) {
-    // pieces of another size (the knob was turned in between): no gradient, and a status
-    const bool other = R.kept->kept_tiles != R.kept_tiles;
+    // nothing kept, or of another call (other sizes, another scale, a knob turned in
+    // between): no gradient, and a status
+    const Kept a = R.kept->kept, b = R.keeps;
+    const bool other = a.tokens != b.tokens || a.dim != b.dim || a.vocab != b.vocab || a.packed != b.packed ||
+                       a.piece_tiles != b.piece_tiles || a.stored != b.stored || !(a.scale2 == b.scale2);
     if (other) n_valid = 0;
     if (row == 0 && lane == 0) {
       R.ctrl->n_valid = n_valid;

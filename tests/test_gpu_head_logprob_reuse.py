@@ -81,3 +81,64 @@ def test_the_gradients_workspace_beside_what_was_kept():
             assert e.value.code == b.MUON_ERR_WORKSPACE
         d = b.muon_head_logprob_grad(x, w, y.cuda(), r, g_logprob=rr.cuda(), dx=True, dw=True, workspace=own)
         ref.check_grads(d, rr.double().numpy(), None, kept=True)
+
+
+@pytest.mark.parametrize("other", ["tokens", "more_tokens", "dim", "vocab", "scale", "alignment", "codes", "kept_nothing", "in_place", "loss"])
+def test_what_another_call_kept_gives_no_gradient(other):
+    """The binding refuses what it can see; the kernel compares what lies in the workspace."""
+    from paper_2502_16982_b200 import binding as b
+
+    T, D, V, S = 200, 128, 3000, 0.8
+    sizes = {"tokens": (70, D, V, S), "more_tokens": (260, D, V, S), "dim": (T, 64, V, S), "vocab": (T, D, 2900, S), "scale": (T, D, V, 0.9)}
+    t, d, v, s = sizes.get(other, (T, D, V, S))
+    ws = torch.zeros(32 << 20, dtype=torch.uint8, device="cuda")
+    x, w, gen = make(t, d, v, 55, offset_w=1 if other == "alignment" else 0)
+    y = torch.randint(0, v, (t,), generator=gen).cuda()
+    made = None
+    if other == "loss":
+        b.muon_head_xent(x, w, y, dx=True, workspace=ws)
+    else:
+        mode = b.muon_debug_set_head_codes(1 if other == "codes" else 0)
+        made = b.muon_head_logprob(x, w, y, logit_scale=s, workspace=ws, keep=other not in ("kept_nothing", "in_place"))
+        b.muon_debug_set_head_codes(mode)
+    if other == "in_place":  # over what was kept before
+        b.muon_head_logprob(x, w, y, logit_scale=s, workspace=ws, keep=True)
+        b.muon_head_logprob(x, w, y, logit_scale=s, workspace=ws)
+    x, w, gen = make(T, D, V, 56)
+    y = torch.randint(0, V, (T,), generator=gen).cuda()
+    r = b.muon_head_logprob(x, w, y, logit_scale=S, keep=False)
+    r.kept = ws
+    g = torch.full((T,), 0.5, device="cuda")
+    own = torch.zeros(b.muon_head_logprob_workspace_bytes(T, D, V, grads=True, keep=True), dtype=torch.uint8, device="cuda")
+    dw = torch.full((V, D), 7.0, device="cuda")
+    dx = torch.full((T, D), 7.0, device="cuda")
+    grad = lambda **k: b.muon_head_logprob_grad(x, w, y, r, g_logprob=g, g_entropy=g, logit_scale=S, workspace=own, **k)
+    grad(dx=dx, dw=dw, accumulate_dw=True)
+    assert b.muon_head_status(own) == b.MUON_ERR_INVALID_ARG
+    assert not dx.any() and bool((dw == 7.0).all())
+    grad(dw=dw)
+    assert b.muon_head_status(own) == b.MUON_ERR_INVALID_ARG and not dw.any()
+    if other in sizes:
+        r.kept_for = made.kept_for
+        with pytest.raises(b.MuonError) as e:
+            grad(dx=True)
+        assert e.value.code == b.MUON_ERR_INVALID_ARG
+
+
+def test_what_the_same_call_kept_after_others_used_the_workspace():
+    from paper_2502_16982_b200 import binding as b
+
+    T, D, V = 200, 128, 3000
+    ws = torch.zeros(32 << 20, dtype=torch.uint8, device="cuda")
+    own = torch.zeros(32 << 20, dtype=torch.uint8, device="cuda")
+    for seed, (t, d, v) in enumerate(((T, D, V), (20, 64, 500), (T, D, V), (0, D, V), (T, D, V))):
+        x, w, gen = make(t, d, v, 57 + seed)
+        y = torch.randint(0, v, (t,), generator=gen)
+        r = b.muon_head_logprob(x, w, y.cuda(), logit_scale=0.8, workspace=ws, keep=True)
+        rr, hh = torch.randn(t, generator=gen), torch.randn(t, generator=gen) * 0.1
+        g = b.muon_head_logprob_grad(x, w, y.cuda(), r, g_logprob=rr.cuda(), g_entropy=hh.cuda(), logit_scale=0.8, dx=True, dw=True, workspace=own)
+        assert b.muon_head_status(own) == 0
+        if t:
+            Reference(f64(x), f64(w), y.numpy(), 0.8).check_grads(g, rr.double().numpy(), hh.double().numpy(), kept=True)
+        else:
+            assert not g.dw.any()
