@@ -595,6 +595,9 @@ __global__ void __launch_bounds__(kRowThreads) logprob_kernel(const RowParams R)
         if (R.lse != nullptr) R.lse[row] = 0.f;
         if (kEntropy) R.entropy[row] = 0.f;
       }
+      // nothing of the product is needed, but a grid that did not wait could end before it,
+      // and what comes next in the stream take the workspace while it is written to
+      ptx::grid_dependency_wait();
       return;
     }
     id = static_cast<int>(raw);
