@@ -651,7 +651,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop, kThreads)
     const float y = x * P.scale2, m = fmaxf(a.m, y);
     if (mine) {
       rescale(a, m);
-      const float d = m == -INFINITY ? kFloor : max_nan(fmaf(x, P.scale2, -m), kFloor), p = ex2(d);
+      // as in the loop; a NaN, which m does not show, shows here
+      const float d = max_nan(fmaf(x, P.scale2, m == -INFINITY ? 0.f : -m), kFloor), p = ex2(d);
       a.s += p;
       a.e = fmaf(p, d, a.e);
     }
