@@ -69,6 +69,12 @@ static_assert(kMaxCluster * kMaxTop <= kSorted && kSorted + kMaxTop <= kThreads 
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kFloor = -200.0f;  // exponents of 2 from here down give 0, and stay finite in products
+// A logit whose exponent of 2 is this far from 0 is a mask, or no logit at all, and counts as the
+// infinity of its sign: the differences below are exact but for the rounding of the reference, at
+// most 64 up to here, of which 2^64 times 2^24 columns is a number.
+constexpr float kFar = 2147483648.0f;
+// The gradient's q = exp(l - lse) needs an lse whose last place is below 1.
+constexpr float kFarLse = 16777216.0f;
 
 struct LogitsParams {
   const void* z;
@@ -245,6 +251,9 @@ __device__ __forceinline__ float value_of(const LogitsParams& P, Key k) {
 struct Sums {
   float m, s, e;
 };
+
+// The reference that a largest logit of exponent y asks for.
+__device__ __forceinline__ float reference_of(float y) { return y >= kFar ? INFINITY : y > -kFar ? y : -INFINITY; }
 
 // (s, e) against a larger reference.
 __device__ __forceinline__ void rescale(Sums& a, float m) {
@@ -587,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop, kThreads)
       bound = fmaxf(bound, threshold);
     }
     const float reference = most * P.scale2;
-    if (reference > a.m) rescale(a, reference);
+    if (reference > fmaxf(a.m, -kFar)) rescale(a, reference_of(reference));
     const float base = a.m == -INFINITY ? 0.f : -a.m;
     const uint64_t from = pair(base, base);
     uint64_t s = 0, w = 0;  // pairs of zeros
@@ -648,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop, kThreads)
     const int column = lane < min(head, P.vocab) ? lane : behind + lane - min(head, P.vocab);
     const bool mine = column < P.vocab;
     const float x = mine ? static_cast<float>(row[column]) : -INFINITY;
-    const float y = x * P.scale2, m = fmaxf(a.m, y);
+    const float m = fmaxf(a.m, reference_of(x * P.scale2));
     if (mine) {
       rescale(a, m);
       // as in the loop; a NaN, which m does not show, shows here
@@ -812,7 +821,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
   }
   const float lse = P.lse[token], h = P.h != nullptr ? P.h[token] : 0.f, r = P.r != nullptr ? P.r[token] : 0.f;
   const float entropy = P.h != nullptr ? P.entropy[token] : 0.f;
-  const bool nothing = !counts || lse == -INFINITY;
+  const bool nothing = !counts || fabsf(lse) >= kFarLse;  // not for a NaN
   const float c0 = -(r + h * entropy) * P.scale, c1 = -h * P.scale;
   const int target = static_cast<int>(y);
   const float at_target = r * P.scale;
