@@ -71,7 +71,7 @@ class Model:
         self.steps += 1
         total = self.all_grads.muon_grad_norm(self.max_norm)
         self.mats_only.muon_clip_grads(self.max_norm, sum_sq=total.sum_sq)
-        self.muon.muon_step(mb.Hyper(lr=lr, wd=0.0))
+        self.muon.muon_step(mb.Hyper(lr=lr, wd=0.0), coef=total.coef)
         mb.muon_adamw_step([self.embed, self.head], [self.embed_grad, self.head_grad], self.moments[0::2],
                            self.moments[1::2], self.steps, lr=lr, wd=0.0, coef=total.coef)
         self.embed16.copy_(self.embed)

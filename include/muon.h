@@ -499,9 +499,10 @@ int muon_adamw_step(const muon_adamw_tensor* tensors, int n_tensors, const muon_
  * muon_clip_grads takes the coefficient from sum_sq, so that data-parallel ranks which
  * hold different tensors can add theirs before it (Sec. 2.3).  Where coef is 1, tensors
  * in place are not touched; a `coef` below 1 multiplies in fp32 and rounds once.  A norm
- * that is not finite clips nothing: coef is then written as NaN and out holds g, so that
- * muon_status finds the matrix and muon_adamw_step_clipped skips the step.  With
- * n_tensors = 0 it only writes norm and coef.
+ * that is not finite clips nothing: coef is then written as NaN and out holds g, unclipped.
+ * Given that coef, muon_step_clipped and muon_adamw_step_clipped skip the step of all they
+ * own, wherever the bad element was; muon_step on its own would step every finite matrix
+ * with its whole gradient.  With n_tensors = 0 it only writes norm and coef.
  *
  * max_norm: 0 to infinity (infinity: never clipped).  Both are asynchronous on `stream`,
  * allocate nothing and may be captured into a CUDA graph (the pointers are then those of
@@ -531,6 +532,17 @@ int muon_clip_grads(const muon_grad_tensor* tensors, int n_tensors, const double
  */
 int muon_adamw_step_clipped(const muon_adamw_tensor* tensors, int n_tensors, const muon_adamw_hparams* hp,
                             const float* coef, int device, void* stream);
+
+/*
+ * muon_step and muon_step_bucket after muon_clip_grads has scaled the gradients by *coef
+ * (DEVICE, one fp32, read when the step runs; it multiplies nothing here).  Where *coef is
+ * NaN - the gradient norm was not finite, be it by an element that is another rank's or
+ * AdamW's - every matrix keeps W and M, and muon_status reports MUON_ERR_NONFINITE with one
+ * of them.
+ */
+int muon_step_clipped(muon_ctx* ctx, const muon_hparams* hp, const float* coef, void* stream);
+
+int muon_step_bucket_clipped(muon_ctx* ctx, const muon_hparams* hp, int bucket, const float* coef, void* stream);
 
 /*
  * Momentum update and Frobenius norm of ONE matrix with no workspace and no

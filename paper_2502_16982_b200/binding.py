@@ -42,6 +42,7 @@ EXPORTED = [
     "muon_debug_wait_expiry",
     "muon_profile_enable", "muon_profile_read", "muon_debug_tmem_bases",
     "muon_momentum_norm_static", "muon_adamw_step", "muon_adamw_step_clipped", "muon_grad_norm", "muon_clip_grads",
+    "muon_step_clipped", "muon_step_bucket_clipped",
     "muon_head_workspace_bytes", "muon_head_xent", "muon_head_distill", "muon_head_status",
     "muon_head_logprob_workspace_bytes", "muon_head_logprob", "muon_head_logprob_grad",
     "muon_logits_logprob", "muon_logits_logprob_grad",
@@ -158,6 +159,8 @@ def lib():
     L.muon_debug_tile_table.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int16), C.c_int,
                                         C.POINTER(C.c_int), C.POINTER(C.c_int)]
     L.muon_step_bucket.argtypes = [C.c_void_p, C.POINTER(muon_hparams), C.c_int, C.c_void_p]
+    L.muon_step_clipped.argtypes = [C.c_void_p, C.POINTER(muon_hparams), C.c_void_p, C.c_void_p]
+    L.muon_step_bucket_clipped.argtypes = [C.c_void_p, C.POINTER(muon_hparams), C.c_int, C.c_void_p, C.c_void_p]
     L.muon_step_host.argtypes = [C.c_void_p, C.POINTER(muon_hparams), C.POINTER(C.POINTER(C.c_void_p)),
                                  C.POINTER(C.POINTER(C.c_void_p)), C.c_void_p]
     L.muon_status.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int)]
@@ -1124,17 +1127,34 @@ class MuonContext:
         self._ctx = ctx
 
     # -- the C calls -------------------------------------------------------
-    def muon_step(self, hp: Hyper, stream=None):
+    def _coef(self, coef):
         import torch
-        s = torch.cuda.current_stream(self.device) if stream is None else stream
-        c_hp = hp.to_c()
-        _check(lib().muon_step(self._ctx, C.byref(c_hp), C.c_void_p(s.cuda_stream)))
+        if coef.dtype != torch.float32 or coef.numel() != 1 or coef.device != torch.device("cuda", self.device):
+            raise MuonError(MUON_ERR_INVALID_ARG, "coef must be one fp32 element on the matrices' device")
+        return coef.data_ptr()
 
-    def muon_step_bucket(self, hp: Hyper, bucket: int, stream=None):
+    def muon_step(self, hp: Hyper, stream=None, coef=None):
+        """``coef``: one fp32 CUDA element that :class:`MuonGrads` clipped the gradients by;
+        where it is NaN, the norm not finite, every matrix keeps W and M, and
+        :meth:`muon_status` says so."""
         import torch
         s = torch.cuda.current_stream(self.device) if stream is None else stream
         c_hp = hp.to_c()
-        _check(lib().muon_step_bucket(self._ctx, C.byref(c_hp), int(bucket), C.c_void_p(s.cuda_stream)))
+        if coef is None:
+            _check(lib().muon_step(self._ctx, C.byref(c_hp), C.c_void_p(s.cuda_stream)))
+        else:
+            _check(lib().muon_step_clipped(self._ctx, C.byref(c_hp), self._coef(coef), C.c_void_p(s.cuda_stream)))
+
+    def muon_step_bucket(self, hp: Hyper, bucket: int, stream=None, coef=None):
+        """:meth:`muon_step` for the matrices of one bucket."""
+        import torch
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        c_hp = hp.to_c()
+        if coef is None:
+            _check(lib().muon_step_bucket(self._ctx, C.byref(c_hp), int(bucket), C.c_void_p(s.cuda_stream)))
+        else:
+            _check(lib().muon_step_bucket_clipped(self._ctx, C.byref(c_hp), int(bucket), self._coef(coef),
+                                                  C.c_void_p(s.cuda_stream)))
 
     def muon_step_host(self, hp: Hyper, g_host, w_host=None, stream=None):
         """g_host / w_host: per group, a list of pinned CPU tensors (dense)."""

@@ -39,7 +39,7 @@ struct MatScal {
   float inv_norm;     // s = 1 / (||U||_F + eps)
   float inv_norm_sq;  // s^2
   float norm;         // ||U||_F
-  int nonfinite;      // 1 if the norm is NaN/Inf
+  int nonfinite;      // 1 if the norm is NaN/Inf, or the clipping coefficient NaN: W stays
 };
 
 // Device status word: {code, first matrix index}.
@@ -130,6 +130,7 @@ struct StreamParams {
   float mu;
   int nesterov;
   const int* g_bad;  // optional: per matrix, non-zero = its gradient is non-finite, leave M as it is
+  const float* coef; // optional: NaN = the gradients' global norm is not finite, leave every M as it is
 };
 
 // Parameters of the TMA-pipelined momentum kernel (64 x 64 tiles).
@@ -146,6 +147,7 @@ struct StreamTmaParams {
   float mu;
   int nesterov;
   const int* g_bad;          // optional: per matrix, non-zero = its gradient is non-finite, leave M as it is
+  const float* coef;         // optional: NaN = the gradients' global norm is not finite, leave every M as it is
 };
 
 }  // namespace muon

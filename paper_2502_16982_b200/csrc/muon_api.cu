@@ -26,7 +26,7 @@ cudaError_t launch_grad_finite(const MatDesc* descs, int count, int rows_max, bo
                                cudaStream_t stream);
 cudaError_t launch_norm_finalise(const float* partials, int tiles_per_matrix, int count, float eps,
                                  const MatDesc* descs, MatScal* scal, float* norms, DevStatus* status,
-                                 cudaStream_t stream);
+                                 const float* coef, cudaStream_t stream);
 cudaError_t launch_update_from_x(const MatDesc* descs, const MatScal* scal, const float* factors,
                                  const __nv_bfloat16* x, long long x_stride, int ldx, int count, int m,
                                  int n, float neg_lr, float decay, bool w_fp32, cudaStream_t stream);
@@ -1005,9 +1005,9 @@ static int check_hparams(const muon_hparams* hp) {
 }
 
 // One Muon step for matrices [first, first + count) of bucket b (at most one
-// chunk), enqueued on `stream`.
-static int step_chunk(muon_ctx* ctx, const muon_hparams* hp, cudaStream_t stream, size_t b, int first, int count,
-                      int* launch_counter) {
+// chunk), enqueued on `stream`.  coef_ptr: NULL, or what the gradients were clipped by.
+static int step_chunk(muon_ctx* ctx, const muon_hparams* hp, const float* coef_ptr, cudaStream_t stream, size_t b, int first,
+                      int count, int* launch_counter) {
   int launches = 0;
   cudaError_t ce = cudaSuccess;
   DevStatus* status = reinterpret_cast<DevStatus*>(ctx->ws + ctx->sizes.off_status);
@@ -1053,6 +1053,7 @@ static int step_chunk(muon_ctx* ctx, const muon_hparams* hp, cudaStream_t stream
     S.mu = hp->mu;
     S.nesterov = hp->nesterov ? 1 : 0;
     S.g_bad = g_bad;
+    S.coef = coef_ptr;
     LaunchTimer lt(ctx, stream, MUON_KERNEL_MOMENTUM);
     ce = launch_momentum_tma(S, B.g_dtype == MUON_DTYPE_FP32, ctx->num_sms, stream);
   } else {
@@ -1067,12 +1068,13 @@ static int step_chunk(muon_ctx* ctx, const muon_hparams* hp, cudaStream_t stream
     S.mu = hp->mu;
     S.nesterov = hp->nesterov ? 1 : 0;
     S.g_bad = g_bad;
+    S.coef = coef_ptr;
     LaunchTimer lt(ctx, stream, MUON_KERNEL_MOMENTUM);
     ce = launch_momentum_cast(S, B.g_dtype == MUON_DTYPE_FP32, stream);
   }
   if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, "momentum kernel launch: %s", cudaGetErrorString(ce));
   ++launches;
-  { LaunchTimer lt(ctx, stream, MUON_KERNEL_NORM); ce = launch_norm_finalise(partials, stream_tiles, count, hp->eps, descs, scal, norms, status, stream); }
+  { LaunchTimer lt(ctx, stream, MUON_KERNEL_NORM); ce = launch_norm_finalise(partials, stream_tiles, count, hp->eps, descs, scal, norms, status, coef_ptr, stream); }
   if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, "norm kernel launch: %s", cudaGetErrorString(ce));
   ++launches;
 
@@ -1263,7 +1265,13 @@ static int step_chunk(muon_ctx* ctx, const muon_hparams* hp, cudaStream_t stream
   return MUON_OK;
 }
 
-int muon_step(muon_ctx* ctx, const muon_hparams* hp, void* stream_v) {
+static int check_coef(const float* coef) {
+  if (!coef) return fail(MUON_ERR_INVALID_ARG, "coef is null");
+  if (reinterpret_cast<uintptr_t>(coef) & 3) return fail(MUON_ERR_ALIGNMENT, "coef not aligned to its element size");
+  return MUON_OK;
+}
+
+static int step_all(muon_ctx* ctx, const muon_hparams* hp, const float* coef, void* stream_v) {
   if (!ctx) return fail(MUON_ERR_INVALID_ARG, "ctx is null");
   DeviceGuard guard(ctx->device);
   int rc = check_hparams(hp);
@@ -1274,7 +1282,7 @@ int muon_step(muon_ctx* ctx, const muon_hparams* hp, void* stream_v) {
     const Bucket& B = ctx->buckets[b];
     const int total = static_cast<int>(B.mats.size());
     for (int first = 0; first < total; first += B.chunk) {
-      rc = step_chunk(ctx, hp, stream, b, first, std::min(B.chunk, total - first), &launches);
+      rc = step_chunk(ctx, hp, coef, stream, b, first, std::min(B.chunk, total - first), &launches);
       if (rc) return rc;
     }
   }
@@ -1282,7 +1290,7 @@ int muon_step(muon_ctx* ctx, const muon_hparams* hp, void* stream_v) {
   return MUON_OK;
 }
 
-int muon_step_bucket(muon_ctx* ctx, const muon_hparams* hp, int bucket, void* stream_v) {
+static int step_bucket(muon_ctx* ctx, const muon_hparams* hp, int bucket, const float* coef, void* stream_v) {
   if (!ctx) return fail(MUON_ERR_INVALID_ARG, "ctx is null");
   if (bucket < 0 || bucket >= static_cast<int>(ctx->buckets.size()))
     return fail(MUON_ERR_INVALID_ARG, "bucket %d out of range (context has %zu)", bucket, ctx->buckets.size());
@@ -1294,11 +1302,27 @@ int muon_step_bucket(muon_ctx* ctx, const muon_hparams* hp, int bucket, void* st
   const Bucket& B = ctx->buckets[bucket];
   const int total = static_cast<int>(B.mats.size());
   for (int first = 0; first < total; first += B.chunk) {
-    rc = step_chunk(ctx, hp, stream, bucket, first, std::min(B.chunk, total - first), &launches);
+    rc = step_chunk(ctx, hp, coef, stream, bucket, first, std::min(B.chunk, total - first), &launches);
     if (rc) return rc;
   }
   ctx->last_launches = launches;
   return MUON_OK;
+}
+
+int muon_step(muon_ctx* ctx, const muon_hparams* hp, void* stream) { return step_all(ctx, hp, nullptr, stream); }
+
+int muon_step_clipped(muon_ctx* ctx, const muon_hparams* hp, const float* coef, void* stream) {
+  const int rc = check_coef(coef);
+  return rc ? rc : step_all(ctx, hp, coef, stream);
+}
+
+int muon_step_bucket(muon_ctx* ctx, const muon_hparams* hp, int bucket, void* stream) {
+  return step_bucket(ctx, hp, bucket, nullptr, stream);
+}
+
+int muon_step_bucket_clipped(muon_ctx* ctx, const muon_hparams* hp, int bucket, const float* coef, void* stream) {
+  const int rc = check_coef(coef);
+  return rc ? rc : step_bucket(ctx, hp, bucket, coef, stream);
 }
 
 int muon_step_host(muon_ctx* ctx, const muon_hparams* hp, const void* const* const* g_host,
@@ -1361,7 +1385,7 @@ int muon_step_host(muon_ctx* ctx, const muon_hparams* hp, const void* const* con
       if (ce == cudaSuccess) ce = cudaEventRecord(ev, ctx->s_in);
       if (ce == cudaSuccess) ce = cudaStreamWaitEvent(stream, ev, 0);
       if (ce != cudaSuccess) return fail(MUON_ERR_CUDA, "stream ordering: %s", cudaGetErrorString(ce));
-      rc = step_chunk(ctx, hp, stream, b, first, count, &launches);
+      rc = step_chunk(ctx, hp, nullptr, stream, b, first, count, &launches);
       if (rc) return rc;
       if (w_host) {
         ce = next_event(&ev);

@@ -83,7 +83,7 @@ momentum_cast_kernel(const StreamParams P) {
   const int col = col0 + cgrp * 8;
   const int valid = min(8, max(0, d.cols - col));
   const bool vec = d.vec_ok != 0;
-  const bool keep_m = P.g_bad != nullptr && P.g_bad[mat] != 0;
+  const bool keep_m = (P.g_bad != nullptr && P.g_bad[mat] != 0) || (P.coef != nullptr && isnan(*P.coef));
 
   float g[kRowsPerThread][8], m[kRowsPerThread][8];
 #pragma unroll
@@ -134,7 +134,7 @@ momentum_cast_kernel(const StreamParams P) {
     if (in) {
       float* mp = d.m + static_cast<long long>(row) * d.ld_m + col;
       if (keep_m) {
-        // a matrix whose gradient was found non-finite keeps its momentum
+        // a matrix whose gradient was found non-finite, or a global norm, keeps its momentum
       } else if (vec && valid == 8) {
         __stcs(reinterpret_cast<float4*>(mp), make_float4(m[p][0], m[p][1], m[p][2], m[p][3]));
         __stcs(reinterpret_cast<float4*>(mp) + 1, make_float4(m[p][4], m[p][5], m[p][6], m[p][7]));
@@ -202,7 +202,7 @@ momentum_cast_kernel(const StreamParams P) {
 __global__ void norm_finalise_kernel(const float* __restrict__ partials, int tiles_per_matrix,
                                      int count, float eps, const MatDesc* __restrict__ descs,
                                      MatScal* __restrict__ scal, float* __restrict__ norms,
-                                     DevStatus* status) {
+                                     DevStatus* status, const float* coef) {
   const int mat = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   if (mat >= count) return;
   const int lane = threadIdx.x & 31;
@@ -215,7 +215,7 @@ __global__ void norm_finalise_kernel(const float* __restrict__ partials, int til
     const float nu = sqrtf(s);
     MatScal r;
     r.norm = nu;
-    r.nonfinite = isfinite(nu) ? 0 : 1;
+    r.nonfinite = isfinite(nu) && !(coef != nullptr && isnan(*coef)) ? 0 : 1;
     const float inv = 1.0f / (nu + eps);
     r.inv_norm = r.nonfinite ? 0.f : inv;
     r.inv_norm_sq = r.nonfinite ? 0.f : inv * inv;
@@ -522,11 +522,11 @@ cudaError_t launch_momentum_cast(const StreamParams& P, bool grad_fp32, cudaStre
 
 cudaError_t launch_norm_finalise(const float* partials, int tiles_per_matrix, int count, float eps,
                                  const MatDesc* descs, MatScal* scal, float* norms,
-                                 DevStatus* status, cudaStream_t stream) {
+                                 DevStatus* status, const float* coef, cudaStream_t stream) {
   if (count == 0) return cudaSuccess;
   const int warps = 4;
   norm_finalise_kernel<<<(count + warps - 1) / warps, warps * 32, 0, stream>>>(
-      partials, tiles_per_matrix, count, eps, descs, scal, norms, status);
+      partials, tiles_per_matrix, count, eps, descs, scal, norms, status, coef);
   return cudaGetLastError();
 }
 

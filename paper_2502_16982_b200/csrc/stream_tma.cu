@@ -106,6 +106,7 @@ momentum_tma_kernel(const __grid_constant__ StreamTmaParams P) {
         ptx::tma_load_3d(base, P.mmaps + mat, inf.col0, inf.row0, 0, bar);
         ptx::tma_load_3d(base + kMBytes, P.gmaps + mat, inf.col0, inf.row0, 0, bar);
       };
+      const bool keep_all = P.coef != nullptr && isnan(*P.coef);
       int issued = 0;
       for (; issued < C::kLookahead && issued < my_tiles; ++issued) issue_loads(issued);
       bool ok = true;
@@ -125,8 +126,8 @@ momentum_tma_kernel(const __grid_constant__ StreamTmaParams P) {
         P.partials[t] = sum;
         const uint32_t base = ptx::smem_u32(smem + s * C::kStageBytes);
         // a matrix whose gradient was found non-finite keeps its momentum (its norm comes out
-        // non-finite all the same, so its weight is kept too)
-        if (P.g_bad == nullptr || P.g_bad[inf.mat] == 0) ptx::tma_store_3d(P.mmaps + inf.mat, inf.col0, inf.row0, 0, base);
+        // non-finite all the same, so its weight is kept too), and all do where the global norm was
+        if (!keep_all && (P.g_bad == nullptr || P.g_bad[inf.mat] == 0)) ptx::tma_store_3d(P.mmaps + inf.mat, inf.col0, inf.row0, 0, base);
         if (inf.transposed) {
           ptx::tma_store_3d(&P.map_x, inf.row0, inf.col0, inf.mat, base + kMBytes + C::kGBytes);
         } else {

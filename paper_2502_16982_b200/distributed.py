@@ -27,7 +27,8 @@ that Sec. 2.3 names.
 This module is plumbing: ``torch.distributed`` for the collectives, the C-ABI
 library (``muon_step_bucket``) for the arithmetic.  ``step_fn(mats, hp)``, with
 ``mats`` a list of (weight, grad, momentum), replaces the library call in tests
-so that the collective logic can run on CPU ranks (gloo).
+so that the collective logic can run on CPU ranks (gloo); where the step is given a
+coefficient it is called with that as well.
 """
 
 from __future__ import annotations
@@ -156,12 +157,14 @@ class DistributedMuon:
             self.dist.all_reduce(flat)
 
     # -- one optimizer step ------------------------------------------------------
-    def step(self, hp, reduce_grads: bool = False, timing: Optional[dict] = None) -> None:
+    def step(self, hp, reduce_grads: bool = False, timing: Optional[dict] = None, coef: Optional[torch.Tensor] = None) -> None:
         """One Muon step on the owned matrices and the exchange of the results.
 
         ``reduce_grads``: the gradient tensors hold this rank's local gradients
         and are summed over the ranks first (reduce-scatter); otherwise they are
-        taken as already reduced on the owner.  ``timing``: a dict that receives
+        taken as already reduced on the owner.  ``coef``: what :meth:`clip_grads` gave;
+        where it is NaN, the norm of all ranks' gradients not finite, no rank's matrices
+        are stepped, and :meth:`status` says so.  ``timing``: a dict that receives
         CUDA events (``start``, ``compute_end``, ``end`` and the pairs
         ``exchanges``) for the benchmark."""
         if self.world == 1:
@@ -169,7 +172,7 @@ class DistributedMuon:
                 timing["start"] = self._mark(torch.cuda.current_stream(self.device))
                 timing["exchanges"] = []
             for u in range(self.n_units):
-                self._compute_unit(u, hp)
+                self._compute_unit(u, hp, coef)
             if timing is not None and self._cuda:
                 timing["compute_end"] = timing["end"] = self._mark(torch.cuda.current_stream(self.device))
             return
@@ -177,7 +180,7 @@ class DistributedMuon:
             for u in range(self.n_units):
                 if reduce_grads:
                     self._reduce_scatter_unit(u)
-                self._compute_unit(u, hp)
+                self._compute_unit(u, hp, coef)
                 self._all_gather_unit(u)
             return
         main = torch.cuda.current_stream(self.device)
@@ -212,7 +215,7 @@ class DistributedMuon:
                 reduce(u + 1)
             if grads_ready[u] is not None:
                 main.wait_event(grads_ready[u])
-            self._compute_unit(u, hp)
+            self._compute_unit(u, hp, coef)
             done = torch.cuda.Event()
             done.record(main)
             comm.wait_event(done)
@@ -229,14 +232,14 @@ class DistributedMuon:
         ev.record(stream)
         return ev
 
-    def _compute_unit(self, u: int, hp) -> None:
+    def _compute_unit(self, u: int, hp, coef=None) -> None:
         lb = self.local_bucket[u]
         if lb is None:
             return
         if self._step_fn is not None:
-            self._step_fn(self.unit_mats[u], hp)
+            self._step_fn(self.unit_mats[u], hp, *(() if coef is None else (coef,)))
         else:
-            self._ctx.muon_step_bucket(hp, lb)
+            self._ctx.muon_step_bucket(hp, lb, coef=coef)
 
     def clip_grads(self, max_norm: float, eps: float = 1e-6, others: Optional[torch.Tensor] = None, reduce_grads: bool = False):
         """Before :meth:`step`: scales this rank's owned gradients so that the global norm of
@@ -245,7 +248,8 @@ class DistributedMuon:
         of the sum of squares of parameters that are not Muon's, each counted by one rank.
         ``reduce_grads``: the gradients are summed over the ranks first, and the step is then
         called without (a norm needs all of them before the first matrix is stepped).
-        Returns what ``muon_clip_grads`` gives; its ``coef`` clips the others' AdamW step.
+        Returns what ``muon_clip_grads`` gives; its ``coef`` goes to :meth:`step` and clips
+        the others' AdamW step.
         ``clip_fn(grads, max_norm, eps, sum_sq)``, with sum_sq None for the sum alone, replaces
         the library call in tests on CPU ranks."""
         if reduce_grads and self.world > 1:
