@@ -87,8 +87,9 @@ struct Cells<__nv_bfloat16> {
   }
 };
 
-// The thread's vectors of a chunk; what lies outside the tensor reads 0.
-template <typename T>
+// The thread's vectors of a chunk; what lies outside the tensor reads 0.  kReadOnly: nothing of
+// the launch writes to the tensor (the path for such data must not be taken otherwise).
+template <bool kReadOnly, typename T>
 __device__ __forceinline__ void load_chunk(const T* g, long long numel, long long first, uint4 (&v)[kVectors]) {
   constexpr int kEach = Cells<T>::kEach;
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(g) & 15) / sizeof(T));
@@ -97,7 +98,8 @@ __device__ __forceinline__ void load_chunk(const T* g, long long numel, long lon
     const long long at = (first + i * kThreads + threadIdx.x) * kEach - shift;
     v[i] = make_uint4(0u, 0u, 0u, 0u);
     if (at >= 0 && at + kEach <= numel) {
-      v[i] = __ldg(reinterpret_cast<const uint4*>(g + at));
+      const uint4* src = reinterpret_cast<const uint4*>(g + at);
+      v[i] = kReadOnly ? __ldg(src) : *src;
     } else if (at < numel && at + kEach > 0) {
       uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -163,10 +165,10 @@ __device__ __forceinline__ double thread_squares(const Tensors<kMost>& T) {
     const Chunk k = find_chunk(T, c);
     uint4 v[kVectors];
     if (bit(T.g_fp32, k.tensor)) {
-      load_chunk(static_cast<const float*>(T.g[k.tensor]), T.numel[k.tensor], k.first, v);
+      load_chunk<true>(static_cast<const float*>(T.g[k.tensor]), T.numel[k.tensor], k.first, v);
       sum += chunk_squares<float>(v);
     } else {
-      load_chunk(static_cast<const __nv_bfloat16*>(T.g[k.tensor]), T.numel[k.tensor], k.first, v);
+      load_chunk<true>(static_cast<const __nv_bfloat16*>(T.g[k.tensor]), T.numel[k.tensor], k.first, v);
       sum += chunk_squares<__nv_bfloat16>(v);
     }
   }
@@ -240,7 +242,7 @@ template <typename T, typename Out>
 __device__ __forceinline__ void scale_chunk(const T* g, Out* out, long long numel, long long first, float coef) {
   constexpr int kEach = Cells<T>::kEach;
   uint4 v[kVectors];
-  load_chunk(g, numel, first, v);
+  load_chunk<false>(g, numel, first, v);
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(g) & 15) / sizeof(T));
 #pragma unroll
   for (int i = 0; i < kVectors; ++i) {
