@@ -31,6 +31,12 @@ constexpr int kThreads = 128;
 // gradients: 2632 us, 2698 with 32 an SM, 2836 with 16; without the streaming stores of p and
 // with as many blocks for the smallest tensor as for the largest 2783.)
 constexpr int kCtasPerSm = 256;
+// Up to so many elements an SM (a launch's, by the gradients' type) a thread has one vector:
+// what fills the device for a moment only wants all threads that there are.  (us, a vector and
+// two: 42957 elements 4.3 and 6.7, 300000 4.7 and 6.6, 65536 + 3 x 1408 4.1 and 6.5, 40 x 100000
+// bf16 23.5 and 26.7, 5000000 26.0 and 31.0; 12 x 1000000 bf16 67.6 and 70.5, fp32 68.3 and 63.7;
+// 8 x 1000000 fp32 46.9 and 44.6; 160 x 100000 91.6 and 91.5, fp32 91.6 and 82.1.)
+constexpr double kLoneElements = 48 * 1024.0, kLoneElementsBf16 = 96 * 1024.0;
 
 struct TensorArg {
   void* p;
@@ -165,7 +171,8 @@ int launch_all(const muon_adamw_tensor* tensors, int n_tensors, const Step& step
     }
     int grid = 0;
     for (int i = 0; i < A.count; ++i) {
-      const long long most = (A.t[i].numel + kThreads * 16 - 1) / (kThreads * 16);  // a trip each
+      const int each = all <= sms * (A.t[i].g_fp32 ? kLoneElements : kLoneElementsBf16) ? 8 : 16;
+      const long long most = (A.t[i].numel + kThreads * each - 1) / (kThreads * each);  // a trip each
       long long share = static_cast<long long>(static_cast<double>(sms) * kCtasPerSm * (A.t[i].numel / all)) + 1;
       if (share > most) share = most;
       grid += static_cast<int>(share);
