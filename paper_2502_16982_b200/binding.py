@@ -409,7 +409,9 @@ class MuonGrads:
     of one handle share its workspace and must be stream-ordered with respect to each
     other; that holds for replays of graphs that captured them, too.  The formulas are
     in include/muon.h; :func:`muon_grad_norm` and :func:`muon_clip_grads` are the same
-    for a list that is used once."""
+    for a list that is used once, which they describe anew with every call (1.2 us of host
+    time a tensor, 1.4 with outputs).  A handle goes on with the tensors it was made of
+    where a program has put others in their place (``p.grad = None`` and a new backward pass)."""
 
     def __init__(self, grads, out=None, workspace=None):
         import torch
@@ -775,7 +777,8 @@ def muon_head_logprob(x, w, targets, logit_scale: float = 1.0, entropy=True, out
     ``keep``: up to 3 GiB of logits stay, as 16-bit codes, with the result until it is let go
     of, and :func:`muon_head_logprob_grad` does not form them again.  By default as torch's
     gradient mode says (not under ``torch.no_grad()``, for scoring) and not in a workspace of
-    the caller's.  Argument marshalling only; the formulas are in include/muon.h."""
+    the caller's.  Scoring outside ``no_grad``, or several batches before the gradient of the
+    first, is better off with ``keep=False``: every result holds its own.  Argument marshalling only; the formulas are in include/muon.h."""
     import torch
     tokens, dim, vocab, dev, target_ptr = _logprob_operands(x, w, targets)
     if keep is None:
@@ -921,7 +924,8 @@ def muon_logits_logprob(logits, targets=None, top: int = 0, logit_scale: float =
     """Log probabilities of ``targets`` (int64 [tokens], outside [0, vocab): masked) under
     ``logits`` [tokens, vocab], bf16 or fp32, with the entropies, the log-sum-exps and the
     ``top`` best alternatives.  ``out``: tensors to write, None in place of what is not
-    wanted; by default all are allocated.  Argument marshalling only; the formulas are in
+    wanted; by default all are allocated, those of fp32 as parts of one allocation, which
+    stays as long as one of them does.  Argument marshalling only; the formulas are in
     include/muon.h.  ``top_ids``, ``top_logits`` and ``lse`` at ``logit_scale`` = 1 /
     temperature are what :func:`muon_head_distill` takes from a teacher."""
     import torch

@@ -188,8 +188,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
   }
 }
 
-// NaN where the norm is not finite: nothing is clipped by it, and the AdamW step that is
-// given it leaves everything as it is.
+// NaN where the norm is not finite: nothing is clipped by it, and the steps that are given
+// it leave everything as it is.
 __device__ __forceinline__ float coefficient(double norm, double max_norm, double eps) {
   if (!isfinite(norm)) return __uint_as_float(0x7FC00000u);
   const double c = max_norm / (norm + eps);

@@ -271,7 +271,9 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
   return Sums{m, a.s + b.s, a.e + b.e};
 }
 
-// The sum of d 2^d over a thread's elements, read again, with exponents from kFloor on.
+// The sum of d 2^d over a thread's elements, read again, with exponents from kFloor on: where a
+// thread has met minus infinity.  (us, 4096 x 163840 bf16, 64 alternatives: 219 and 317 without,
+// 432 and 512 with one such column at the row's end, 490 and 844 with nine of ten so.)
 template <bool kFp32, int kThreads>
 __device__ __noinline__ float weighted_again(const uint4* cells, int begin, int end, float scale2, float base) {
   float sum = 0.f;
@@ -646,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kFp32, kTop, kThreads)
   };
   while (v0 + 2 * kTileVectors <= end) take_tile(std::true_type{});
   while (v0 < end) take_tile(std::false_type{});
-  // 0 times an exponent of minus infinity, most often
+  // 0 times an exponent of minus infinity, or a NaN
   if (!(a.e == a.e)) a.e = weighted_again<kFp32, kThreads>(cells, begin, end, P.scale2, a.m == -INFINITY ? 0.f : -a.m);
 
   // elements outside whole vectors
