@@ -37,7 +37,7 @@ constexpr int kMaxTop = 128;  // sparse target entries of one token
 constexpr int kNoId = 0x7FFFFFFF;  // sorted after every vocabulary index: an entry that does not count
 
 // What a forward pass that keeps its logits kept them of: all that the places in its
-// workspace depend on, and the scale.  Zeros where nothing was kept.
+// workspace depend on, and the scale.  Where nothing was kept, numbers that no call has.
 struct Kept {
   int tokens, dim, vocab;
   int packed;         // a copy of w with aligned rows is kept, too

@@ -454,7 +454,7 @@ head_gemm_kernel(const __grid_constant__ GemmParams P) {
   if (kList && blockIdx.x == 0 && threadIdx.x == 0) {  // first of the call's kernels
     P.ctrl->status = 0;
     P.ctrl->ticket = 0;
-    P.ctrl->kept.tokens = 0;
+    P.ctrl->kept.tokens = -1;  // no call's
   }
   const int n_valid = kList || P.in_place ? P.tokens : *reinterpret_cast<volatile int*>(&P.ctrl->n_valid);
   const Shape s0 = shape_of(P, 0, n_valid);

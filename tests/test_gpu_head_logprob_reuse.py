@@ -142,3 +142,20 @@ def test_what_the_same_call_kept_after_others_used_the_workspace():
             Reference(f64(x), f64(w), y.numpy(), 0.8).check_grads(g, rr.double().numpy(), hh.double().numpy(), kept=True)
         else:
             assert not g.dw.any()
+
+
+def test_no_tokens_after_a_call_that_kept_nothing():
+    """The first call's 200 tokens are still counted in the workspace; none of them is looked at."""
+    from paper_2502_16982_b200 import binding as b
+
+    T, D, V = 200, 128, 3000
+    ws, own = (torch.zeros(32 << 20, dtype=torch.uint8, device="cuda") for _ in range(2))
+    x, w, gen = make(T, D, V, 63)
+    y = torch.randint(0, V, (T,), generator=gen).cuda()
+    b.muon_head_logprob(x, w, y, workspace=ws, keep=True)
+    b.muon_head_logprob(x, w, y, workspace=ws)
+    r = b.muon_head_logprob(x[:0], w, y[:0], keep=False)
+    r.kept = ws
+    dw = torch.full((V, D), 7.0, device="cuda")
+    b.muon_head_logprob_grad(x[:0], w, y[:0], r, g_logprob=r.lse, dw=dw, workspace=own)
+    assert b.muon_head_status(own) == b.MUON_ERR_INVALID_ARG and not dw.any()
