@@ -859,8 +859,8 @@ int muon_head_logprob_grad(const muon_logprob_args* args, const muon_logprob_gra
  * statistics of its row NaN; among the alternatives a NaN counts as minus infinity.
  * Exponents are l log2(e) in fp32 and sums are fp32: a logit for which that is 2^31 or more
  * in magnitude (the lowest number of bf16 or fp32 as a mask, -1e30, -1e10) counts as the
- * infinity of its sign, except for its place among the alternatives and its own log
- * probability.  The gradient takes q from lse as fp32 holds it: where that is 2^24 or more
+ * infinity of its sign, except for its place among the alternatives and, up to fp32's
+ * range, its own log probability.  The gradient takes q from lse as fp32 holds it: where that is 2^24 or more
  * in magnitude (a row of nothing but masks of -1e9) its last place is 1 and more, and the
  * row's gradient is 0.  Results are the same bits from call to call.  Asynchronous on `stream`; no workspace, allocates nothing, does not
  * synchronise; may be captured into a CUDA graph.
